@@ -90,7 +90,7 @@ typedef enum {
 } moeq_status;
 
 typedef enum { MOEQ_ACT_RELU = 0, MOEQ_ACT_SWIGLU = 1 } moeq_act;
-typedef enum { MOEQ_F32 = 0, MOEQ_BF16 = 1 } moeq_dtype;
+typedef enum { MOEQ_F32 = 0, MOEQ_BF16 = 1, MOEQ_F16 = 2 /* the operators beside the layer */ } moeq_dtype;
 typedef enum { MOEQ_OUT_CANONICAL = 0, MOEQ_OUT_COLUMNS = 1 } moeq_out_layout;
 typedef enum { MOEQ_IN_CANONICAL = 0, MOEQ_IN_STREAM = 1 } moeq_in_layout;
 
@@ -275,6 +275,93 @@ moeq_status moe_prepare_in(const void *q, const void *s, int64_t rows, int64_t c
                            int32_t group, void *stream_buf, void *stream);
 moeq_status moe_unprepare_in(const void *stream_buf, int64_t rows, int64_t cols, int32_t bits,
                              int32_t group, void *q, void *s, void *stream);
+
+/* ---- operators beside the layer ------------------------------------------------------------
+ *
+ * Sorting the (token, choice) pairs of a routing by expert and back, low-rank adapters of many requests (or of the experts)
+ * beside a shared projection, and distillation from a teacher's top logits, with their gradients.
+ *   - All pointers are device pointers; calls enqueue on `stream` and return, allocate nothing and can be captured into a
+ *     graph. Elements are fp32, bf16 or fp16 (moeq_dtype); sums are held in fp32.
+ *   - Matrices have contiguous rows and a row stride in elements, at any alignment of an element. An input whose rows are all
+ *     the same one may have stride 0. Outputs must not overlap inputs, unless it is said.
+ *   - Indices that come with the call (experts, slots, adapter ids, a teacher's indices) are data: one that is out of its range
+ *     means "none" and never leads to an access. */
+
+/* Pairs i = token * top_k + choice, stably sorted by expert idx[i]: offsets [n_experts + 1] (rows of expert e: offsets[e] to
+ * offsets[e + 1]), order [pairs] (the pair in every place) and slot [pairs] (the place of every pair). Pairs without an expert
+ * (idx outside [0, n_experts)) come last, in their order, as ~pair and ~place (negative). n_experts <= 1024, pairs <= 2^28.
+ * ws: moe_sort_bytes (0 for calls of up to some thousand pairs). */
+size_t moe_sort_bytes(int32_t n_tokens, int32_t top_k, int32_t n_experts);
+moeq_status moe_sort_pairs(const int32_t *idx, int32_t n_tokens, int32_t top_k, int32_t n_experts, int32_t *offsets,
+                           int32_t *order, int32_t *slot, void *ws, size_t ws_bytes, void *stream);
+
+/* rows[slot[i]] = x[i / top_k] for every pair; zeros in the places of pairs without an expert. */
+moeq_status moe_gather_rows(const int32_t *slot, int32_t n_tokens, int32_t top_k, int32_t d, int32_t dtype, const void *x,
+                            int64_t x_stride, void *rows, int64_t rows_stride, void *stream);
+
+/* y[t] = sum over j of gate[t][j] * rows[slot[t][j]], in fp32 in the order of j; gate_opt NULL: all ones (the gradient of
+ * moe_gather_rows). Pairs without an expert add nothing, whatever their gate and row hold. y_dtype: dtype or MOEQ_F32. */
+moeq_status moe_combine_rows(const int32_t *slot, const float *gate_opt, int32_t n_tokens, int32_t top_k, int32_t d,
+                             int32_t dtype, const void *rows, int64_t rows_stride, int32_t y_dtype, void *y,
+                             int64_t y_stride, void *stream);
+
+/* The gradient of moe_combine_rows: drows[slot[i]] = gate[i] * dy[t] (in dtype), dgate[i] = dy[t] . rows[slot[i]]; zeros for
+ * pairs without an expert. dgate_opt NULL: not wanted (rows is not read then). */
+moeq_status moe_combine_rows_backward(const int32_t *slot, const float *gate_opt, int32_t n_tokens, int32_t top_k, int32_t d,
+                                      int32_t dtype, const void *rows, int64_t rows_stride, int32_t dy_dtype,
+                                      const void *dy, int64_t dy_stride, void *drows, int64_t drows_stride,
+                                      float *dgate_opt, void *stream);
+
+/* Low-rank adapters: a [n_adapters][rank][d_in], b [n_adapters][d_out][rank] in dtype, scale [n_adapters] fp32, all contiguous
+ * device memory that the caller keeps. rank <= 64, n_adapters <= 1024, d_in and d_out <= 32768. */
+typedef struct {
+  int32_t n_adapters, rank, d_in, d_out, dtype;
+  const void *a, *b;
+  const float *scale;
+} moeq_adapters;
+
+/* Workspace of a call of up to max_tokens tokens (0 for an invalid description); calls that share one must be ordered. */
+size_t moe_adapters_workspace_bytes(const moeq_adapters *adapters, int32_t max_tokens, int32_t backward);
+
+/* y[t] = base[t] + scale_a B_a A_a x[t], a = ids[t]; a row whose id is outside [0, n_adapters) has no adapter: y = base.
+ * base_opt NULL: zeros; base may be y itself. base and y are y_dtype: dtype or MOEQ_F32. At most 65535 tokens. A x is held in
+ * fp32. An infinity in a row's x, A or B may come out as a NaN. */
+moeq_status moe_adapters_forward(const moeq_adapters *adapters, const void *x, int64_t x_stride, const int32_t *ids,
+                                 int32_t n_tokens, const void *base_opt, int64_t base_stride, int32_t y_dtype, void *y,
+                                 int64_t y_stride, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient: dx[t] = dx_base[t] + scale_a A_a^T B_a^T dy[t] (dx_opt NULL: not wanted; dx_base_opt NULL: zeros, and it may be
+ * dx itself), dA [n][rank][d_in] and dB [n][d_out][rank] in fp32, contiguous, zeros for adapters without rows. dy, dx_base and dx
+ * are dy_dtype: dtype or MOEQ_F32. The sums' order does not depend on timing: the same call gives the same bits. */
+moeq_status moe_adapters_backward(const moeq_adapters *adapters, const void *x, int64_t x_stride, const int32_t *ids,
+                                  int32_t n_tokens, int32_t dy_dtype, const void *dy, int64_t dy_stride,
+                                  const void *dx_base_opt, int64_t dx_base_stride, void *dx_opt, int64_t dx_stride,
+                                  float *dA, float *dB, void *ws, size_t ws_bytes, void *stream);
+
+/* Distillation. Of a row of student logits z [vocab], a teacher's logits u at `top` indices (contiguous [n_tokens][top]),
+ * temperature tau and weight w (weight_opt NULL: ones): s = z / tau, p = softmax(u / tau) over the entries whose index lies in
+ * [0, vocab),
+ *     loss = w tau^2 sum_j p_j (log p_j - s[idx_j] + lse),   lse = log sum exp(s),
+ *     dloss/dz = w tau (softmax(s) - p at the indices; an index given twice counts twice).
+ * Rows of weight 0, and rows whose teacher's entries have no index or are all minus infinity, have loss 0 and gradient 0
+ * whatever their logits hold. A student's logit of minus infinity has probability 0 (a teacher's entry there makes the loss
+ * infinite). top <= 1024, n_tokens <= 2^24. */
+size_t moe_distill_workspace_bytes(int32_t n_tokens, int32_t vocab, int32_t dtype);
+/* loss [n_tokens] and, if wanted, lse [n_tokens] (of every row, whatever its weight). */
+moeq_status moe_distill_forward(const void *logits, int64_t stride, int32_t dtype, int32_t n_tokens, int32_t vocab,
+                                const int32_t *top_idx, const float *top_logits, int32_t top, float temperature,
+                                const float *weight_opt, float *loss, float *lse_opt, void *ws, size_t ws_bytes,
+                                void *stream);
+/* dlogits [n_tokens][vocab] in dtype, times dloss [n_tokens], from the forward's lse. */
+moeq_status moe_distill_backward(const void *logits, int64_t stride, int32_t dtype, int32_t n_tokens, int32_t vocab,
+                                 const int32_t *top_idx, const float *top_logits, int32_t top, float temperature,
+                                 const float *weight_opt, const float *lse, const float *dloss, void *dlogits,
+                                 int64_t dstride, void *stream);
+/* Both in one call: loss [n_tokens] and the gradient of their sum. */
+moeq_status moe_distill_loss_grad(const void *logits, int64_t stride, int32_t dtype, int32_t n_tokens, int32_t vocab,
+                                  const int32_t *top_idx, const float *top_logits, int32_t top, float temperature,
+                                  const float *weight_opt, float *loss, void *dlogits, int64_t dstride, void *ws,
+                                  size_t ws_bytes, void *stream);
 
 /* Measurement aid, per layer. While `which` names a kernel, every moe_layer_forward call on THIS
  * layer records start_event just before and stop_event just after that kernel on the call's stream

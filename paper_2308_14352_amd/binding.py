@@ -14,7 +14,7 @@ LIB_PATH = os.environ.get("MOEQ_LIB") or os.path.join(_HERE, "libmoeq.so")
 
 MOEQ_OK, MOEQ_EINVAL, MOEQ_EUNSUPPORTED, MOEQ_EWORKSPACE, MOEQ_EDEVICE = range(5)
 MOEQ_ACT_RELU, MOEQ_ACT_SWIGLU = 0, 1
-MOEQ_F32, MOEQ_BF16 = 0, 1
+MOEQ_F32, MOEQ_BF16, MOEQ_F16 = 0, 1, 2
 MOEQ_OUT_CANONICAL, MOEQ_OUT_COLUMNS = 0, 1
 MOEQ_IN_CANONICAL, MOEQ_IN_STREAM = 0, 1
 
@@ -39,6 +39,11 @@ class moeq_layer_desc(C.Structure):
                 ("router_w", C.c_void_p), ("router_bias", C.c_void_p),
                 ("experts", C.POINTER(moeq_expert)), ("out_layout", C.c_int32), ("in_layout", C.c_int32),
                 ("group_in", C.c_int32), ("group_out", C.c_int32)]
+
+
+class moeq_adapters(C.Structure):
+    _fields_ = [("n_adapters", C.c_int32), ("rank", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32), ("dtype", C.c_int32),
+                ("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p)]
 
 
 _lib = None
@@ -97,6 +102,22 @@ def lib():
     for fn in (L.moe_prepare_out, L.moe_unprepare_out):
         fn.restype = C.c_int
         fn.argtypes = [vp, vp, i64, i64, i32, i32, vp, vp, vp]
+    f32 = C.c_float
+    for name, res, args in (
+            ("moe_sort_bytes", sz, [i32, i32, i32]),
+            ("moe_sort_pairs", C.c_int, [vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]),
+            ("moe_gather_rows", C.c_int, [vp, i32, i32, i32, i32, vp, i64, vp, i64, vp]),
+            ("moe_combine_rows", C.c_int, [vp, vp, i32, i32, i32, i32, vp, i64, i32, vp, i64, vp]),
+            ("moe_combine_rows_backward", C.c_int, [vp, vp, i32, i32, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, vp]),
+            ("moe_adapters_workspace_bytes", sz, [vp, i32, i32]),
+            ("moe_adapters_forward", C.c_int, [vp, vp, i64, vp, i32, vp, i64, i32, vp, i64, vp, sz, vp]),
+            ("moe_adapters_backward", C.c_int, [vp, vp, i64, vp, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]),
+            ("moe_distill_workspace_bytes", sz, [i32, i32, i32]),
+            ("moe_distill_forward", C.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, vp, sz, vp]),
+            ("moe_distill_backward", C.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, vp, i64, vp]),
+            ("moe_distill_loss_grad", C.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp, sz, vp])):
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = res, args
     _lib = L
     return L
 
@@ -104,7 +125,10 @@ def lib():
 EXPORTS = ["moe_status_str", "moe_layer_profile_kernel", "moe_layer_table_bytes", "moe_packed_bytes", "moe_layer_create",
            "moe_layer_destroy", "moe_workspace_bytes", "moe_layer_path", "moe_router_topk", "moe_expert_ffn_q",
            "moe_layer_forward", "moe_layer_forward_routed", "moe_layer_forward_static", "moe_static_scratch_bytes", "moe_quantize_pack", "moe_unpack_codes", "moe_dequantize", "moe_prepare_out",
-           "moe_unprepare_out", "moe_prepare_in", "moe_unprepare_in", "moe_stream_bytes"]
+           "moe_unprepare_out", "moe_prepare_in", "moe_unprepare_in", "moe_stream_bytes",
+           "moe_sort_bytes", "moe_sort_pairs", "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward",
+           "moe_adapters_workspace_bytes", "moe_adapters_forward", "moe_adapters_backward",
+           "moe_distill_workspace_bytes", "moe_distill_forward", "moe_distill_backward", "moe_distill_loss_grad"]
 
 
 def status_str(st):
@@ -368,3 +392,229 @@ def moe_layer_forward_routed(layer, x, idx, gate, y=None, ws=None, stream=None):
     _check(lib().moe_layer_forward_routed(layer.handle, _ptr(x), T, _ptr(idx), _ptr(gate), _ptr(y), _ptr(ws),
                                           ws.numel(), _stream(stream)), "moe_layer_forward_routed")
     return y
+
+
+# ---- operators beside the layer ----------------------------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: MOEQ_F32, torch.bfloat16: MOEQ_BF16, torch.float16: MOEQ_F16}
+
+
+def _need(ok, what):
+    if not ok:
+        raise MoeqError(MOEQ_EINVAL, what)
+
+
+def _dtype(t, what):
+    _need(t in _DTYPES, what)
+    return _DTYPES[t]
+
+
+def _empty(shape, dtype, device, stream):
+    """A tensor for a call on `stream`: memory that the allocator knows to be that stream's."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _matrix(t, rows, cols, what, dtype=None):
+    """The row stride of a [rows][cols] tensor with contiguous rows."""
+    _need(t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and (dtype is None or t.dtype is dtype), what)
+    _need(cols == 1 or t.stride(1) == 1, what)
+    return t.stride(0)
+
+
+def _plain(t, shape, dtype, what):
+    _need(t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous(), what)
+
+
+class PairSort:
+    """The order of a call's (token, choice) pairs by expert: int32 tensors offsets [n_experts + 1], order [pairs] (the pair in
+    every place) and slot [pairs] (the place of every pair); pairs without an expert come last, as ~pair and ~place."""
+
+    def __init__(self, offsets, order, slot, n_tokens, top_k, n_experts):
+        self.offsets, self.order, self.slot = offsets, order, slot
+        self.n_tokens, self.top_k, self.n_experts = n_tokens, top_k, n_experts
+
+
+def moe_sort_pairs(idx, n_experts, stream=None):
+    """idx: device int32 [T][k], the experts that a router chose (outside [0, n_experts): none) -> PairSort."""
+    _need(idx.dim() == 2, "moe_sort_pairs")
+    T, k = idx.shape
+    _plain(idx, (T, k), torch.int32, "moe_sort_pairs")
+    P = T * k
+    ws = int(lib().moe_sort_bytes(T, k, n_experts))
+    buf = _empty((n_experts + 1 + 2 * P + ws // 4,), torch.int32, idx.device, stream)
+    offsets, order, slot, rest = buf.split((n_experts + 1, P, P, ws // 4))
+    at = buf.data_ptr()
+    at_order = at + 4 * (n_experts + 1)
+    _check(lib().moe_sort_pairs(idx.data_ptr(), T, k, n_experts, at, at_order, at_order + 4 * P, at_order + 8 * P, ws,
+                                _stream(stream)), "moe_sort_pairs")
+    return PairSort(offsets, order, slot, T, k, n_experts)
+
+
+def moe_gather_rows(sort, x, rows=None, stream=None):
+    """The tokens' rows [T][d] in the order of the sort: rows [pairs][d] (zeros for pairs without an expert)."""
+    T, k, d = sort.n_tokens, sort.top_k, x.shape[-1]
+    xs = _matrix(x, T, d, "moe_gather_rows")
+    if rows is None:
+        rows = _empty((T * k, d), x.dtype, x.device, stream)
+    _check(lib().moe_gather_rows(sort.slot.data_ptr(), T, k, d, _dtype(x.dtype, "moe_gather_rows"), x.data_ptr(), xs,
+                                 rows.data_ptr(), _matrix(rows, T * k, d, "moe_gather_rows", x.dtype), _stream(stream)),
+           "moe_gather_rows")
+    return rows
+
+
+def moe_combine_rows(sort, rows, gate=None, dtype=None, y=None, stream=None):
+    """Rows in the order of the sort back to tokens: y[t] = sum of gate[t][j] * row (gate None: ones, the gradient of
+    moe_gather_rows). dtype: of y, the rows' own (default) or fp32."""
+    T, k, d = sort.n_tokens, sort.top_k, rows.shape[-1]
+    rs = _matrix(rows, T * k, d, "moe_combine_rows")
+    if gate is not None:
+        _plain(gate, (T, k), torch.float32, "moe_combine_rows")
+    if y is None:
+        y = _empty((T, d), dtype or rows.dtype, rows.device, stream)
+    _check(lib().moe_combine_rows(sort.slot.data_ptr(), _ptr(gate), T, k, d, _dtype(rows.dtype, "moe_combine_rows"),
+                                  rows.data_ptr(), rs, _dtype(y.dtype, "moe_combine_rows"), y.data_ptr(),
+                                  _matrix(y, T, d, "moe_combine_rows", dtype), _stream(stream)), "moe_combine_rows")
+    return y
+
+
+def moe_combine_rows_backward(sort, dy, rows, gate=None, drows=None, stream=None):
+    """The gradient of moe_combine_rows: (drows [pairs][d] in the rows' dtype, dgate [T][k] fp32)."""
+    T, k, d = sort.n_tokens, sort.top_k, rows.shape[-1]
+    what = "moe_combine_rows_backward"
+    rs, ds = _matrix(rows, T * k, d, what), _matrix(dy, T, d, what)
+    if gate is not None:
+        _plain(gate, (T, k), torch.float32, what)
+    if drows is None:
+        drows = _empty((T * k, d), rows.dtype, rows.device, stream)
+    dgate = _empty((T, k), torch.float32, rows.device, stream)
+    _check(lib().moe_combine_rows_backward(sort.slot.data_ptr(), _ptr(gate), T, k, d, _dtype(rows.dtype, what), rows.data_ptr(), rs,
+                                           _dtype(dy.dtype, what), dy.data_ptr(), ds, drows.data_ptr(),
+                                           _matrix(drows, T * k, d, what, rows.dtype), dgate.data_ptr(), _stream(stream)), what)
+    return drows, dgate
+
+
+class Adapters:
+    """Low-rank adapters a [n][rank][d_in], b [n][d_out][rank] (one dtype) with scale [n] fp32: device tensors that are borrowed,
+    not copied, so that an update in place is seen by the next call."""
+
+    def __init__(self, a, b, scale):
+        what = "Adapters"
+        _need(a.dim() == 3 and b.dim() == 3 and a.shape[0] == b.shape[0] and a.shape[1] == b.shape[2], what)
+        n, r, d_in = a.shape
+        _plain(a, (n, r, d_in), a.dtype, what)
+        _plain(b, (n, b.shape[1], r), a.dtype, what)
+        _plain(scale, (n,), torch.float32, what)
+        self.a, self.b, self.scale = a, b, scale
+        self.n_adapters, self.rank, self.d_in, self.d_out, self.dtype = n, r, d_in, b.shape[1], a.dtype
+        self._desc = moeq_adapters(n, r, d_in, self.d_out, _dtype(a.dtype, what), a.data_ptr(), b.data_ptr(), scale.data_ptr())
+        self.handle = C.addressof(self._desc)
+        self._ws, self._bytes = None, {}
+
+    def workspace_bytes(self, max_tokens, backward=False):
+        return int(lib().moe_adapters_workspace_bytes(self.handle, max_tokens, int(backward)))
+
+    def workspace(self, n_tokens, backward=False):
+        need = self._bytes.get((n_tokens, backward))
+        if need is None:
+            need = self._bytes[(n_tokens, backward)] = max(self.workspace_bytes(n_tokens, backward), 16)
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.a.device)
+        return self._ws
+
+
+def moe_adapters_forward(adapters, x, ids, base=None, y=None, ws=None, stream=None):
+    """y[t] = base[t] + scale_a B_a A_a x[t] with a = ids[t] (int32; outside [0, n): no adapter). base: [T][d_out] or None
+    (zeros), may be y itself. y: in the adapters' dtype (default) or fp32. Calls that share a workspace (the adapters' own unless
+    one is passed) have to be ordered."""
+    T, what = x.shape[0], "moe_adapters_forward"
+    xs = _matrix(x, T, adapters.d_in, what, adapters.dtype)
+    _plain(ids, (T,), torch.int32, what)
+    if y is None:
+        y = _empty((T, adapters.d_out), adapters.dtype if base is None else base.dtype, x.device, stream)
+    bs = 0 if base is None else _matrix(base, T, adapters.d_out, what, y.dtype)
+    if ws is None:
+        ws = adapters.workspace(T)
+    _check(lib().moe_adapters_forward(adapters.handle, x.data_ptr(), xs, ids.data_ptr(), T, _ptr(base), bs, _dtype(y.dtype, what),
+                                      y.data_ptr(), _matrix(y, T, adapters.d_out, what), ws.data_ptr(), ws.numel(),
+                                      _stream(stream)), what)
+    return y
+
+
+def moe_adapters_backward(adapters, x, ids, dy, dx_base=None, dx=None, want_dx=True, ws=None, stream=None):
+    """The gradient of moe_adapters_forward: (dx [T][d_in] in dy's dtype, dA [n][rank][d_in] fp32, dB [n][d_out][rank] fp32).
+    dx_base: added to dx (the gradient through the shared projection), may be dx itself."""
+    T, what = x.shape[0], "moe_adapters_backward"
+    xs, ys = _matrix(x, T, adapters.d_in, what, adapters.dtype), _matrix(dy, T, adapters.d_out, what)
+    _plain(ids, (T,), torch.int32, what)
+    if dx is None and want_dx:
+        dx = _empty((T, adapters.d_in), dy.dtype, x.device, stream)
+    dxs = 0 if dx is None else _matrix(dx, T, adapters.d_in, what, dy.dtype)
+    bs = 0 if dx_base is None else _matrix(dx_base, T, adapters.d_in, what, dy.dtype)
+    dA = _empty(adapters.a.shape, torch.float32, x.device, stream)
+    dB = _empty(adapters.b.shape, torch.float32, x.device, stream)
+    if ws is None:
+        ws = adapters.workspace(T, True)
+    _check(lib().moe_adapters_backward(adapters.handle, x.data_ptr(), xs, ids.data_ptr(), T, _dtype(dy.dtype, what), dy.data_ptr(), ys,
+                                       _ptr(dx_base), bs, _ptr(dx), dxs, dA.data_ptr(), dB.data_ptr(), ws.data_ptr(), ws.numel(),
+                                       _stream(stream)), what)
+    return dx, dA, dB
+
+
+def _distill(logits, top_idx, top_logits, weight, what):
+    _need(logits.dim() == 2 and top_idx.dim() == 2, what)
+    T, V = logits.shape
+    K = top_idx.shape[1]
+    _plain(top_idx, (T, K), torch.int32, what)
+    _plain(top_logits, (T, K), torch.float32, what)
+    if weight is not None:
+        _plain(weight, (T,), torch.float32, what)
+    return T, V, K, _dtype(logits.dtype, what), _matrix(logits, T, V, what)
+
+
+def _distill_ws(T, V, dt, device, stream):
+    need = int(lib().moe_distill_workspace_bytes(T, V, dt))
+    return (None, 0) if need == 0 else (_empty((need,), torch.uint8, device, stream), need)
+
+
+def moe_distill_forward(logits, top_idx, top_logits, temperature=1.0, weight=None, stream=None):
+    """Distillation from a teacher's top logits [T][K] fp32 at top_idx [T][K] int32 (outside [0, V): no entry): (loss [T], lse [T])
+    with loss = w tau^2 KL(softmax(top_logits / tau) || softmax(logits / tau)) and lse = log sum exp(logits / tau)."""
+    what = "moe_distill_forward"
+    T, V, K, dt, ls = _distill(logits, top_idx, top_logits, weight, what)
+    out = _empty((2, T), torch.float32, logits.device, stream)
+    ws, need = _distill_ws(T, V, dt, logits.device, stream)
+    at = out.data_ptr()
+    _check(lib().moe_distill_forward(logits.data_ptr(), ls, dt, T, V, top_idx.data_ptr(), top_logits.data_ptr(), K, temperature,
+                                     _ptr(weight), at, at + 4 * T, _ptr(ws), need, _stream(stream)), what)
+    return out[0], out[1]
+
+
+def moe_distill_backward(logits, top_idx, top_logits, lse, dloss, temperature=1.0, weight=None, dlogits=None, stream=None):
+    """dlogits [T][V] in the logits' dtype from the forward's lse and the gradients of the losses, both [T] fp32."""
+    what = "moe_distill_backward"
+    T, V, K, dt, ls = _distill(logits, top_idx, top_logits, weight, what)
+    _plain(lse, (T,), torch.float32, what)
+    _plain(dloss, (T,), torch.float32, what)
+    if dlogits is None:
+        dlogits = _empty((T, V), logits.dtype, logits.device, stream)
+    _check(lib().moe_distill_backward(logits.data_ptr(), ls, dt, T, V, top_idx.data_ptr(), top_logits.data_ptr(), K, temperature,
+                                      _ptr(weight), lse.data_ptr(), dloss.data_ptr(), dlogits.data_ptr(),
+                                      _matrix(dlogits, T, V, what, logits.dtype), _stream(stream)), what)
+    return dlogits
+
+
+def moe_distill_loss_grad(logits, top_idx, top_logits, temperature=1.0, weight=None, dlogits=None, stream=None):
+    """(loss [T], the gradient of the losses' sum with respect to the logits [T][V]) in one call."""
+    what = "moe_distill_loss_grad"
+    T, V, K, dt, ls = _distill(logits, top_idx, top_logits, weight, what)
+    loss = _empty((T,), torch.float32, logits.device, stream)
+    if dlogits is None:
+        dlogits = _empty((T, V), logits.dtype, logits.device, stream)
+    ws, need = _distill_ws(T, V, dt, logits.device, stream)
+    _check(lib().moe_distill_loss_grad(logits.data_ptr(), ls, dt, T, V, top_idx.data_ptr(), top_logits.data_ptr(), K, temperature,
+                                       _ptr(weight), loss.data_ptr(), dlogits.data_ptr(),
+                                       _matrix(dlogits, T, V, what, logits.dtype), _ptr(ws), need, _stream(stream)), what)
+    return loss, dlogits

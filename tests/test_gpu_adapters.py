@@ -1,0 +1,233 @@
+"""Low-rank adapters of many requests and their gradient against plain arithmetic in 64 bits on the host: one row to many, every rank
+class, widths that end inside a vector or tile, rows without an adapter, adapters without rows, every pair of types."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2308_14352_amd as moeq
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+PAIRS = [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")]
+
+
+def rng_of(*parts):
+    return np.random.default_rng([ord(c) for c in repr(parts)])
+
+
+def strided(t, pad, shift):
+    buf = torch.full((t.shape[0] * (t.shape[1] + pad) + shift,), float("nan"), dtype=t.dtype, device=t.device)
+    v = buf[shift:].view(t.shape[0], t.shape[1] + pad)[:, :t.shape[1]]
+    v.copy_(t)
+    return v
+
+
+def make(rng, T, n, r, d_in, d_out, t, out):
+    f = lambda *s, by=1.0: torch.from_numpy(rng.normal(size=s) * by)
+    return dict(A=f(n, r, d_in, by=d_in**-0.5).to(t), B=f(n, d_out, r, by=0.3).to(t), scale=(f(n) * 0.5 + 1).float(),
+                x=f(T, d_in).to(t), dy=f(T, d_out).to(out), base=f(T, d_out).to(out), dx_base=f(T, d_in).to(out))
+
+
+def ids_of(rng, T, n, how):
+    if how == "none":
+        return rng.choice(np.array([-1, n, 2**31 - 1, -2**31]), size=T).astype(np.int32)
+    if how == "one":
+        return np.full(T, n - 1, np.int32)
+    if how == "sorted":
+        return np.sort(rng.integers(0, n, size=T)).astype(np.int32)
+    ids = rng.integers(-1, n + 1, size=T)                 # -1 and n: none
+    return ids.astype(np.int32)
+
+
+def reference(m, ids, n):
+    """Outputs in 64 bits, and the sums of the magnitudes that they are made of (for the tolerances)."""
+    d = {k: v.double().numpy() for k, v in m.items()}
+    y, dx = d["base"].copy(), d["dx_base"].copy()
+    ym, dxm = np.abs(y), np.abs(dx)
+    dA, dB = np.zeros_like(d["A"]), np.zeros_like(d["B"])
+    dAm, dBm = np.zeros_like(dA), np.zeros_like(dB)
+    for a in range(n):
+        t = np.nonzero(ids == a)[0]
+        if not t.size:
+            continue
+        A, B, c, x, dy = d["A"][a], d["B"][a], d["scale"][a], d["x"][t], d["dy"][t]
+        h, g = x @ A.T, dy @ B
+        hm, gm = np.abs(x) @ np.abs(A).T, np.abs(dy) @ np.abs(B)
+        y[t] += c * h @ B.T
+        ym[t] += abs(c) * hm @ np.abs(B).T
+        dx[t] += c * g @ A
+        dxm[t] += abs(c) * gm @ np.abs(A)
+        dA[a], dAm[a] = c * g.T @ x, abs(c) * gm.T @ np.abs(x)
+        dB[a], dBm[a] = c * dy.T @ h, abs(c) * np.abs(dy).T @ hm
+    return dict(y=(y, ym), dx=(dx, dxm), dA=(dA, dAm), dB=(dB, dBm))
+
+
+def check(got, want, mag, steps):
+    """Sums of `steps` fp32 roundings in a row, independent of each other: each is at most half a step (2^-24) of a partial sum that
+    the magnitudes bound, together the square root of their number, 8 times that for the largest of all; and the output's own."""
+    half = torch.finfo(got.dtype).eps / 2
+    tol = 8 * (steps + 16) ** 0.5 * 2.0**-24 * mag + half * np.abs(want) * 1.001 + (2.0**-25 if got.dtype == torch.float16 else 0)
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert np.isfinite(err).all() and (err <= tol).all(), float((err / np.maximum(tol, 1e-300)).max())
+
+
+CASES = [  # T, n, r, d_in, d_out, ids
+    (1, 1, 1, 1, 1, "one"), (1, 4, 8, 64, 32, "mixed"), (2, 3, 5, 7, 9, "mixed"), (9, 32, 16, 256, 512, "mixed"), (16, 2, 4, 100, 129, "one"),
+    (17, 2, 32, 130, 64, "one"), (33, 1, 64, 96, 200, "one"), (64, 9, 33, 128, 65, "mixed"), (65, 5, 16, 1000, 36, "mixed"),
+    (64, 3, 17, 40, 1100, "none"), (80, 3, 2, 31, 33, "none"), (200, 70, 3, 65, 640, "mixed"), (333, 4, 64, 513, 257, "sorted"),
+    (777, 16, 8, 1024, 96, "sorted"), (1500, 2, 12, 64, 128, "one"), (2500, 1, 48, 72, 520, "mixed"), (300, 1024, 1, 16, 24, "mixed")]
+
+
+@pytest.mark.parametrize("kind,out", PAIRS)
+@pytest.mark.parametrize("T,n,r,d_in,d_out,how", CASES)
+def test_forward_and_backward(T, n, r, d_in, d_out, how, kind, out):
+    rng = rng_of(T, n, r, d_in, d_out, how, kind, out)
+    m = make(rng, T, n, r, d_in, d_out, TYPES[kind], TYPES[out])
+    ids = ids_of(rng, T, n, how)
+    want = reference(m, ids, n)
+    # rows without an adapter and adapters without rows may hold anything
+    off = (ids < 0) | (ids >= n)
+    m["x"][torch.from_numpy(off)], m["dy"][torch.from_numpy(off)] = float("nan"), float("inf")
+    unused = torch.tensor([a not in set(ids.tolist()) for a in range(n)])
+    m["A"][unused], m["B"][unused], m["scale"][unused] = float("inf"), float("nan"), float("nan")
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ids = torch.from_numpy(ids).to(DEV)
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    y = moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"])
+    check(y, *want["y"], d_in + r)
+    dx, dA, dB = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], dx_base=g["dx_base"])
+    check(dx, *want["dx"], d_out + r)
+    check(dA, *want["dA"], d_out + T)
+    check(dB, *want["dB"], d_in + T)
+    assert (dA[unused.to(DEV)] == 0).all() and (dB[unused.to(DEV)] == 0).all()
+    # rows at another stride and alignment, in place of the base, without the gradient of x, twice: the same bits
+    s = {k: strided(g[k], 5, 3) for k in ("x", "dy", "base", "dx_base")}
+    y2 = moeq.moe_adapters_forward(ad, s["x"], ids, base=s["base"], y=s["base"])
+    dx2, dA2, dB2 = moeq.moe_adapters_backward(ad, s["x"], ids, s["dy"], dx_base=s["dx_base"], dx=s["dx_base"])
+    assert torch.equal(y, y2) and torch.equal(dx, dx2) and torch.equal(dA, dA2) and torch.equal(dB, dB2)
+    none, dA2, dB2 = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], want_dx=False)
+    assert none is None and torch.equal(dA, dA2) and torch.equal(dB, dB2)
+
+
+@pytest.mark.parametrize("kind,out", PAIRS)
+def test_without_a_base_and_with_a_shared_one(kind, out):
+    rng = rng_of("base", kind, out)
+    T, n, r, d_in, d_out = 70, 4, 8, 72, 136
+    m = make(rng, T, n, r, d_in, d_out, TYPES[kind], TYPES[out])
+    ids = ids_of(rng, T, n, "mixed")
+    m["dx_base"].zero_()
+    m["base"][:] = m["base"][:1].clone()
+    want = reference(m, ids, n)
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ad, ids = moeq.Adapters(g["A"], g["B"], g["scale"]), torch.from_numpy(ids).to(DEV)
+    check(moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"][:1].expand(T, d_out)), *want["y"], d_in + r)
+    check(moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"])[0], *want["dx"], d_out + r)
+    y0 = moeq.moe_adapters_forward(ad, g["x"], ids, y=torch.empty((T, d_out), dtype=TYPES[out], device=DEV))
+    b = m["base"].double().numpy()
+    check(y0, want["y"][0] - b, want["y"][1] - np.abs(b), d_in + r)
+    # all rows one row, of x and of dy: the gradients of a broadcast input
+    x1, dy1 = g["x"][:1].expand(T, d_in), g["dy"][:1].expand(T, d_out)
+    m2 = dict(m, x=m["x"][:1].expand(T, d_in), dy=m["dy"][:1].expand(T, d_out))
+    want = reference(m2, ids.cpu().numpy(), n)
+    dx, dA, dB = moeq.moe_adapters_backward(ad, x1, ids, dy1)
+    check(dx, *want["dx"], d_out + r)
+    check(dA, *want["dA"], d_out + T)
+    check(dB, *want["dB"], d_in + T)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+def test_a_row_that_is_not_finite_stays_alone(kind):
+    rng = rng_of("nan", kind)
+    T, n, r, d = 100, 3, 16, 256
+    m = make(rng, T, n, r, d, d, TYPES[kind], TYPES[kind])
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ids = torch.from_numpy(ids_of(rng, T, n, "mixed")).to(DEV)
+    ids[5], ids[50] = 1, 1
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    y = moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"])
+    _, dA, dB = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"])
+    g["x"][5, 7], g["x"][50, 200] = float("nan"), float("inf")
+    y2 = moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"])
+    rest = [t for t in range(T) if t not in (5, 50)]
+    assert torch.equal(y[rest], y2[rest]) and not y2[[5, 50]].isfinite().any()
+    _, dA2, dB2 = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"])
+    others = [0, 2]
+    assert torch.equal(dA[others], dA2[others]) and torch.equal(dB[others], dB2[others])
+    assert not dB2[1].isfinite().any() and not dA2[1][:, [7, 200]].isfinite().any()
+
+
+def test_no_rows():
+    A, B, s = torch.randn((3, 4, 8), device=DEV), torch.randn((3, 16, 4), device=DEV), torch.ones(3, device=DEV)
+    ad = moeq.Adapters(A, B, s)
+    none = torch.empty((0,), dtype=torch.int32, device=DEV)
+    assert moeq.moe_adapters_forward(ad, A.new_empty((0, 8)), none).shape == (0, 16)
+    dx, dA, dB = moeq.moe_adapters_backward(ad, A.new_empty((0, 8)), none, A.new_empty((0, 16)))
+    assert dx.shape == (0, 8) and (dA == 0).all() and (dB == 0).all() and dA.shape == A.shape and dB.shape == B.shape
+
+
+def test_gradient_against_differences():
+    """sum(y * c) is linear in x, in A and in B: differences along a direction have no error of their own but the roundings."""
+    rng = rng_of("differences")
+    T, n, r, d_in, d_out = 90, 4, 8, 64, 96
+    new = lambda *s: torch.from_numpy(rng.normal(size=s).astype(np.float32)).to(DEV)
+    A, B, scale, x, c = new(n, r, d_in), new(n, d_out, r), new(n), new(T, d_in), new(T, d_out)
+    ids = torch.from_numpy(ids_of(rng, T, n, "mixed")).to(DEV)
+    loss = lambda a, b, v: (moeq.moe_adapters_forward(moeq.Adapters(a, b, scale), v, ids).double() * c.double()).sum().item()
+    dx, dA, dB = moeq.moe_adapters_backward(moeq.Adapters(A, B, scale), x, ids, c)
+    vA, vB, vx = new(n, r, d_in), new(n, d_out, r), new(T, d_in)
+    # elements of y are sums of 64 x 8 products of either sign, some 23 in size with the largest partial sums some 100: half a step
+    # of those in each of T * d_out, added up as their square root, and the gradients' roundings against directions of size 1
+    tol = 4 * 100 * 2.0**-23 * (T * d_out) ** 0.5 * 2
+    for plus, minus, grad, v in ((loss(A + vA, B, x), loss(A - vA, B, x), dA, vA), (loss(A, B + vB, x), loss(A, B - vB, x), dB, vB),
+                                 (loss(A, B, x + vx), loss(A, B, x - vx), dx, vx)):
+        assert abs((plus - minus) / 2 - (grad.double() * v.double()).sum().item()) < tol
+
+
+@pytest.mark.parametrize("T", (9, 700))
+def test_replays_of_a_graph(T):
+    rng = rng_of("graph", T)
+    n, r, d_in, d_out = 5, 16, 256, 384
+    m = make(rng, T, n, r, d_in, d_out, torch.bfloat16, torch.bfloat16)
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ids = torch.from_numpy(ids_of(rng, T, n, "mixed")).to(DEV)
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    ws = torch.empty(ad.workspace_bytes(T, True), dtype=torch.uint8, device=DEV)
+    step = lambda w: [moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"], ws=w),
+                      *moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], dx_base=g["dx_base"], ws=w)]
+    step(ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step(ws)
+    other = torch.empty_like(ws)
+    for k in range(4):
+        g["x"].normal_()
+        g["A"].normal_(std=0.1)
+        ids.copy_(torch.from_numpy(ids_of(rng, T, n, ("mixed", "one", "none", "sorted")[k])).to(DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step(other)))
+
+
+def test_another_stream_and_wide_offsets():
+    """Rows far apart: the last begins more than 2^32 bytes behind the first."""
+    T, n, r, d = 3, 2, 8, 64
+    far = 300_000_000
+    buf = torch.empty(far * 4 * (T - 1) // 2 + 2 * d, dtype=torch.bfloat16, device=DEV)
+    x = torch.as_strided(buf, (T, d), (far * 2, 1))
+    A, B, s = (torch.randn(k, device=DEV).to(torch.bfloat16) for k in ((n, r, d), (n, d, r), (n,)))
+    ad = moeq.Adapters(A, B, s.float())
+    v = torch.randn((T, d), device=DEV).to(torch.bfloat16)
+    ids = torch.tensor([0, 1, 0], dtype=torch.int32, device=DEV)
+    want = moeq.moe_adapters_forward(ad, v, ids)
+    gA, gB = moeq.moe_adapters_backward(ad, v, ids, want)[1:]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        x.copy_(v)
+    got = moeq.moe_adapters_forward(ad, x, ids, stream=side)
+    dx, dA, dB = moeq.moe_adapters_backward(ad, x, ids, got, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(dA, gA) and torch.equal(dB, gB)
