@@ -320,7 +320,8 @@ typedef struct {
   const float *scale;
 } moeq_adapters;
 
-/* Workspace of a call of up to max_tokens tokens (0 for an invalid description); calls that share one must be ordered. */
+/* Workspace of a call of up to max_tokens tokens (0 for an invalid description); that of the backward pass serves both. Calls that
+ * share one must be ordered. */
 size_t moe_adapters_workspace_bytes(const moeq_adapters *adapters, int32_t max_tokens, int32_t backward);
 
 /* y[t] = base[t] + scale_a B_a A_a x[t], a = ids[t]; a row whose id is outside [0, n_adapters) has no adapter: y = base.
