@@ -9,8 +9,12 @@
 // products of pieces whose places add up to 2 or less are taken (those left out are below 2^-23 of the product) and summed in fp32.
 // bf16 with bf16 and fp16 with fp16 are one product. h and g are held as three pieces.
 //
+// Requests. Loads stand in straight lines without conditions, at addresses that are moved into the matrix where a piece would pass its
+// end (and what comes twice by that meets a zero or is not stored): behind a condition the compiler waits for every load under way
+// instead of counting them.
+//
 // Order of the rows. k_adapter_plan sorts them by adapter, every adapter's rows padded to whole tiles of TP (places; rowof[place] is
-// the row or -1). Calls of up to kInlineTokens rows find their tiles by themselves: the tile b holds row b's adapter and those of
+// the row, or ~row in padding, where row is one of the same adapter: it is read again and counts nothing). Calls of up to kInlineTokens rows find their tiles by themselves: the tile b holds row b's adapter and those of
 // its rows from b on, where b is each 16th of them.
 #include <algorithm>
 
@@ -25,16 +29,17 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kInlineTokens = 64;
 
-// ---- operands of the matrix instructions ----
+// ---- operands of the matrix instructions: eight elements as they lie in memory, 4 words (16-bit types) or 8 ----
 template <typename T> constexpr int kPieces = sizeof(T) == 4 ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;
+template <typename T> constexpr int kWords = 2 * sizeof(T);
+template <typename T> struct Eight { uint32_t w[kWords<T>]; };
 
-struct Bits8 { uint32_t w[4]; };      // eight 16-bit elements
-
-__device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
 // The upper 16 bits of eight fp32 values as bf16, which are then taken off the values.
 __device__ __forceinline__ bf16x8 peel(float (&v)[8]) {
-  Bits8 b;
+  Eight<__bf16> b;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t x = __builtin_bit_cast(uint32_t, v[2 * i]), y = __builtin_bit_cast(uint32_t, v[2 * i + 1]);
@@ -44,19 +49,56 @@ __device__ __forceinline__ bf16x8 peel(float (&v)[8]) {
   }
   return __builtin_bit_cast(bf16x8, b);
 }
+__device__ __forceinline__ void cut(float (&f)[8], bf16x8 (&p)[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) p[i] = peel(f);
+}
 // Eight elements as pieces.
 template <typename T>
-__device__ __forceinline__ void cut(const T (&v)[8], bf16x8 (&p)[kPieces<T>]) {
+__device__ __forceinline__ void cut(const Eight<T>& v, bf16x8 (&p)[kPieces<T>]) {
   if constexpr (kPieces<T> == 1) {
-    __builtin_memcpy(&p[0], v, 16);
+    p[0] = __builtin_bit_cast(bf16x8, v);
   } else {
     float f[8];
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (float)v[i];
+      for (int i = 0; i < 8; ++i) f[i] = __builtin_bit_cast(float, v.w[i]);
+    } else {
+      const f16x8 h = __builtin_bit_cast(f16x8, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = (float)h[i];
+    }
 #pragma unroll
     for (int i = 0; i < kPieces<T>; ++i) p[i] = peel(f);
   }
 }
+// Operand j of the N that lie beside each other in eight rows of memory: v[e] holds N elements of row e.
+template <typename T, int N>
+__device__ __forceinline__ Eight<T> column(const uint32_t (&v)[8][(N * sizeof(T) + 3) / 4], int j) {
+  Eight<T> r;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.w[e] = v[e][j];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = j % 2 ? high_halves(v[2 * i][j / 2], v[2 * i + 1][j / 2]) : low_halves(v[2 * i][j / 2], v[2 * i + 1][j / 2]);
+  }
+  return r;
+}
+template <typename T, int N>
+__device__ __forceinline__ void load_words(uint32_t (&v)[(N * sizeof(T) + 3) / 4], const T* p) {
+  if constexpr (N * sizeof(T) == 2) {
+    uint16_t u;
+    __builtin_memcpy(&u, p, 2);
+    v[0] = u;
+  } else {
+    __builtin_memcpy(v, p, N * sizeof(T));
+  }
+}
+
+// Matrix instructions work on all lanes, whatever is masked off, and a short branch that no lane takes may be run masked instead of
+// jumped over: every condition around them has to be one that the compiler knows to be the same for the whole wavefront.
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 __device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // Operands of several pieces: the rows of the product from a, the columns from b.
@@ -70,167 +112,182 @@ __device__ __forceinline__ f32x4 mma(const bf16x8 (&a)[NA], const bf16x8 (&b)[NB
   return c;
 }
 
-template <typename T>
-__device__ __forceinline__ void load8(T (&v)[8], const T* p) { __builtin_memcpy(v, p, sizeof(v)); }
-template <typename T>
-__device__ __forceinline__ void load8_some(T (&v)[8], const T* p, int n) {
-  if (n >= 8) return load8(v, p);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0.f;
-}
-
 // ---- the plan ----
 struct Segment { int32_t a, from, to, part; };      // rows of an adapter in places [from, to); part: index of its partial sums, or -1
 struct Plan {
   int32_t *rowof, *tile_adapter;      // [places], [places / TP]: the adapter of a tile, n: none, -1: not used
   Segment* segments;                  // backward: the work items of the weights' gradients
   Segment* split;                     // adapters of several segments: {adapter, first part, number of parts}
-  int32_t places, tiles, n_segments, n_split, seg_rows;
+  int32_t places, tiles, n_segments, n_split, seg_shift;
 };
 
-__global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict__ ids, int T, int64_t run, int n, int TP, Plan plan) {
-  __shared__ int cnt[kSortCounts], start[kSortMaxExperts + 2], total[kSortMaxExperts + 2], segs[kSortMaxExperts + 2], parts[kSortMaxExperts + 2], n_split;
+__global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict__ ids, int T, int run, int n, int TP, Plan plan) {
+  __shared__ int cnt[kSortCounts], start[kSortMaxExperts + 1], total[kSortMaxExperts + 1], segs[kSortMaxExperts + 1], parts[kSortMaxExperts + 1], n_split;
   if (threadIdx.x == 0) n_split = 0;
-  sort_count(ids, 0, T, run, n, cnt);
-  for (int e = threadIdx.x; e <= n; e += blockDim.x) {
-    total[e] = sort_total(cnt, n, e);
-    start[e] = (total[e] + TP - 1) / TP * TP;
-    const int s = max(1, (start[e] + plan.seg_rows - 1) / max(1, plan.seg_rows));
-    segs[e] = s;
-    parts[e] = s > 1 && e < n ? s : 0;
-  }
-  __syncthreads();
-  sort_scan(n, start);
-  const int end = start[n] + (total[n] + TP - 1) / TP * TP;
-  for (int e = threadIdx.x; e <= n; e += blockDim.x)
-    for (int i = total[e]; i % TP; ++i) plan.rowof[start[e] + i] = -1;
   // the bin of a place: the last one that starts at or before it
-  auto bin_of = [&](const int* from, int at) {
+  auto last_at = [&](const int* from, int at) {
     int lo = 0, hi = n + 1;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (from[mid] <= at) lo = mid; else hi = mid;
+      const bool in = from[mid] <= at;
+      lo = in ? mid : lo;
+      hi = in ? hi : mid;
     }
     return lo;
   };
-  for (int i = threadIdx.x; i < plan.tiles; i += blockDim.x) plan.tile_adapter[i] = i * TP < end ? bin_of(start, i * TP) : -1;
+  sort_pairs(ids, T, run, n, cnt,
+             [&](int e, int all) {
+               const int rows = (all + TP - 1) & -TP, s = max(1, (rows + (1 << plan.seg_shift) - 1) >> plan.seg_shift);
+               total[e] = all;
+               start[e] = rows;
+               segs[e] = s;
+               parts[e] = s > 1 && e < n ? s : 0;
+             },
+             [&] {
+               // three scans by three wavefronts (by one after the other in workgroups of fewer)
+               const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
+               for (int k = wave; k < (plan.segments ? 3 : 1); k += waves) sort_scan(n, k == 0 ? start : k == 1 ? segs : parts);
+             },
+             [&](int i, int number, int e) {
+               const int p = start[e] + number;
+               plan.rowof[p] = i;
+               if (number == 0)
+                 for (int k = total[e]; k % TP; ++k) plan.rowof[p + k] = ~i;
+             });
+  const int end = start[n] + ((total[n] + TP - 1) & -TP);
+  for (int i = threadIdx.x; i < plan.tiles; i += blockDim.x) plan.tile_adapter[i] = i * TP < end ? last_at(start, i * TP) : -1;
   if (plan.segments) {
-    sort_scan(n, segs);
-    sort_scan(n, parts);
     for (int i = threadIdx.x; i < plan.n_segments; i += blockDim.x) {
-      const int a = bin_of(segs, i);
+      const int a = last_at(segs, i);
       Segment s{-1, 0, 0, -1};
       if (a < n) {
-        const int k = i - segs[a], rows = (total[a] + TP - 1) / TP * TP, many = segs[a + 1] - segs[a];
+        const int k = i - segs[a], rows = (total[a] + TP - 1) & -TP, many = segs[a + 1] - segs[a];
         s.a = a;
-        s.from = start[a] + k * plan.seg_rows;
-        s.to = start[a] + min((k + 1) * plan.seg_rows, rows);
-        if (many > 1) s.part = parts[a] + k;
+        s.from = start[a] + (k << plan.seg_shift);
+        s.to = start[a] + min((k + 1) << plan.seg_shift, rows);
+        if (many > 1) {
+          s.part = parts[a] + k;
+          if (k == 0) plan.split[atomicAdd(&n_split, 1)] = Segment{a, parts[a], many, 0};      // (in any order: each is added up by itself)
+        }
       }
       plan.segments[i] = s;
     }
-    for (int a = threadIdx.x; a < n; a += blockDim.x)       // (in any order: each is added up by itself)
-      if (segs[a + 1] - segs[a] > 1) plan.split[atomicAdd(&n_split, 1)] = Segment{a, parts[a], segs[a + 1] - segs[a], 0};
     __syncthreads();
     for (int i = n_split + threadIdx.x; i < plan.n_split; i += blockDim.x) plan.split[i] = Segment{-1, 0, 0, 0};
   }
-  sort_place(ids, 0, T, run, n, start, cnt, [&](int i, int p, int) { plan.rowof[p] = i; });
 }
 
-// The tile of a workgroup: its adapter (n: none; -1: nothing to do) and its rows, 16 MT of them from place 16 MT tile.
-template <int ROWS>
-__device__ __forceinline__ int find_tile(const Plan& plan, const int32_t* ids, int T, int n, int TP, int tile, int* rows) {
-  if (plan.tile_adapter) {
-    const int a = plan.tile_adapter[tile * ROWS / TP];
-    if (threadIdx.x < ROWS) rows[threadIdx.x] = a < 0 ? -1 : plan.rowof[tile * ROWS + threadIdx.x];
-    __syncthreads();
-    return a;
-  }
+// A tile of 16 rows: its adapter (n: none; -1: nothing to do), and the row of lane m = lane % 16 (~row: padding). By every wavefront
+// for itself.
+template <bool FEW>
+__device__ __forceinline__ int find_tile(const Plan& plan, const int32_t* ids, int T, int n, int TP, int tile, int& row) {
   const int lane = threadIdx.x & 63;
-  const int id = lane < T ? key_of(ids, lane, n) : -1, mine = __builtin_amdgcn_readlane(id, tile);
+  if constexpr (!FEW) {
+    row = plan.rowof[tile * 16 + (lane & 15)];
+    return plan.tile_adapter[tile * 16 / TP];
+  }
+  const int id = lane < T ? bin_of(ids[lane], n) : -1, mine = __builtin_amdgcn_readlane(id, tile);
   const uint64_t same = __ballot(id == mine);
   const int before = __popcll(same & ((1ull << tile) - 1));
-  if (before % 16) return -1;
-  if (threadIdx.x < 16) rows[threadIdx.x] = -1;
-  __syncthreads();
-  if (threadIdx.x < 64 && id == mine) {
-    const int k = __popcll(same & ((1ull << lane) - 1)) - before;
-    if (k >= 0 && k < 16) rows[k] = lane;
-  }
-  __syncthreads();
-  return mine;
+  // the tile's rows send their numbers to the lanes that take them; a lane that gets none reads 0
+  const int k = __popcll(same & ((1ull << lane) - 1)) - before;
+  int got = 0;
+  if (id == mine && k >= 0 && k < 16) got = lane + 1;
+  got = __builtin_amdgcn_ds_permute(4 * (got ? k : 63), got);      // (lanes that send none send 0 to a lane that nobody asks)
+  row = __shfl(got, lane & 15) - 1;
+  return before % 16 ? -1 : mine;
 }
 
-// h as bf16 pieces in the two orders that the products need: by place (rank contiguous, RK of it, zeros beyond the rank), and by
-// rank (places contiguous).
+// h on its way from the narrowing to the widening products. Sorted calls: as bf16 pieces in the two orders that the products need, by
+// place (an operand's slots contiguous) and by rank (places contiguous). Calls of few rows: in fp32 by row, one part per share of the columns.
 struct Pieces {
   uint16_t* by_place;      // [places][3][RK] or null
-  uint16_t* by_rank;       // [3][16 RT][places] or null
-  int32_t RK, RR, places;
+  uint16_t* by_rank;       // [3][RR][places] or null
+  float* parts;            // [splits][T][RR] or null
+  int32_t RK, RR, places, splits;
 };
+// Slots of the widening product's operands, RK of them in groups of eight: the rank index that a slot takes its weights from. The last
+// group, where the rank is no multiple of eight, begins before its place, so that eight elements can be read; a rank below eight takes
+// its last four, or single ones. h is zero in the slots that come twice by that.
+__device__ __forceinline__ int slot_source(int slot, int rank) {
+  const int e = slot & 7;
+  return rank >= 8 ? min(slot - e, rank - 8) + e : rank >= 4 ? (e < 4 ? e : rank - 8 + e) : min(e, rank - 1);
+}
+__device__ __forceinline__ int slot_of(int r, int rank) {
+  const int g = r & ~7;
+  return rank >= 8 ? (g + 8 <= rank ? r : g + r - (rank - 8)) : rank >= 4 ? (r < 4 ? r : r + 8 - rank) : r;
+}
 
-// ---- h = scale * (rows) A^T: products of 16 (rank) x 16 MT (rows), the columns split over the wavefronts ----
-// A rank index: of wavefront lane m of the product's rows and tile j. Beyond the rank the last ones are computed again.
+// ---- h = scale * (rows) A^T: products of 16 (rank) x 16 MT (rows), the columns split over the wavefronts (and workgroups) ----
+// A rank index: of lane m of the product's rows and tile j. Beyond the rank the last ones are computed again.
 template <int RT>
 __device__ __forceinline__ int rank_of(int m, int j, int rank) { return min(RT * m, rank - RT) + j; }
 
-constexpr int kShrinkWaves = 8;
-
 template <typename X, typename W, int RT, int MT, bool TRANS>
 struct Shrink {
-  static constexpr bool kSame16 = std::is_same<X, W>::value && sizeof(X) == 2;
+  static constexpr bool kHalf = std::is_same<X, _Float16>::value && std::is_same<W, _Float16>::value;
   static constexpr int KS = sizeof(X) == 2 && sizeof(W) == 2 ? 2 : 1;      // 32-column steps of a unit: 128 bytes of a row
-  struct Unit { X x[KS][MT][8]; W w[KS][RT][8]; };
+  static constexpr int kWidth = 32 * KS;
+  // units that are under way in a wavefront: some 64 registers of them
+  static constexpr int kRegs = KS * (MT * kWords<X> + (TRANS ? 8 * ((RT * (int)sizeof(W) + 3) / 4) : RT * kWords<W>)), DEPTH = kRegs <= 16 ? 4 : kRegs <= 24 ? 3 : 2;
+  struct Unit {
+    Eight<X> x[KS][MT];
+    Eight<W> w[TRANS ? 1 : KS][TRANS ? 1 : RT];
+    uint32_t t[TRANS ? KS : 1][8][(RT * sizeof(W) + 3) / 4];
+  };
 
   const X* xrow[MT];
   const W* wrow;
-  int64_t wstep;
   int d, rank, m, q;
 
-  template <bool TAIL>
   __device__ __forceinline__ void load(Unit& u, int unit) const {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const int c = (unit * KS + s) * 32 + 8 * q, left = d - c;
+      const int c = min(unit * kWidth + 32 * s + 8 * q, d - 8);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        if (TAIL) load8_some(u.x[s][t], xrow[t] + c, left); else load8(u.x[s][t], xrow[t] + c);
-      }
+      for (int t = 0; t < MT; ++t) load_words<X, 8>(u.x[s][t].w, xrow[t] + c);
       if constexpr (!TRANS) {
 #pragma unroll
-        for (int j = 0; j < RT; ++j) {
-          const W* p = wrow + (int64_t)rank_of<RT>(m, j, rank) * d + c;
-          if (TAIL) load8_some(u.w[s][j], p, left); else load8(u.w[s][j], p);
-        }
+        for (int j = 0; j < RT; ++j) load_words<W, 8>(u.w[s][j].w, wrow + (int64_t)rank_of<RT>(m, j, rank) * d + c);
       } else {
         const W* p = wrow + (int64_t)c * rank + rank_of<RT>(m, 0, rank);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          W v[RT] = {};
-          if (!TAIL || e < left) __builtin_memcpy(v, p + e * rank, sizeof(v));
-#pragma unroll
-          for (int j = 0; j < RT; ++j) u.w[s][j][e] = v[j];
-        }
+        for (int e = 0; e < 8; ++e) load_words<W, RT>(u.t[s][e], p + e * rank);
       }
     }
   }
-  __device__ __forceinline__ void multiply(const Unit& u, f32x4 (&acc)[RT][MT]) const {
+  __device__ __forceinline__ void multiply(Unit& u, int unit, f32x4 (&acc)[RT][MT]) const {
+    if ((unit + 1) * kWidth > d) {
+      // the last columns: what was read before a piece's own place counts nothing
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int c = unit * kWidth + 32 * s + 8 * q, lead = c - min(c, d - 8);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int i = 0; i < kWords<X>; ++i) {
+            const uint32_t keep = sizeof(X) == 4 ? (i >= lead ? ~0u : 0u) : (2 * i >= lead ? 0xffffu : 0u) | (2 * i + 1 >= lead ? 0xffff0000u : 0u);
+            u.x[s][t].w[i] &= keep;
+          }
+      }
+    }
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      if constexpr (std::is_same<X, _Float16>::value && kSame16) {
+      Eight<W> w[RT];
+#pragma unroll
+      for (int j = 0; j < RT; ++j) {
+        if constexpr (TRANS) w[j] = column<W, RT>(u.t[s], j); else w[j] = u.w[s][j];
+      }
+      if constexpr (kHalf) {
 #pragma unroll
         for (int j = 0; j < RT; ++j)
 #pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            f16x8 a, b;
-            __builtin_memcpy(&a, u.w[s][j], 16);
-            __builtin_memcpy(&b, u.x[s][t], 16);
-            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, acc[j][t], 0, 0, 0);
-          }
+          for (int t = 0; t < MT; ++t)
+            acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w[j]), __builtin_bit_cast(f16x8, u.x[s][t]), acc[j][t], 0, 0, 0);
       } else {
         bf16x8 a[RT][kPieces<W>], b[MT][kPieces<X>];
 #pragma unroll
-        for (int j = 0; j < RT; ++j) cut(u.w[s][j], a[j]);
+        for (int j = 0; j < RT; ++j) cut(w[j], a[j]);
 #pragma unroll
         for (int t = 0; t < MT; ++t) cut(u.x[s][t], b[t]);
 #pragma unroll
@@ -240,176 +297,237 @@ struct Shrink {
       }
     }
   }
+  // The units first, first + step, ... below end.
+  __device__ __forceinline__ void run(int first, int step, int end, f32x4 (&acc)[RT][MT]) const {
+    const int n = first < end ? (end - first + step - 1) / step : 0, full = n / DEPTH, rest = n - full * DEPTH;
+    Unit u[DEPTH];
+    int at = first;
+    if (full) {
+#pragma unroll
+      for (int i = 0; i < DEPTH; ++i) load(u[i], at + i * step);
+      for (int k = 1; k < full; ++k) {
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i, at += step) {
+          multiply(u[i], at, acc);
+          load(u[i], at + DEPTH * step);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < DEPTH; ++i, at += step) multiply(u[i], at, acc);
+    }
+    if (rest) {
+#pragma unroll
+      for (int i = 0; i < DEPTH - 1; ++i) load(u[i], at + (i < rest ? i : 0) * step);
+#pragma unroll
+      for (int i = 0; i < DEPTH - 1; ++i)
+        if (i < rest) multiply(u[i], at + i * step, acc);
+    }
+  }
 };
 
-template <typename X, typename W, int RT, int MT, bool TRANS>
+template <typename X, typename W, int RT, int MT, bool TRANS, int WAVES, bool FEW>
 __device__ __forceinline__ void shrink(const AdapterArgs& P, const Plan& plan, int TP, const void* in, int64_t stride, int d, const Pieces& h,
-                                       f32x4* red, int* rows) {
+                                       f32x4* red) {
   using S = Shrink<X, W, RT, MT, TRANS>;
-  const int tile = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int a = find_tile<16 * MT>(plan, P.ids, P.T, P.n, TP, tile, rows);
+  const int tile = blockIdx.x * MT, lane = threadIdx.x & 63, wave = wave_index();
+  int rows[MT];
+  const int a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile, rows[0]);
   if (a < 0 || a == P.n) return;
+#pragma unroll
+  for (int t = 1; t < MT; ++t) find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile + t, rows[t]);
   S s;
   s.d = d, s.rank = P.rank, s.m = lane & 15, s.q = lane >> 4;
 #pragma unroll
-  for (int t = 0; t < MT; ++t) s.xrow[t] = (const X*)in + max(rows[16 * t + s.m], 0) * stride;      // (columns of the product do not meet: padding may hold any row)
+  for (int t = 0; t < MT; ++t) s.xrow[t] = (const X*)in + (rows[t] ^ (rows[t] >> 31)) * stride;      // (columns of the product do not meet: padding may hold any row)
   s.wrow = (const W*)(TRANS ? P.B : P.A) + (int64_t)a * P.rank * d;
   f32x4 acc[RT][MT] = {};
-  const int width = 32 * S::KS, whole = d / width;
-  typename S::Unit u[2];
-  int k = wave;
-  if (k < whole) s.template load<false>(u[0], k);
-  while (k < whole) {
-    const int k1 = k + kShrinkWaves;
-    if (k1 < whole) s.template load<false>(u[1], k1);
-    s.multiply(u[0], acc);
-    if (k1 >= whole) break;
-    k = k1 + kShrinkWaves;
-    if (k < whole) s.template load<false>(u[0], k);
-    s.multiply(u[1], acc);
-  }
-  if (whole * width < d && wave == whole % kShrinkWaves) {
-    s.template load<true>(u[0], whole);
-    s.multiply(u[0], acc);
-  }
+  const int units = (d + S::kWidth - 1) / S::kWidth;
+  s.run(FEW ? blockIdx.y * WAVES + wave : wave, FEW ? WAVES * h.splits : WAVES, units, acc);
 #pragma unroll
-  for (int half = 1; half >= 0; --half) {                      // eight wavefronts to four, and those below
-    if (wave / (kShrinkWaves / 2) == half)
+  for (int half = 1; half >= 0; --half) {                      // the upper half of the wavefronts, and the lower one added to it
+    if (wave / (WAVES / 2) == half)
 #pragma unroll
       for (int j = 0; j < RT; ++j)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          f32x4& v = red[(((wave % (kShrinkWaves / 2)) * RT + j) * MT + t) * 64 + lane];
+          f32x4& v = red[(((wave % (WAVES / 2)) * RT + j) * MT + t) * 64 + lane];
           v = half ? acc[j][t] : acc[j][t] + v;
         }
     __syncthreads();
   }
   const float scale = P.scale[a];
-  for (int i = threadIdx.x; i < RT * MT * 64; i += blockDim.x) {
-    const int l = i & 63, t = (i >> 6) % MT, j = (i >> 6) / MT, row = rows[16 * t + (l & 15)], place = (tile * MT + t) * 16 + (l & 15);
+  for (int i = threadIdx.x; i < RT * MT * 64; i += WAVES * 64) {
+    const int t = (i >> 6) % MT, j = (i >> 6) / MT, row = MT == 1 || t == 0 ? rows[0] : rows[MT - 1], place = (tile + t) * 16 + s.m;
     f32x4 v = red[i];
 #pragma unroll
-    for (int w = 1; w < kShrinkWaves / 2; ++w) v += red[w * RT * MT * 64 + i];
+    for (int w = 1; w < WAVES / 2; ++w) v += red[w * RT * MT * 64 + i];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int r = rank_of<RT>(4 * (l >> 4) + e, j, P.rank);      // (an index that comes twice has the same sums twice)
-      float f = row < 0 ? 0.f : v[e] * scale;
+      const int r = rank_of<RT>(4 * s.q + e, j, P.rank);      // (an index that comes twice has the same sums twice)
+      if constexpr (FEW) {
+        if (row >= 0) h.parts[((int64_t)blockIdx.y * P.T + row) * h.RR + r] = v[e] * scale;
+      } else {
+        float f = row < 0 ? 0.f : v[e] * scale;
 #pragma unroll
-      for (int p = 0; p < 3; ++p) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, f);
-        f -= __builtin_bit_cast(float, b & 0xffff0000u);
-        if (h.by_place) h.by_place[((int64_t)place * 3 + p) * h.RK + r] = b >> 16;
-        if (h.by_rank) h.by_rank[(int64_t)(p * h.RR + r) * h.places + place] = b >> 16;
+        for (int p = 0; p < 3; ++p) {
+          const uint32_t b = __builtin_bit_cast(uint32_t, f);
+          f -= __builtin_bit_cast(float, b & 0xffff0000u);
+          if (h.by_place) h.by_place[((int64_t)place * 3 + p) * h.RK + slot_of(r, P.rank)] = b >> 16;
+          if (h.by_rank) h.by_rank[(int64_t)(p * h.RR + r) * h.places + place] = b >> 16;
+        }
       }
     }
   }
-  if (h.by_place)
-    for (int i = threadIdx.x; i < 48 * MT * (h.RK - P.rank); i += blockDim.x)
-      h.by_place[((int64_t)tile * MT * 48 + i / (h.RK - P.rank)) * h.RK + P.rank + i % (h.RK - P.rank)] = 0;
+  if (!FEW && h.by_place && P.rank < h.RK)
+    for (int i = threadIdx.x; i < 48 * MT * h.RK; i += WAVES * 64) {
+      const int slot = i & (h.RK - 1), r = slot_source(slot, P.rank);
+      if (slot_of(r, P.rank) != slot) h.by_place[(int64_t)tile * 48 * h.RK + i] = 0;
+    }
 }
 
-template <typename W, int RT, int MT>
-__global__ __launch_bounds__(kShrinkWaves * 64) void k_adapter_down(AdapterArgs P, Plan plan, int TP, Pieces h) {
-  __shared__ f32x4 red[kShrinkWaves / 2 * RT * MT * 64];
-  __shared__ int rows[16 * MT];
-  shrink<W, W, RT, MT, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, red, rows);
+template <typename W, int RT, int MT, int WAVES, bool FEW>
+__global__ __launch_bounds__(WAVES * 64) void k_adapter_down(AdapterArgs P, Plan plan, int TP, Pieces h) {
+  __shared__ f32x4 red[WAVES / 2 * RT * MT * 64];
+  shrink<W, W, RT, MT, false, WAVES, FEW>(P, plan, TP, P.x, P.x_stride, P.d_in, h, red);
 }
 // Backward: h of the rows of x in the first half of the grid's second dimension, g of those of dy in the other.
-template <typename W, typename Y, int RT, int MT>
-__global__ __launch_bounds__(kShrinkWaves * 64) void k_adapter_down_both(AdapterArgs P, Plan plan, int TP, Pieces h, Pieces g) {
-  __shared__ f32x4 red[kShrinkWaves / 2 * RT * MT * 64];
-  __shared__ int rows[16 * MT];
-  if (blockIdx.y == 0) shrink<W, W, RT, MT, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, red, rows);
-  else shrink<Y, W, RT, MT, true>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, red, rows);
+template <typename W, typename Y, int RT, int MT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_adapter_down_both(AdapterArgs P, Plan plan, int TP, Pieces h, Pieces g) {
+  __shared__ f32x4 red[WAVES / 2 * RT * MT * 64];
+  if (blockIdx.y == 0) shrink<W, W, RT, MT, false, WAVES, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, red);
+  else shrink<Y, W, RT, MT, true, WAVES, false>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, red);
 }
 
-// ---- out = base + h B^T (TRANS: + g A): a wavefront holds the weights of 16 NJ columns and takes 16 rows at a time ----
-// Column of the product's row 4 q + i of tile j: four lanes store 64 consecutive bytes.
-template <typename Y, int NJ>
-__device__ __forceinline__ int column_of(int m, int j) {
-  constexpr int VE = 16 / sizeof(Y);
-  return 4 * VE * ((m & 3) * (NJ / VE) + j / VE) + VE * (m >> 2) + j % VE;
-}
+// ---- out = base + h B^T (TRANS: + g A): a wavefront takes 16 NJ columns of 16 MT rows ----
+// Columns of the product's row 4 q + i, in groups of VE that are 16 bytes of the output: four lanes store 64 consecutive bytes. Group g
+// of NJ / VE; a group that would pass the last column begins before it.
+template <typename Y, typename W, int RKS, int NJ, int MT, bool TRANS, bool FEW>
+__global__ __launch_bounds__(256) void k_adapter_up(AdapterArgs P, Plan plan, int TP, Pieces hp, int d) {
+  constexpr int VE = 16 / sizeof(Y), NG = NJ / VE;
+  const int lane = threadIdx.x & 63, c0 = (blockIdx.x * 4 + wave_index()) * 16 * NJ, m = lane & 15, q = lane >> 4, rank = P.rank;
+  if (c0 >= d) return;
+  const int tile = blockIdx.y * MT;
+  int rows[MT];
+  const int a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile, rows[0]);
+  if (a < 0) return;
+#pragma unroll
+  for (int t = 1; t < MT; ++t) find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile + t, rows[t]);
+  auto group = [&](int row, int g) { return c0 + 4 * VE * ((row & 3) * NG + g) + VE * (row >> 2); };
 
-template <typename Y, typename W, int RKS, int NJ, bool TRANS>
-__global__ __launch_bounds__(256) void k_adapter_up(AdapterArgs P, Plan plan, int TP, Pieces h, int d, int per) {
-  constexpr int VE = 16 / sizeof(Y), NW = kPieces<W>;
-  __shared__ int rows[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
-  const int c0 = (blockIdx.x * 4 + wave) * 16 * NJ, rank = P.rank;
-  bf16x8 w[NJ][RKS][NW];
-  int held = -1;
-  for (int tile = blockIdx.y * per; tile < (int)(blockIdx.y + 1) * per && tile < plan.places / 16; ++tile) {
-    __syncthreads();
-    const int a = find_tile<16>(plan, P.ids, P.T, P.n, TP, tile, rows);
-    if (a < 0) { if (plan.tile_adapter) return; continue; }
-    if (c0 >= d) continue;
-    f32x4 acc[NJ] = {};
-    if (a < P.n) {
-      if (a != held) {
-        held = a;
-        const W* W0 = (const W*)(TRANS ? P.A : P.B) + (int64_t)a * rank * d;
+  struct Group { uint32_t w[4]; };
+  Group base[MT][4][NG] = {};
+  if (P.base)
 #pragma unroll
-        for (int s = 0; s < RKS; ++s) {
-          const int r0 = 32 * s + 8 * q;
-          if constexpr (!TRANS) {
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-              W v[8] = {};
-              if (r0 < rank) load8_some(v, W0 + (int64_t)min(c0 + column_of<Y, NJ>(m, j), d - 1) * rank + r0, rank - r0);
-              cut(v, w[j][s]);
-            }
-          } else {
-#pragma unroll
-            for (int j0 = 0; j0 < NJ; j0 += 4) {
-              const int c = c0 + column_of<Y, NJ>(m, j0);
-              W v[4][8] = {};
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (r0 + e < rank) {
-                  const W* p = W0 + (int64_t)(r0 + e) * d + c;
-                  W u[4] = {};
-                  if (c + 4 <= d) {
-                    __builtin_memcpy(u, p, sizeof(u));
-                  } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                      if (c + j < d) u[j] = p[j];
-                  }
-#pragma unroll
-                  for (int j = 0; j < 4; ++j) v[j][e] = u[j];
-                }
-#pragma unroll
-              for (int j = 0; j < 4; ++j) cut(v[j], w[j0 + j][s]);
-            }
-          }
-        }
-      }
-      const uint16_t* hp = h.by_place + (int64_t)(tile * 16 + m) * 3 * h.RK + 8 * q;
-      bf16x8 b[RKS][3];
-#pragma unroll
-      for (int s = 0; s < RKS; ++s)
-#pragma unroll
-        for (int p = 0; p < 3; ++p) __builtin_memcpy(&b[s][p], hp + p * h.RK + 32 * s, 16);
-#pragma unroll
-      for (int s = 0; s < RKS; ++s)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[j] = mma(w[j][s], b[s], acc[j]);
-    }
-    const int row = rows[m];
-    if (row >= 0)
+    for (int t = 0; t < MT; ++t) {
+      const Y* from = (const Y*)P.base + (rows[t] ^ (rows[t] >> 31)) * P.base_stride;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int g = 0; g < NJ / VE; ++g) {
-          const int c = c0 + column_of<Y, NJ>(4 * q + i, g * VE), n = d - c;
-          if (n <= 0) continue;
-          float v[VE] = {};
-          if (P.base) load_some(v, (const Y*)P.base + row * P.base_stride + c, n);
+        for (int g = 0; g < NG; ++g) __builtin_memcpy(base[t][i][g].w, from + min(group(4 * q + i, g), d - VE), 16);
+    }
+  f32x4 acc[MT][NJ] = {};
+  if (a < P.n) {
+    const W* W0 = (const W*)(TRANS ? P.A : P.B) + (int64_t)a * rank * d;
+    // weights: eight slots of a column (a row of B), or four columns of eight slots (rows of A)
+    Eight<W> w[TRANS ? 1 : RKS][TRANS ? 1 : NJ];
+    uint32_t wt[TRANS ? RKS : 1][TRANS ? NJ / 4 : 1][8][sizeof(W)];
+    if constexpr (!TRANS) {
+      if (rank >= 8) {
 #pragma unroll
-          for (int e = 0; e < VE; ++e) v[e] += acc[g * VE + e][i];
-          store_some((Y*)P.out + row * P.out_stride + c, v, n);
+        for (int s = 0; s < RKS; ++s)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+            load_words<W, 8>(w[s][j].w, W0 + (int64_t)(min(group(m, j / VE), d - VE) + j % VE) * rank + min(32 * s + 8 * q, rank - 8));
+      } else {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const W* p = W0 + (int64_t)(min(group(m, j / VE), d - VE) + j % VE) * rank;
+          W v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = p[slot_source(e, rank)];
+          __builtin_memcpy(w[0][j].w, v, sizeof(v));
         }
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < RKS; ++s)
+#pragma unroll
+        for (int g = 0; g < NJ / 4; ++g)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            load_words<W, 4>(wt[s][g][e], W0 + (int64_t)slot_source(32 * s + 8 * q + e, rank) * d + min(group(m, g * 4 / VE), d - VE) + g * 4 % VE);
+    }
+    bf16x8 b[MT][RKS][3];
+    if constexpr (!FEW) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int s = 0; s < RKS; ++s)
+#pragma unroll
+          for (int p = 0; p < 3; ++p)
+            __builtin_memcpy(&b[t][s][p], hp.by_place + ((int64_t)((tile + t) * 16 + m) * 3 + p) * hp.RK + 32 * s + 8 * q, 16);
+    } else {
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int s = 0; s < RKS; ++s) {
+          float f[8] = {};
+          const float* from = hp.parts + (int64_t)(rows[t] ^ (rows[t] >> 31)) * hp.RR;
+          if (rank >= 8) {
+            from += min(32 * s + 8 * q, rank - 8);
+#pragma unroll 4
+            for (int k = 0; k < hp.splits; ++k, from += (int64_t)P.T * hp.RR) {
+              float v[8];
+              __builtin_memcpy(v, from, sizeof(v));
+#pragma unroll
+              for (int e = 0; e < 8; ++e) f[e] += v[e];
+            }
+          } else {
+            for (int k = 0; k < hp.splits; ++k, from += (int64_t)P.T * hp.RR)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) f[e] += from[slot_source(e, rank)];
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int slot = 32 * s + 8 * q + e;
+            f[e] = slot_of(slot_source(slot, rank), rank) == slot ? f[e] : 0.f;
+          }
+          cut(f, b[t][s]);
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < RKS; ++s)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        Eight<W> v;
+        if constexpr (TRANS) v = column<W, 4>(wt[s][j / 4], j % 4); else v = w[s][j];
+        bf16x8 p[kPieces<W>];
+        cut(v, p);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t][j] = mma(p, b[t][s], acc[t][j]);
+      }
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    if (rows[t] < 0) continue;
+    Y* out = (Y*)P.out + rows[t] * P.out_stride;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const int c = group(4 * q + i, g), at = min(c, d - VE);
+        Y v[VE];
+        __builtin_memcpy(v, base[t][i][g].w, 16);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) v[e] = (Y)(acc[t][g * VE + e][i] + (float)v[e]);
+        if (at == c) {
+          __builtin_memcpy(out + c, v, 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VE; ++e)
+            if (at + e >= c) out[at + e] = v[e];
+        }
+      }
   }
 }
 
@@ -421,43 +539,59 @@ __device__ __forceinline__ void weight_grad(const AdapterArgs& P, const Plan& pl
   constexpr int NJ = 16 / sizeof(X);
   const Segment seg = plan.segments[blockIdx.y];
   if (seg.a < 0) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4, rank = P.rank;
-  const int c0 = slice * 16 * NJ, c = c0 + NJ * m, left = d - c;
-  const X* x = (const X*)in + c;
+  const int lane = threadIdx.x & 63, wave = wave_index(), m = lane & 15, q = lane >> 4, rank = P.rank;
+  float* to = seg.part < 0 ? out + (int64_t)seg.a * rank * d : part + (int64_t)seg.part * rank * (P.d_in + P.d_out);
+  // (lanes past the last column take the last ones again, with the same sums)
+  const int c0 = slice * 16 * NJ;
+  const X* x = (const X*)in + min(c0 + NJ * m, d - NJ);
   f32x4 acc[RT][NJ] = {};
-  for (int p = seg.from + 32 * wave; p < seg.to; p += 128) {
-    int row[8];
-    __builtin_memcpy(row, plan.rowof + p + 8 * q, 32);
-    X v[8][NJ] = {};
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (row[e] >= 0) {
-        const X* at = x + row[e] * stride;
-        if (left >= NJ) {
-          __builtin_memcpy(v[e], at, 16);
-        } else {
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-            if (j < left) v[e][j] = at[j];
-        }
-      }
-    bf16x8 a[RT][3];
+  // The rows of a step are requested a step ahead, their numbers two; h with the rows where there are registers for that.
+  constexpr bool kAhead = RT < 4;
+  struct Step { uint32_t v[8][4]; bf16x8 a[kAhead ? RT : 1][3]; };
+  auto numbers = [&](int (&row)[8], int p) { __builtin_memcpy(row, plan.rowof + min(p, seg.to - 32) + 8 * q, 32); };
+  auto request_h = [&](bf16x8 (&a)[RT][3], int p) {
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
         const int r = min(4 * RT * (m >> 2) + 4 * t + (m & 3), rank - 1);      // (rows of the product do not meet)
-        __builtin_memcpy(&a[t][k], h.by_rank + (int64_t)(k * h.RR + r) * h.places + p + 8 * q, 16);
+        __builtin_memcpy(&a[t][k], h.by_rank + (int64_t)(k * h.RR + r) * h.places + min(p, seg.to - 32) + 8 * q, 16);
       }
+  };
+  auto request = [&](Step& s, const int (&row)[8], int p) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) __builtin_memcpy(s.v[e], x + (row[e] ^ (row[e] >> 31)) * stride, 16);
+    if constexpr (kAhead) request_h(s.a, p);
+  };
+  auto multiply = [&](const Step& s, const bf16x8 (&a)[RT][3]) {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      X u[8];
       bf16x8 b[kPieces<X>];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = v[e][j];
-      cut(u, b);
+      cut(column<X, NJ>(s.v, j), b);
 #pragma unroll
       for (int t = 0; t < RT; ++t) acc[t][j] = mma(a[t], b, acc[t][j]);
+    }
+  };
+  const int first = seg.from + 32 * wave;
+  if (first < seg.to) {
+    int row[8];
+    Step next;
+    numbers(row, first);
+    request(next, row, first);
+    numbers(row, first + 128);
+    for (int p = first; p < seg.to; p += 128) {
+      const Step now = next;
+      if constexpr (kAhead) {
+        request(next, row, p + 128);
+        numbers(row, p + 256);
+        multiply(now, now.a);
+      } else {
+        bf16x8 a[RT][3];
+        request_h(a, p);
+        request(next, row, p + 128);
+        numbers(row, p + 256);
+        multiply(now, a);
+      }
     }
   }
   // four wavefronts to two, and those in the stores
@@ -477,12 +611,10 @@ __device__ __forceinline__ void weight_grad(const AdapterArgs& P, const Plan& pl
         v = acc[t][j] + v;
       }
   __syncthreads();
-  float* to = seg.part < 0 ? out + (int64_t)seg.a * rank * d : part + (int64_t)seg.part * rank * (P.d_in + P.d_out);
   for (int i = threadIdx.x; i < kTiles; i += 256) {
     // columns one after the other (dA), or the four rank indices of a column and those of its other tiles (dB)
     const int k = TRANS ? i / (4 * RT) : i % (16 * NJ), rt = TRANS ? i % (4 * RT) : i / (16 * NJ);
-    const int qq = rt / RT, t = rt % RT, r = 4 * rt, at = (t * NJ + k % NJ) * 64 + qq * 16 + k / NJ, col = c0 + k;
-    if (col >= d) continue;
+    const int qq = rt / RT, t = rt % RT, r = 4 * rt, at = (t * NJ + k % NJ) * 64 + qq * 16 + k / NJ, col = min(c0 + k / NJ * NJ, d - NJ) + k % NJ;
     const f32x4 v = red[at] + red[kTiles + at];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -491,7 +623,7 @@ __device__ __forceinline__ void weight_grad(const AdapterArgs& P, const Plan& pl
 }
 
 template <typename W, typename Y, int RT>
-__global__ __launch_bounds__(256) void k_adapter_weights(AdapterArgs P, Plan plan, Pieces h, Pieces g, int slices_a, float* part) {
+__global__ __launch_bounds__(256, RT < 4 ? 2 : 1) void k_adapter_weights(AdapterArgs P, Plan plan, Pieces h, Pieces g, int slices_a, float* part) {
   constexpr int NJ = 16 / sizeof(W) > 16 / sizeof(Y) ? 16 / sizeof(W) : 16 / sizeof(Y);
   __shared__ f32x4 red[2 * RT * NJ * 64];
   const int s = blockIdx.x;
@@ -511,77 +643,147 @@ __global__ __launch_bounds__(256) void k_adapter_join(AdapterArgs P, Plan plan, 
   }
 }
 
+// ---- rows of less than 16 bytes' worth of elements (d_in or d_out below 8): a thread or a workgroup an element, in fp32 ----
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ float block_sum(float v, float* part) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) v += __shfl_xor(v, m);
+  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = (part[0] + part[1]) + (part[2] + part[3]);
+  __syncthreads();
+  return v;
+}
+
+// h[t][j] = scale * sum of in[t][i] * W(j, i): W = A (rows of r), or B read across its rows (TRANS).
+template <typename X, typename W, bool TRANS>
+__global__ __launch_bounds__(kThreads) void k_narrow_down(AdapterArgs P, const void* in, int64_t stride, int d, float* h) {
+  __shared__ float part[4];
+  const int t = blockIdx.x, a = P.ids[t], r = P.rank;
+  const bool on = (uint32_t)a < (uint32_t)P.n;
+  for (int j = 0; j < r; ++j) {
+    float sum = 0.f;
+    if (on)
+      for (int i = threadIdx.x; i < d; i += kThreads) {
+        const W* w = (const W*)(TRANS ? P.B : P.A) + (int64_t)a * r * d + (TRANS ? (int64_t)i * r + j : (int64_t)j * d + i);
+        sum = fmaf((float)((const X*)in)[t * stride + i], (float)*w, sum);
+      }
+    sum = block_sum(sum, part);
+    if (threadIdx.x == 0) h[(int64_t)t * r + j] = on ? sum * P.scale[a] : 0.f;
+  }
+}
+
+// out[t][i] = base + sum of h[t][j] * W(i, j): W = B (rows of d_out), or A read across its rows (TRANS).
+template <typename Y, typename W, bool TRANS>
+__global__ __launch_bounds__(kThreads) void k_narrow_up(AdapterArgs P, const float* h, int d) {
+  const int t = blockIdx.y, i = blockIdx.x * kThreads + threadIdx.x, a = P.ids[t], r = P.rank;
+  if (i >= d) return;
+  float sum = 0.f;
+  if ((uint32_t)a < (uint32_t)P.n)
+    for (int j = 0; j < r; ++j) {
+      const W* w = (const W*)(TRANS ? P.A : P.B) + (int64_t)a * r * d + (TRANS ? (int64_t)j * d + i : (int64_t)i * r + j);
+      sum = fmaf(h[(int64_t)t * r + j], (float)*w, sum);
+    }
+  const float base = P.base ? (float)((const Y*)P.base)[t * P.base_stride + i] : 0.f;
+  ((Y*)P.out)[t * P.out_stride + i] = (Y)(base + sum);
+}
+
+// dW of adapter blockIdx.z, rank index blockIdx.y: dA[a][j][i] = sum of h[t][j] * in[t][i] (TRANS: at dB[a][i][j]).
+template <typename X, bool TRANS>
+__global__ __launch_bounds__(kThreads) void k_narrow_weights(AdapterArgs P, const void* in, int64_t stride, int d, const float* h, float* out) {
+  const int i = blockIdx.x * kThreads + threadIdx.x, j = blockIdx.y, a = blockIdx.z, r = P.rank;
+  if (i >= d) return;
+  float sum = 0.f;
+  for (int t = 0; t < P.T; ++t)
+    if (P.ids[t] == a) sum = fmaf(h[(int64_t)t * r + j], (float)((const X*)in)[t * stride + i], sum);
+  out[(int64_t)a * r * d + (TRANS ? (int64_t)i * r + j : (int64_t)j * d + i)] = sum;
+}
+
 // ---- host side ----
+enum Form { kNarrow, kFew, kSorted };
 struct Setup {
+  Form form;
   Plan plan;
   Pieces h, g;
-  float* part;
+  float *part, *narrow_h, *narrow_g;
   int TP, RT, RKS;
   size_t total;
 };
 
-// Rows of a segment of the weights' gradients: 1024, fewer where that leaves too few workgroups for the chip, more in long calls
-// (the partial sums are rank x (d_in + d_out) floats a segment).
-int segment_rows(const AdapterArgs& a) {
+// Rows of a segment of the weights' gradients, as a power of two: 1024, fewer where that leaves too few workgroups for the chip, more
+// in long calls (the partial sums are rank x (d_in + d_out) floats a segment).
+int segment_shift(const AdapterArgs& a) {
   const int64_t slices = (a.d_in + 127) / 128 + (a.d_out + 127) / 128;
-  int rows = 1024;
-  while (rows > 256 && slices * ((a.T + rows - 1) / rows) < 512) rows /= 2;
-  while ((a.T + rows - 1) / rows > 16) rows *= 2;
-  return rows;
+  int k = 10;
+  while (k > 8 && slices * ((a.T >> k) + 1) < 512) --k;
+  while ((a.T >> k) >= 16) ++k;
+  return k;
+}
+
+constexpr int kFewWaves = 4;
+inline int few_splits(const AdapterArgs& a) {
+  const int units = a.dtype == MOEQ_F32 ? (a.d_in + 31) / 32 : (a.d_in + 63) / 64;
+  return (units + 2 * kFewWaves - 1) / (2 * kFewWaves);
 }
 
 Setup set_up(const AdapterArgs& a, bool backward) {
   Setup s = {};
-  const bool inl = !backward && a.T <= kInlineTokens;
+  s.form = a.d_in < 8 || a.d_out < 8 ? kNarrow : !backward && a.T <= kInlineTokens ? kFew : kSorted;
   s.RT = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
   s.RKS = a.rank <= 32 ? 1 : 2;
-  s.TP = backward ? 32 : 16;
-  Plan& p = s.plan;
-  // every bin that has rows adds at most a tile less a row of padding
-  const int pad = (s.TP - 1) * std::min(a.T, a.n + 1);
-  p.places = inl ? 16 * a.T : (a.T + pad) / s.TP * s.TP;
-  p.tiles = p.places / s.TP;
-  // what is set aside never falls with the number of rows, so that the workspace of a call serves the smaller ones
-  const int room = inl || backward ? p.places : std::max(p.places, 16 * kInlineTokens);
-  const int room_split = std::min(16, a.T / 256) + pad / 256 + 1;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* q = a.ws ? (char*)a.ws + at : nullptr;
     at += (bytes + 255) / 256 * 256;
     return (void*)q;
   };
-  if (!inl) {
-    p.rowof = (int32_t*)take((size_t)room * 4);
-    p.tile_adapter = (int32_t*)take((size_t)room / s.TP * 4);
-  }
+  // what is set aside never falls with the number of rows, so that the workspace of a call serves the smaller ones
   const int RK = 32 * s.RKS, RR = 16 * s.RT;
-  auto pieces = [&](bool by_place, bool by_rank) {
-    Pieces h{nullptr, nullptr, RK, RR, p.places};
-    if (by_place) h.by_place = (uint16_t*)take((size_t)room * 3 * RK * 2);
-    if (by_rank) h.by_rank = (uint16_t*)take((size_t)room * 3 * RR * 2);
-    return h;
-  };
-  if (!backward) {
-    s.h = pieces(true, false);
-  } else {
-    p.seg_rows = segment_rows(a);
-    p.n_segments = a.n + 1 + p.places / p.seg_rows;
-    p.n_split = p.places / p.seg_rows;
-    p.segments = (Segment*)take((size_t)(a.n + 1 + room_split) * sizeof(Segment));
-    p.split = (Segment*)take((size_t)room_split * sizeof(Segment));
-    s.h = pieces(false, true);
-    s.g = pieces(a.out || !a.ws, true);
-    // (segments of at least 256 rows, at most 16 of them in the rows themselves: segment_rows)
-    s.part = (float*)take((size_t)2 * room_split * a.rank * (a.d_in + a.d_out) * 4);
+  if (s.form == kNarrow) {
+    s.narrow_h = (float*)take((size_t)a.T * a.rank * 4);
+    if (backward) s.narrow_g = (float*)take((size_t)a.T * a.rank * 4);
+  }
+  if (!backward && s.form != kNarrow) {
+    s.h = Pieces{nullptr, nullptr, (float*)take((size_t)few_splits(a) * std::min(a.T, kInlineTokens) * RR * 4), RK, RR, 0, few_splits(a)};
+    if (s.form == kSorted) at = 0;
+  }
+  if (s.form == kSorted) {
+    Plan& p = s.plan;
+    s.TP = backward || a.T >= 64 * (int64_t)a.n ? 32 : 16;
+    // every bin that has rows adds at most a tile less a row of padding (room: of either tile)
+    const int pad = (s.TP - 1) * std::min(a.T, a.n + 1), room = a.T + 31 * std::min(a.T, a.n + 1), room_split = std::min(16, a.T / 256) + room / 256 - a.T / 256 + 1;
+    p.places = (a.T + pad) / s.TP * s.TP;
+    p.tiles = p.places / s.TP;
+    p.rowof = (int32_t*)take((size_t)room * 4);
+    p.tile_adapter = (int32_t*)take((size_t)room / 16 * 4 + 4);
+    auto pieces = [&](bool by_place, bool by_rank) {
+      Pieces h{nullptr, nullptr, nullptr, RK, RR, p.places, 0};
+      if (by_place) h.by_place = (uint16_t*)take((size_t)room * 3 * RK * 2);
+      if (by_rank) h.by_rank = (uint16_t*)take((size_t)room * 3 * RR * 2);
+      return h;
+    };
+    if (!backward) {
+      s.h = pieces(true, false);
+    } else {
+      p.seg_shift = segment_shift(a);
+      p.n_segments = a.n + 1 + (p.places >> p.seg_shift);
+      p.n_split = p.places >> p.seg_shift;
+      p.segments = (Segment*)take((size_t)(a.n + 1 + room_split) * sizeof(Segment));
+      p.split = (Segment*)take((size_t)room_split * sizeof(Segment));
+      s.h = pieces(false, true);
+      s.g = pieces(a.out || !a.ws, true);
+      // (segments of at least 256 rows, at most 16 of them in the rows themselves: segment_shift)
+      s.part = (float*)take((size_t)2 * room_split * a.rank * (a.d_in + a.d_out) * 4);
+    }
   }
   s.total = at;
   return s;
 }
 
 hipError_t launch_plan(const AdapterArgs& a, const Setup& s, hipStream_t st) {
-  if (!s.plan.tile_adapter) return hipSuccess;
   const int waves = sort_waves(a.T, a.n);
-  const int64_t run = (a.T + waves * 64 - 1) / (waves * 64) * 64;
+  const int run = (a.T + waves * 64 - 1) / (waves * 64) * 64;
   hipLaunchKernelGGL(k_adapter_plan, dim3(1), dim3(waves * 64), 0, st, a.ids, a.T, run, a.n, s.TP, s.plan);
   return hipGetLastError();
 }
@@ -597,15 +799,35 @@ hipError_t with_rank(int RT, F&& f) {
   return f(std::integral_constant<int, 4>{});
 }
 
-// Rows and columns of the expanding kernel: 16-row tiles of a workgroup, which then loads its weights once for them.
-template <typename Y, typename W, int RKS, bool TRANS>
-hipError_t launch_up(const AdapterArgs& a, const Setup& s, const Pieces& h, int d, hipStream_t st) {
+template <typename Y, typename W, int RKS, int MT, bool TRANS, bool FEW>
+hipError_t launch_up(const AdapterArgs& a, const Setup& s, const Pieces& h, int d, int tiles, hipStream_t st) {
   constexpr int NJ = sizeof(W) == 4 ? 4 : 8;
-  const int cols = (d + 64 * NJ - 1) / (64 * NJ), tiles = s.plan.places / 16;
-  int per = 1;
-  while (s.plan.tile_adapter && per < 4 && (int64_t)cols * tiles / (2 * per) >= 1024) per *= 2;
-  hipLaunchKernelGGL((k_adapter_up<Y, W, RKS, NJ, TRANS>), dim3(cols, (tiles + per - 1) / per), dim3(256), 0, st, a, s.plan, s.TP, h, d, per);
+  hipLaunchKernelGGL((k_adapter_up<Y, W, RKS, NJ, MT, TRANS, FEW>), dim3((d + 64 * NJ - 1) / (64 * NJ), tiles), dim3(256), 0, st, a, s.plan, s.TP, h, d);
   return hipGetLastError();
+}
+
+hipError_t narrow_forward(const AdapterArgs& a, const Setup& s, hipStream_t st) {
+  return with_types(a, [&](auto tag, auto ytag) {
+    using W = decltype(tag);
+    using Y = decltype(ytag);
+    hipLaunchKernelGGL((k_narrow_down<W, W, false>), dim3(a.T), dim3(kThreads), 0, st, a, a.x, a.x_stride, a.d_in, s.narrow_h);
+    hipLaunchKernelGGL((k_narrow_up<Y, W, false>), dim3((a.d_out + kThreads - 1) / kThreads, a.T), dim3(kThreads), 0, st, a, s.narrow_h, a.d_out);
+    return hipGetLastError();
+  });
+}
+hipError_t narrow_backward(const AdapterArgs& a, const Setup& s, hipStream_t st) {
+  return with_types(a, [&](auto tag, auto ytag) {
+    using W = decltype(tag);
+    using Y = decltype(ytag);
+    if (a.T) {
+      hipLaunchKernelGGL((k_narrow_down<W, W, false>), dim3(a.T), dim3(kThreads), 0, st, a, a.x, a.x_stride, a.d_in, s.narrow_h);
+      hipLaunchKernelGGL((k_narrow_down<Y, W, true>), dim3(a.T), dim3(kThreads), 0, st, a, a.dy, a.dy_stride, a.d_out, s.narrow_g);
+      if (a.out) hipLaunchKernelGGL((k_narrow_up<Y, W, true>), dim3((a.d_in + kThreads - 1) / kThreads, a.T), dim3(kThreads), 0, st, a, s.narrow_g, a.d_in);
+    }
+    hipLaunchKernelGGL((k_narrow_weights<W, false>), dim3((a.d_in + kThreads - 1) / kThreads, a.rank, a.n), dim3(kThreads), 0, st, a, a.x, a.x_stride, a.d_in, s.narrow_g, a.dA);
+    hipLaunchKernelGGL((k_narrow_weights<Y, true>), dim3((a.d_out + kThreads - 1) / kThreads, a.rank, a.n), dim3(kThreads), 0, st, a, a.dy, a.dy_stride, a.d_out, s.narrow_h, a.dB);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace
@@ -613,28 +835,40 @@ hipError_t launch_up(const AdapterArgs& a, const Setup& s, const Pieces& h, int 
 size_t adapter_ws_bytes(const AdapterArgs& a, bool backward) {
   AdapterArgs b = a;
   b.ws = nullptr;
-  const size_t forward = set_up(b, false).total;
-  return backward ? std::max(forward, set_up(b, true).total) : forward;       // (what serves the backward pass serves both)
+  // (what serves the backward pass serves both, and what serves many rows the few that take another form)
+  size_t n = set_up(b, false).total;
+  if (backward) n = std::max(n, set_up(b, true).total);
+  b.T = std::min(b.T, kInlineTokens);
+  return std::max(n, set_up(b, false).total);
 }
 
 hipError_t launch_adapters_forward(const AdapterArgs& a, hipStream_t st) {
   if (a.T == 0) return hipSuccess;
   const Setup s = set_up(a, false);
-  if (hipError_t e = launch_plan(a, s, st); e != hipSuccess) return e;
+  if (s.form == kNarrow) return narrow_forward(a, s, st);
+  if (s.form == kSorted)
+    if (hipError_t e = launch_plan(a, s, st); e != hipSuccess) return e;
   return with_types(a, [&](auto tag, auto ytag) {
     using W = decltype(tag);
     using Y = decltype(ytag);
     return with_rank(s.RT, [&](auto rt) {
-      constexpr int RT = decltype(rt)::value, RKS = RT == 4 ? 2 : 1, MT = 1;
-      hipLaunchKernelGGL((k_adapter_down<W, RT, MT>), dim3(s.plan.places / (16 * MT)), dim3(kShrinkWaves * 64), 0, st, a, s.plan, s.TP, s.h);
+      constexpr int RT = decltype(rt)::value, RKS = RT == 4 ? 2 : 1;
+      if (s.form == kFew) {
+        hipLaunchKernelGGL((k_adapter_down<W, RT, 1, kFewWaves, true>), dim3(a.T, s.h.splits), dim3(kFewWaves * 64), 0, st, a, s.plan, s.TP, s.h);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        return launch_up<Y, W, RKS, 1, false, true>(a, s, s.h, a.d_out, a.T, st);
+      }
+      hipLaunchKernelGGL((k_adapter_down<W, RT, 1, 8, false>), dim3(s.plan.places / 16), dim3(512), 0, st, a, s.plan, s.TP, s.h);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-      return launch_up<Y, W, RKS, false>(a, s, s.h, a.d_out, st);
+      if (s.TP == 32) return launch_up<Y, W, RKS, 2, false, false>(a, s, s.h, a.d_out, s.plan.places / 32, st);
+      return launch_up<Y, W, RKS, 1, false, false>(a, s, s.h, a.d_out, s.plan.places / 16, st);
     });
   });
 }
 
 hipError_t launch_adapters_backward(const AdapterArgs& a, hipStream_t st) {
   const Setup s = set_up(a, true);
+  if (s.form == kNarrow) return narrow_backward(a, s, st);
   if (hipError_t e = launch_plan(a, s, st); e != hipSuccess) return e;
   return with_types(a, [&](auto tag, auto ytag) {
     using W = decltype(tag);
@@ -642,12 +876,12 @@ hipError_t launch_adapters_backward(const AdapterArgs& a, hipStream_t st) {
     return with_rank(s.RT, [&](auto rt) {
       constexpr int RT = decltype(rt)::value, RKS = RT == 4 ? 2 : 1, MT = 2;
       if (a.T) {
-        hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT>), dim3(s.plan.places / (16 * MT), 2), dim3(kShrinkWaves * 64), 0, st, a, s.plan, s.TP, s.h, s.g);
+        hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT, 8>), dim3(s.plan.places / (16 * MT), 2), dim3(512), 0, st, a, s.plan, s.TP, s.h, s.g);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         if (a.out)
-          if (hipError_t e = launch_up<Y, W, RKS, true>(a, s, s.g, a.d_in, st); e != hipSuccess) return e;
+          if (hipError_t e = launch_up<Y, W, RKS, 2, true, false>(a, s, s.g, a.d_in, s.plan.places / 32, st); e != hipSuccess) return e;
       }
-      const int sa = (a.d_in + 16 * (16 / sizeof(W)) - 1) / (16 * (16 / (int)sizeof(W))), sb = (a.d_out + 16 * (16 / (int)sizeof(Y)) - 1) / (16 * (16 / (int)sizeof(Y)));
+      const int sa = (a.d_in + 256 / (int)sizeof(W) - 1) / (256 / (int)sizeof(W)), sb = (a.d_out + 256 / (int)sizeof(Y) - 1) / (256 / (int)sizeof(Y));
       hipLaunchKernelGGL((k_adapter_weights<W, Y, RT>), dim3(sa + sb, s.plan.n_segments), dim3(256), 0, st, a, s.plan, s.h, s.g, sa, s.part);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       if (s.plan.n_split) {

@@ -11,25 +11,21 @@ namespace {
 constexpr int64_t kSortOne = 16384;      // pairs that one workgroup sorts alone
 constexpr int64_t kSortChunk = 4096;     // pairs of a workgroup beyond
 
-// Where a pair and its place are written.
-struct PutPair {
-  int E;
-  int32_t *order, *slot;
-  __device__ __forceinline__ void operator()(int i, int p, int e) const {
-    order[p] = e < E ? i : ~i;
-    slot[i] = e < E ? p : ~p;
-  }
-};
-
-__global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ idx, int64_t pairs, int64_t run, int E,
+__global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ idx, int pairs, int run, int E,
                                                    int32_t* __restrict__ offsets, int32_t* __restrict__ order, int32_t* __restrict__ slot) {
   __shared__ int cnt[kSortCounts], place[kSortMaxExperts + 1];
-  sort_count(idx, 0, pairs, run, E, cnt);
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) place[e] = sort_total(cnt, E, e);
-  __syncthreads();
-  sort_scan(E, place);
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) offsets[e] = place[e];
-  sort_place(idx, 0, pairs, run, E, place, cnt, PutPair{E, order, slot});
+  sort_pairs(idx, pairs, run, E, cnt, [&](int e, int n) { place[e] = n; },
+             [&] {
+               if (threadIdx.x < 64) {
+                 sort_scan(E, place);
+                 for (int e = threadIdx.x; e <= E; e += 64) offsets[e] = place[e];
+               }
+             },
+             [&](int i, int number, int e) {
+               const int p = place[e] + number;
+               order[p] = e < E ? i : ~i;
+               slot[i] = e < E ? p : ~p;
+             });
 }
 
 __global__ __launch_bounds__(1024) void k_sort_count(const int32_t* __restrict__ idx, int64_t pairs, int E, int32_t* __restrict__ counts) {
@@ -37,35 +33,43 @@ __global__ __launch_bounds__(1024) void k_sort_count(const int32_t* __restrict__
   for (int e = threadIdx.x; e <= E; e += blockDim.x) cnt[e] = 0;
   __syncthreads();
   const int64_t a = blockIdx.x * kSortChunk, b = min(a + kSortChunk, pairs);
-  for (int64_t i = a + threadIdx.x; i < b; i += blockDim.x) atomicAdd(&cnt[key_of(idx, i, E)], 1);
+  for (int64_t i = a + threadIdx.x; i < b; i += blockDim.x) atomicAdd(&cnt[bin_of(idx[i], E)], 1);
   __syncthreads();
   for (int e = threadIdx.x; e <= E; e += blockDim.x) counts[(int64_t)blockIdx.x * (E + 1) + e] = cnt[e];
 }
 
-__global__ __launch_bounds__(1024) void k_sort_chunk(const int32_t* __restrict__ idx, int64_t pairs, int64_t run, int E,
+__global__ __launch_bounds__(1024) void k_sort_chunk(const int32_t* __restrict__ idx, int64_t pairs, int run, int E,
                                                      const int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
                                                      int32_t* __restrict__ order, int32_t* __restrict__ slot) {
   __shared__ int cnt[kSortCounts], place[kSortMaxExperts + 1], ahead[kSortMaxExperts + 1];
   const int chunks = gridDim.x, me = blockIdx.x;
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) {
-    int before = 0, all = 0;
-    for (int c = 0; c < chunks; ++c) {
-      const int n = counts[(int64_t)c * (E + 1) + e];
-      before += c < me ? n : 0;
-      all += n;
-    }
-    place[e] = all;
-    ahead[e] = before;
-  }
-  __syncthreads();
-  sort_scan(E, place);
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) {
-    if (me == 0) offsets[e] = place[e];
-    place[e] += ahead[e];
-  }
-  const int64_t a = me * kSortChunk, b = min(a + kSortChunk, pairs);
-  sort_count(idx, a, b, run, E, cnt);                  // (its barriers also stand behind the sums above)
-  sort_place(idx, a, b, run, E, place, cnt, PutPair{E, order, slot});
+  const int64_t a = me * kSortChunk;
+  sort_pairs(idx + a, (int)min(kSortChunk, pairs - a), run, E, cnt,
+             [&](int e, int) {
+               int before = 0, all = 0;
+#pragma unroll 8
+               for (int c = 0; c < chunks; ++c) {
+                 const int v = counts[(int64_t)c * (E + 1) + e];
+                 before += c < me ? v : 0;
+                 all += v;
+               }
+               place[e] = all;
+               ahead[e] = before;
+             },
+             [&] {
+               if (threadIdx.x < 64) {
+                 sort_scan(E, place);
+                 for (int e = threadIdx.x; e <= E; e += 64) {
+                   if (me == 0) offsets[e] = place[e];
+                   ahead[e] += place[e];
+                 }
+               }
+             },
+             [&](int i, int number, int e) {
+               const int p = ahead[e] + number, pair = (int)a + i;
+               order[p] = e < E ? pair : ~pair;
+               slot[pair] = e < E ? p : ~p;
+             });
 }
 
 // ---- rows. G threads take a token's row in pieces of VE elements.
@@ -178,9 +182,9 @@ hipError_t launch_sort_pairs(const int32_t* idx, int64_t pairs, int32_t experts,
   const bool one = pairs <= kSortOne;
   const int64_t span = one ? pairs : kSortChunk;
   const int waves = sort_waves(span, experts);
-  const int64_t run = (span + waves * 64 - 1) / (waves * 64) * 64;
+  const int run = (int)((span + waves * 64 - 1) / (waves * 64) * 64);
   if (one) {
-    hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(waves * 64), 0, st, idx, pairs, run, experts, offsets, order, slot);
+    hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(waves * 64), 0, st, idx, (int)pairs, run, experts, offsets, order, slot);
     return hipGetLastError();
   }
   const int chunks = (int)((pairs + kSortChunk - 1) / kSortChunk);

@@ -6,98 +6,102 @@
 namespace moeq {
 namespace {
 
-// ---- the sort: stable, by counting. A wavefront owns a run of consecutive pairs, so a pair's place is the sum of: the pairs of
-// smaller experts, those of its expert in the runs before, and those before it in the run (64 at a time, by ballots on the bits of
-// the expert). All counts are integers, so the order never depends on timing.
-constexpr int kSortCounts = 8208;        // counters in LDS: 16 wavefronts x 513 bins or 8 x 1025
+// A wavefront owns a run of consecutive pairs, so a pair's place is the sum of: the pairs of smaller bins, those of its bin in the
+// runs before, and those before it in the run (64 at a time, by ballots on the bits of the bin). All counts are integers, so the
+// order never depends on timing. The run is gone through twice by the same loop, once to count and once to place: what a launch
+// executes once costs some 200 cycles per 64 bytes of code, so that loops unrolled to keep what was counted in registers took longer.
+constexpr int kSortCounts = 4112;        // counters in LDS: 16 wavefronts x 257 bins, 8 x 513 or 4 x 1025
 
 inline int sort_waves(int64_t pairs, int32_t experts) {
-  const int most = experts <= 512 ? 16 : 8;
+  const int most = experts <= 256 ? 16 : experts <= 512 ? 8 : 4;
   const int64_t need = (pairs + 63) / 64;
   return need < 1 ? 1 : need < most ? (int)need : most;
 }
 
-__device__ __forceinline__ int key_of(const int32_t* idx, int64_t i, int E) {
-  const int e = idx[i];
-  return (uint32_t)e < (uint32_t)E ? e : E;
+__device__ __forceinline__ int bin_of(int e, int E) { return (uint32_t)e < (uint32_t)E ? e : E; }
+
+// The sum of the lanes up to this one, within rows of 16 and beyond, by moves between lanes that are part of the addition (through LDS
+// a step is some 100 cycles).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_from(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int row_sum_to(int v) {
+  v = add_from<0x111, 0xf>(v);
+  v = add_from<0x112, 0xf>(v);
+  v = add_from<0x114, 0xf>(v);
+  return add_from<0x118, 0xf>(v);
+}
+__device__ __forceinline__ int wave_sum_to(int v) {
+  v = row_sum_to(v);
+  v = add_from<0x142, 0xa>(v);        // the last lane of rows 0 and 2 to rows 1 and 3
+  return add_from<0x143, 0xc>(v);     // lane 31 to rows 2 and 3
 }
 
-// Counts of this workgroup's pairs [first, last) into cnt[wave][bin].
-__device__ __forceinline__ void sort_count(const int32_t* idx, int64_t first, int64_t last, int64_t run, int E, int* cnt) {
-  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// v[bin] = the sum of the values before it, by the calling wavefront.
+__device__ __forceinline__ void sort_scan(int E, int* v) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int e0 = 0; e0 <= E; e0 += 64) {
+    const int e = e0 + lane, n = e <= E ? v[e] : 0, at = wave_sum_to(n);
+    if (e <= E) v[e] = before + at - n;
+    before += __builtin_amdgcn_readlane(at, 63);
+  }
+}
+
+// The pairs idx[0, n) of a workgroup, `run` of them a wavefront. After counting, totals(bin, count) is called for every bin by one
+// thread, then starts() by all (with barriers before and behind), then put(pair, number, bin) for every pair with its number in the bin.
+template <typename Totals, typename Starts, typename Put>
+__device__ __forceinline__ void sort_pairs(const int32_t* idx, int n, int run, int E, int* cnt, Totals&& totals, Starts&& starts, Put&& put) {
+  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, bits = 32 - __builtin_clz(E);
+  const int a = wave * run, b = min(a + run, n);
+  int* mine = cnt + wave * (E + 1);
+  constexpr int kNext = 4;                      // 64 pairs that are on their way ahead of those worked on
+  int next[kNext];
+  auto request = [&](int i) { return idx[min(i + lane, n - 1)]; };
+  if (a < b)
+#pragma unroll
+    for (int j = 0; j < kNext; ++j) next[j] = request(a + 64 * j);
   for (int i = threadIdx.x; i < waves * (E + 1); i += blockDim.x) cnt[i] = 0;
   __syncthreads();
-  const int64_t a = first + wave * run, b = min(a + run, last);
-  for (int64_t i = a + lane; i < b; i += 64) atomicAdd(&cnt[wave * (E + 1) + key_of(idx, i, E)], 1);
-  __syncthreads();
-}
-
-// cnt[wave][bin] becomes the place of the wavefront's next pair of that bin: place[bin] + the counts of the wavefronts before.
-// put(pair, place, bin) takes them.
-template <typename Put>
-__device__ __forceinline__ void sort_place(const int32_t* idx, int64_t first, int64_t last, int64_t run, int E, const int* place,
-                                           int* cnt, Put&& put) {
-  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) {
-    int at = place[e];
-    for (int w = 0; w < waves; ++w) {
-      const int n = cnt[w * (E + 1) + e];
-      cnt[w * (E + 1) + e] = at;
-      at += n;
+  for (int placing = 0;; ++placing) {
+    for (int i0 = a; i0 < b; i0 += 64) {
+      const int i = i0 + lane, key = bin_of(next[0], E);
+      const bool in = i < b;
+#pragma unroll
+      for (int j = 0; j + 1 < kNext; ++j) next[j] = next[j + 1];
+      next[kNext - 1] = request(i0 + 64 * kNext);
+      // the lanes that hold the same bin; runs of one bin, as sorted ids have them, are seen at once
+      uint64_t same = __ballot(in);
+      if (__ballot(in && key != __builtin_amdgcn_readfirstlane(key)))
+        for (int j = 0; j < bits; ++j) {
+          const bool one = (key >> j) & 1;
+          const uint64_t m = __ballot(one);
+          same &= one ? m : ~m;
+        }
+      if (in) {
+        const int rank = __popcll(same & ((1ull << lane) - 1)), at = mine[key] + rank;
+        __builtin_amdgcn_wave_barrier();                 // every lane has read before the first of the bin counts on
+        if (rank == 0) mine[key] = at + __popcll(same);
+        if (placing) put(i, at, key);
+      }
+      __builtin_amdgcn_wave_barrier();
     }
+    if (placing) return;
+    if (a < b)
+#pragma unroll
+      for (int j = 0; j < kNext; ++j) next[j] = request(a + 64 * j);
+    __syncthreads();
+    // 16 lanes take the counts of a bin (of one wavefront: a lane), which become the numbers of the wavefronts' first pairs in it
+    const int shift = waves > 1 ? 4 : 0;
+    for (int i = threadIdx.x; i < (E + 1) << shift; i += blockDim.x) {
+      const int w = shift ? i & 15 : 0, e = i >> shift, c = w < waves ? cnt[w * (E + 1) + e] : 0;
+      const int at = shift ? row_sum_to(c) : c;
+      if (w < waves) cnt[w * (E + 1) + e] = at - c;
+      if (w == (1 << shift) - 1) totals(e, at);
+    }
+    __syncthreads();
+    starts();
+    __syncthreads();
   }
-  __syncthreads();
-  const int bits = 32 - __builtin_clz(E);
-  const int64_t a = first + wave * run, b = min(a + run, last);
-  for (int64_t i0 = a; i0 < b; i0 += 64) {
-    const int64_t i = i0 + lane;
-    const bool in = i < b;
-    const int key = in ? key_of(idx, i, E) : 0;
-    uint64_t same = __ballot(in);
-    for (int j = 0; j < bits; ++j) {
-      const bool one = (key >> j) & 1;
-      const uint64_t m = __ballot(one);
-      same &= one ? m : ~m;
-    }
-    if (in) {
-      const int rank = __popcll(same & ((1ull << lane) - 1));
-      int* next = &cnt[wave * (E + 1) + key];
-      const int p = *next + rank;
-      __builtin_amdgcn_wave_barrier();                 // every lane has read before the first of the bin counts on
-      if (rank == 0) *next = p + __popcll(same);
-      put((int)i, p, key);
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
-}
-
-// Counts of all wavefronts together.
-__device__ __forceinline__ int sort_total(const int* cnt, int E, int e) {
-  const int waves = blockDim.x >> 6;
-  int n = 0;
-  for (int w = 0; w < waves; ++w) n += cnt[w * (E + 1) + e];
-  return n;
-}
-
-// place[bin] = the sum of the totals before it; by the first wavefront.
-__device__ __forceinline__ void sort_scan(int E, int* place) {
-  if (threadIdx.x < 64) {
-    const int lane = threadIdx.x, per = (E + 1 + 63) / 64, a = lane * per, b = min(a + per, E + 1);
-    int sum = 0;
-    for (int e = a; e < b; ++e) sum += place[e];
-    int before = sum;
-    for (int s = 1; s < 64; s <<= 1) {
-      const int v = __shfl_up(before, s);
-      if (lane >= s) before += v;
-    }
-    before -= sum;
-    for (int e = a; e < b; ++e) {
-      const int n = place[e];
-      place[e] = before;
-      before += n;
-    }
-  }
-  __syncthreads();
 }
 
 }  // namespace

@@ -69,7 +69,8 @@ def check(got, want, mag, steps):
     half = torch.finfo(got.dtype).eps / 2
     tol = 8 * (steps + 16) ** 0.5 * 2.0**-24 * mag + half * np.abs(want) * 1.001 + (2.0**-25 if got.dtype == torch.float16 else 0)
     err = np.abs(got.double().cpu().numpy() - want)
-    assert np.isfinite(err).all() and (err <= tol).all(), float((err / np.maximum(tol, 1e-300)).max())
+    off = float((err / np.maximum(tol, 1e-300)).max()) if np.isfinite(err).all() else float("nan")
+    assert off <= 1.0
 
 
 CASES = [  # T, n, r, d_in, d_out, ids
