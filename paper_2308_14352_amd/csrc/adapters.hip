@@ -7,7 +7,7 @@
 //
 // Precision. A fp32 operand is cut into three bf16 pieces of 8 bits each by truncation, a fp16 one into two, both exactly; the
 // products of pieces whose places add up to 2 or less are taken (those left out are below 2^-23 of the product) and summed in fp32.
-// bf16 with bf16 and fp16 with fp16 are one product. h and g are held as three pieces.
+// bf16 with bf16 and fp16 with fp16 are one product. h and g are held in fp32 and cut where they are operands, or kept as three pieces.
 //
 // Requests. Loads stand in straight lines without conditions, at addresses that are moved into the matrix where a piece would pass its
 // end (and what comes twice by that meets a zero or is not stored): behind a condition the compiler waits for every load under way
@@ -177,38 +177,35 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict
   }
 }
 
-// A tile of 16 rows: its adapter (n: none; -1: nothing to do), and the row of lane m = lane % 16 (~row: padding). By every wavefront
-// for itself.
+// A tile of 16 rows: its adapter (n: none; -1: nothing to do), and for every lane the row of a place of its own (~row: padding). By
+// every wavefront for itself.
 template <bool FEW>
-__device__ __forceinline__ int find_tile(const Plan& plan, const int32_t* ids, int T, int n, int TP, int tile, int& row) {
-  const int lane = threadIdx.x & 63;
-  if constexpr (!FEW) {
-    row = plan.rowof[tile * 16 + (lane & 15)];
-    return plan.tile_adapter[tile * 16 / TP];
-  }
-  const int id = lane < T ? bin_of(ids[lane], n) : -1, mine = __builtin_amdgcn_readlane(id, tile);
-  const uint64_t same = __ballot(id == mine);
-  const int before = __popcll(same & ((1ull << tile) - 1));
-  // the tile's rows send their numbers to the lanes that take them; a lane that gets none reads 0
-  const int k = __popcll(same & ((1ull << lane) - 1)) - before;
-  int got = 0;
-  if (id == mine && k >= 0 && k < 16) got = lane + 1;
-  got = __builtin_amdgcn_ds_permute(4 * (got ? k : 63), got);      // (lanes that send none send 0 to a lane that nobody asks)
-  row = __shfl(got, lane & 15) - 1;
-  return before % 16 ? -1 : mine;
+__device__ __forceinline__ int find_tile(const Plan& plan, const int32_t* ids, int T, int n, int TP, int tile) {
+  if constexpr (!FEW) return plan.tile_adapter[tile * 16 / TP];
+  const int lane = threadIdx.x & 63, id = lane < T ? bin_of(ids[lane], n) : -1, mine = __builtin_amdgcn_readlane(id, tile);
+  return __popcll(__ballot(id == mine) & ((1ull << tile) - 1)) % 16 ? -1 : mine;
 }
+template <bool FEW>
+__device__ __forceinline__ int find_row(const Plan& plan, const int32_t* ids, int T, int n, int tile, int place) {
+  if constexpr (!FEW) return plan.rowof[tile * 16 + place];
+  const int lane = threadIdx.x & 63, id = lane < T ? bin_of(ids[lane], n) : -1, mine = __builtin_amdgcn_readlane(id, tile);
+  // the tile's rows send their numbers to the lanes that stand for their places; a lane that gets none reads 0
+  const int k = __popcll(__ballot(id == mine) & ~((1ull << tile) - 1) & ((1ull << lane) - 1)), to = id == mine && lane >= tile && k < 16 ? k : 63;
+  const int got = __builtin_amdgcn_ds_permute(4 * to, to < 63 ? lane + 1 : 0);      // (lanes that send none send 0 to a lane that nobody asks)
+  return __shfl(got, place) - 1;
+}
+__device__ __forceinline__ int real_row(int row) { return row ^ (row >> 31); }
 
-// h on its way from the narrowing to the widening products. Sorted calls: as bf16 pieces in the two orders that the products need, by
-// place (an operand's slots contiguous) and by rank (places contiguous). Calls of few rows: in fp32 by row, one part per share of the columns.
+// h on its way from the narrowing to the widening products: in fp32 by place, one part per share of the columns, and as bf16 pieces by
+// rank (places contiguous), as the weights' gradients need it.
 struct Pieces {
-  uint16_t* by_place;      // [places][3][RK] or null
+  float* parts;            // [splits][places][RR] or null
   uint16_t* by_rank;       // [3][RR][places] or null
-  float* parts;            // [splits][T][RR] or null
-  int32_t RK, RR, places, splits;
+  int32_t RR, places, splits;
 };
-// Slots of the widening product's operands, RK of them in groups of eight: the rank index that a slot takes its weights from. The last
-// group, where the rank is no multiple of eight, begins before its place, so that eight elements can be read; a rank below eight takes
-// its last four, or single ones. h is zero in the slots that come twice by that.
+// Slots of the widening product's operands, in groups of eight: the rank index that a slot takes its weights from. The last group, where
+// the rank is no multiple of eight, begins before its place, so that eight elements can be read; a rank below eight takes its last four,
+// or single ones. h is zero in the slots that come twice by that.
 __device__ __forceinline__ int slot_source(int slot, int rank) {
   const int e = slot & 7;
   return rank >= 8 ? min(slot - e, rank - 8) + e : rank >= 4 ? (e < 4 ? e : rank - 8 + e) : min(e, rank - 1);
@@ -223,34 +220,50 @@ __device__ __forceinline__ int slot_of(int r, int rank) {
 template <int RT>
 __device__ __forceinline__ int rank_of(int m, int j, int rank) { return min(RT * m, rank - RT) + j; }
 
+// 16-bit operands of two steps of 32 columns. A load takes eight rows of 128 bytes (a whole line of the cache) instead of sixteen of 64:
+// lanes of m < 8 hold the first step's piece of rows m and m + 8, those of m >= 8 the second's of rows m - 8 and m; half of them change places.
+__device__ __forceinline__ void exchange(uint32_t (&a)[4], uint32_t (&b)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t x = a[i], y = b[i];
+    a[i] = __builtin_amdgcn_update_dpp(x, y, 0x128, 0xf, 0xc, false);      // lanes 8..15 of a row of 16: from the lane 8 below
+    b[i] = __builtin_amdgcn_update_dpp(y, x, 0x128, 0xf, 0x3, false);
+  }
+}
+
 template <typename X, typename W, int RT, int MT, bool TRANS>
 struct Shrink {
   static constexpr bool kHalf = std::is_same<X, _Float16>::value && std::is_same<W, _Float16>::value;
   static constexpr int KS = sizeof(X) == 2 && sizeof(W) == 2 ? 2 : 1;      // 32-column steps of a unit: 128 bytes of a row
+  static constexpr bool kLines = KS == 2;
   static constexpr int kWidth = 32 * KS;
   // units that are under way in a wavefront: some 64 registers of them
-  static constexpr int kRegs = KS * (MT * kWords<X> + (TRANS ? 8 * ((RT * (int)sizeof(W) + 3) / 4) : RT * kWords<W>)), DEPTH = kRegs <= 16 ? 4 : kRegs <= 24 ? 3 : 2;
+  static constexpr int kRegs = KS * (MT * kWords<X> + (TRANS ? 8 * ((RT * (int)sizeof(W) + 3) / 4) : RT * kWords<W>)), DEPTH = kRegs <= 16 ? 4 : kRegs <= 24 ? 3 : kRegs <= 48 ? 2 : 1;
   struct Unit {
     Eight<X> x[KS][MT];
     Eight<W> w[TRANS ? 1 : KS][TRANS ? 1 : RT];
     uint32_t t[TRANS ? KS : 1][8][(RT * sizeof(W) + 3) / 4];
   };
 
-  const X* xrow[MT];
+  const X* xrow[MT][KS];      // rows of the lane's loads
   const W* wrow;
   int d, rank, m, q;
+
+  // the row (of 16) and the column of load s
+  __device__ __forceinline__ int row_of(int s) const { return kLines ? 8 * s + (m & 7) : m; }
+  __device__ __forceinline__ int column_of(int unit, int s) const { return unit * kWidth + 8 * q + (kLines ? 32 * (m >> 3) : 32 * s); }
 
   __device__ __forceinline__ void load(Unit& u, int unit) const {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const int c = min(unit * kWidth + 32 * s + 8 * q, d - 8);
+      const int c = min(column_of(unit, s), d - 8);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) load_words<X, 8>(u.x[s][t].w, xrow[t] + c);
+      for (int t = 0; t < MT; ++t) load_words<X, 8>(u.x[s][t].w, xrow[t][s] + c);
       if constexpr (!TRANS) {
 #pragma unroll
-        for (int j = 0; j < RT; ++j) load_words<W, 8>(u.w[s][j].w, wrow + (int64_t)rank_of<RT>(m, j, rank) * d + c);
+        for (int j = 0; j < RT; ++j) load_words<W, 8>(u.w[s][j].w, wrow + (int64_t)rank_of<RT>(row_of(s), j, rank) * d + c);
       } else {
-        const W* p = wrow + (int64_t)c * rank + rank_of<RT>(m, 0, rank);
+        const W* p = wrow + (int64_t)min(unit * kWidth + 32 * s + 8 * q, d - 8) * rank + rank_of<RT>(m, 0, rank);
 #pragma unroll
         for (int e = 0; e < 8; ++e) load_words<W, RT>(u.t[s][e], p + e * rank);
       }
@@ -261,7 +274,7 @@ struct Shrink {
       // the last columns: what was read before a piece's own place counts nothing
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const int c = unit * kWidth + 32 * s + 8 * q, lead = c - min(c, d - 8);
+        const int c = column_of(unit, s), lead = c - min(c, d - 8);
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -270,6 +283,13 @@ struct Shrink {
             u.x[s][t].w[i] &= keep;
           }
       }
+    }
+    if constexpr (kLines) {
+#pragma unroll
+      for (int t = 0; t < MT; ++t) exchange(u.x[0][t].w, u.x[1][t].w);
+      if constexpr (!TRANS)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) exchange(u.w[0][j].w, u.w[1][j].w);
     }
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
@@ -325,24 +345,28 @@ struct Shrink {
   }
 };
 
+// split: which share of the columns, of h.splits.
 template <typename X, typename W, int RT, int MT, bool TRANS, int WAVES, bool FEW>
 __device__ __forceinline__ void shrink(const AdapterArgs& P, const Plan& plan, int TP, const void* in, int64_t stride, int d, const Pieces& h,
-                                       f32x4* red) {
+                                       int split, f32x4* red) {
   using S = Shrink<X, W, RT, MT, TRANS>;
   const int tile = blockIdx.x * MT, lane = threadIdx.x & 63, wave = wave_index();
-  int rows[MT];
-  const int a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile, rows[0]);
-  if (a < 0 || a == P.n) return;
-#pragma unroll
-  for (int t = 1; t < MT; ++t) find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile + t, rows[t]);
   S s;
   s.d = d, s.rank = P.rank, s.m = lane & 15, s.q = lane >> 4;
+  int rows[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) s.xrow[t] = (const X*)in + (rows[t] ^ (rows[t] >> 31)) * stride;      // (columns of the product do not meet: padding may hold any row)
+  for (int t = 0; t < MT; ++t) {
+    rows[t] = find_row<FEW>(plan, P.ids, P.T, P.n, tile + t, s.m);
+#pragma unroll
+    for (int k = 0; k < S::KS; ++k)      // (columns of the product do not meet: padding may hold any row)
+      s.xrow[t][k] = (const X*)in + real_row(S::kLines ? find_row<FEW>(plan, P.ids, P.T, P.n, tile + t, s.row_of(k)) : rows[t]) * stride;
+  }
+  const int a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile);
+  if (a < 0 || a == P.n) return;
   s.wrow = (const W*)(TRANS ? P.B : P.A) + (int64_t)a * P.rank * d;
+  const float scale = P.scale[a];
   f32x4 acc[RT][MT] = {};
-  const int units = (d + S::kWidth - 1) / S::kWidth;
-  s.run(FEW ? blockIdx.y * WAVES + wave : wave, FEW ? WAVES * h.splits : WAVES, units, acc);
+  s.run(split * WAVES + wave, WAVES * h.splits, (d + S::kWidth - 1) / S::kWidth, acc);
 #pragma unroll
   for (int half = 1; half >= 0; --half) {                      // the upper half of the wavefronts, and the lower one added to it
     if (wave / (WAVES / 2) == half)
@@ -355,76 +379,71 @@ __device__ __forceinline__ void shrink(const AdapterArgs& P, const Plan& plan, i
         }
     __syncthreads();
   }
-  const float scale = P.scale[a];
   for (int i = threadIdx.x; i < RT * MT * 64; i += WAVES * 64) {
-    const int t = (i >> 6) % MT, j = (i >> 6) / MT, row = MT == 1 || t == 0 ? rows[0] : rows[MT - 1], place = (tile + t) * 16 + s.m;
+    const int t = (i >> 6) % MT, j = (i >> 6) / MT, place = (tile + t) * 16 + s.m;
+    int row = rows[0];
+#pragma unroll
+    for (int k = 1; k < MT; ++k) row = t == k ? rows[k] : row;
     f32x4 v = red[i];
 #pragma unroll
     for (int w = 1; w < WAVES / 2; ++w) v += red[w * RT * MT * 64 + i];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = rank_of<RT>(4 * s.q + e, j, P.rank);      // (an index that comes twice has the same sums twice)
-      if constexpr (FEW) {
-        if (row >= 0) h.parts[((int64_t)blockIdx.y * P.T + row) * h.RR + r] = v[e] * scale;
-      } else {
-        float f = row < 0 ? 0.f : v[e] * scale;
+      float f = row < 0 ? 0.f : v[e] * scale;
+      if (h.parts) h.parts[((int64_t)split * h.places + place) * h.RR + r] = f;
+      if (!FEW && h.by_rank)
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
           const uint32_t b = __builtin_bit_cast(uint32_t, f);
           f -= __builtin_bit_cast(float, b & 0xffff0000u);
-          if (h.by_place) h.by_place[((int64_t)place * 3 + p) * h.RK + slot_of(r, P.rank)] = b >> 16;
-          if (h.by_rank) h.by_rank[(int64_t)(p * h.RR + r) * h.places + place] = b >> 16;
+          h.by_rank[(int64_t)(p * h.RR + r) * h.places + place] = b >> 16;
         }
-      }
     }
   }
-  if (!FEW && h.by_place && P.rank < h.RK)
-    for (int i = threadIdx.x; i < 48 * MT * h.RK; i += WAVES * 64) {
-      const int slot = i & (h.RK - 1), r = slot_source(slot, P.rank);
-      if (slot_of(r, P.rank) != slot) h.by_place[(int64_t)tile * 48 * h.RK + i] = 0;
-    }
 }
 
-template <typename W, int RT, int MT, int WAVES, bool FEW>
-__global__ __launch_bounds__(WAVES * 64) void k_adapter_down(AdapterArgs P, Plan plan, int TP, Pieces h) {
-  __shared__ f32x4 red[WAVES / 2 * RT * MT * 64];
-  shrink<W, W, RT, MT, false, WAVES, FEW>(P, plan, TP, P.x, P.x_stride, P.d_in, h, red);
+template <typename W, int RT, int MT, bool FEW>
+__global__ __launch_bounds__(256) void k_adapter_down(AdapterArgs P, Plan plan, int TP, Pieces h) {
+  __shared__ f32x4 red[2 * RT * MT * 64];
+  shrink<W, W, RT, MT, false, 4, FEW>(P, plan, TP, P.x, P.x_stride, P.d_in, h, blockIdx.y, red);
 }
 // Backward: h of the rows of x in the first half of the grid's second dimension, g of those of dy in the other.
-template <typename W, typename Y, int RT, int MT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void k_adapter_down_both(AdapterArgs P, Plan plan, int TP, Pieces h, Pieces g) {
-  __shared__ f32x4 red[WAVES / 2 * RT * MT * 64];
-  if (blockIdx.y == 0) shrink<W, W, RT, MT, false, WAVES, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, red);
-  else shrink<Y, W, RT, MT, true, WAVES, false>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, red);
+template <typename W, typename Y, int RT, int MT>
+__global__ __launch_bounds__(512) void k_adapter_down_both(AdapterArgs P, Plan plan, int TP, Pieces h, Pieces g) {
+  __shared__ f32x4 red[4 * RT * MT * 64];
+  if (blockIdx.y == 0) shrink<W, W, RT, MT, false, 8, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, 0, red);
+  else shrink<Y, W, RT, MT, true, 8, false>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, 0, red);
 }
 
 // ---- out = base + h B^T (TRANS: + g A): a wavefront takes 16 NJ columns of 16 MT rows ----
-// Columns of the product's row 4 q + i, in groups of VE that are 16 bytes of the output: four lanes store 64 consecutive bytes. Group g
-// of NJ / VE; a group that would pass the last column begins before it.
+// A lane holds groups of VE columns, 16 bytes of the output, of four rows: sixteen lanes read and store 256 consecutive bytes. A group
+// that would pass the last column begins before it.
 template <typename Y, typename W, int RKS, int NJ, int MT, bool TRANS, bool FEW>
-__global__ __launch_bounds__(256) void k_adapter_up(AdapterArgs P, Plan plan, int TP, Pieces hp, int d) {
+__global__ __launch_bounds__(256, 2) void k_adapter_up(AdapterArgs P, Plan plan, int TP, Pieces h, int d) {
   constexpr int VE = 16 / sizeof(Y), NG = NJ / VE;
   const int lane = threadIdx.x & 63, c0 = (blockIdx.x * 4 + wave_index()) * 16 * NJ, m = lane & 15, q = lane >> 4, rank = P.rank;
   if (c0 >= d) return;
   const int tile = blockIdx.y * MT;
-  int rows[MT];
-  const int a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile, rows[0]);
-  if (a < 0) return;
+  int rows[MT][4];
 #pragma unroll
-  for (int t = 1; t < MT; ++t) find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile + t, rows[t]);
-  auto group = [&](int row, int g) { return c0 + 4 * VE * ((row & 3) * NG + g) + VE * (row >> 2); };
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rows[t][i] = find_row<FEW>(plan, P.ids, P.T, P.n, tile + t, 4 * q + i);
+  const int a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile);
+  if (a < 0) return;
+  auto group = [&](int g) { return c0 + 16 * VE * g + VE * m; };
 
   struct Group { uint32_t w[4]; };
   Group base[MT][4][NG] = {};
   if (P.base)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-      const Y* from = (const Y*)P.base + (rows[t] ^ (rows[t] >> 31)) * P.base_stride;
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int g = 0; g < NG; ++g) __builtin_memcpy(base[t][i][g].w, from + min(group(4 * q + i, g), d - VE), 16);
-    }
+        for (int g = 0; g < NG; ++g)
+          __builtin_memcpy(base[t][i][g].w, (const Y*)P.base + real_row(rows[t][i]) * P.base_stride + min(group(g), d - VE), 16);
   f32x4 acc[MT][NJ] = {};
   if (a < P.n) {
     const W* W0 = (const W*)(TRANS ? P.A : P.B) + (int64_t)a * rank * d;
@@ -437,11 +456,11 @@ __global__ __launch_bounds__(256) void k_adapter_up(AdapterArgs P, Plan plan, in
         for (int s = 0; s < RKS; ++s)
 #pragma unroll
           for (int j = 0; j < NJ; ++j)
-            load_words<W, 8>(w[s][j].w, W0 + (int64_t)(min(group(m, j / VE), d - VE) + j % VE) * rank + min(32 * s + 8 * q, rank - 8));
+            load_words<W, 8>(w[s][j].w, W0 + (int64_t)(min(group(j / VE), d - VE) + j % VE) * rank + min(32 * s + 8 * q, rank - 8));
       } else {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-          const W* p = W0 + (int64_t)(min(group(m, j / VE), d - VE) + j % VE) * rank;
+          const W* p = W0 + (int64_t)(min(group(j / VE), d - VE) + j % VE) * rank;
           W v[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = p[slot_source(e, rank)];
@@ -455,46 +474,36 @@ __global__ __launch_bounds__(256) void k_adapter_up(AdapterArgs P, Plan plan, in
         for (int g = 0; g < NJ / 4; ++g)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            load_words<W, 4>(wt[s][g][e], W0 + (int64_t)slot_source(32 * s + 8 * q + e, rank) * d + min(group(m, g * 4 / VE), d - VE) + g * 4 % VE);
+            load_words<W, 4>(wt[s][g][e], W0 + (int64_t)slot_source(32 * s + 8 * q + e, rank) * d + min(group(g * 4 / VE), d - VE) + g * 4 % VE);
     }
     bf16x8 b[MT][RKS][3];
-    if constexpr (!FEW) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int s = 0; s < RKS; ++s)
-#pragma unroll
-          for (int p = 0; p < 3; ++p)
-            __builtin_memcpy(&b[t][s][p], hp.by_place + ((int64_t)((tile + t) * 16 + m) * 3 + p) * hp.RK + 32 * s + 8 * q, 16);
-    } else {
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int s = 0; s < RKS; ++s) {
-          float f[8] = {};
-          const float* from = hp.parts + (int64_t)(rows[t] ^ (rows[t] >> 31)) * hp.RR;
-          if (rank >= 8) {
-            from += min(32 * s + 8 * q, rank - 8);
+      for (int s = 0; s < RKS; ++s) {
+        float f[8] = {};
+        const float* from = h.parts + (int64_t)((tile + t) * 16 + m) * h.RR;
+        if (rank >= 8) {
+          from += min(32 * s + 8 * q, rank - 8);
 #pragma unroll 4
-            for (int k = 0; k < hp.splits; ++k, from += (int64_t)P.T * hp.RR) {
-              float v[8];
-              __builtin_memcpy(v, from, sizeof(v));
+          for (int k = 0; k < h.splits; ++k, from += (int64_t)h.places * h.RR) {
+            float v[8];
+            __builtin_memcpy(v, from, sizeof(v));
 #pragma unroll
-              for (int e = 0; e < 8; ++e) f[e] += v[e];
-            }
-          } else {
-            for (int k = 0; k < hp.splits; ++k, from += (int64_t)P.T * hp.RR)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) f[e] += from[slot_source(e, rank)];
+            for (int e = 0; e < 8; ++e) f[e] += v[e];
           }
+        } else {
+          for (int k = 0; k < h.splits; ++k, from += (int64_t)h.places * h.RR)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int slot = 32 * s + 8 * q + e;
-            f[e] = slot_of(slot_source(slot, rank), rank) == slot ? f[e] : 0.f;
-          }
-          cut(f, b[t][s]);
+            for (int e = 0; e < 8; ++e) f[e] += from[slot_source(e, rank)];
         }
-    }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int slot = 32 * s + 8 * q + e;
+          f[e] = slot_of(slot_source(slot, rank), rank) == slot ? f[e] : 0.f;
+        }
+        cut(f, b[t][s]);
+      }
 #pragma unroll
     for (int s = 0; s < RKS; ++s)
 #pragma unroll
@@ -504,18 +513,18 @@ __global__ __launch_bounds__(256) void k_adapter_up(AdapterArgs P, Plan plan, in
         bf16x8 p[kPieces<W>];
         cut(v, p);
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t][j] = mma(p, b[t][s], acc[t][j]);
+        for (int t = 0; t < MT; ++t) acc[t][j] = mma(b[t][s], p, acc[t][j]);
       }
   }
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    if (rows[t] < 0) continue;
-    Y* out = (Y*)P.out + rows[t] * P.out_stride;
+  for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+      if (rows[t][i] < 0) continue;
+      Y* out = (Y*)P.out + rows[t][i] * P.out_stride;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const int c = group(4 * q + i, g), at = min(c, d - VE);
+        const int c = group(g), at = min(c, d - VE);
         Y v[VE];
         __builtin_memcpy(v, base[t][i][g].w, 16);
 #pragma unroll
@@ -528,7 +537,7 @@ __global__ __launch_bounds__(256) void k_adapter_up(AdapterArgs P, Plan plan, in
             if (at + e >= c) out[at + e] = v[e];
         }
       }
-  }
+    }
 }
 
 // ---- dA = sum of g x^T, dB = sum of h dy^T: products of 16 (rank) x 16 NJ (columns), the places split over the wavefronts ----
@@ -707,7 +716,7 @@ struct Setup {
   Plan plan;
   Pieces h, g;
   float *part, *narrow_h, *narrow_g;
-  int TP, RT, RKS;
+  int TP, RT, MT;
   size_t total;
 };
 
@@ -721,58 +730,56 @@ int segment_shift(const AdapterArgs& a) {
   return k;
 }
 
-constexpr int kFewWaves = 4;
-inline int few_splits(const AdapterArgs& a) {
+// Shares of the columns in the narrowing products of the forward pass, each a workgroup of four wavefronts: as many as give the chip
+// two workgroups per compute unit, while a wavefront has two units of 128 bytes of its rows or more.
+inline int column_splits(const AdapterArgs& a, int tiles) {
   const int units = a.dtype == MOEQ_F32 ? (a.d_in + 31) / 32 : (a.d_in + 63) / 64;
-  return (units + 2 * kFewWaves - 1) / (2 * kFewWaves);
+  int k = 1;
+  while (k < 8 && units >= 16 * k && tiles * k < 512) k *= 2;
+  return k;
 }
 
 Setup set_up(const AdapterArgs& a, bool backward) {
   Setup s = {};
   s.form = a.d_in < 8 || a.d_out < 8 ? kNarrow : !backward && a.T <= kInlineTokens ? kFew : kSorted;
   s.RT = a.rank <= 16 ? 1 : a.rank <= 32 ? 2 : 4;
-  s.RKS = a.rank <= 32 ? 1 : 2;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* q = a.ws ? (char*)a.ws + at : nullptr;
     at += (bytes + 255) / 256 * 256;
     return (void*)q;
   };
-  // what is set aside never falls with the number of rows, so that the workspace of a call serves the smaller ones
-  const int RK = 32 * s.RKS, RR = 16 * s.RT;
+  const int RR = 16 * s.RT;
   if (s.form == kNarrow) {
     s.narrow_h = (float*)take((size_t)a.T * a.rank * 4);
     if (backward) s.narrow_g = (float*)take((size_t)a.T * a.rank * 4);
-  }
-  if (!backward && s.form != kNarrow) {
-    s.h = Pieces{nullptr, nullptr, (float*)take((size_t)few_splits(a) * std::min(a.T, kInlineTokens) * RR * 4), RK, RR, 0, few_splits(a)};
-    if (s.form == kSorted) at = 0;
-  }
-  if (s.form == kSorted) {
+  } else if (s.form == kFew) {
+    s.h = Pieces{(float*)take((size_t)8 * a.T * 16 * RR * 4), nullptr, RR, 16 * a.T, column_splits(a, a.T)};
+  } else {
     Plan& p = s.plan;
-    s.TP = backward || a.T >= 64 * (int64_t)a.n ? 32 : 16;
-    // every bin that has rows adds at most a tile less a row of padding (room: of either tile)
-    const int pad = (s.TP - 1) * std::min(a.T, a.n + 1), room = a.T + 31 * std::min(a.T, a.n + 1), room_split = std::min(16, a.T / 256) + room / 256 - a.T / 256 + 1;
+    // Rows of a tile: as many as share the weights that are read for them, unless that is mostly padding.
+    s.MT = a.T < 64 * (int64_t)a.n ? 1 : s.RT == 1 || a.T < 256 * (int64_t)a.n || backward ? 2 : 4;
+    s.TP = backward ? 32 : 16 * s.MT;
+    // every bin that has rows adds at most a tile less a row of padding (room: of the largest tile)
+    const int pad = (s.TP - 1) * std::min(a.T, a.n + 1), most = 63 * std::min(a.T, a.n + 1), room = a.T + most, room_split = std::min(16, a.T / 256) + most / 256 + 1;
     p.places = (a.T + pad) / s.TP * s.TP;
     p.tiles = p.places / s.TP;
     p.rowof = (int32_t*)take((size_t)room * 4);
     p.tile_adapter = (int32_t*)take((size_t)room / 16 * 4 + 4);
-    auto pieces = [&](bool by_place, bool by_rank) {
-      Pieces h{nullptr, nullptr, nullptr, RK, RR, p.places, 0};
-      if (by_place) h.by_place = (uint16_t*)take((size_t)room * 3 * RK * 2);
-      if (by_rank) h.by_rank = (uint16_t*)take((size_t)room * 3 * RR * 2);
-      return h;
-    };
     if (!backward) {
-      s.h = pieces(true, false);
+      s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, p.tiles)};
+      // (several shares only of less than 512 tiles)
+      s.h.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 512 * 64)) * RR * 4);
     } else {
       p.seg_shift = segment_shift(a);
       p.n_segments = a.n + 1 + (p.places >> p.seg_shift);
       p.n_split = p.places >> p.seg_shift;
       p.segments = (Segment*)take((size_t)(a.n + 1 + room_split) * sizeof(Segment));
       p.split = (Segment*)take((size_t)room_split * sizeof(Segment));
-      s.h = pieces(false, true);
-      s.g = pieces(a.out || !a.ws, true);
+      s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, 1};
+      s.g = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, 1};
+      float* parts = (float*)take((size_t)room * RR * 4);
+      s.g.parts = a.out ? parts : nullptr;
       // (segments of at least 256 rows, at most 16 of them in the rows themselves: segment_shift)
       s.part = (float*)take((size_t)2 * room_split * a.rank * (a.d_in + a.d_out) * 4);
     }
@@ -799,10 +806,16 @@ hipError_t with_rank(int RT, F&& f) {
   return f(std::integral_constant<int, 4>{});
 }
 
+// Rows in tiles of 16 MT, or of 16 where the weights take the registers (two steps of the rank).
 template <typename Y, typename W, int RKS, int MT, bool TRANS, bool FEW>
-hipError_t launch_up(const AdapterArgs& a, const Setup& s, const Pieces& h, int d, int tiles, hipStream_t st) {
-  constexpr int NJ = sizeof(W) == 4 ? 4 : 8;
-  hipLaunchKernelGGL((k_adapter_up<Y, W, RKS, NJ, MT, TRANS, FEW>), dim3((d + 64 * NJ - 1) / (64 * NJ), tiles), dim3(256), 0, st, a, s.plan, s.TP, h, d);
+hipError_t launch_up(const AdapterArgs& a, const Setup& s, const Pieces& h, int d, hipStream_t st) {
+  constexpr int NJ = sizeof(W) == 4 ? 4 : 8, M = RKS == 2 ? 1 : MT;
+  hipLaunchKernelGGL((k_adapter_up<Y, W, RKS, NJ, M, TRANS, FEW>), dim3((d + 64 * NJ - 1) / (64 * NJ), FEW ? a.T : s.plan.places / (16 * M)), dim3(256), 0, st, a, s.plan, s.TP, h, d);
+  return hipGetLastError();
+}
+template <typename W, int RT, int MT, bool FEW>
+hipError_t launch_down(const AdapterArgs& a, const Setup& s, hipStream_t st) {
+  hipLaunchKernelGGL((k_adapter_down<W, RT, MT, FEW>), dim3(FEW ? a.T : s.plan.places / (16 * MT), s.h.splits), dim3(256), 0, st, a, s.plan, s.TP, s.h);
   return hipGetLastError();
 }
 
@@ -853,15 +866,12 @@ hipError_t launch_adapters_forward(const AdapterArgs& a, hipStream_t st) {
     using Y = decltype(ytag);
     return with_rank(s.RT, [&](auto rt) {
       constexpr int RT = decltype(rt)::value, RKS = RT == 4 ? 2 : 1;
-      if (s.form == kFew) {
-        hipLaunchKernelGGL((k_adapter_down<W, RT, 1, kFewWaves, true>), dim3(a.T, s.h.splits), dim3(kFewWaves * 64), 0, st, a, s.plan, s.TP, s.h);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        return launch_up<Y, W, RKS, 1, false, true>(a, s, s.h, a.d_out, a.T, st);
-      }
-      hipLaunchKernelGGL((k_adapter_down<W, RT, 1, 8, false>), dim3(s.plan.places / 16), dim3(512), 0, st, a, s.plan, s.TP, s.h);
-      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-      if (s.TP == 32) return launch_up<Y, W, RKS, 2, false, false>(a, s, s.h, a.d_out, s.plan.places / 32, st);
-      return launch_up<Y, W, RKS, 1, false, false>(a, s, s.h, a.d_out, s.plan.places / 16, st);
+      hipError_t e = s.form == kFew ? launch_down<W, RT, 1, true>(a, s, st) : s.MT == 1 ? launch_down<W, RT, 1, false>(a, s, st)
+                   : s.MT == 2 || RT == 1 ? launch_down<W, RT, 2, false>(a, s, st) : launch_down<W, RT, RT == 1 ? 2 : 4, false>(a, s, st);
+      if (e != hipSuccess) return e;
+      if (s.form == kFew) return launch_up<Y, W, RKS, 1, false, true>(a, s, s.h, a.d_out, st);
+      if (s.MT == 1) return launch_up<Y, W, RKS, 1, false, false>(a, s, s.h, a.d_out, st);
+      return launch_up<Y, W, RKS, 2, false, false>(a, s, s.h, a.d_out, st);
     });
   });
 }
@@ -876,10 +886,10 @@ hipError_t launch_adapters_backward(const AdapterArgs& a, hipStream_t st) {
     return with_rank(s.RT, [&](auto rt) {
       constexpr int RT = decltype(rt)::value, RKS = RT == 4 ? 2 : 1, MT = 2;
       if (a.T) {
-        hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT, 8>), dim3(s.plan.places / (16 * MT), 2), dim3(512), 0, st, a, s.plan, s.TP, s.h, s.g);
+        hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT>), dim3(s.plan.places / (16 * MT), 2), dim3(512), 0, st, a, s.plan, s.TP, s.h, s.g);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
         if (a.out)
-          if (hipError_t e = launch_up<Y, W, RKS, 2, true, false>(a, s, s.g, a.d_in, s.plan.places / 32, st); e != hipSuccess) return e;
+          if (hipError_t e = launch_up<Y, W, RKS, 2, true, false>(a, s, s.g, a.d_in, st); e != hipSuccess) return e;
       }
       const int sa = (a.d_in + 256 / (int)sizeof(W) - 1) / (256 / (int)sizeof(W)), sb = (a.d_out + 256 / (int)sizeof(Y) - 1) / (256 / (int)sizeof(Y));
       hipLaunchKernelGGL((k_adapter_weights<W, Y, RT>), dim3(sa + sb, s.plan.n_segments), dim3(256), 0, st, a, s.plan, s.h, s.g, sa, s.part);
