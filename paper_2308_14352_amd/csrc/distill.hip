@@ -2,99 +2,397 @@
 // weight w: s = z / tau, q = softmax(s), p = softmax(u / tau) over the entries that have an index,
 //   loss = w tau^2 sum_j p_j (log p_j - s[idx_j] + lse(s)),   dloss/dz = w tau (q - p at the indices).
 // A row of weight 0, or without a teacher's entry, has no loss and no gradient.
+//
+// One pass over a row: it is held in registers (up to 256 KB) between the maximum, the sum and the gradient, every thread with a maximum
+// and a sum of its own that are joined once. Longer rows, and calls of few rows, are cut into chunks of a workgroup each: a kernel writes
+// every chunk's maximum and sum, and the next joins them and goes on (the second reading of a row comes from the cache where it fits).
+// Differences z - max are taken before the scaling, so that a probability's error does not grow with the size of the logits. The
+// gradient is written without the teacher's part first; its K elements are written again behind a barrier.
+#include <algorithm>
+#include <type_traits>
+
 #include "operators.h"
 
 namespace moeq {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-template <bool MAX>
-__device__ __forceinline__ float block_fold(float v, float* part) {
-  const int waves = blockDim.x / 64;
+// ---- folds over a wavefront, by moves between lanes that are part of the operation ----
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float from_lane(float v, float none) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+template <typename Op>
+__device__ __forceinline__ float fold(float v, float none, Op op) {
+  v = op(v, from_lane<0x111, 0xf>(v, none));
+  v = op(v, from_lane<0x112, 0xf>(v, none));
+  v = op(v, from_lane<0x114, 0xf>(v, none));
+  v = op(v, from_lane<0x118, 0xf>(v, none));
+  v = op(v, from_lane<0x142, 0xa>(v, none));      // the last lane of rows 0 and 2 to rows 1 and 3
+  v = op(v, from_lane<0x143, 0xc>(v, none));      // lane 31 to rows 2 and 3
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ float wave_max(float v) { return fold(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float wave_sum(float v) { return fold(v, 0.f, [](float a, float b) { return a + b; }); }
+
+// A maximum of logits and the sum of exp2((z - max) c) that belongs to it; minus infinity counts from 0.
+struct Stat { float m, s; };
+__device__ __forceinline__ float origin(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float rescale(Stat a, float m, float c) { return a.s * __builtin_amdgcn_exp2f((origin(a.m) - origin(m)) * c); }
+
+// ---- a piece of a row in registers: vectors of 16 bytes, v = thread + i threads ----
+template <typename T, int NV>
+struct Held {
+  static constexpr int VE = 16 / sizeof(T);
+  struct Words { uint32_t w[4]; } raw[NV];
+  __device__ __forceinline__ void load(const T* z, int n, int threads) {      // n: vectors, at least one
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const float o = __shfl_xor(v, m);
-    v = MAX ? fmaxf(v, o) : v + o;
+    for (int i = 0; i < NV; ++i) __builtin_memcpy(raw[i].w, z + (int64_t)min((int)threadIdx.x + i * threads, n - 1) * VE, 16);
   }
+  // As fp32, anew every time: kept from one use to the next the values would take twice the registers of 16-bit logits.
+  __device__ __forceinline__ void get(int i, float (&v)[VE]) const {
+    Words r = raw[i];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(r.w[e]));
+    }
+    T t[VE];
+    __builtin_memcpy(t, r.w, 16);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[e] = (float)t[e];
+  }
+};
+
+// The statistics of a workgroup's piece: n vectors in `held` and `rest` single elements behind them (`last` for the threads below).
+template <typename T, int NV>
+__device__ __forceinline__ Stat piece_stat(const Held<T, NV>& held, int n, int threads, bool rest, float last, float c, Stat* sh) {
+  constexpr int VE = Held<T, NV>::VE;
+  Stat a{-INFINITY, 0.f};
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if ((int)threadIdx.x + i * threads < n) {
+      float v[VE];
+      held.get(i, v);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) a.m = fmaxf(a.m, v[e]);
+    }
+  if (rest) a.m = fmaxf(a.m, last);
+  const float m = wave_max(a.m), o = origin(m);      // (one maximum a wavefront: no thread rescales)
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if ((int)threadIdx.x + i * threads < n) {
+      float v[VE];
+      held.get(i, v);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) a.s += __builtin_amdgcn_exp2f((v[e] - o) * c);
+    }
+  if (rest) a.s += __builtin_amdgcn_exp2f((last - o) * c);
+  a.s = wave_sum(a.s);
+  if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = Stat{m, a.s};
   __syncthreads();
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
-  __syncthreads();
-  v = part[0];
-  for (int w = 1; w < waves; ++w) v = MAX ? fmaxf(v, part[w]) : v + part[w];
-  return v;
+  Stat all{-INFINITY, 0.f};
+  for (int w = 0; w < threads / 64; ++w) all.m = fmaxf(all.m, sh[w].m);
+  for (int w = 0; w < threads / 64; ++w) all.s += rescale(sh[w], all.m, c);
+  return all;
+}
+// Several pieces' statistics as one, by a wavefront.
+__device__ __forceinline__ Stat join(const Stat* part, int n, float c) {
+  float m = -INFINITY, s = 0.f;
+  for (int i = threadIdx.x % 64; i < n; i += 64) m = fmaxf(m, part[i].m);
+  m = wave_max(m);
+  for (int i = threadIdx.x % 64; i < n; i += 64) s += rescale(part[i], m, c);
+  return Stat{m, wave_sum(s)};
 }
 
-// A logit of minus infinity has no probability, also where a whole row has none.
-__device__ __forceinline__ float prob(float z, float it, float lse) { return z == -INFINITY ? 0.f : expf(z * it - lse); }
+// ---- the teacher's entries of a row, in LDS: index (-1: none), probability, logit of the student ----
+struct Teacher {
+  int idx[kDistillMaxTop];
+  float p[kDistillMaxTop], z[kDistillMaxTop];
+  bool any;
+};
+// By the first wavefront (a barrier has to follow). Returns sum of p log p, in all its lanes.
+template <typename T>
+__device__ __forceinline__ float take_teacher(const DistillArgs& A, int t, const T* z, Teacher& sh) {
+  const int lane = threadIdx.x & 63;
+  const float it = 1.f / A.temperature;
+  const int32_t* idx = A.top_idx + (int64_t)t * A.K;
+  const float* u = A.top_logits + (int64_t)t * A.K;
+  float top = -INFINITY, sum = 0.f, plogp = 0.f;
+  for (int j = lane; j < A.K; j += 64) {
+    const int i = idx[j];
+    const bool ok = (uint32_t)i < (uint32_t)A.V;
+    sh.idx[j] = ok ? i : -1;
+    sh.p[j] = ok ? u[j] : -INFINITY;
+    sh.z[j] = ok ? (float)z[i] : 0.f;
+    top = ok ? fmaxf(top, u[j]) : top;
+  }
+  top = wave_max(top);
+  const float o = origin(top);
+  for (int j = lane; j < A.K; j += 64) {
+    const float e = __builtin_amdgcn_exp2f((sh.p[j] - o) * it * kLog2e);
+    sum += e;
+  }
+  sum = wave_sum(sum);
+  const float log_sum = __builtin_amdgcn_logf(sum) * kLn2;
+  for (int j = lane; j < A.K; j += 64) {
+    const float lp = (sh.p[j] - o) * it - log_sum, p = __builtin_amdgcn_exp2f(lp * kLog2e);
+    plogp += p > 0.f ? p * lp : 0.f;
+    sh.p[j] = top == -INFINITY ? 0.f : p;
+  }
+  if (lane == 0) sh.any = top != -INFINITY;
+  return wave_sum(plogp);
+}
+// The loss from there, by the first wavefront: w tau^2 (sum p log p - sum p ((z_j - m) / tau - log S)).
+__device__ __forceinline__ float row_loss(const DistillArgs& A, const Teacher& sh, Stat st, float w, float plogp) {
+  const float it = 1.f / A.temperature, o = origin(st.m), log_s = __builtin_amdgcn_logf(st.s) * kLn2;
+  float cross = 0.f;
+  for (int j = threadIdx.x & 63; j < A.K; j += 64)
+    if (sh.p[j] > 0.f) cross += sh.z[j] == -INFINITY ? -INFINITY : sh.p[j] * ((sh.z[j] - o) * it - log_s);
+  cross = wave_sum(cross);
+  return sh.any && w != 0.f ? w * A.temperature * A.temperature * (plogp - cross) : 0.f;
+}
+// The teacher's elements of a gradient in columns [c0, c1): scale * (q - p), q = exp2((z - o) c) * inv.
+template <typename T>
+__device__ __forceinline__ void put_teacher(const DistillArgs& A, const Teacher& sh, T* dz, int c0, int c1, float o, float c, float inv, float scale) {
+  for (int j = threadIdx.x; j < A.K; j += blockDim.x) {
+    const int at = sh.idx[j];
+    if (at < c0 || at >= c1) continue;
+    float p = 0.f;      // (an index that comes twice counts twice, and is written twice alike)
+    for (int i = 0; i < A.K; ++i) p += sh.idx[i] == at ? sh.p[i] : 0.f;
+    const float q = __builtin_amdgcn_exp2f((sh.z[j] - o) * c) * inv;
+    dz[at] = (T)(scale * (q - p));
+  }
+}
+// The gradient without the teacher's part.
+template <typename T, int NV>
+__device__ __forceinline__ void put_piece(const Held<T, NV>& held, T* dz, int n, int threads, bool rest, float last, T* dlast, float o, float c, float by) {
+  constexpr int VE = Held<T, NV>::VE;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if ((int)threadIdx.x + i * threads < n) {
+      float v[VE];
+      held.get(i, v);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - o) * c) * by;
+      store_n(dz + ((int)threadIdx.x + i * threads) * VE, v);
+    }
+  if (rest) *dlast = (T)(__builtin_amdgcn_exp2f((last - o) * c) * by);
+}
+template <typename T>
+__device__ __forceinline__ void put_zeros(T* dz, int V) {
+  constexpr int VE = 16 / sizeof(T);
+  const float zero[VE] = {};
+  for (int i = threadIdx.x; i < V / VE; i += blockDim.x) store_n(dz + (int64_t)i * VE, zero);
+  if ((int)threadIdx.x < V % VE) dz[V / VE * VE + threadIdx.x] = (T)0.f;
+}
+
+// ---- a row a workgroup: loss, log-sum-exp and gradient, whichever are wanted ----
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void k_distill_row(DistillArgs A) {
+  constexpr int VE = 16 / sizeof(T);
+  __shared__ Teacher teacher;
+  __shared__ Stat sh[THREADS / 64];
+  const int t = blockIdx.x, V = A.V, n = V / VE;
+  const T* z = (const T*)A.logits + (int64_t)t * A.stride;
+  T* dz = A.dlogits ? (T*)A.dlogits + (int64_t)t * A.dstride : nullptr;
+  const float w = A.weight ? A.weight[t] : 1.f, c = kLog2e / A.temperature;
+  if (w == 0.f && !A.lse) {
+    if (threadIdx.x == 0) A.loss[t] = 0.f;
+    if (dz) put_zeros(dz, V);
+    return;
+  }
+  Held<T, NV> held;
+  if (n) held.load(z, n, THREADS);
+  const bool rest = (int)threadIdx.x < V % VE;
+  const float last = rest ? (float)z[n * VE + threadIdx.x] : 0.f;
+  const float plogp = threadIdx.x < 64 ? take_teacher(A, t, z, teacher) : 0.f;
+  const Stat st = piece_stat(held, n, THREADS, rest, last, c, sh);
+  if (threadIdx.x < 64) {
+    const float loss = row_loss(A, teacher, st, w, plogp);
+    if (threadIdx.x == 0) {
+      A.loss[t] = loss;
+      if (A.lse) A.lse[t] = origin(st.m) / A.temperature + __builtin_amdgcn_logf(st.s) * kLn2;
+    }
+  }
+  if (!dz) return;
+  if (!teacher.any) return put_zeros(dz, V);
+  const float o = origin(st.m), inv = st.s == 0.f ? 0.f : 1.f / st.s, scale = w * A.temperature;
+  put_piece(held, dz, n, THREADS, rest, last, dz + n * VE + threadIdx.x, o, c, inv * scale);
+  __syncthreads();
+  put_teacher(A, teacher, dz, 0, V, o, c, inv, scale);
+}
+
+// ---- rows in chunks of a workgroup: vectors [chunk * per, ...), the single elements of the end with the last one ----
+constexpr int kChunkThreads = 256, kChunkVectors = 8;
 
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_distill(DistillArgs A, bool grad) {
-  __shared__ float part[16];
-  const int t = blockIdx.x, V = A.V, K = A.K;
-  const T* z = (const T*)A.logits + (int64_t)t * A.stride;
-  const int32_t* idx = A.top_idx + (int64_t)t * K;
-  const float* u = A.top_logits + (int64_t)t * K;
-  const float it = 1.f / A.temperature;
-  float w = A.weight ? A.weight[t] : 1.f, lse;
-  if (A.lse_in) {
-    lse = A.lse_in[t];
-    w *= A.dloss[t];
-  } else {
-    float m = -INFINITY, s = 0.f;
-    for (int i = threadIdx.x; i < V; i += kThreads) m = fmaxf(m, (float)z[i]);
-    m = block_fold<true>(m, part);
-    const float m0 = m == -INFINITY ? 0.f : m;
-    for (int i = threadIdx.x; i < V; i += kThreads) s += expf(((float)z[i] - m0) * it);
-    lse = logf(block_fold<false>(s, part)) + m0 * it;
-    if (A.lse && threadIdx.x == 0) A.lse[t] = lse;
-  }
-  float top = -INFINITY, sum = 0.f;
-  for (int j = threadIdx.x; j < K; j += kThreads)
-    if ((uint32_t)idx[j] < (uint32_t)V) top = fmaxf(top, u[j]);
-  top = block_fold<true>(top, part);
-  const bool none = w == 0.f || top == -INFINITY;
-  for (int j = threadIdx.x; j < K; j += kThreads)
-    if ((uint32_t)idx[j] < (uint32_t)V && !none) sum += expf((u[j] - top) * it);
-  sum = block_fold<false>(sum, part);
-  if (A.loss) {
-    float l = 0.f;
-    for (int j = threadIdx.x; j < K; j += kThreads)
-      if ((uint32_t)idx[j] < (uint32_t)V && !none) {
-        const float lp = (u[j] - top) * it - logf(sum), p = expf(lp);
-        const float zj = (float)z[idx[j]];
-        if (p > 0.f) l += zj == -INFINITY ? INFINITY : p * (lp - (zj * it - lse));
-      }
-    l = block_fold<false>(l, part);
-    if (threadIdx.x == 0) A.loss[t] = none ? 0.f : w * A.temperature * A.temperature * l;
-  }
-  if (!grad) return;
-  T* dz = (T*)A.dlogits + (int64_t)t * A.dstride;
-  const float c = w * A.temperature;
-  for (int i = threadIdx.x; i < V; i += kThreads) dz[i] = none ? (T)0.f : (T)(c * prob((float)z[i], it, lse));
+__global__ __launch_bounds__(kChunkThreads) void k_distill_stat(DistillArgs A, int per) {
+  constexpr int VE = 16 / sizeof(T);
+  __shared__ Stat sh[kChunkThreads / 64];
+  const int t = blockIdx.y, all = A.V / VE, first = blockIdx.x * per, n = min(per, all - first);
+  if (A.weight && !A.lse && A.weight[t] == 0.f) return;
+  const T* z = (const T*)A.logits + (int64_t)t * A.stride + (int64_t)first * VE;
+  Held<T, kChunkVectors> held;
+  held.load(z, n, kChunkThreads);
+  const bool rest = first + n == all && (int)threadIdx.x < A.V % VE;
+  const Stat st = piece_stat(held, n, kChunkThreads, rest, rest ? (float)z[n * VE + threadIdx.x] : 0.f, kLog2e / A.temperature, sh);
+  if (threadIdx.x == 0) ((Stat*)A.ws)[(int64_t)t * gridDim.x + blockIdx.x] = st;
+}
+
+// Loss and log-sum-exp of a row, a wavefront each, from its chunks' statistics.
+template <typename T>
+__global__ __launch_bounds__(64) void k_distill_join(DistillArgs A, int chunks) {
+  __shared__ Teacher teacher;
+  const int t = blockIdx.x;
+  const float w = A.weight ? A.weight[t] : 1.f;
+  const float plogp = take_teacher(A, t, (const T*)A.logits + (int64_t)t * A.stride, teacher);
+  const Stat st = join((const Stat*)A.ws + (int64_t)t * chunks, chunks, kLog2e / A.temperature);
   __syncthreads();
-  for (int j = threadIdx.x; j < K; j += kThreads) {
-    if (none || (uint32_t)idx[j] >= (uint32_t)V) continue;
-    float p = 0.f;
-    for (int i = 0; i < K; ++i)
-      if (idx[i] == idx[j]) p += expf((u[i] - top) * it) / sum;
-    dz[idx[j]] = (T)(c * (prob((float)z[idx[j]], it, lse) - p));
+  const float loss = row_loss(A, teacher, st, w, plogp);
+  if (threadIdx.x == 0) {
+    A.loss[t] = loss;
+    if (A.lse) A.lse[t] = origin(st.m) / A.temperature + __builtin_amdgcn_logf(st.s) * kLn2;
   }
 }
 
-hipError_t launch(const DistillArgs& a, bool grad, hipStream_t st) {
-  if (a.T == 0) return hipSuccess;
-  return with_type(a.dtype, [&](auto tag) {
-    hipLaunchKernelGGL(k_distill<decltype(tag)>, dim3(a.T), dim3(kThreads), 0, st, a, grad);
-    return hipGetLastError();
-  });
+// The gradient of a chunk: from the chunks' statistics (with the loss, by the first one), or from a saved log-sum-exp.
+template <typename T, bool SAVED>
+__global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, int per, int chunks) {
+  constexpr int VE = 16 / sizeof(T);
+  __shared__ Teacher teacher;
+  __shared__ Stat sh;
+  const int t = blockIdx.y, all = A.V / VE, first = blockIdx.x * per, n = min(per, all - first), c0 = first * VE;
+  const int c1 = first + n == all ? A.V : c0 + n * VE;
+  const T* z = (const T*)A.logits + (int64_t)t * A.stride;
+  T* dz = (T*)A.dlogits + (int64_t)t * A.dstride;
+  float w = A.weight ? A.weight[t] : 1.f;
+  const float c = kLog2e / A.temperature;
+  if (w == 0.f) {
+    if (!SAVED && blockIdx.x == 0 && threadIdx.x == 0) A.loss[t] = 0.f;
+    return put_zeros(dz + c0, c1 - c0);
+  }
+  Held<T, kChunkVectors> held;
+  if (n > 0) held.load(z + c0, n, kChunkThreads);
+  const bool rest = c1 == A.V && (int)threadIdx.x < A.V % VE;
+  const float last = rest ? (float)z[c0 + n * VE + threadIdx.x] : 0.f;
+  if (threadIdx.x < 64) {
+    const float plogp = take_teacher(A, t, z, teacher);
+    if constexpr (!SAVED) {
+      const Stat st = join((const Stat*)A.ws + (int64_t)t * chunks, chunks, c);
+      if (threadIdx.x == 0) sh = st;
+      if (blockIdx.x == 0) {
+        const float loss = row_loss(A, teacher, st, w, plogp);
+        if (threadIdx.x == 0) A.loss[t] = loss;
+      }
+    }
+  }
+  __syncthreads();
+  if (!teacher.any) return put_zeros(dz + c0, c1 - c0);
+  float o, inv, scale = w * A.temperature;
+  if constexpr (SAVED) {
+    // exp(z / tau - lse): the sum's logarithm as an origin of the logits, and nothing left to divide by
+    o = A.lse_in[t] * A.temperature, inv = 1.f;
+    scale *= A.dloss[t];
+    if (A.lse_in[t] == -INFINITY) o = 0.f;
+  } else {
+    o = origin(sh.m), inv = sh.s == 0.f ? 0.f : 1.f / sh.s;
+  }
+  put_piece(held, dz + c0, n, kChunkThreads, rest, last, dz + c0 + n * VE + threadIdx.x, o, c, inv * scale);
+  __syncthreads();
+  put_teacher(A, teacher, dz, c0, c1, o, c, inv, scale);
+}
+
+// ---- host side ----
+// Vectors of a chunk and their number in a row: full chunks, or shorter ones (of a vector a thread or more) where the rows are too few
+// to give every compute unit four workgroups.
+struct Chunks { int per, n; };
+Chunks chunks_of(int32_t T, int32_t V, int32_t dtype) {
+  const int64_t all = std::max<int64_t>(1, V / (16 / dtype_bytes(dtype)));
+  int64_t n = (all + kChunkThreads * kChunkVectors - 1) / (kChunkThreads * kChunkVectors);
+  while (n * T < 1024 && all / (2 * n) >= kChunkThreads) n *= 2;
+  const int64_t per = (all + n - 1) / n;
+  return Chunks{(int)per, (int)((all + per - 1) / per)};
+}
+// Rows that go a workgroup each: short ones, and those that fit the registers where there are enough of them for the chip.
+bool by_rows(int32_t T, int32_t V, int32_t dtype) {
+  const int64_t all = V / (16 / dtype_bytes(dtype));
+  return all <= 1024 || (all <= 16384 && T >= 128);
+}
+
+template <typename T>
+hipError_t launch_rows(const DistillArgs& a, hipStream_t st) {
+  const int all = a.V / (16 / (int)sizeof(T));
+  if (all <= 1024) hipLaunchKernelGGL((k_distill_row<T, 256, 4>), dim3(a.T), dim3(256), 0, st, a);
+  else if (all <= 4096) hipLaunchKernelGGL((k_distill_row<T, 512, 8>), dim3(a.T), dim3(512), 0, st, a);
+  else if (all <= 8192) hipLaunchKernelGGL((k_distill_row<T, 1024, 8>), dim3(a.T), dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((k_distill_row<T, 1024, 16>), dim3(a.T), dim3(1024), 0, st, a);
+  return hipGetLastError();
+}
+// Rows of one launch of the chunked kernels (the grid's second dimension).
+constexpr int32_t kRowsOfLaunch = 65535;
+template <typename F>
+hipError_t in_launches(DistillArgs a, F&& f) {
+  while (a.T > 0) {
+    DistillArgs b = a;
+    b.T = a.T < kRowsOfLaunch ? a.T : kRowsOfLaunch;
+    if (hipError_t e = f(b); e != hipSuccess) return e;
+    const int64_t sz = dtype_bytes(a.dtype), k = b.T;
+    a.T -= b.T;
+    a.logits = (const char*)a.logits + k * a.stride * sz;
+    a.top_idx += k * a.K, a.top_logits += k * a.K;
+    if (a.weight) a.weight += k;
+    if (a.lse_in) a.lse_in += k;
+    if (a.dloss) a.dloss += k;
+    if (a.loss) a.loss += k;
+    if (a.lse) a.lse += k;
+    if (a.dlogits) a.dlogits = (char*)a.dlogits + k * a.dstride * sz;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
-size_t distill_ws_bytes(int32_t, int32_t, int32_t) { return 0; }
-hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t st) { return launch(a, false, st); }
-hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t st) { return launch(a, true, st); }
-hipError_t launch_distill_loss_grad(const DistillArgs& a, hipStream_t st) { return launch(a, true, st); }
+size_t distill_ws_bytes(int32_t T, int32_t V, int32_t dtype) {
+  if (T <= 0 || by_rows(T, V, dtype)) return 0;
+  return (size_t)(T < kRowsOfLaunch ? T : kRowsOfLaunch) * chunks_of(T, V, dtype).n * sizeof(Stat);
+}
+
+hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t st) {
+  return with_type(a.dtype, [&](auto tag) {
+    using T = decltype(tag);
+    if (by_rows(a.T, a.V, a.dtype)) return launch_rows<T>(a, st);
+    const Chunks k = chunks_of(a.T, a.V, a.dtype);
+    return in_launches(a, [&](const DistillArgs& b) {
+      hipLaunchKernelGGL(k_distill_stat<T>, dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per);
+      hipLaunchKernelGGL(k_distill_join<T>, dim3(b.T), dim3(64), 0, st, b, k.n);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t st) {
+  return with_type(a.dtype, [&](auto tag) {
+    using T = decltype(tag);
+    const Chunks k = chunks_of(a.T, a.V, a.dtype);
+    return in_launches(a, [&](const DistillArgs& b) {
+      hipLaunchKernelGGL((k_distill_grad<T, true>), dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per, k.n);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t launch_distill_loss_grad(const DistillArgs& a, hipStream_t st) {
+  return with_type(a.dtype, [&](auto tag) {
+    using T = decltype(tag);
+    if (by_rows(a.T, a.V, a.dtype)) return launch_rows<T>(a, st);
+    const Chunks k = chunks_of(a.T, a.V, a.dtype);
+    return in_launches(a, [&](const DistillArgs& b) {
+      hipLaunchKernelGGL(k_distill_stat<T>, dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per);
+      hipLaunchKernelGGL((k_distill_grad<T, false>), dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per, k.n);
+      return hipGetLastError();
+    });
+  });
+}
 
 }  // namespace moeq
