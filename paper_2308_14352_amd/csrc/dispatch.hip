@@ -72,103 +72,146 @@ __global__ __launch_bounds__(1024) void k_sort_chunk(const int32_t* __restrict__
              });
 }
 
-// ---- rows. G threads take a token's row in pieces of VE elements.
-__device__ __forceinline__ int place_of(int s, int pairs) { return s < 0 ? ~s : s; }
-// Whether an entry of slot points to a row at all (entries come from the caller).
-__device__ __forceinline__ bool has_row(int s, int pairs) { return (uint32_t)place_of(s, pairs) < (uint32_t)pairs; }
+// ---- rows. G threads take a token's row in pieces of VE elements, KB of its choices at a time. Loads stand in straight lines at
+// addresses that exist (of dropped pairs: their place's, of entries that point nowhere: the first row's), so that they are on their way
+// together; what they bring is not used then. A row's last piece, where the width is no multiple of VE, begins before its place and is
+// read and written twice alike; rows shorter than a piece go element by element. ----
+struct Choice { int place; bool row, kept; float gate; };      // row: has a place at all (entries come from the caller)
 
-template <typename T, int G>
+template <int KB>
+__device__ __forceinline__ void take_choices(const RowsArgs& A, int t, int j0, Choice (&c)[KB]) {
+  const int pairs = A.T * A.k;
+#pragma unroll
+  for (int j = 0; j < KB; ++j) {
+    const int64_t i = (int64_t)t * A.k + min(j0 + j, A.k - 1);
+    const int s = A.slot[i], place = s < 0 ? ~s : s;
+    c[j].row = place < pairs && j0 + j < A.k;
+    c[j].kept = s >= 0 && c[j].row;
+    c[j].place = place < pairs ? place : 0;
+    c[j].gate = A.gate ? A.gate[i] : 1.f;
+  }
+}
+// The threads' pieces of a row of d elements: f(first element, elements) with compile-time VE where the row has as many.
+template <int VE, int G, typename F>
+__device__ __forceinline__ void for_pieces(int d, F&& f) {
+  if (d >= VE) {
+    for (int c = (threadIdx.x % G) * VE; c < d; c += G * VE) f(min(c, d - VE), std::integral_constant<int, VE>{}, min(c, d - VE) == c);
+  } else {
+    for (int c = threadIdx.x % G; c < d; c += G) f(c, std::integral_constant<int, 1>{}, true);
+  }
+}
+
+template <typename T, int G, int KB>
 __global__ __launch_bounds__(256) void k_gather_rows(RowsArgs A) {
-  constexpr int VE = 16 / sizeof(T);
   const int t = blockIdx.x * (256 / G) + threadIdx.x / G;
   if (t >= A.T) return;
   const T* x = (const T*)A.a + (int64_t)t * A.a_stride;
-  for (int c = (threadIdx.x % G) * VE; c < A.d; c += G * VE) {
-    const int n = min(VE, A.d - c);
-    float v[VE], z[VE] = {};
-    load_some(v, x + c, n);
-    for (int j = 0; j < A.k; ++j) {
-      const int s = A.slot[(int64_t)t * A.k + j];
-      if (!has_row(s, A.T * A.k)) continue;
-      T* to = (T*)A.out + (int64_t)place_of(s, 0) * A.out_stride + c;
-      store_some(to, s >= 0 ? v : z, n);
-    }
+  for (int j0 = 0; j0 < A.k; j0 += KB) {
+    Choice ch[KB];
+    take_choices(A, t, j0, ch);
+    for_pieces<16 / sizeof(T), G>(A.d, [&](int c, auto size, bool) {
+      constexpr int N = decltype(size)::value;
+      T v[N], z[N] = {};
+      __builtin_memcpy(v, x + c, sizeof(v));
+#pragma unroll
+      for (int j = 0; j < KB; ++j)
+        if (ch[j].row) __builtin_memcpy((T*)A.out + (int64_t)ch[j].place * A.out_stride + c, ch[j].kept ? v : z, sizeof(v));
+    });
   }
 }
 
 // y[t] = sum of gate * row over the token's choices, in their order, in fp32.
-template <typename T, typename Y, int G>
+template <typename T, typename Y, int G, int KB>
 __global__ __launch_bounds__(256) void k_combine_rows(RowsArgs A) {
-  constexpr int VE = 16 / (sizeof(T) < sizeof(Y) ? sizeof(T) : sizeof(Y));
   const int t = blockIdx.x * (256 / G) + threadIdx.x / G;
   if (t >= A.T) return;
-  const int64_t i0 = (int64_t)t * A.k;
-  for (int c = (threadIdx.x % G) * VE; c < A.d; c += G * VE) {
-    const int n = min(VE, A.d - c);
-    float acc[VE] = {};
-    for (int j = 0; j < A.k; ++j) {
-      const int s = A.slot[i0 + j];
-      if (s < 0 || !has_row(s, A.T * A.k)) continue;
-      const float g = A.gate ? A.gate[i0 + j] : 1.f;
-      float v[VE];
-      load_some(v, (const T*)A.a + (int64_t)s * A.a_stride + c, n);
+  Choice ch[KB];
+  take_choices(A, t, 0, ch);
+  for_pieces<16 / (sizeof(T) < sizeof(Y) ? sizeof(T) : sizeof(Y)), G>(A.d, [&](int c, auto size, bool) {
+    constexpr int N = decltype(size)::value;
+    float acc[N] = {};
+    auto add = [&](const Choice (&ch)[KB]) {
+      float v[KB][N];
 #pragma unroll
-      for (int i = 0; i < VE; ++i) acc[i] = fmaf(g, v[i], acc[i]);
+      for (int j = 0; j < KB; ++j) load_n(v[j], (const T*)A.a + (int64_t)ch[j].place * A.a_stride + c);
+#pragma unroll
+      for (int j = 0; j < KB; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = ch[j].kept ? fmaf(ch[j].gate, v[j][i], acc[i]) : acc[i];
+    };
+    add(ch);
+    for (int j0 = KB; j0 < A.k; j0 += KB) {
+      Choice more[KB];
+      take_choices(A, t, j0, more);
+      add(more);
     }
-    store_some((Y*)A.out + (int64_t)t * A.out_stride + c, acc, n);
-  }
+    store_n((Y*)A.out + (int64_t)t * A.out_stride + c, acc);
+  });
 }
 
 // drows = gate * dy, dgate = dy . row, of all choices of a token.
-template <typename T, typename Y, int G>
+template <typename T, typename Y, int G, int KB>
 __global__ __launch_bounds__(256) void k_combine_grad(RowsArgs A) {
-  constexpr int VE = 16 / (sizeof(T) < sizeof(Y) ? sizeof(T) : sizeof(Y));
-  __shared__ float part[4];
+  __shared__ float part[4][KB];
   const int t = blockIdx.x * (256 / G) + threadIdx.x / G, me = threadIdx.x % G;
-  if (t >= A.T) return;
+  if (t >= A.T) return;                       // (G = 256: the whole workgroup)
   const Y* dy = (const Y*)A.dy + (int64_t)t * A.dy_stride;
-  for (int j = 0; j < A.k; ++j) {
-    const int64_t i = (int64_t)t * A.k + j;
-    const int s = A.slot[i];
-    const bool row = has_row(s, A.T * A.k), kept = row && s >= 0;
-    const float g = !kept ? 0.f : A.gate ? A.gate[i] : 1.f;
-    float sum = 0.f;
-    if (row)
-      for (int c = me * VE; c < A.d; c += G * VE) {
-        const int n = min(VE, A.d - c);
-        float v[VE] = {}, r[VE], o[VE] = {};
-        if (kept) {
-          load_some(v, dy + c, n);
-          if (A.dgate) {
-            load_some(r, (const T*)A.a + (int64_t)s * A.a_stride + c, n);
+  for (int j0 = 0; j0 < A.k; j0 += KB) {
+    Choice ch[KB];
+    take_choices(A, t, j0, ch);
+    float sum[KB] = {};
+    for_pieces<16 / (sizeof(T) < sizeof(Y) ? sizeof(T) : sizeof(Y)), G>(A.d, [&](int c, auto size, bool whole) {
+      constexpr int N = decltype(size)::value;
+      float v[N], r[KB][N] = {};
+      load_n(v, dy + c);
+      if (A.dgate)
 #pragma unroll
-            for (int e = 0; e < VE; ++e) sum = fmaf(v[e], r[e], sum);
-          }
+        for (int j = 0; j < KB; ++j) load_n(r[j], (const T*)A.a + (int64_t)ch[j].place * A.a_stride + c);
 #pragma unroll
-          for (int e = 0; e < VE; ++e) o[e] = g * v[e];
+      for (int j = 0; j < KB; ++j) {
+        float o[N];
+        // (elements that the piece before has as well count once: those from the piece's own place on)
+        const int first = whole ? 0 : N - A.d % N;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          sum[j] = i >= first ? fmaf(v[i], r[j][i], sum[j]) : sum[j];
+          o[i] = ch[j].kept ? ch[j].gate * v[i] : 0.f;
         }
-        store_some((T*)A.out + (int64_t)place_of(s, 0) * A.out_stride + c, o, n);
+        if (ch[j].row) store_n((T*)A.out + (int64_t)ch[j].place * A.out_stride + c, o);
       }
+    });
     if (!A.dgate) continue;
 #pragma unroll
-    for (int m = 1; m < (G < 64 ? G : 64); m <<= 1) sum += __shfl_xor(sum, m);
+    for (int j = 0; j < KB; ++j)
+#pragma unroll
+      for (int m = 1; m < (G < 64 ? G : 64); m <<= 1) sum[j] += __shfl_xor(sum[j], m);
     if (G == 256) {
-      if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = sum;
       __syncthreads();
-      sum = (part[0] + part[1]) + (part[2] + part[3]);
+      if (threadIdx.x % 64 == 0)
+#pragma unroll
+        for (int j = 0; j < KB; ++j) part[threadIdx.x / 64][j] = sum[j];
       __syncthreads();
+#pragma unroll
+      for (int j = 0; j < KB; ++j) sum[j] = (part[0][j] + part[1][j]) + (part[2][j] + part[3][j]);
     }
-    if (me == 0) A.dgate[i] = kept ? sum : 0.f;
+#pragma unroll
+    for (int j = 0; j < KB; ++j)
+      if (me == 0 && j0 + j < A.k) A.dgate[(int64_t)t * A.k + j0 + j] = ch[j].kept ? sum[j] : 0.f;
   }
 }
 
-// Threads of a token: as many as its row has pieces of 16 bytes, as far as there are such groups.
+// Threads of a token: as many as its row has pieces of 16 bytes, as far as there are such groups; choices at a time: all up to four.
 template <typename F>
-hipError_t by_width(int d, int ve, F&& f) {
+hipError_t by_width(int d, int k, int ve, F&& f) {
   const int pieces = (d + ve - 1) / ve;
-  if (pieces <= 16) return f(std::integral_constant<int, 16>{});
-  if (pieces <= 128) return f(std::integral_constant<int, 64>{});
-  return f(std::integral_constant<int, 256>{});
+  auto with_k = [&](auto g) {
+    if (k == 1) return f(g, std::integral_constant<int, 1>{});
+    if (k == 2) return f(g, std::integral_constant<int, 2>{});
+    return f(g, std::integral_constant<int, 4>{});
+  };
+  if (pieces <= 16) return with_k(std::integral_constant<int, 16>{});
+  if (pieces <= 128) return with_k(std::integral_constant<int, 64>{});
+  return with_k(std::integral_constant<int, 256>{});
 }
 
 }  // namespace
@@ -197,9 +240,9 @@ hipError_t launch_sort_pairs(const int32_t* idx, int64_t pairs, int32_t experts,
 hipError_t launch_gather_rows(const RowsArgs& a, int32_t dtype, hipStream_t st) {
   return with_type(dtype, [&](auto tag) {
     using T = decltype(tag);
-    return by_width(a.d, 16 / sizeof(T), [&](auto g) {
-      constexpr int G = decltype(g)::value;
-      hipLaunchKernelGGL((k_gather_rows<T, G>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
+    return by_width(a.d, a.k, 16 / sizeof(T), [&](auto g, auto kb) {
+      constexpr int G = decltype(g)::value, KB = decltype(kb)::value;
+      hipLaunchKernelGGL((k_gather_rows<T, G, KB>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
       return hipGetLastError();
     });
   });
@@ -217,9 +260,9 @@ hipError_t launch_combine_rows(const RowsArgs& a, int32_t dtype, int32_t y_dtype
   return with_types(dtype, y_dtype, [&](auto tag, auto ytag) {
     using T = decltype(tag);
     using Y = decltype(ytag);
-    return by_width(a.d, 16 / sizeof(T), [&](auto g) {
-      constexpr int G = decltype(g)::value;
-      hipLaunchKernelGGL((k_combine_rows<T, Y, G>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
+    return by_width(a.d, a.k, 16 / sizeof(T), [&](auto g, auto kb) {
+      constexpr int G = decltype(g)::value, KB = decltype(kb)::value;
+      hipLaunchKernelGGL((k_combine_rows<T, Y, G, KB>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
       return hipGetLastError();
     });
   });
@@ -229,9 +272,9 @@ hipError_t launch_combine_rows_backward(const RowsArgs& a, int32_t dtype, int32_
   return with_types(dtype, dy_dtype, [&](auto tag, auto ytag) {
     using T = decltype(tag);
     using Y = decltype(ytag);
-    return by_width(a.d, 16 / sizeof(T), [&](auto g) {
-      constexpr int G = decltype(g)::value;
-      hipLaunchKernelGGL((k_combine_grad<T, Y, G>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
+    return by_width(a.d, a.k, 16 / sizeof(T), [&](auto g, auto kb) {
+      constexpr int G = decltype(g)::value, KB = decltype(kb)::value;
+      hipLaunchKernelGGL((k_combine_grad<T, Y, G, KB>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
       return hipGetLastError();
     });
   });
