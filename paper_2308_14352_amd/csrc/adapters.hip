@@ -122,7 +122,8 @@ struct Plan {
 };
 
 __global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict__ ids, int T, int run, int n, int TP, Plan plan) {
-  __shared__ int cnt[kSortCounts], start[kSortMaxExperts + 1], total[kSortMaxExperts + 1], segs[kSortMaxExperts + 1], parts[kSortMaxExperts + 1], n_split;
+  __shared__ SortShared sh;
+  __shared__ int start[kSortMaxExperts + 1], total[kSortMaxExperts + 1], segs[kSortMaxExperts + 1], parts[kSortMaxExperts + 1], n_split;
   if (threadIdx.x == 0) n_split = 0;
   // the bin of a place: the last one that starts at or before it
   auto last_at = [&](const int* from, int at) {
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict
     }
     return lo;
   };
-  sort_pairs(ids, T, run, n, cnt,
+  sort_pairs(ids, T, run, n, sh,
              [&](int e, int all) {
                const int rows = (all + TP - 1) & -TP, s = max(1, (rows + (1 << plan.seg_shift) - 1) >> plan.seg_shift);
                total[e] = all;
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict
                const int p = start[e] + number;
                plan.rowof[p] = i;
                if (number == 0)
-                 for (int k = total[e]; k % TP; ++k) plan.rowof[p + k] = ~i;
+                 for (int k = total[e], end = (k + TP - 1) & -TP; k < end; ++k) plan.rowof[p + k] = ~i;
              });
   const int end = start[n] + ((total[n] + TP - 1) & -TP);
   for (int i = threadIdx.x; i < plan.tiles; i += blockDim.x) plan.tile_adapter[i] = i * TP < end ? last_at(start, i * TP) : -1;
@@ -199,8 +200,8 @@ __device__ __forceinline__ int real_row(int row) { return row ^ (row >> 31); }
 // h on its way from the narrowing to the widening products: in fp32 by place, one part per share of the columns, and as bf16 pieces by
 // rank (places contiguous), as the weights' gradients need it.
 struct Pieces {
-  float* parts;            // [splits][places][RR] or null
-  uint16_t* by_rank;       // [3][RR][places] or null
+  float* parts;            // [splits][places][RR]
+  uint16_t* by_rank;       // [3][RR][places], backward
   int32_t RR, places, splits;
 };
 // Slots of the widening product's operands, in groups of eight: the rank index that a slot takes its weights from. The last group, where
@@ -390,15 +391,8 @@ __device__ __forceinline__ void shrink(const AdapterArgs& P, const Plan& plan, i
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = rank_of<RT>(4 * s.q + e, j, P.rank);      // (an index that comes twice has the same sums twice)
-      float f = row < 0 ? 0.f : v[e] * scale;
-      if (h.parts) h.parts[((int64_t)split * h.places + place) * h.RR + r] = f;
-      if (!FEW && h.by_rank)
-#pragma unroll
-        for (int p = 0; p < 3; ++p) {
-          const uint32_t b = __builtin_bit_cast(uint32_t, f);
-          f -= __builtin_bit_cast(float, b & 0xffff0000u);
-          h.by_rank[(int64_t)(p * h.RR + r) * h.places + place] = b >> 16;
-        }
+      const float f = row < 0 ? 0.f : v[e] * scale;
+      h.parts[((int64_t)split * h.places + place) * h.RR + r] = f;
     }
   }
 }
@@ -410,125 +404,180 @@ __global__ __launch_bounds__(256) void k_adapter_down(AdapterArgs P, Plan plan, 
 }
 // Backward: h of the rows of x in the first half of the grid's second dimension, g of those of dy in the other.
 template <typename W, typename Y, int RT, int MT>
-__global__ __launch_bounds__(512) void k_adapter_down_both(AdapterArgs P, Plan plan, int TP, Pieces h, Pieces g) {
-  __shared__ f32x4 red[4 * RT * MT * 64];
-  if (blockIdx.y == 0) shrink<W, W, RT, MT, false, 8, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, 0, red);
-  else shrink<Y, W, RT, MT, true, 8, false>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, 0, red);
+__global__ __launch_bounds__(256) void k_adapter_down_both(AdapterArgs P, Plan plan, int TP, Pieces h, Pieces g) {
+  __shared__ f32x4 red[2 * RT * MT * 64];
+  if ((int)blockIdx.y < h.splits) shrink<W, W, RT, MT, false, 4, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, blockIdx.y, red);
+  else shrink<Y, W, RT, MT, true, 4, false>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, blockIdx.y - h.splits, red);
 }
 
-// ---- out = base + h B^T (TRANS: + g A): a wavefront takes 16 NJ columns of 16 MT rows ----
+// The parts of h (of g) added up in order: as pieces by rank, and in fp32 in the place of the first part. 32 places a workgroup.
+__global__ __launch_bounds__(256) void k_adapter_pieces(Pieces h, Pieces g) {
+  __shared__ float sum[32 * 65];
+  const Pieces p = blockIdx.y ? g : h;
+  const int first = blockIdx.x * 32, shift = 31 - __builtin_clz(p.RR);
+  float* from = p.parts + (int64_t)first * p.RR;
+  const int64_t step = (int64_t)p.places * p.RR;
+  for (int i = threadIdx.x * 4; i < 32 * p.RR; i += 1024) {
+    f32x4 v[8] = {}, s = {};
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = *(const f32x4*)(from + min(k, p.splits - 1) * step + i);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += k < p.splits ? v[k][e] : 0.f;
+    if (p.splits > 1) *(f32x4*)(from + i) = s;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[(i >> shift) * 65 + (i & (p.RR - 1)) + e] = s[e];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * p.RR; i += 256) {
+    const int place = i & 31, r = i >> 5;
+    float f = sum[place * 65 + r];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const uint32_t b = __builtin_bit_cast(uint32_t, f);
+      f -= __builtin_bit_cast(float, b & 0xffff0000u);
+      p.by_rank[(int64_t)(k * p.RR + r) * p.places + first + place] = b >> 16;
+    }
+  }
+}
+
+// ---- out = base + h B^T (TRANS: + g A): a wavefront takes 16 NJ columns of `per` tiles of 16 rows, one after the other with the same
+// weights (tiles on their way together would be twice the code, which a launch of few rows fetches once for each workgroup's sake) ----
 // A lane holds groups of VE columns, 16 bytes of the output, of four rows: sixteen lanes read and store 256 consecutive bytes. A group
 // that would pass the last column begins before it.
-template <typename Y, typename W, int RKS, int NJ, int MT, bool TRANS, bool FEW>
-__global__ __launch_bounds__(256, 2) void k_adapter_up(AdapterArgs P, Plan plan, int TP, Pieces h, int d) {
+
+// Eight slots from `at` on of a row of `rank` elements. KIND: 0 for ranks of eight and more, 1 of four and more, 2 below (the choice is
+// made once, around all loads).
+template <typename T, int KIND>
+__device__ __forceinline__ void load_slots(uint32_t (&w)[kWords<T>], const T* row, int at, int rank) {
+  if constexpr (KIND == 0) {
+    load_words<T, 8>(w, row + min(at, rank - 8));
+  } else if constexpr (KIND == 1) {
+    __builtin_memcpy(w, row, 4 * sizeof(T));
+    __builtin_memcpy(w + kWords<T> / 2, row + rank - 4, 4 * sizeof(T));
+  } else {
+    T v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = row[min(e, rank - 1)];
+    __builtin_memcpy(w, v, sizeof(v));
+  }
+}
+template <typename F>
+__device__ __forceinline__ void by_rank_kind(int rank, F&& f) {
+  if (rank >= 8) f(std::integral_constant<int, 0>{});
+  else if (rank >= 4) f(std::integral_constant<int, 1>{});
+  else f(std::integral_constant<int, 2>{});
+}
+
+template <typename Y, typename W, int RKS, int NJ, bool TRANS, bool FEW>
+__global__ __launch_bounds__(256, RKS == 1 ? 3 : 2) void k_adapter_up(AdapterArgs P, Plan plan, int TP, Pieces h, int d, int per) {
   constexpr int VE = 16 / sizeof(Y), NG = NJ / VE;
   const int lane = threadIdx.x & 63, c0 = (blockIdx.x * 4 + wave_index()) * 16 * NJ, m = lane & 15, q = lane >> 4, rank = P.rank;
   if (c0 >= d) return;
-  const int tile = blockIdx.y * MT;
-  int rows[MT][4];
-#pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) rows[t][i] = find_row<FEW>(plan, P.ids, P.T, P.n, tile + t, 4 * q + i);
-  const int a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, tile);
+  const int first = blockIdx.y * per, a = find_tile<FEW>(plan, P.ids, P.T, P.n, TP, first);
   if (a < 0) return;
   auto group = [&](int g) { return c0 + 16 * VE * g + VE * m; };
 
-  struct Group { uint32_t w[4]; };
-  Group base[MT][4][NG] = {};
-  if (P.base)
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-          __builtin_memcpy(base[t][i][g].w, (const Y*)P.base + real_row(rows[t][i]) * P.base_stride + min(group(g), d - VE), 16);
-  f32x4 acc[MT][NJ] = {};
-  if (a < P.n) {
-    const W* W0 = (const W*)(TRANS ? P.A : P.B) + (int64_t)a * rank * d;
-    // weights: eight slots of a column (a row of B), or four columns of eight slots (rows of A)
-    Eight<W> w[TRANS ? 1 : RKS][TRANS ? 1 : NJ];
-    uint32_t wt[TRANS ? RKS : 1][TRANS ? NJ / 4 : 1][8][sizeof(W)];
-    if constexpr (!TRANS) {
-      if (rank >= 8) {
-#pragma unroll
-        for (int s = 0; s < RKS; ++s)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-            load_words<W, 8>(w[s][j].w, W0 + (int64_t)(min(group(j / VE), d - VE) + j % VE) * rank + min(32 * s + 8 * q, rank - 8));
-      } else {
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const W* p = W0 + (int64_t)(min(group(j / VE), d - VE) + j % VE) * rank;
-          W v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = p[slot_source(e, rank)];
-          __builtin_memcpy(w[0][j].w, v, sizeof(v));
-        }
-      }
-    } else {
+  // weights: eight slots of a column (a row of B), or four columns of eight slots (rows of A)
+  const W* W0 = (const W*)(TRANS ? P.A : P.B) + (int64_t)min(a, P.n - 1) * rank * d;
+  Eight<W> w[TRANS ? 1 : RKS][TRANS ? 1 : NJ];
+  uint32_t wt[TRANS ? RKS : 1][TRANS ? NJ / 4 : 1][8][sizeof(W)];
+  if constexpr (!TRANS) {
+    by_rank_kind(rank, [&](auto kind) {
 #pragma unroll
       for (int s = 0; s < RKS; ++s)
 #pragma unroll
-        for (int g = 0; g < NJ / 4; ++g)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            load_words<W, 4>(wt[s][g][e], W0 + (int64_t)slot_source(32 * s + 8 * q + e, rank) * d + min(group(g * 4 / VE), d - VE) + g * 4 % VE);
-    }
-    bf16x8 b[MT][RKS][3];
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int s = 0; s < RKS; ++s) {
-        float f[8] = {};
-        const float* from = h.parts + (int64_t)((tile + t) * 16 + m) * h.RR;
-        if (rank >= 8) {
-          from += min(32 * s + 8 * q, rank - 8);
-#pragma unroll 4
-          for (int k = 0; k < h.splits; ++k, from += (int64_t)h.places * h.RR) {
-            float v[8];
-            __builtin_memcpy(v, from, sizeof(v));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] += v[e];
-          }
-        } else {
-          for (int k = 0; k < h.splits; ++k, from += (int64_t)h.places * h.RR)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] += from[slot_source(e, rank)];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int slot = 32 * s + 8 * q + e;
-          f[e] = slot_of(slot_source(slot, rank), rank) == slot ? f[e] : 0.f;
-        }
-        cut(f, b[t][s]);
-      }
+        for (int j = 0; j < NJ; ++j)
+          load_slots<W, decltype(kind)::value>(w[s][j].w, W0 + (int64_t)(min(group(j / VE), d - VE) + j % VE) * rank, 32 * s + 8 * q, rank);
+    });
+  } else {
 #pragma unroll
     for (int s = 0; s < RKS; ++s)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        Eight<W> v;
-        if constexpr (TRANS) v = column<W, 4>(wt[s][j / 4], j % 4); else v = w[s][j];
-        bf16x8 p[kPieces<W>];
-        cut(v, p);
+      for (int g = 0; g < NJ / 4; ++g)
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t][j] = mma(b[t][s], p, acc[t][j]);
-      }
+        for (int e = 0; e < 8; ++e)
+          load_words<W, 4>(wt[s][g][e], W0 + (int64_t)slot_source(32 * s + 8 * q + e, rank) * d + min(group(g * 4 / VE), d - VE) + g * 4 % VE);
   }
+  uint32_t once[RKS] = {};      // a bit for each of the lane's slots that is not a repetition
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
+  for (int s = 0; s < RKS; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int slot = 32 * s + 8 * q + e;
+      once[s] |= (slot_of(slot_source(slot, rank), rank) == slot ? 1u : 0u) << e;
+    }
+#pragma unroll 1
+  for (int tile = first; tile < first + per; ++tile) {
+    int rows[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) rows[i] = find_row<FEW>(plan, P.ids, P.T, P.n, tile, 4 * q + i);
+    struct Group { uint32_t w[4]; } base[4][NG] = {};
+    if (P.base)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Y* from = (const Y*)P.base + real_row(rows[i]) * P.base_stride;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) __builtin_memcpy(base[i][g].w, from + min(group(g), d - VE), 16);
+      }
+    f32x4 acc[NJ] = {};
+    if (a < P.n) {
+      bf16x8 b[RKS][3];
+      float f[RKS][8] = {};
+      by_rank_kind(rank, [&](auto kind) {
+        const float* from = h.parts + (int64_t)(tile * 16 + m) * h.RR;
+        auto add = [&](int first, auto count) {      // parts from `first` on, those past the last one read again and not added
+          constexpr int N = decltype(count)::value;
+          Eight<float> v[N][RKS];
+#pragma unroll
+          for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int s = 0; s < RKS; ++s)
+              load_slots<float, decltype(kind)::value>(v[k][s].w, from + min(first + k, h.splits - 1) * (int64_t)h.places * h.RR, 32 * s + 8 * q, rank);
+#pragma unroll
+          for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int s = 0; s < RKS; ++s)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) f[s][e] += first + k < h.splits ? __builtin_bit_cast(float, v[k][s].w[e]) : 0.f;
+        };
+        if (h.splits == 1) add(0, std::integral_constant<int, 1>{});
+        else
+          for (int k = 0; k < h.splits; k += 4) add(k, std::integral_constant<int, 4>{});
+      });
+#pragma unroll
+      for (int s = 0; s < RKS; ++s) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[s][e] = (once[s] >> e) & 1 ? f[s][e] : 0.f;
+        cut(f[s], b[s]);
+      }
+#pragma unroll
+      for (int s = 0; s < RKS; ++s)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          Eight<W> v;
+          if constexpr (TRANS) v = column<W, 4>(wt[s][j / 4], j % 4); else v = w[s][j];
+          if constexpr (std::is_same<W, _Float16>::value) {      // (cut anew for every tile: the pieces of all would not fit the registers)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(v.w[i]));
+          }
+          bf16x8 p[kPieces<W>];
+          cut(v, p);
+          acc[j] = mma(b[s], p, acc[j]);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (rows[t][i] < 0) continue;
-      Y* out = (Y*)P.out + rows[t][i] * P.out_stride;
+      if (rows[i] < 0) continue;
+      Y* out = (Y*)P.out + rows[i] * P.out_stride;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         const int c = group(g), at = min(c, d - VE);
         Y v[VE];
-        __builtin_memcpy(v, base[t][i][g].w, 16);
+        __builtin_memcpy(v, base[i][g].w, 16);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) v[e] = (Y)(acc[t][g * VE + e][i] + (float)v[e]);
+        for (int e = 0; e < VE; ++e) v[e] = (Y)(acc[g * VE + e][i] + (float)v[e]);
         if (at == c) {
           __builtin_memcpy(out + c, v, 16);
         } else {
@@ -538,6 +587,7 @@ __global__ __launch_bounds__(256, 2) void k_adapter_up(AdapterArgs P, Plan plan,
         }
       }
     }
+  }
 }
 
 // ---- dA = sum of g x^T, dB = sum of h dy^T: products of 16 (rank) x 16 NJ (columns), the places split over the wavefronts ----
@@ -730,12 +780,12 @@ int segment_shift(const AdapterArgs& a) {
   return k;
 }
 
-// Shares of the columns in the narrowing products of the forward pass, each a workgroup of four wavefronts: as many as give the chip
-// two workgroups per compute unit, while a wavefront has two units of 128 bytes of its rows or more.
-inline int column_splits(const AdapterArgs& a, int tiles) {
-  const int units = a.dtype == MOEQ_F32 ? (a.d_in + 31) / 32 : (a.d_in + 63) / 64;
+// Shares of the columns in the narrowing products, each a workgroup of four wavefronts: as many as give the chip `want` workgroups,
+// while a wavefront has two units of 128 bytes of its rows or more.
+inline int column_splits(const AdapterArgs& a, int d, int tiles, int want) {
+  const int units = a.dtype == MOEQ_F32 ? (d + 31) / 32 : (d + 63) / 64;
   int k = 1;
-  while (k < 8 && units >= 16 * k && tiles * k < 512) k *= 2;
+  while (k < 8 && units >= 16 * k && tiles * k < want) k *= 2;
   return k;
 }
 
@@ -754,12 +804,13 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     s.narrow_h = (float*)take((size_t)a.T * a.rank * 4);
     if (backward) s.narrow_g = (float*)take((size_t)a.T * a.rank * 4);
   } else if (s.form == kFew) {
-    s.h = Pieces{(float*)take((size_t)8 * a.T * 16 * RR * 4), nullptr, RR, 16 * a.T, column_splits(a, a.T)};
+    s.h = Pieces{(float*)take((size_t)8 * a.T * 16 * RR * 4), nullptr, RR, 16 * a.T, column_splits(a, a.d_in, a.T, 512)};
   } else {
     Plan& p = s.plan;
-    // Rows of a tile: as many as share the weights that are read for them, unless that is mostly padding.
-    s.MT = a.T < 64 * (int64_t)a.n ? 1 : s.RT == 1 || a.T < 256 * (int64_t)a.n || backward ? 2 : 4;
-    s.TP = backward ? 32 : 16 * s.MT;
+    // Rows of a tile: as many as share the weights that are read for them, unless that is mostly padding (or, of 64, leaves the chip's
+    // last round of workgroups half empty). The narrowing products take 16 MT of them at a time, two or four times their rank at most.
+    s.TP = backward ? (a.T >= 16384 && a.T >= 512 * (int64_t)a.n ? 64 : 32) : a.T < 64 * (int64_t)a.n ? 16 : a.T < 256 * (int64_t)a.n || a.T < 8192 ? 32 : 64;
+    s.MT = s.TP == 64 ? (s.RT == 1 || backward ? 2 : 4) : s.TP / 16;
     // every bin that has rows adds at most a tile less a row of padding (room: of the largest tile)
     const int pad = (s.TP - 1) * std::min(a.T, a.n + 1), most = 63 * std::min(a.T, a.n + 1), room = a.T + most, room_split = std::min(16, a.T / 256) + most / 256 + 1;
     p.places = (a.T + pad) / s.TP * s.TP;
@@ -767,7 +818,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     p.rowof = (int32_t*)take((size_t)room * 4);
     p.tile_adapter = (int32_t*)take((size_t)room / 16 * 4 + 4);
     if (!backward) {
-      s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, p.tiles)};
+      s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, a.d_in, p.tiles, 512)};
       // (several shares only of less than 512 tiles)
       s.h.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 512 * 64)) * RR * 4);
     } else {
@@ -776,10 +827,12 @@ Setup set_up(const AdapterArgs& a, bool backward) {
       p.n_split = p.places >> p.seg_shift;
       p.segments = (Segment*)take((size_t)(a.n + 1 + room_split) * sizeof(Segment));
       p.split = (Segment*)take((size_t)room_split * sizeof(Segment));
-      s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, 1};
-      s.g = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, 1};
-      float* parts = (float*)take((size_t)room * RR * 4);
-      s.g.parts = a.out ? parts : nullptr;
+      s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, column_splits(a, std::min(a.d_in, a.d_out), p.tiles, 1024)};
+      s.g = s.h;
+      s.g.by_rank = (uint16_t*)take((size_t)room * 3 * RR * 2);
+      // (several shares only of less than 1024 tiles)
+      s.h.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 1024 * 32)) * RR * 4);
+      s.g.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 1024 * 32)) * RR * 4);
       // (segments of at least 256 rows, at most 16 of them in the rows themselves: segment_shift)
       s.part = (float*)take((size_t)2 * room_split * a.rank * (a.d_in + a.d_out) * 4);
     }
@@ -806,11 +859,11 @@ hipError_t with_rank(int RT, F&& f) {
   return f(std::integral_constant<int, 4>{});
 }
 
-// Rows in tiles of 16 MT, or of 16 where the weights take the registers (two steps of the rank).
-template <typename Y, typename W, int RKS, int MT, bool TRANS, bool FEW>
+template <typename Y, typename W, int RKS, bool TRANS, bool FEW>
 hipError_t launch_up(const AdapterArgs& a, const Setup& s, const Pieces& h, int d, hipStream_t st) {
-  constexpr int NJ = sizeof(W) == 4 ? 4 : 8, M = RKS == 2 ? 1 : MT;
-  hipLaunchKernelGGL((k_adapter_up<Y, W, RKS, NJ, M, TRANS, FEW>), dim3((d + 64 * NJ - 1) / (64 * NJ), FEW ? a.T : s.plan.places / (16 * M)), dim3(256), 0, st, a, s.plan, s.TP, h, d);
+  constexpr int NJ = sizeof(W) == 4 ? 4 : 8;
+  const int per = FEW ? 1 : s.TP / 16;
+  hipLaunchKernelGGL((k_adapter_up<Y, W, RKS, NJ, TRANS, FEW>), dim3((d + 64 * NJ - 1) / (64 * NJ), FEW ? a.T : s.plan.tiles), dim3(256), 0, st, a, s.plan, s.TP, h, d, per);
   return hipGetLastError();
 }
 template <typename W, int RT, int MT, bool FEW>
@@ -869,9 +922,8 @@ hipError_t launch_adapters_forward(const AdapterArgs& a, hipStream_t st) {
       hipError_t e = s.form == kFew ? launch_down<W, RT, 1, true>(a, s, st) : s.MT == 1 ? launch_down<W, RT, 1, false>(a, s, st)
                    : s.MT == 2 || RT == 1 ? launch_down<W, RT, 2, false>(a, s, st) : launch_down<W, RT, RT == 1 ? 2 : 4, false>(a, s, st);
       if (e != hipSuccess) return e;
-      if (s.form == kFew) return launch_up<Y, W, RKS, 1, false, true>(a, s, s.h, a.d_out, st);
-      if (s.MT == 1) return launch_up<Y, W, RKS, 1, false, false>(a, s, s.h, a.d_out, st);
-      return launch_up<Y, W, RKS, 2, false, false>(a, s, s.h, a.d_out, st);
+      if (s.form == kFew) return launch_up<Y, W, RKS, false, true>(a, s, s.h, a.d_out, st);
+      return launch_up<Y, W, RKS, false, false>(a, s, s.h, a.d_out, st);
     });
   });
 }
@@ -886,19 +938,23 @@ hipError_t launch_adapters_backward(const AdapterArgs& a, hipStream_t st) {
     return with_rank(s.RT, [&](auto rt) {
       constexpr int RT = decltype(rt)::value, RKS = RT == 4 ? 2 : 1, MT = 2;
       if (a.T) {
-        hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT>), dim3(s.plan.places / (16 * MT), 2), dim3(512), 0, st, a, s.plan, s.TP, s.h, s.g);
+        hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT>), dim3(s.plan.places / (16 * MT), 2 * s.h.splits), dim3(256), 0, st, a, s.plan, s.TP, s.h, s.g);
+        hipLaunchKernelGGL(k_adapter_pieces, dim3(s.plan.places / 32, 2), dim3(256), 0, st, s.h, s.g);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        if (a.out)
-          if (hipError_t e = launch_up<Y, W, RKS, 2, true, false>(a, s, s.g, a.d_in, st); e != hipSuccess) return e;
       }
+      // (the weights' gradients first: what the products before them read of x and dy may still be in the cache)
       const int sa = (a.d_in + 256 / (int)sizeof(W) - 1) / (256 / (int)sizeof(W)), sb = (a.d_out + 256 / (int)sizeof(Y) - 1) / (256 / (int)sizeof(Y));
       hipLaunchKernelGGL((k_adapter_weights<W, Y, RT>), dim3(sa + sb, s.plan.n_segments), dim3(256), 0, st, a, s.plan, s.h, s.g, sa, s.part);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       if (s.plan.n_split) {
         const int64_t all = (int64_t)a.rank * (a.d_in + a.d_out);
         hipLaunchKernelGGL(k_adapter_join, dim3((unsigned)std::min<int64_t>((all + 255) / 256, 1024), s.plan.n_split), dim3(256), 0, st, a, s.plan, s.part);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       }
-      return hipGetLastError();
+      if (!a.T || !a.out) return hipSuccess;
+      Pieces g = s.g;
+      g.splits = 1;
+      return launch_up<Y, W, RKS, true, false>(a, s, g, a.d_in, st);
     });
   });
 }

@@ -13,8 +13,9 @@ constexpr int64_t kSortChunk = 4096;     // pairs of a workgroup beyond
 
 __global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ idx, int pairs, int run, int E,
                                                    int32_t* __restrict__ offsets, int32_t* __restrict__ order, int32_t* __restrict__ slot) {
-  __shared__ int cnt[kSortCounts], place[kSortMaxExperts + 1];
-  sort_pairs(idx, pairs, run, E, cnt, [&](int e, int n) { place[e] = n; },
+  __shared__ SortShared sh;
+  __shared__ int place[kSortMaxExperts + 1];
+  sort_pairs(idx, pairs, run, E, sh, [&](int e, int n) { place[e] = n; },
              [&] {
                if (threadIdx.x < 64) {
                  sort_scan(E, place);
@@ -41,10 +42,11 @@ __global__ __launch_bounds__(1024) void k_sort_count(const int32_t* __restrict__
 __global__ __launch_bounds__(1024) void k_sort_chunk(const int32_t* __restrict__ idx, int64_t pairs, int run, int E,
                                                      const int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
                                                      int32_t* __restrict__ order, int32_t* __restrict__ slot) {
-  __shared__ int cnt[kSortCounts], place[kSortMaxExperts + 1], ahead[kSortMaxExperts + 1];
+  __shared__ SortShared sh;
+  __shared__ int place[kSortMaxExperts + 1], ahead[kSortMaxExperts + 1];
   const int chunks = gridDim.x, me = blockIdx.x;
   const int64_t a = me * kSortChunk;
-  sort_pairs(idx + a, (int)min(kSortChunk, pairs - a), run, E, cnt,
+  sort_pairs(idx + a, (int)min(kSortChunk, pairs - a), run, E, sh,
              [&](int e, int) {
                int before = 0, all = 0;
 #pragma unroll 8
