@@ -395,8 +395,26 @@ def moe_layer_forward_routed(layer, x, idx, gate, y=None, ws=None, stream=None):
 
 
 # ---- operators beside the layer ----------------------------------------------------------------------------------------------
+# The checks of their tensors, the memory of their outputs and the C ABI calls are in the extension module _calls (csrc/calls.cpp):
+# most of these calls are a kernel or two of a few microseconds.
 
 _DTYPES = {torch.float32: MOEQ_F32, torch.bfloat16: MOEQ_BF16, torch.float16: MOEQ_F16}
+_native = None
+
+
+def _load():
+    global _native
+    L = lib()
+    if not os.path.exists(os.path.join(_HERE, "_calls.so")):
+        from . import build as _build
+        _build.build()
+    from . import _calls
+    names = ("moe_sort_bytes", "moe_sort_pairs", "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward",
+             "moe_adapters_forward", "moe_adapters_backward", "moe_distill_workspace_bytes", "moe_distill_forward",
+             "moe_distill_backward", "moe_distill_loss_grad")
+    _calls.bind(MoeqError, lambda: _stream(None), *[C.cast(getattr(L, n), C.c_void_p).value for n in names])
+    _native = _calls
+    return _calls
 
 
 def _need(ok, what):
@@ -404,33 +422,11 @@ def _need(ok, what):
         raise MoeqError(MOEQ_EINVAL, what)
 
 
-def _dtype(t, what):
-    _need(t in _DTYPES, what)
-    return _DTYPES[t]
-
-
-def _empty(shape, dtype, device, stream):
-    """A tensor for a call on `stream`: memory that the allocator knows to be that stream's."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _matrix(t, rows, cols, what, dtype=None):
-    """The row stride of a [rows][cols] tensor with contiguous rows."""
-    _need(t.is_cuda and t.dim() == 2 and t.shape[0] == rows and t.shape[1] == cols and (dtype is None or t.dtype is dtype), what)
-    _need(cols == 1 or t.stride(1) == 1, what)
-    return t.stride(0)
-
-
-def _plain(t, shape, dtype, what):
-    _need(t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous(), what)
-
-
 class PairSort:
     """The order of a call's (token, choice) pairs by expert: int32 tensors offsets [n_experts + 1], order [pairs] (the pair in
     every place) and slot [pairs] (the place of every pair); pairs without an expert come last, as ~pair and ~place."""
+
+    __slots__ = ("offsets", "order", "slot", "n_tokens", "top_k", "n_experts")
 
     def __init__(self, offsets, order, slot, n_tokens, top_k, n_experts):
         self.offsets, self.order, self.slot = offsets, order, slot
@@ -439,61 +435,35 @@ class PairSort:
 
 def moe_sort_pairs(idx, n_experts, stream=None):
     """idx: device int32 [T][k], the experts that a router chose (outside [0, n_experts): none) -> PairSort."""
-    _need(idx.dim() == 2, "moe_sort_pairs")
-    T, k = idx.shape
-    _plain(idx, (T, k), torch.int32, "moe_sort_pairs")
-    P = T * k
-    ws = int(lib().moe_sort_bytes(T, k, n_experts))
-    buf = _empty((n_experts + 1 + 2 * P + ws // 4,), torch.int32, idx.device, stream)
-    offsets, order, slot, rest = buf.split((n_experts + 1, P, P, ws // 4))
-    at = buf.data_ptr()
-    at_order = at + 4 * (n_experts + 1)
-    _check(lib().moe_sort_pairs(idx.data_ptr(), T, k, n_experts, at, at_order, at_order + 4 * P, at_order + 8 * P, ws,
-                                _stream(stream)), "moe_sort_pairs")
-    return PairSort(offsets, order, slot, T, k, n_experts)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_sort_pairs(idx, n_experts)
+    return PairSort(*(_native or _load()).sort_pairs(idx, n_experts))
 
 
 def moe_gather_rows(sort, x, rows=None, stream=None):
     """The tokens' rows [T][d] in the order of the sort: rows [pairs][d] (zeros for pairs without an expert)."""
-    T, k, d = sort.n_tokens, sort.top_k, x.shape[-1]
-    xs = _matrix(x, T, d, "moe_gather_rows")
-    if rows is None:
-        rows = _empty((T * k, d), x.dtype, x.device, stream)
-    _check(lib().moe_gather_rows(sort.slot.data_ptr(), T, k, d, _dtype(x.dtype, "moe_gather_rows"), x.data_ptr(), xs,
-                                 rows.data_ptr(), _matrix(rows, T * k, d, "moe_gather_rows", x.dtype), _stream(stream)),
-           "moe_gather_rows")
-    return rows
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_gather_rows(sort, x, rows)
+    return (_native or _load()).gather_rows(sort.slot, sort.n_tokens, sort.top_k, x, rows)
 
 
 def moe_combine_rows(sort, rows, gate=None, dtype=None, y=None, stream=None):
     """Rows in the order of the sort back to tokens: y[t] = sum of gate[t][j] * row (gate None: ones, the gradient of
     moe_gather_rows). dtype: of y, the rows' own (default) or fp32."""
-    T, k, d = sort.n_tokens, sort.top_k, rows.shape[-1]
-    rs = _matrix(rows, T * k, d, "moe_combine_rows")
-    if gate is not None:
-        _plain(gate, (T, k), torch.float32, "moe_combine_rows")
-    if y is None:
-        y = _empty((T, d), dtype or rows.dtype, rows.device, stream)
-    _check(lib().moe_combine_rows(sort.slot.data_ptr(), _ptr(gate), T, k, d, _dtype(rows.dtype, "moe_combine_rows"),
-                                  rows.data_ptr(), rs, _dtype(y.dtype, "moe_combine_rows"), y.data_ptr(),
-                                  _matrix(y, T, d, "moe_combine_rows", dtype), _stream(stream)), "moe_combine_rows")
-    return y
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_combine_rows(sort, rows, gate, dtype, y)
+    return (_native or _load()).combine_rows(sort.slot, sort.n_tokens, sort.top_k, rows, gate, dtype, y)
 
 
 def moe_combine_rows_backward(sort, dy, rows, gate=None, drows=None, stream=None):
     """The gradient of moe_combine_rows: (drows [pairs][d] in the rows' dtype, dgate [T][k] fp32)."""
-    T, k, d = sort.n_tokens, sort.top_k, rows.shape[-1]
-    what = "moe_combine_rows_backward"
-    rs, ds = _matrix(rows, T * k, d, what), _matrix(dy, T, d, what)
-    if gate is not None:
-        _plain(gate, (T, k), torch.float32, what)
-    if drows is None:
-        drows = _empty((T * k, d), rows.dtype, rows.device, stream)
-    dgate = _empty((T, k), torch.float32, rows.device, stream)
-    _check(lib().moe_combine_rows_backward(sort.slot.data_ptr(), _ptr(gate), T, k, d, _dtype(rows.dtype, what), rows.data_ptr(), rs,
-                                           _dtype(dy.dtype, what), dy.data_ptr(), ds, drows.data_ptr(),
-                                           _matrix(drows, T * k, d, what, rows.dtype), dgate.data_ptr(), _stream(stream)), what)
-    return drows, dgate
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_combine_rows_backward(sort, dy, rows, gate, drows)
+    return (_native or _load()).combine_rows_backward(sort.slot, sort.n_tokens, sort.top_k, dy, rows, gate, drows)
 
 
 class Adapters:
@@ -502,14 +472,13 @@ class Adapters:
 
     def __init__(self, a, b, scale):
         what = "Adapters"
-        _need(a.dim() == 3 and b.dim() == 3 and a.shape[0] == b.shape[0] and a.shape[1] == b.shape[2], what)
+        _need(a.dim() == 3 and b.dim() == 3 and scale.dim() == 1 and a.dtype in _DTYPES and b.dtype is a.dtype, what)
         n, r, d_in = a.shape
-        _plain(a, (n, r, d_in), a.dtype, what)
-        _plain(b, (n, b.shape[1], r), a.dtype, what)
-        _plain(scale, (n,), torch.float32, what)
+        _need(b.shape[0] == n and b.shape[2] == r and scale.shape[0] == n and scale.dtype is torch.float32, what)
+        _need(all(t.is_cuda and t.is_contiguous() for t in (a, b, scale)), what)
         self.a, self.b, self.scale = a, b, scale
         self.n_adapters, self.rank, self.d_in, self.d_out, self.dtype = n, r, d_in, b.shape[1], a.dtype
-        self._desc = moeq_adapters(n, r, d_in, self.d_out, _dtype(a.dtype, what), a.data_ptr(), b.data_ptr(), scale.data_ptr())
+        self._desc = moeq_adapters(n, r, d_in, self.d_out, _DTYPES[a.dtype], a.data_ptr(), b.data_ptr(), scale.data_ptr())
         self.handle = C.addressof(self._desc)
         self._ws, self._bytes = None, {}
 
@@ -527,94 +496,44 @@ class Adapters:
 
 def moe_adapters_forward(adapters, x, ids, base=None, y=None, ws=None, stream=None):
     """y[t] = base[t] + scale_a B_a A_a x[t] with a = ids[t] (int32; outside [0, n): no adapter). base: [T][d_out] or None
-    (zeros), may be y itself. y: in the adapters' dtype (default) or fp32. Calls that share a workspace (the adapters' own unless
-    one is passed) have to be ordered."""
-    T, what = x.shape[0], "moe_adapters_forward"
-    xs = _matrix(x, T, adapters.d_in, what, adapters.dtype)
-    _plain(ids, (T,), torch.int32, what)
-    if y is None:
-        y = _empty((T, adapters.d_out), adapters.dtype if base is None else base.dtype, x.device, stream)
-    bs = 0 if base is None else _matrix(base, T, adapters.d_out, what, y.dtype)
-    if ws is None:
-        ws = adapters.workspace(T)
-    _check(lib().moe_adapters_forward(adapters.handle, x.data_ptr(), xs, ids.data_ptr(), T, _ptr(base), bs, _dtype(y.dtype, what),
-                                      y.data_ptr(), _matrix(y, T, adapters.d_out, what), ws.data_ptr(), ws.numel(),
-                                      _stream(stream)), what)
-    return y
+    (zeros), may be y itself. y: in the adapters' dtype or fp32 (default: the base's, or the adapters'). Calls that share a workspace
+    (the adapters' own unless one is passed) have to be ordered."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_adapters_forward(adapters, x, ids, base, y, ws)
+    return (_native or _load()).adapters_forward(adapters.handle, x, ids, base, y, adapters.workspace(len(x)) if ws is None else ws)
 
 
 def moe_adapters_backward(adapters, x, ids, dy, dx_base=None, dx=None, want_dx=True, ws=None, stream=None):
     """The gradient of moe_adapters_forward: (dx [T][d_in] in dy's dtype, dA [n][rank][d_in] fp32, dB [n][d_out][rank] fp32).
     dx_base: added to dx (the gradient through the shared projection), may be dx itself."""
-    T, what = x.shape[0], "moe_adapters_backward"
-    xs, ys = _matrix(x, T, adapters.d_in, what, adapters.dtype), _matrix(dy, T, adapters.d_out, what)
-    _plain(ids, (T,), torch.int32, what)
-    if dx is None and want_dx:
-        dx = _empty((T, adapters.d_in), dy.dtype, x.device, stream)
-    dxs = 0 if dx is None else _matrix(dx, T, adapters.d_in, what, dy.dtype)
-    bs = 0 if dx_base is None else _matrix(dx_base, T, adapters.d_in, what, dy.dtype)
-    dA = _empty(adapters.a.shape, torch.float32, x.device, stream)
-    dB = _empty(adapters.b.shape, torch.float32, x.device, stream)
-    if ws is None:
-        ws = adapters.workspace(T, True)
-    _check(lib().moe_adapters_backward(adapters.handle, x.data_ptr(), xs, ids.data_ptr(), T, _dtype(dy.dtype, what), dy.data_ptr(), ys,
-                                       _ptr(dx_base), bs, _ptr(dx), dxs, dA.data_ptr(), dB.data_ptr(), ws.data_ptr(), ws.numel(),
-                                       _stream(stream)), what)
-    return dx, dA, dB
-
-
-def _distill(logits, top_idx, top_logits, weight, what):
-    _need(logits.dim() == 2 and top_idx.dim() == 2, what)
-    T, V = logits.shape
-    K = top_idx.shape[1]
-    _plain(top_idx, (T, K), torch.int32, what)
-    _plain(top_logits, (T, K), torch.float32, what)
-    if weight is not None:
-        _plain(weight, (T,), torch.float32, what)
-    return T, V, K, _dtype(logits.dtype, what), _matrix(logits, T, V, what)
-
-
-def _distill_ws(T, V, dt, device, stream):
-    need = int(lib().moe_distill_workspace_bytes(T, V, dt))
-    return (None, 0) if need == 0 else (_empty((need,), torch.uint8, device, stream), need)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_adapters_backward(adapters, x, ids, dy, dx_base, dx, want_dx, ws)
+    return (_native or _load()).adapters_backward(adapters.handle, x, ids, dy, dx_base, dx, bool(want_dx),
+                                                  adapters.workspace(len(x), True) if ws is None else ws)
 
 
 def moe_distill_forward(logits, top_idx, top_logits, temperature=1.0, weight=None, stream=None):
     """Distillation from a teacher's top logits [T][K] fp32 at top_idx [T][K] int32 (outside [0, V): no entry): (loss [T], lse [T])
     with loss = w tau^2 KL(softmax(top_logits / tau) || softmax(logits / tau)) and lse = log sum exp(logits / tau)."""
-    what = "moe_distill_forward"
-    T, V, K, dt, ls = _distill(logits, top_idx, top_logits, weight, what)
-    out = _empty((2, T), torch.float32, logits.device, stream)
-    ws, need = _distill_ws(T, V, dt, logits.device, stream)
-    at = out.data_ptr()
-    _check(lib().moe_distill_forward(logits.data_ptr(), ls, dt, T, V, top_idx.data_ptr(), top_logits.data_ptr(), K, temperature,
-                                     _ptr(weight), at, at + 4 * T, _ptr(ws), need, _stream(stream)), what)
-    return out[0], out[1]
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_distill_forward(logits, top_idx, top_logits, temperature, weight)
+    return (_native or _load()).distill_forward(logits, top_idx, top_logits, temperature, weight)
 
 
 def moe_distill_backward(logits, top_idx, top_logits, lse, dloss, temperature=1.0, weight=None, dlogits=None, stream=None):
     """dlogits [T][V] in the logits' dtype from the forward's lse and the gradients of the losses, both [T] fp32."""
-    what = "moe_distill_backward"
-    T, V, K, dt, ls = _distill(logits, top_idx, top_logits, weight, what)
-    _plain(lse, (T,), torch.float32, what)
-    _plain(dloss, (T,), torch.float32, what)
-    if dlogits is None:
-        dlogits = _empty((T, V), logits.dtype, logits.device, stream)
-    _check(lib().moe_distill_backward(logits.data_ptr(), ls, dt, T, V, top_idx.data_ptr(), top_logits.data_ptr(), K, temperature,
-                                      _ptr(weight), lse.data_ptr(), dloss.data_ptr(), dlogits.data_ptr(),
-                                      _matrix(dlogits, T, V, what, logits.dtype), _stream(stream)), what)
-    return dlogits
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_distill_backward(logits, top_idx, top_logits, lse, dloss, temperature, weight, dlogits)
+    return (_native or _load()).distill_backward(logits, top_idx, top_logits, temperature, weight, lse, dloss, dlogits)
 
 
 def moe_distill_loss_grad(logits, top_idx, top_logits, temperature=1.0, weight=None, dlogits=None, stream=None):
     """(loss [T], the gradient of the losses' sum with respect to the logits [T][V]) in one call."""
-    what = "moe_distill_loss_grad"
-    T, V, K, dt, ls = _distill(logits, top_idx, top_logits, weight, what)
-    loss = _empty((T,), torch.float32, logits.device, stream)
-    if dlogits is None:
-        dlogits = _empty((T, V), logits.dtype, logits.device, stream)
-    ws, need = _distill_ws(T, V, dt, logits.device, stream)
-    _check(lib().moe_distill_loss_grad(logits.data_ptr(), ls, dt, T, V, top_idx.data_ptr(), top_logits.data_ptr(), K, temperature,
-                                       _ptr(weight), loss.data_ptr(), dlogits.data_ptr(),
-                                       _matrix(dlogits, T, V, what, logits.dtype), _ptr(ws), need, _stream(stream)), what)
-    return loss, dlogits
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_distill_loss_grad(logits, top_idx, top_logits, temperature, weight, dlogits)
+    return (_native or _load()).distill_loss_grad(logits, top_idx, top_logits, temperature, weight, dlogits)

@@ -1,12 +1,14 @@
-"""Builds libmoeq.so (HIP kernels + C ABI) for gfx950 with hipcc, in-tree."""
+"""Builds libmoeq.so (HIP kernels + C ABI) for gfx950 with hipcc, and _calls.so (the native side of the binding), in-tree."""
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoeq.so")
+CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["api.cpp", "router.hip", "ffn_decode.hip", "decode_fused.hip", "decode_small.hip", "decode_stream.hip", "decode_batch.hip", "prefill.hip", "group_gemm.hip", "quant.hip",
            "operators.cpp", "dispatch.hip", "adapters.hip", "distill.hip"]
 
@@ -22,11 +24,21 @@ def sources():
     return [os.path.join(CSRC, s) for s in SOURCES]
 
 
+def calls_command():
+    """The extension module behind binding.py: host code against the headers and libraries of the torch that imports it."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    return ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+            "-I", os.path.join(at, "include"), "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+            "-I", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), os.path.join(CSRC, "calls.cpp"), "-o", CALLS,
+            "-L" + os.path.join(at, "lib"), "-lc10", "-ltorch_cpu", "-ltorch", "-ltorch_python"]
+
+
 def stale():
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
-    deps = sources() + [os.path.join(CSRC, "moeq_internal.h"), os.path.join(CSRC, "decode_core.h"),
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
+    deps = sources() + [os.path.join(CSRC, "calls.cpp"), os.path.join(CSRC, "moeq_internal.h"), os.path.join(CSRC, "decode_core.h"),
                         os.path.join(CSRC, "small_split.h"), os.path.join(CSRC, "operators.h"), os.path.join(CSRC, "sort_core.h"), os.path.join(ROOT, "include", "moeq.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -34,7 +46,7 @@ def stale():
 def build(verbose=False):
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objs = []
-    procs = []
+    procs = [(cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)) for cmd in [calls_command()]]
     for src in sources():
         obj = os.path.join(CSRC, os.path.basename(src) + ".o")
         cmd = [hipcc] + FLAGS + ["-c", src, "-o", obj]
@@ -46,7 +58,7 @@ def build(verbose=False):
         out, _ = p.communicate()
         out = "\n".join(l for l in out.splitlines() if "packed-fp32-ops" not in l)
         if p.returncode != 0:
-            raise RuntimeError("hipcc failed: %s\n%s" % (" ".join(cmd), out))
+            raise RuntimeError("build failed: %s\n%s" % (" ".join(cmd), out))
         if verbose and out.strip():
             print(out)
     link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", LIB]
