@@ -1,0 +1,74 @@
+"""The operators together, as healing.py uses them: gradients of the whole path against differences of its loss, and that training on a
+teacher's top logits brings a layer of 2-bit experts nearer to it."""
+import pytest
+import torch
+
+from paper_2308_14352_amd import healing
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def setup(tokens, seed=3):
+    teacher, student, g = healing.teacher_and_student(d=128, f=256, n_experts=6, seed=seed)
+    head = torch.randn((1000, 128), device=DEV, generator=g) * 0.3
+    adapted = healing.AdaptedLayer(student, rank=8, generator=g)
+    batch = next(healing.teacher_batches(teacher, head, g, 1, tokens=tokens, top=16))
+    return teacher, adapted, head, g, batch
+
+
+def test_a_fresh_adapter_changes_nothing():
+    _, adapted, _, _, (x, _, _) = setup(50)
+    y, _ = adapted.forward(x)
+    assert torch.equal(y, healing.B.moe_layer_forward(adapted.layer, x))
+
+
+def test_gradients_against_differences():
+    """The logits are linear in B and in A, the loss of a row is smooth in them: along a direction that moves a logit by s, its second
+    difference is at most s^2 / 4 and its third below s^3, so a central difference with a step h is off by h^2 s^3 / 6 a row."""
+    _, adapted, head, g, (x, idx, top) = setup(60)
+    ad = adapted.adapters
+    ad.b.normal_(generator=g).mul_(0.1)
+    _, dA, dB = healing.loss_and_gradients(adapted, head, x, idx, top)
+
+    def total(t, v, by):
+        t.add_(v, alpha=by)
+        y, _ = adapted.forward(x)
+        t.add_(v, alpha=-by)
+        return healing.B.moe_distill_forward(y @ head.t(), idx, top)[0].double().sum().item()
+
+    h = 2.0**-6
+    for t, grad in ((ad.a, dA), (ad.b, dB)):
+        v = torch.randn(t.shape, device=DEV, generator=g) * (0.1 if t is ad.b else 1 / 128**0.5)
+        y0 = adapted.forward(x)[0]
+        t.add_(v)
+        s = ((adapted.forward(x)[0] - y0) @ head.t()).abs().amax(1).double()      # the largest move of each row's logits
+        t.sub_(v)
+        diff = (total(t, v, h) - total(t, v, -h)) / (2 * h)
+        # losses of up to 20 in fp32, whose logits come from sums of 128 products off by some 2^-22 of their size of 30
+        tol = h * h / 6 * (s**3).sum().item() + 60**0.5 * 2.0**-22 * 60 / (2 * h)
+        assert abs(diff - (grad.double() * v.double()).sum().item()) < tol
+
+
+def test_healing_brings_the_student_nearer_to_its_teacher():
+    teacher, adapted, head, g, _ = setup(8)
+    losses = [loss.item() for loss in healing.heal(adapted, head, healing.teacher_batches(teacher, head, g, 60, tokens=512, top=16), lr=5e-3)]
+    assert sum(losses[-5:]) < 0.9 * sum(losses[:5]), losses[::10]
+
+
+def test_graph_of_a_training_step():
+    """The path's own calls are captured; what lies between them are torch's products."""
+    _, adapted, head, _, (x, idx, top) = setup(300)
+    step = lambda: healing.loss_and_gradients(adapted, head, x, idx, top)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for _ in range(3):
+        x.normal_()
+        adapted.adapters.b.normal_(std=0.05)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, step()):
+            assert torch.allclose(a, b, rtol=1e-3, atol=1e-4)       # (the library's products may take another form in a capture)
