@@ -579,7 +579,7 @@ __global__ __launch_bounds__(256, RKS == 1 ? 3 : 2) void k_adapter_up(AdapterArg
 #pragma unroll
         for (int e = 0; e < VE; ++e) v[e] = (Y)(acc[g * VE + e][i] + (float)v[e]);
         if (at == c) {
-          __builtin_memcpy(out + c, v, 16);
+          stream_out(out + c, v);
         } else {
 #pragma unroll
           for (int e = 0; e < VE; ++e)

@@ -111,14 +111,27 @@ __global__ __launch_bounds__(256) void k_gather_rows(RowsArgs A) {
   for (int j0 = 0; j0 < A.k; j0 += KB) {
     Choice ch[KB];
     take_choices(A, t, j0, ch);
-    for_pieces<16 / sizeof(T), G>(A.d, [&](int c, auto size, bool) {
-      constexpr int N = decltype(size)::value;
-      T v[N], z[N] = {};
-      __builtin_memcpy(v, x + c, sizeof(v));
+    // (two pieces on their way together: a thread has two or four of a wide row, and the whole call is one round of workgroups)
+    constexpr int VE = 16 / sizeof(T);
+    if (A.d >= VE) {
+      for (int c = (threadIdx.x % G) * VE; c < A.d; c += 2 * G * VE) {
+        T v[2][VE], z[VE] = {};
+        const int at[2] = {min(c, A.d - VE), min(c + G * VE, A.d - VE)};
 #pragma unroll
-      for (int j = 0; j < KB; ++j)
-        if (ch[j].row) __builtin_memcpy((T*)A.out + (int64_t)ch[j].place * A.out_stride + c, ch[j].kept ? v : z, sizeof(v));
-    });
+        for (int i = 0; i < 2; ++i) __builtin_memcpy(v[i], x + at[i], 16);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (i == 0 || c + G * VE < A.d)
+#pragma unroll
+            for (int j = 0; j < KB; ++j)
+              if (ch[j].row) stream_out((T*)A.out + (int64_t)ch[j].place * A.out_stride + at[i], ch[j].kept ? v[i] : z);
+      }
+    } else {
+      for (int c = threadIdx.x % G; c < A.d; c += G)
+#pragma unroll
+        for (int j = 0; j < KB; ++j)
+          if (ch[j].row) ((T*)A.out)[(int64_t)ch[j].place * A.out_stride + c] = ch[j].kept ? x[c] : (T)0.f;
+    }
   }
 }
 
@@ -147,7 +160,7 @@ __global__ __launch_bounds__(256) void k_combine_rows(RowsArgs A) {
       take_choices(A, t, j0, more);
       add(more);
     }
-    store_n((Y*)A.out + (int64_t)t * A.out_stride + c, acc);
+    stream_n((Y*)A.out + (int64_t)t * A.out_stride + c, acc);
   });
 }
 
@@ -179,7 +192,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(RowsArgs A) {
           sum[j] = i >= first ? fmaf(v[i], r[j][i], sum[j]) : sum[j];
           o[i] = ch[j].kept ? ch[j].gate * v[i] : 0.f;
         }
-        if (ch[j].row) store_n((T*)A.out + (int64_t)ch[j].place * A.out_stride + c, o);
+        if (ch[j].row) stream_n((T*)A.out + (int64_t)ch[j].place * A.out_stride + c, o);
       }
     });
     if (!A.dgate) continue;

@@ -41,6 +41,20 @@ struct Stat { float m, s; };
 __device__ __forceinline__ float origin(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ float rescale(Stat a, float m, float c) { return a.s * __builtin_amdgcn_exp2f((origin(a.m) - origin(m)) * c); }
 
+// ---- a row as vectors of 16 bytes that lie on a multiple of 16 in the gradient (in the logits, where there is none), with single
+// elements before the first and behind the last: rows of an odd length begin anywhere, and a store across two lines is two of them ----
+template <typename T>
+struct Span {
+  static constexpr int VE = 16 / sizeof(T);
+  int V, head, n;        // elements, those before the first vector, vectors
+  __device__ __forceinline__ Span(const T* at, int V) : V(V) {
+    head = min((int)(-(uintptr_t)at % 16 / sizeof(T)), V);
+    n = (V - head) / VE;
+  }
+  __device__ __forceinline__ int singles() const { return V - n * VE; }
+  __device__ __forceinline__ int single(int i) const { return i < head ? i : i + n * VE; }      // element of the i-th single one
+};
+
 // ---- a piece of a row in registers: vectors of 16 bytes, v = thread + i threads ----
 template <typename T, int NV>
 struct Held {
@@ -175,39 +189,45 @@ __device__ __forceinline__ void put_piece(const Held<T, NV>& held, T* dz, int n,
       held.get(i, v);
 #pragma unroll
       for (int e = 0; e < VE; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - o) * c) * by;
-      store_n(dz + ((int)threadIdx.x + i * threads) * VE, v);
+      stream_n(dz + ((int)threadIdx.x + i * threads) * VE, v);
     }
   if (rest) *dlast = (T)(__builtin_amdgcn_exp2f((last - o) * c) * by);
 }
 template <typename T>
-__device__ __forceinline__ void put_zeros(T* dz, int V) {
+__device__ __forceinline__ void put_zeros(T* dz, int n, bool rest, T* dlast) {
   constexpr int VE = 16 / sizeof(T);
   const float zero[VE] = {};
-  for (int i = threadIdx.x; i < V / VE; i += blockDim.x) store_n(dz + (int64_t)i * VE, zero);
-  if ((int)threadIdx.x < V % VE) dz[V / VE * VE + threadIdx.x] = (T)0.f;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) stream_n(dz + (int64_t)i * VE, zero);
+  if (rest) *dlast = (T)0.f;
+}
+// Before elements are written again by other threads: the workgroup's stores have arrived.
+__device__ __forceinline__ void stores_done() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
 }
 
 // ---- a row a workgroup: loss, log-sum-exp and gradient, whichever are wanted ----
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void k_distill_row(DistillArgs A) {
-  constexpr int VE = 16 / sizeof(T);
   __shared__ Teacher teacher;
   __shared__ Stat sh[THREADS / 64];
-  const int t = blockIdx.x, V = A.V, n = V / VE;
+  const int t = blockIdx.x;
   const T* z = (const T*)A.logits + (int64_t)t * A.stride;
   T* dz = A.dlogits ? (T*)A.dlogits + (int64_t)t * A.dstride : nullptr;
+  const Span<T> row(dz ? dz : z, A.V);
+  const bool rest = (int)threadIdx.x < row.singles();
+  const int single = row.single(threadIdx.x);
   const float w = A.weight ? A.weight[t] : 1.f, c = kLog2e / A.temperature;
   if (w == 0.f && !A.lse) {
     if (threadIdx.x == 0) A.loss[t] = 0.f;
-    if (dz) put_zeros(dz, V);
+    if (dz) put_zeros(dz + row.head, row.n, rest, dz + single);
     return;
   }
   Held<T, NV> held;
-  if (n) held.load(z, n, THREADS);
-  const bool rest = (int)threadIdx.x < V % VE;
-  const float last = rest ? (float)z[n * VE + threadIdx.x] : 0.f;
+  if (row.n) held.load(z + row.head, row.n, THREADS);
+  const float last = rest ? (float)z[single] : 0.f;
   const float plogp = threadIdx.x < 64 ? take_teacher(A, t, z, teacher) : 0.f;
-  const Stat st = piece_stat(held, n, THREADS, rest, last, c, sh);
+  const Stat st = piece_stat(held, row.n, THREADS, rest, last, c, sh);
   if (threadIdx.x < 64) {
     const float loss = row_loss(A, teacher, st, w, plogp);
     if (threadIdx.x == 0) {
@@ -216,27 +236,28 @@ __global__ __launch_bounds__(THREADS) void k_distill_row(DistillArgs A) {
     }
   }
   if (!dz) return;
-  if (!teacher.any) return put_zeros(dz, V);
+  if (!teacher.any) return put_zeros(dz + row.head, row.n, rest, dz + single);
   const float o = origin(st.m), inv = st.s == 0.f ? 0.f : 1.f / st.s, scale = w * A.temperature;
-  put_piece(held, dz, n, THREADS, rest, last, dz + n * VE + threadIdx.x, o, c, inv * scale);
-  __syncthreads();
-  put_teacher(A, teacher, dz, 0, V, o, c, inv, scale);
+  put_piece(held, dz + row.head, row.n, THREADS, rest, last, dz + single, o, c, inv * scale);
+  stores_done();
+  put_teacher(A, teacher, dz, 0, A.V, o, c, inv, scale);
 }
 
-// ---- rows in chunks of a workgroup: vectors [chunk * per, ...), the single elements of the end with the last one ----
+// ---- rows in chunks of a workgroup: vectors [chunk * per, ...); the single elements with the last chunk ----
 constexpr int kChunkThreads = 256, kChunkVectors = 8;
 
 template <typename T>
 __global__ __launch_bounds__(kChunkThreads) void k_distill_stat(DistillArgs A, int per) {
-  constexpr int VE = 16 / sizeof(T);
   __shared__ Stat sh[kChunkThreads / 64];
-  const int t = blockIdx.y, all = A.V / VE, first = blockIdx.x * per, n = min(per, all - first);
+  const int t = blockIdx.y;
   if (A.weight && !A.lse && A.weight[t] == 0.f) return;
-  const T* z = (const T*)A.logits + (int64_t)t * A.stride + (int64_t)first * VE;
+  const T* z = (const T*)A.logits + (int64_t)t * A.stride;
+  const Span<T> row(z, A.V);
+  const int first = blockIdx.x * per, n = min(per, row.n - first);
   Held<T, kChunkVectors> held;
-  held.load(z, n, kChunkThreads);
-  const bool rest = first + n == all && (int)threadIdx.x < A.V % VE;
-  const Stat st = piece_stat(held, n, kChunkThreads, rest, rest ? (float)z[n * VE + threadIdx.x] : 0.f, kLog2e / A.temperature, sh);
+  if (n > 0) held.load(z + row.head + (int64_t)first * Span<T>::VE, n, kChunkThreads);
+  const bool rest = blockIdx.x + 1 == gridDim.x && (int)threadIdx.x < row.singles();
+  const Stat st = piece_stat(held, n, kChunkThreads, rest, rest ? (float)z[row.single(threadIdx.x)] : 0.f, kLog2e / A.temperature, sh);
   if (threadIdx.x == 0) ((Stat*)A.ws)[(int64_t)t * gridDim.x + blockIdx.x] = st;
 }
 
@@ -259,23 +280,24 @@ __global__ __launch_bounds__(64) void k_distill_join(DistillArgs A, int chunks) 
 // The gradient of a chunk: from the chunks' statistics (with the loss, by the first one), or from a saved log-sum-exp.
 template <typename T, bool SAVED>
 __global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, int per, int chunks) {
-  constexpr int VE = 16 / sizeof(T);
   __shared__ Teacher teacher;
   __shared__ Stat sh;
-  const int t = blockIdx.y, all = A.V / VE, first = blockIdx.x * per, n = min(per, all - first), c0 = first * VE;
-  const int c1 = first + n == all ? A.V : c0 + n * VE;
+  const int t = blockIdx.y;
   const T* z = (const T*)A.logits + (int64_t)t * A.stride;
   T* dz = (T*)A.dlogits + (int64_t)t * A.dstride;
+  const Span<T> row(dz, A.V);
+  const int first = blockIdx.x * per, n = min(per, row.n - first), at = row.head + first * Span<T>::VE;
+  const bool rest = blockIdx.x + 1 == gridDim.x && (int)threadIdx.x < row.singles();
+  const int single = row.single(threadIdx.x);
   float w = A.weight ? A.weight[t] : 1.f;
   const float c = kLog2e / A.temperature;
   if (w == 0.f) {
     if (!SAVED && blockIdx.x == 0 && threadIdx.x == 0) A.loss[t] = 0.f;
-    return put_zeros(dz + c0, c1 - c0);
+    return put_zeros(dz + at, n, rest, dz + single);
   }
   Held<T, kChunkVectors> held;
-  if (n > 0) held.load(z + c0, n, kChunkThreads);
-  const bool rest = c1 == A.V && (int)threadIdx.x < A.V % VE;
-  const float last = rest ? (float)z[c0 + n * VE + threadIdx.x] : 0.f;
+  if (n > 0) held.load(z + at, n, kChunkThreads);
+  const float last = rest ? (float)z[single] : 0.f;
   if (threadIdx.x < 64) {
     const float plogp = take_teacher(A, t, z, teacher);
     if constexpr (!SAVED) {
@@ -288,7 +310,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, i
     }
   }
   __syncthreads();
-  if (!teacher.any) return put_zeros(dz + c0, c1 - c0);
+  if (!teacher.any) return put_zeros(dz + at, n, rest, dz + single);
   float o, inv, scale = w * A.temperature;
   if constexpr (SAVED) {
     // exp(z / tau - lse): the sum's logarithm as an origin of the logits, and nothing left to divide by
@@ -298,9 +320,14 @@ __global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, i
   } else {
     o = origin(sh.m), inv = sh.s == 0.f ? 0.f : 1.f / sh.s;
   }
-  put_piece(held, dz + c0, n, kChunkThreads, rest, last, dz + c0 + n * VE + threadIdx.x, o, c, inv * scale);
-  __syncthreads();
-  put_teacher(A, teacher, dz, c0, c1, o, c, inv, scale);
+  put_piece(held, dz + at, n, kChunkThreads, rest, last, dz + single, o, c, inv * scale);
+  stores_done();
+  // the teacher's entries among this chunk's vectors, and, with the last chunk, among the single elements
+  put_teacher(A, teacher, dz, at, at + max(n, 0) * Span<T>::VE, o, c, inv, scale);
+  if (blockIdx.x + 1 == gridDim.x) {
+    put_teacher(A, teacher, dz, 0, row.head, o, c, inv, scale);
+    put_teacher(A, teacher, dz, row.head + row.n * Span<T>::VE, A.V, o, c, inv, scale);
+  }
 }
 
 // ---- host side ----
