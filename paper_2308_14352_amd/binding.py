@@ -480,18 +480,19 @@ class Adapters:
         self.n_adapters, self.rank, self.d_in, self.d_out, self.dtype = n, r, d_in, b.shape[1], a.dtype
         self._desc = moeq_adapters(n, r, d_in, self.d_out, _DTYPES[a.dtype], a.data_ptr(), b.data_ptr(), scale.data_ptr())
         self.handle = C.addressof(self._desc)
-        self._ws, self._bytes = None, {}
+        self._ws, self._ready = None, {}
 
     def workspace_bytes(self, max_tokens, backward=False):
         return int(lib().moe_adapters_workspace_bytes(self.handle, max_tokens, int(backward)))
 
     def workspace(self, n_tokens, backward=False):
-        need = self._bytes.get((n_tokens, backward))
-        if need is None:
-            need = self._bytes[(n_tokens, backward)] = max(self.workspace_bytes(n_tokens, backward), 16)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device=self.a.device)
-        return self._ws
+        ws = self._ready.get((n_tokens, backward))
+        if ws is None:
+            need = max(self.workspace_bytes(n_tokens, backward), 16)
+            if self._ws is None or self._ws.numel() < need:
+                self._ws, self._ready = torch.empty(need, dtype=torch.uint8, device=self.a.device), {}
+            ws = self._ready[(n_tokens, backward)] = self._ws
+        return ws
 
 
 def moe_adapters_forward(adapters, x, ids, base=None, y=None, ws=None, stream=None):

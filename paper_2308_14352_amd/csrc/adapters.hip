@@ -346,8 +346,8 @@ struct Shrink {
   }
 };
 
-// split: which share of the columns, of h.splits.
-template <typename X, typename W, int RT, int MT, bool TRANS, int WAVES, bool FEW>
+// split: which share of the columns, of h.splits. PIECES: the pieces by rank as well (of all columns).
+template <typename X, typename W, int RT, int MT, bool TRANS, int WAVES, bool FEW, bool PIECES>
 __device__ __forceinline__ void shrink(const AdapterArgs& P, const Plan& plan, int TP, const void* in, int64_t stride, int d, const Pieces& h,
                                        int split, f32x4* red) {
   using S = Shrink<X, W, RT, MT, TRANS>;
@@ -391,8 +391,15 @@ __device__ __forceinline__ void shrink(const AdapterArgs& P, const Plan& plan, i
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = rank_of<RT>(4 * s.q + e, j, P.rank);      // (an index that comes twice has the same sums twice)
-      const float f = row < 0 ? 0.f : v[e] * scale;
+      float f = row < 0 ? 0.f : v[e] * scale;
       h.parts[((int64_t)split * h.places + place) * h.RR + r] = f;
+      if constexpr (PIECES)
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          const uint32_t b = __builtin_bit_cast(uint32_t, f);
+          f -= __builtin_bit_cast(float, b & 0xffff0000u);
+          h.by_rank[(int64_t)(p * h.RR + r) * h.places + place] = b >> 16;
+        }
     }
   }
 }
@@ -400,14 +407,14 @@ __device__ __forceinline__ void shrink(const AdapterArgs& P, const Plan& plan, i
 template <typename W, int RT, int MT, bool FEW>
 __global__ __launch_bounds__(256) void k_adapter_down(AdapterArgs P, Plan plan, int TP, Pieces h) {
   __shared__ f32x4 red[2 * RT * MT * 64];
-  shrink<W, W, RT, MT, false, 4, FEW>(P, plan, TP, P.x, P.x_stride, P.d_in, h, blockIdx.y, red);
+  shrink<W, W, RT, MT, false, 4, FEW, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, blockIdx.y, red);
 }
 // Backward: h of the rows of x in the first half of the grid's second dimension, g of those of dy in the other.
-template <typename W, typename Y, int RT, int MT>
+template <typename W, typename Y, int RT, int MT, bool WHOLE>
 __global__ __launch_bounds__(256) void k_adapter_down_both(AdapterArgs P, Plan plan, int TP, Pieces h, Pieces g) {
   __shared__ f32x4 red[2 * RT * MT * 64];
-  if ((int)blockIdx.y < h.splits) shrink<W, W, RT, MT, false, 4, false>(P, plan, TP, P.x, P.x_stride, P.d_in, h, blockIdx.y, red);
-  else shrink<Y, W, RT, MT, true, 4, false>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, blockIdx.y - h.splits, red);
+  if ((int)blockIdx.y < h.splits) shrink<W, W, RT, MT, false, 4, false, WHOLE>(P, plan, TP, P.x, P.x_stride, P.d_in, h, blockIdx.y, red);
+  else shrink<Y, W, RT, MT, true, 4, false, WHOLE>(P, plan, TP, P.dy, P.dy_stride, P.d_out, g, blockIdx.y - h.splits, red);
 }
 
 // The parts of h (of g) added up in order: as pieces by rank, and in fp32 in the place of the first part. 32 places a workgroup.
@@ -782,10 +789,10 @@ int segment_shift(const AdapterArgs& a) {
 
 // Shares of the columns in the narrowing products, each a workgroup of four wavefronts: as many as give the chip `want` workgroups,
 // while a wavefront has two units of 128 bytes of its rows or more.
-inline int column_splits(const AdapterArgs& a, int d, int tiles, int want) {
+inline int column_splits(const AdapterArgs& a, int d, int tiles, int want, int least) {
   const int units = a.dtype == MOEQ_F32 ? (d + 31) / 32 : (d + 63) / 64;
   int k = 1;
-  while (k < 8 && units >= 16 * k && tiles * k < want) k *= 2;
+  while (k < 8 && units >= least * k && tiles * k < want) k *= 2;
   return k;
 }
 
@@ -804,7 +811,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     s.narrow_h = (float*)take((size_t)a.T * a.rank * 4);
     if (backward) s.narrow_g = (float*)take((size_t)a.T * a.rank * 4);
   } else if (s.form == kFew) {
-    s.h = Pieces{(float*)take((size_t)8 * a.T * 16 * RR * 4), nullptr, RR, 16 * a.T, column_splits(a, a.d_in, a.T, 512)};
+    s.h = Pieces{(float*)take((size_t)8 * a.T * 16 * RR * 4), nullptr, RR, 16 * a.T, column_splits(a, a.d_in, a.T, 512, 16)};
   } else {
     Plan& p = s.plan;
     // Rows of a tile: as many as share the weights that are read for them, unless that is mostly padding (or, of 64, leaves the chip's
@@ -818,7 +825,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     p.rowof = (int32_t*)take((size_t)room * 4);
     p.tile_adapter = (int32_t*)take((size_t)room / 16 * 4 + 4);
     if (!backward) {
-      s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, a.d_in, p.tiles, 512)};
+      s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, a.d_in, p.tiles, 512, 16)};
       // (several shares only of less than 512 tiles)
       s.h.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 512 * 64)) * RR * 4);
     } else {
@@ -827,7 +834,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
       p.n_split = p.places >> p.seg_shift;
       p.segments = (Segment*)take((size_t)(a.n + 1 + room_split) * sizeof(Segment));
       p.split = (Segment*)take((size_t)room_split * sizeof(Segment));
-      s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, column_splits(a, std::min(a.d_in, a.d_out), p.tiles, 1024)};
+      s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, column_splits(a, std::min(a.d_in, a.d_out), p.tiles, 512, 32)};
       s.g = s.h;
       s.g.by_rank = (uint16_t*)take((size_t)room * 3 * RR * 2);
       // (several shares only of less than 1024 tiles)
@@ -938,8 +945,11 @@ hipError_t launch_adapters_backward(const AdapterArgs& a, hipStream_t st) {
     return with_rank(s.RT, [&](auto rt) {
       constexpr int RT = decltype(rt)::value, RKS = RT == 4 ? 2 : 1, MT = 2;
       if (a.T) {
-        hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT>), dim3(s.plan.places / (16 * MT), 2 * s.h.splits), dim3(256), 0, st, a, s.plan, s.TP, s.h, s.g);
-        hipLaunchKernelGGL(k_adapter_pieces, dim3(s.plan.places / 32, 2), dim3(256), 0, st, s.h, s.g);
+        const dim3 grid(s.plan.places / (16 * MT), 2 * s.h.splits);
+        if (s.h.splits == 1) hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT, true>), grid, dim3(256), 0, st, a, s.plan, s.TP, s.h, s.g);
+        else hipLaunchKernelGGL((k_adapter_down_both<W, Y, RT, MT, false>), grid, dim3(256), 0, st, a, s.plan, s.TP, s.h, s.g);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        if (s.h.splits > 1) hipLaunchKernelGGL(k_adapter_pieces, dim3(s.plan.places / 32, 2), dim3(256), 0, st, s.h, s.g);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       }
       // (the weights' gradients first: what the products before them read of x and dy may still be in the cache)
