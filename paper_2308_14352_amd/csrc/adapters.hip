@@ -777,12 +777,13 @@ struct Setup {
   size_t total;
 };
 
-// Rows of a segment of the weights' gradients, as a power of two: 1024, fewer where that leaves too few workgroups for the chip, more
-// in long calls (the partial sums are rank x (d_in + d_out) floats a segment).
+// Rows of a segment of the weights' gradients, as a power of two: 1024, fewer where that leaves too few workgroups for the chip (but not
+// in calls that are one segment, which need no sums to be joined: a launch less), more in long calls (the partial sums are
+// rank x (d_in + d_out) floats a segment).
 int segment_shift(const AdapterArgs& a) {
   const int64_t slices = (a.d_in + 127) / 128 + (a.d_out + 127) / 128;
   int k = 10;
-  while (k > 8 && slices * ((a.T >> k) + 1) < 512) --k;
+  while (k > 8 && a.T > 1024 && slices * ((a.T >> k) + 1) < 512) --k;
   while ((a.T >> k) >= 16) ++k;
   return k;
 }
@@ -831,7 +832,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     } else {
       p.seg_shift = segment_shift(a);
       p.n_segments = a.n + 1 + (p.places >> p.seg_shift);
-      p.n_split = p.places >> p.seg_shift;
+      p.n_split = a.T <= 1 << p.seg_shift ? 0 : p.places >> p.seg_shift;
       p.segments = (Segment*)take((size_t)(a.n + 1 + room_split) * sizeof(Segment));
       p.split = (Segment*)take((size_t)room_split * sizeof(Segment));
       s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, column_splits(a, std::min(a.d_in, a.d_out), p.tiles, 512, 32)};
