@@ -480,7 +480,7 @@ class Adapters:
         self.n_adapters, self.rank, self.d_in, self.d_out, self.dtype = n, r, d_in, b.shape[1], a.dtype
         self._desc = moeq_adapters(n, r, d_in, self.d_out, _DTYPES[a.dtype], a.data_ptr(), b.data_ptr(), scale.data_ptr())
         self.handle = C.addressof(self._desc)
-        self._ws, self._ready = None, {}
+        self._ws, self._ready, self._outgrown = None, {}, []
 
     def workspace_bytes(self, max_tokens, backward=False):
         return int(lib().moe_adapters_workspace_bytes(self.handle, max_tokens, int(backward)))
@@ -490,6 +490,10 @@ class Adapters:
         if ws is None:
             need = max(self.workspace_bytes(n_tokens, backward), 16)
             if self._ws is None or self._ws.numel() < need:
+                # (a captured graph or another stream may still use the one before: it is kept, and twice as large a one taken)
+                if self._ws is not None:
+                    self._outgrown.append(self._ws)
+                    need = max(need, 2 * self._ws.numel())
                 self._ws, self._ready = torch.empty(need, dtype=torch.uint8, device=self.a.device), {}
             ws = self._ready[(n_tokens, backward)] = self._ws
         return ws

@@ -232,3 +232,31 @@ def test_another_stream_and_wide_offsets():
     dx, dA, dB = moeq.moe_adapters_backward(ad, x, ids, got, stream=side)
     side.synchronize()
     assert torch.equal(got, want) and torch.equal(dA, gA) and torch.equal(dB, gB)
+
+
+def test_a_graph_keeps_the_workspace_that_it_was_captured_with():
+    """The adapters' own workspace grows with a longer call: what a graph was captured with is not given away."""
+    rng = rng_of("outgrown")
+    n, r, d = 5, 16, 256
+    m = make(rng, 200, n, r, d, d, torch.bfloat16, torch.bfloat16)
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ids = torch.from_numpy(ids_of(rng, 200, n, "mixed")).to(DEV)
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    step = lambda k: moeq.moe_adapters_forward(ad, g["x"][:k], ids[:k])
+    want = step(200).clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step(200)
+    size, place = ad._ws.numel(), ad._ws.data_ptr()
+    long = torch.randn((5000, d), device=DEV).to(torch.bfloat16)
+    moeq.moe_adapters_forward(ad, long, torch.zeros(5000, dtype=torch.int32, device=DEV))
+    assert ad._ws.numel() >= 2 * size
+    others = [torch.full((size,), 7, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    assert all(t.data_ptr() != place for t in others)
+    for _ in range(3):
+        held.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(held, want) and torch.equal(step(200), want)
+    assert all(bool((t == 7).all()) for t in others)
