@@ -290,7 +290,7 @@ moeq_status moe_unprepare_in(const void *stream_buf, int64_t rows, int64_t cols,
 /* Pairs i = token * top_k + choice, stably sorted by expert idx[i]: offsets [n_experts + 1] (rows of expert e: offsets[e] to
  * offsets[e + 1]), order [pairs] (the pair in every place) and slot [pairs] (the place of every pair). Pairs without an expert
  * (idx outside [0, n_experts)) come last, in their order, as ~pair and ~place (negative). n_experts <= 1024, pairs <= 2^28.
- * ws: moe_sort_bytes (0 for calls of up to some thousand pairs). */
+ * ws: moe_sort_bytes (0 for calls of up to 8192 pairs). */
 size_t moe_sort_bytes(int32_t n_tokens, int32_t top_k, int32_t n_experts);
 moeq_status moe_sort_pairs(const int32_t *idx, int32_t n_tokens, int32_t top_k, int32_t n_experts, int32_t *offsets,
                            int32_t *order, int32_t *slot, void *ws, size_t ws_bytes, void *stream);
@@ -325,8 +325,9 @@ typedef struct {
 size_t moe_adapters_workspace_bytes(const moeq_adapters *adapters, int32_t max_tokens, int32_t backward);
 
 /* y[t] = base[t] + scale_a B_a A_a x[t], a = ids[t]; a row whose id is outside [0, n_adapters) has no adapter: y = base.
- * base_opt NULL: zeros; base may be y itself. base and y are y_dtype: dtype or MOEQ_F32. At most 65535 tokens. A x is held in
- * fp32. An infinity in a row's x, A or B may come out as a NaN. */
+ * base_opt NULL: zeros; base may be y itself. base and y are y_dtype: dtype or MOEQ_F32. At most 65535 tokens. Products are
+ * of the operands' full bits (fp32 as sums of three bf16 pieces, fp16 of two where it meets another type), sums and A x in fp32. An
+ * infinity in a row's x, A or B may come out as a NaN. */
 moeq_status moe_adapters_forward(const moeq_adapters *adapters, const void *x, int64_t x_stride, const int32_t *ids,
                                  int32_t n_tokens, const void *base_opt, int64_t base_stride, int32_t y_dtype, void *y,
                                  int64_t y_stride, void *ws, size_t ws_bytes, void *stream);

@@ -9,6 +9,12 @@
 // products of pieces whose places add up to 2 or less are taken (those left out are below 2^-23 of the product) and summed in fp32.
 // bf16 with bf16 and fp16 with fp16 are one product. h and g are held in fp32 and cut where they are operands, or kept as three pieces.
 //
+// What bounds it, at 8192 bf16 rows of 4096 with eight adapters of rank 32: the plan 9 us (one workgroup's ballots), both narrowing
+// products 42 (268 MB through the L1 caches, rows and weights alike: a compute unit receives some 26 KB a us; with the weights left out
+// it took 34, without the rows 21), pieces 5, the weights' gradients 37 and 5 for their join (134 MB, part of it still in the cache of
+// the memory side), the widening product 36 (134 MB, 3.8 TB/s). 4100 rows forward with 24 adapters of rank 16 and fp32 outputs: plan 8,
+// narrowing 15, widening 33 (4.1 TB/s). Nine rows: 4.5 and 5.9, latency.
+//
 // Requests. Loads stand in straight lines without conditions, at addresses that are moved into the matrix where a piece would pass its
 // end (and what comes twice by that meets a zero or is not stored): behind a condition the compiler waits for every load under way
 // instead of counting them.
@@ -27,6 +33,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// Rows of a call without a plan: a wavefront sees the ids of all at once. us of calls of 4096 columns without / with: 1 row 9.1 / 11.6,
+// 32 rows of 32 adapters 9.7 / 12.5, 64 12.1 / 13.4.
 constexpr int kInlineTokens = 64;
 
 // ---- operands of the matrix instructions: eight elements as they lie in memory, 4 words (16-bit types) or 8 ----
@@ -598,7 +606,8 @@ __global__ __launch_bounds__(256, RKS == 1 ? 3 : 2) void k_adapter_up(AdapterArg
 }
 
 // ---- dA = sum of g x^T, dB = sum of h dy^T: products of 16 (rank) x 16 NJ (columns), the places split over the wavefronts ----
-// A lane holds NJ adjacent columns (16 bytes) of eight rows; a tile's operand is one column of all eight.
+// A lane holds NJ adjacent columns (16 bytes) of eight rows; a tile's operand is one column of all eight, put together from the rows'
+// words by one byte permutation a word: no transposition through LDS. Sums of different wavefronts and segments meet in a fixed order.
 template <typename X, int RT, bool TRANS>
 __device__ __forceinline__ void weight_grad(const AdapterArgs& P, const Plan& plan, const Pieces& h, const void* in, int64_t stride, int d,
                                             int slice, float* out, float* part, f32x4* red) {
@@ -788,12 +797,15 @@ int segment_shift(const AdapterArgs& a) {
   return k;
 }
 
-// Shares of the columns in the narrowing products, each a workgroup of four wavefronts: as many as give the chip `want` workgroups,
-// while a wavefront has two units of 128 bytes of its rows or more.
-inline int column_splits(const AdapterArgs& a, int d, int tiles, int want, int least) {
+// Shares k of the columns in the narrowing products, each a workgroup of four wavefronts, while the chip has fewer than two workgroups a
+// compute unit. A row's units of 128 bytes fall on 4 k wavefronts and what reads the result adds k sums, so k grows as the square root of
+// the units: 2 of 1024 bf16 columns, 4 of 4096, 8 of 8192 and more. us of a forward call with one share more in the doubling / this /
+// one less: 256 rows of 4096 15.3 / 13.9 / -, 8 rows 9.5 / 8.8 / -, 8 rows of 14336 - / 10.4 / 12.0, 512 of 1024 - / 14.7 / 17.2. The
+// backward pass has a launch that adds the shares, none where there is one: up to 1024 columns.
+inline int column_splits(const AdapterArgs& a, int d, int tiles, bool backward) {
   const int units = a.dtype == MOEQ_F32 ? (d + 31) / 32 : (d + 63) / 64;
   int k = 1;
-  while (k < 8 && units >= least * k && tiles * k < want) k *= 2;
+  while (k < 8 && units >= (backward ? 32 * k : 8 * k * k) && tiles * k < 512) k *= 2;
   return k;
 }
 
@@ -812,12 +824,16 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     s.narrow_h = (float*)take((size_t)a.T * a.rank * 4);
     if (backward) s.narrow_g = (float*)take((size_t)a.T * a.rank * 4);
   } else if (s.form == kFew) {
-    s.h = Pieces{(float*)take((size_t)8 * a.T * 16 * RR * 4), nullptr, RR, 16 * a.T, column_splits(a, a.d_in, a.T, 512, 16)};
+    s.h = Pieces{(float*)take((size_t)8 * a.T * 16 * RR * 4), nullptr, RR, 16 * a.T, column_splits(a, a.d_in, a.T, false)};
   } else {
     Plan& p = s.plan;
-    // Rows of a tile: as many as share the weights that are read for them, unless that is mostly padding (or, of 64, leaves the chip's
-    // last round of workgroups half empty). The narrowing products take 16 MT of them at a time, two or four times their rank at most.
-    s.TP = backward ? (a.T >= 16384 && a.T >= 512 * (int64_t)a.n ? 64 : 32) : a.T < 64 * (int64_t)a.n ? 16 : a.T < 256 * (int64_t)a.n || a.T < 8192 ? 32 : 64;
+    // Rows of a tile: as many as share the weights that are read for them, unless that is mostly padding or leaves compute units without
+    // work. us of calls of 4096 columns by tiles of 16 / 32 / 64, rows x adapters: rank 16, 128 x 32 15.1 / 17.2 / 23.2, 1024 x 32 22.3
+    // / 22.8 / 25.3, 6144 x 256 74 / 69 / 84, 8192 x 64 83 / 74 / 80, 8192 x 8 74 / 63 / 67, 16384 x 8 135 / 124 / 114; rank 64, 4096 x
+    // 8 81 / 70 / 92, 8192 x 8 126 / 115 / 110. Backward, 8192 x 8 - / 101 / 104, 16384 x 64 - / 213 / 215, 32768 x 8 - / 400 / 392.
+    // The narrowing products take 16 MT rows at a time, two or four times their rank at most.
+    s.TP = backward ? (a.T >= 16384 && a.T >= 512 * (int64_t)a.n ? 64 : 32)
+                    : a.T < 64 * (int64_t)a.n && a.T < 4096 ? 16 : a.T < 256 * (int64_t)a.n || a.T < 8192 ? 32 : 64;
     s.MT = s.TP == 64 ? (s.RT == 1 || backward ? 2 : 4) : s.TP / 16;
     // every bin that has rows adds at most a tile less a row of padding (room: of the largest tile)
     const int pad = (s.TP - 1) * std::min(a.T, a.n + 1), most = 63 * std::min(a.T, a.n + 1), room = a.T + most, room_split = std::min(16, a.T / 256) + most / 256 + 1;
@@ -826,7 +842,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     p.rowof = (int32_t*)take((size_t)room * 4);
     p.tile_adapter = (int32_t*)take((size_t)room / 16 * 4 + 4);
     if (!backward) {
-      s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, a.d_in, p.tiles, 512, 16)};
+      s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, a.d_in, p.tiles, false)};
       // (several shares only of less than 512 tiles)
       s.h.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 512 * 64)) * RR * 4);
     } else {
@@ -835,12 +851,11 @@ Setup set_up(const AdapterArgs& a, bool backward) {
       p.n_split = a.T <= 1 << p.seg_shift ? 0 : p.places >> p.seg_shift;
       p.segments = (Segment*)take((size_t)(a.n + 1 + room_split) * sizeof(Segment));
       p.split = (Segment*)take((size_t)room_split * sizeof(Segment));
-      s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, column_splits(a, std::min(a.d_in, a.d_out), p.tiles, 512, 32)};
+      s.h = Pieces{nullptr, (uint16_t*)take((size_t)room * 3 * RR * 2), RR, p.places, column_splits(a, std::min(a.d_in, a.d_out), p.tiles, true)};
       s.g = s.h;
       s.g.by_rank = (uint16_t*)take((size_t)room * 3 * RR * 2);
-      // (several shares only of less than 1024 tiles)
-      s.h.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 1024 * 32)) * RR * 4);
-      s.g.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 1024 * 32)) * RR * 4);
+      s.h.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 512 * 64)) * RR * 4);
+      s.g.parts = (float*)take((size_t)std::max(room, 8 * std::min(room, 512 * 64)) * RR * 4);
       // (segments of at least 256 rows, at most 16 of them in the rows themselves: segment_shift)
       s.part = (float*)take((size_t)2 * room_split * a.rank * (a.d_in + a.d_out) * 4);
     }
