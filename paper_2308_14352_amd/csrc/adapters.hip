@@ -13,7 +13,7 @@
 // products 42 (268 MB through the L1 caches, rows and weights alike: a compute unit receives some 26 KB a us; with the weights left out
 // it took 34, without the rows 21), pieces 5, the weights' gradients 37 and 5 for their join (134 MB, part of it still in the cache of
 // the memory side), the widening product 36 (134 MB, 3.8 TB/s). 4100 rows forward with 24 adapters of rank 16 and fp32 outputs: plan 8,
-// narrowing 15, widening 33 (4.1 TB/s). Nine rows: 4.5 and 5.9, latency.
+// narrowing 15, widening 33 (4.1 TB/s). Nine rows: 4.6 and 5.2, latency.
 //
 // Requests. Loads stand in straight lines without conditions, at addresses that are moved into the matrix where a piece would pass its
 // end (and what comes twice by that meets a zero or is not stored): behind a condition the compiler waits for every load under way

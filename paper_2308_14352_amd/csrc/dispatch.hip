@@ -77,7 +77,7 @@ __global__ __launch_bounds__(1024) void k_sort_chunk(const int32_t* __restrict__
 }
 
 // ---- rows. Memory bounds all three: every row is read once and written once, the sums are registers of the thread that holds the
-// piece. 2048 bf16 rows of 4096 to two places each: 9.3 us, 5.4 TB/s; 1117 tokens from two fp32 rows of 1024: 4.0 us; the gradient of
+// piece. 2048 bf16 rows of 4096 to two places each: 9.3 us, 5.4 TB/s; 1117 tokens from two fp32 rows of 1024: 3.6 us; the gradient of
 // 8192 tokens with two rows of 4096: 61 us, 5.5 TB/s (a large copy: 5.2).
 // G threads take a token's row in pieces of VE elements, KB of its choices at a time. Loads stand in straight lines at
 // addresses that exist (of dropped pairs: their place's, of entries that point nowhere: the first row's), so that they are on their way
