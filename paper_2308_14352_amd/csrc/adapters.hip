@@ -20,8 +20,9 @@
 // instead of counting them.
 //
 // Order of the rows. k_adapter_plan sorts them by adapter, every adapter's rows padded to whole tiles of TP (places; rowof[place] is
-// the row, or ~row in padding, where row is one of the same adapter: it is read again and counts nothing). Calls of up to kInlineTokens rows find their tiles by themselves: the tile b holds row b's adapter and those of
-// its rows from b on, where b is each 16th of them.
+// the row, or ~row in padding, where row is one of the same adapter: it is read again and counts nothing). Calls of up to
+// kInlineTokens rows find their tiles by themselves: the tile b holds row b's adapter and those of its rows from b on, where b is each
+// 16th of them.
 #include <algorithm>
 
 #include "sort_core.h"
@@ -36,6 +37,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // Rows of a call without a plan: a wavefront sees the ids of all at once. us of calls of 4096 columns without / with: 1 row 9.1 / 11.6,
 // 32 rows of 32 adapters 9.7 / 12.5, 64 12.1 / 13.4.
 constexpr int kInlineTokens = 64;
+// Rows that one workgroup plans alone; beyond, chunks of them do, and a launch ahead of them counts. us of forward calls of 4096 columns,
+// alone / in chunks: 12288 rows of 8 adapters 92 / 88, 16384 of 64 128 / 118, of 1024 columns 58 / 47 (8192 ids, the sort by itself: 9.1 /
+// 8.9).
+constexpr int kPlanOne = 8192;
 
 // ---- operands of the matrix instructions: eight elements as they lie in memory, 4 words (16-bit types) or 8 ----
 template <typename T> constexpr int kPieces = sizeof(T) == 4 ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;
@@ -126,11 +131,15 @@ struct Plan {
   int32_t *rowof, *tile_adapter;      // [places], [places / TP]: the adapter of a tile, n: none, -1: not used
   Segment* segments;                  // backward: the work items of the weights' gradients
   Segment* split;                     // adapters of several segments: {adapter, first part, number of parts}
+  int32_t* counts;                    // [chunks][n + 1]
   int32_t places, tiles, n_segments, n_split, seg_shift;
 };
 
+template <bool CHUNKS>
 __global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict__ ids, int T, int run, int n, int TP, Plan plan) {
   __shared__ SortShared sh;
+  __shared__ int ahead[CHUNKS ? kSortMaxExperts + 1 : 1];
+  const int first = CHUNKS ? blockIdx.x * (int)kSortChunk : 0;
   __shared__ int start[kSortMaxExperts + 1], total[kSortMaxExperts + 1], segs[kSortMaxExperts + 1], parts[kSortMaxExperts + 1], n_split;
   if (threadIdx.x == 0) n_split = 0;
   // the bin of a place: the last one that starts at or before it
@@ -144,8 +153,9 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict
     }
     return lo;
   };
-  sort_pairs(ids, T, run, n, sh,
+  sort_pairs(ids + first, CHUNKS ? min((int)kSortChunk, T - first) : T, run, n, sh,
              [&](int e, int all) {
+               if (CHUNKS) all = count_all(plan.counts, gridDim.x, blockIdx.x, n, e, ahead[e]);
                const int rows = (all + TP - 1) & -TP, s = max(1, (rows + (1 << plan.seg_shift) - 1) >> plan.seg_shift);
                total[e] = all;
                start[e] = rows;
@@ -158,14 +168,15 @@ __global__ __launch_bounds__(1024) void k_adapter_plan(const int32_t* __restrict
                for (int k = wave; k < (plan.segments ? 3 : 1); k += waves) sort_scan(n, k == 0 ? start : k == 1 ? segs : parts);
              },
              [&](int i, int number, int e) {
+               if (CHUNKS) i += first, number += ahead[e];
                const int p = start[e] + number;
                plan.rowof[p] = i;
                if (number == 0)
                  for (int k = total[e], end = (k + TP - 1) & -TP; k < end; ++k) plan.rowof[p + k] = ~i;
              });
   const int end = start[n] + ((total[n] + TP - 1) & -TP);
-  for (int i = threadIdx.x; i < plan.tiles; i += blockDim.x) plan.tile_adapter[i] = i * TP < end ? last_at(start, i * TP) : -1;
-  if (plan.segments) {
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < plan.tiles; i += gridDim.x * blockDim.x) plan.tile_adapter[i] = i * TP < end ? last_at(start, i * TP) : -1;
+  if (plan.segments && blockIdx.x == 0) {
     for (int i = threadIdx.x; i < plan.n_segments; i += blockDim.x) {
       const int a = last_at(segs, i);
       Segment s{-1, 0, 0, -1};
@@ -841,6 +852,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     p.tiles = p.places / s.TP;
     p.rowof = (int32_t*)take((size_t)room * 4);
     p.tile_adapter = (int32_t*)take((size_t)room / 16 * 4 + 4);
+    if (a.T > kPlanOne) p.counts = (int32_t*)take((size_t)((a.T + kSortChunk - 1) / kSortChunk) * (a.n + 1) * 4);
     if (!backward) {
       s.h = Pieces{nullptr, nullptr, RR, p.places, column_splits(a, a.d_in, p.tiles, false)};
       // (several shares only of less than 512 tiles)
@@ -865,9 +877,17 @@ Setup set_up(const AdapterArgs& a, bool backward) {
 }
 
 hipError_t launch_plan(const AdapterArgs& a, const Setup& s, hipStream_t st) {
-  const int waves = sort_waves(a.T, a.n);
-  const int run = (a.T + waves * 64 - 1) / (waves * 64) * 64;
-  hipLaunchKernelGGL(k_adapter_plan, dim3(1), dim3(waves * 64), 0, st, a.ids, a.T, run, a.n, s.TP, s.plan);
+  const bool one = a.T <= kPlanOne;
+  const int span = one ? a.T : (int)kSortChunk, waves = sort_waves(span, a.n);
+  const int run = (span + waves * 64 - 1) / (waves * 64) * 64;
+  if (one) {
+    hipLaunchKernelGGL(k_adapter_plan<false>, dim3(1), dim3(waves * 64), 0, st, a.ids, a.T, run, a.n, s.TP, s.plan);
+    return hipGetLastError();
+  }
+  const int chunks = (int)((a.T + kSortChunk - 1) / kSortChunk);
+  hipLaunchKernelGGL(k_sort_count, dim3(chunks), dim3(1024), 0, st, a.ids, (int64_t)a.T, a.n, s.plan.counts);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_adapter_plan<true>, dim3(chunks), dim3(waves * 64), 0, st, a.ids, a.T, run, a.n, s.TP, s.plan);
   return hipGetLastError();
 }
 

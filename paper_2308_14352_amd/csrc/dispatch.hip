@@ -8,10 +8,9 @@
 namespace moeq {
 namespace {
 
-// Pairs that one workgroup sorts alone, and those of a workgroup beyond, where a kernel that counts goes ahead. us alone / in chunks:
+// Pairs that one workgroup sorts alone; beyond, they go in chunks, and a kernel that counts goes ahead. us alone / in chunks:
 // 4096 pairs of 8 experts 5.9 / 8.3, of 128 8.1 / 10.6; 6144 7.5 / 8.6 and 10.6 / 11.5; 8192 9.1 / 8.9 and 13.0 / 11.7; 32768 36 / 9.1.
 constexpr int64_t kSortOne = 6144;
-constexpr int64_t kSortChunk = 4096;
 
 __global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ idx, int pairs, int run, int E,
                                                    int32_t* __restrict__ offsets, int32_t* __restrict__ order, int32_t* __restrict__ slot) {
@@ -31,16 +30,6 @@ __global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ i
              });
 }
 
-__global__ __launch_bounds__(1024) void k_sort_count(const int32_t* __restrict__ idx, int64_t pairs, int E, int32_t* __restrict__ counts) {
-  __shared__ int cnt[kSortMaxExperts + 1];
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) cnt[e] = 0;
-  __syncthreads();
-  const int64_t a = blockIdx.x * kSortChunk, b = min(a + kSortChunk, pairs);
-  for (int64_t i = a + threadIdx.x; i < b; i += blockDim.x) atomicAdd(&cnt[bin_of(idx[i], E)], 1);
-  __syncthreads();
-  for (int e = threadIdx.x; e <= E; e += blockDim.x) counts[(int64_t)blockIdx.x * (E + 1) + e] = cnt[e];
-}
-
 __global__ __launch_bounds__(1024) void k_sort_chunk(const int32_t* __restrict__ idx, int64_t pairs, int run, int E,
                                                      const int32_t* __restrict__ counts, int32_t* __restrict__ offsets,
                                                      int32_t* __restrict__ order, int32_t* __restrict__ slot) {
@@ -50,15 +39,7 @@ __global__ __launch_bounds__(1024) void k_sort_chunk(const int32_t* __restrict__
   const int64_t a = me * kSortChunk;
   sort_pairs(idx + a, (int)min(kSortChunk, pairs - a), run, E, sh,
              [&](int e, int) {
-               int before = 0, all = 0;
-#pragma unroll 8
-               for (int c = 0; c < chunks; ++c) {
-                 const int v = counts[(int64_t)c * (E + 1) + e];
-                 before += c < me ? v : 0;
-                 all += v;
-               }
-               place[e] = all;
-               ahead[e] = before;
+               place[e] = count_all(counts, chunks, me, E, e, ahead[e]);
              },
              [&] {
                if (threadIdx.x < 64) {

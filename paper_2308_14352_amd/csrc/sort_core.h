@@ -115,5 +115,30 @@ __device__ __forceinline__ void sort_pairs(const int32_t* idx, int n, int run, i
   }
 }
 
+// Sorts of several workgroups: a chunk's pairs of every bin (counts [chunks][E + 1]), and from those, a bin's pairs in all chunks and in
+// the ones ahead of `me`.
+constexpr int64_t kSortChunk = 4096;     // pairs
+__global__ __launch_bounds__(1024) void k_sort_count(const int32_t* __restrict__ idx, int64_t pairs, int E, int32_t* __restrict__ counts) {
+  __shared__ int cnt[kSortMaxExperts + 1];
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) cnt[e] = 0;
+  __syncthreads();
+  const int64_t a = blockIdx.x * kSortChunk, b = min(a + kSortChunk, pairs);
+  for (int64_t i = a + threadIdx.x; i < b; i += blockDim.x) atomicAdd(&cnt[bin_of(idx[i], E)], 1);
+  __syncthreads();
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) counts[(int64_t)blockIdx.x * (E + 1) + e] = cnt[e];
+}
+
+__device__ __forceinline__ int count_all(const int32_t* __restrict__ counts, int chunks, int me, int E, int e, int& ahead) {
+  int before = 0, all = 0;
+#pragma unroll 8
+  for (int c = 0; c < chunks; ++c) {
+    const int v = counts[(int64_t)c * (E + 1) + e];
+    before += c < me ? v : 0;
+    all += v;
+  }
+  ahead = before;
+  return all;
+}
+
 }  // namespace
 }  // namespace moeq

@@ -260,3 +260,29 @@ def test_a_graph_keeps_the_workspace_that_it_was_captured_with():
         torch.cuda.synchronize()
         assert torch.equal(held, want) and torch.equal(step(200), want)
     assert all(bool((t == 7).all()) for t in others)
+
+
+# rows that several workgroups plan, in tiles of every size, and the longest call
+LONG = [(8192, 3, 16, 72, 64, "mixed"), (8193, 40, 20, 64, 72, "mixed"), (16384, 4, 33, 40, 64, "sorted"), (17003, 300, 8, 48, 40, "mixed"),
+        (20000, 3, 64, 64, 24, "sorted"), (33000, 1, 17, 24, 40, "one"), (12289, 1024, 2, 16, 24, "mixed"), (65535, 7, 4, 16, 24, "mixed")]
+
+
+@pytest.mark.parametrize("kind,out", PAIRS)
+@pytest.mark.parametrize("T,n,r,d_in,d_out,how", LONG)
+def test_long_calls(T, n, r, d_in, d_out, how, kind, out):
+    rng = rng_of("long", T, n, r, d_in, d_out, how, kind, out)
+    m = make(rng, T, n, r, d_in, d_out, TYPES[kind], TYPES[out])
+    ids = ids_of(rng, T, n, how)
+    want = reference(m, ids, n)
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ids = torch.from_numpy(ids).to(DEV)
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    y = moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"])
+    check(y, *want["y"], d_in + r)
+    dx, dA, dB = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], dx_base=g["dx_base"])
+    check(dx, *want["dx"], d_out + r)
+    check(dA, *want["dA"], d_out + T)
+    check(dB, *want["dB"], d_in + T)
+    again = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], dx_base=g["dx_base"])
+    assert torch.equal(moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"]), y)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dA, dB)))
