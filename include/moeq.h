@@ -290,7 +290,7 @@ moeq_status moe_unprepare_in(const void *stream_buf, int64_t rows, int64_t cols,
 /* Pairs i = token * top_k + choice, stably sorted by expert idx[i]: offsets [n_experts + 1] (rows of expert e: offsets[e] to
  * offsets[e + 1]), order [pairs] (the pair in every place) and slot [pairs] (the place of every pair). Pairs without an expert
  * (idx outside [0, n_experts)) come last, in their order, as ~pair and ~place (negative). n_experts <= 1024, pairs <= 2^28.
- * ws: moe_sort_bytes (0 for calls of up to 8192 pairs). */
+ * ws: moe_sort_bytes (0 for calls of up to 6144 pairs). */
 size_t moe_sort_bytes(int32_t n_tokens, int32_t top_k, int32_t n_experts);
 moeq_status moe_sort_pairs(const int32_t *idx, int32_t n_tokens, int32_t top_k, int32_t n_experts, int32_t *offsets,
                            int32_t *order, int32_t *slot, void *ws, size_t ws_bytes, void *stream);

@@ -199,3 +199,12 @@ def test_replays_of_a_graph_and_another_stream():
     got = [s.offsets, s.order, s.slot, rows, y, *moeq.moe_combine_rows_backward(s, y, rows, gate, stream=side)]
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("T,k,E", [(6144, 1, 8), (6145, 1, 8), (4096, 1, 1024), (4097, 2, 300), (2048, 3, 64), (2049, 3, 64), (4096, 4, 128)])
+def test_sort_around_the_chunks(T, k, E):
+    rng = rng_of("chunks", T, k, E)
+    idx = routing(rng, T, k, E, 0.02)
+    s = moeq.moe_sort_pairs(torch.from_numpy(idx).to(DEV), E)
+    for got, want in zip((s.offsets, s.order, s.slot), sorted_on_host(idx, E)):
+        assert np.array_equal(got.cpu().numpy(), want)

@@ -203,3 +203,26 @@ def test_replays_of_a_graph_and_another_stream(T, V, kind):
     got = step(stream=side)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# rows that lie in registers, by their vectors of 16 bytes: the last of each form, the first of the next, and those taken for a gradient only
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("T,vectors,rest", [
+    (3, 1024, 3), (3, 1025, 0), (2, 4096, 0), (3, 4097, 1), (2, 8192, 3), (3, 8193, 0), (128, 8193, 2), (129, 12001, 1), (127, 16384, 0),
+    (128, 16384, 3), (128, 16385, 0)])
+def test_rows_of_every_form(T, vectors, rest, kind):
+    rng = rng_of("forms", T, vectors, rest, kind)
+    t = TYPES[kind]
+    V = vectors * (16 // t.itemsize) + rest
+    z = torch.from_numpy(rng.normal(size=(T, V)).astype(np.float32) * 2.5).to(t)
+    idx, u = teacher(rng, z, 20)
+    # a tenth masked, though not where the teacher is; a row of nothing; a row whose teacher points nowhere; a row of no weight
+    masked = torch.from_numpy(rng.random((T, V)) < 0.1).scatter_(1, idx.long(), False)
+    z[masked] = float("-inf")
+    w = torch.from_numpy(rng.random(T) + 0.5).float()
+    w[0] = 0
+    if T > 2:
+        idx[1] = -1
+    if T > 100:
+        z[100], w[100] = float("-inf"), 0
+    check_all(z, idx, u, 2.0, w, put=lambda t: strided(t, 3, 1))
