@@ -346,8 +346,8 @@ moeq_status moe_adapters_backward(const moeq_adapters *adapters, const void *x, 
  *     loss = w tau^2 sum_j p_j (log p_j - s[idx_j] + lse),   lse = log sum exp(s),
  *     dloss/dz = w tau (softmax(s) - p at the indices; an index given twice counts twice).
  * Rows of weight 0, and rows whose teacher's entries have no index or are all minus infinity, have loss 0 and gradient 0
- * whatever their logits hold. A student's logit of minus infinity has probability 0 (a teacher's entry there makes the loss
- * infinite). top <= 1024, n_tokens <= 2^24. */
+ * whatever their logits hold; a NaN or plus infinity among a teacher's entries makes the loss, and the gradient at the row's
+ * indices, NaN. A student's logit of minus infinity has probability 0 (a teacher's entry there makes the loss infinite). top <= 1024, n_tokens <= 2^24. */
 size_t moe_distill_workspace_bytes(int32_t n_tokens, int32_t vocab, int32_t dtype);
 /* loss [n_tokens] and, if wanted, lse [n_tokens] (of every row, whatever its weight). */
 moeq_status moe_distill_forward(const void *logits, int64_t stride, int32_t dtype, int32_t n_tokens, int32_t vocab,

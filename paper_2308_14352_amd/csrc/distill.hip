@@ -128,7 +128,8 @@ struct Teacher {
   float p[kDistillMaxTop], z[kDistillMaxTop];
   bool any;
 };
-// By the first wavefront (a barrier has to follow). Returns sum of p log p, in all its lanes.
+// By the first wavefront (a barrier has to follow). Returns sum of p log p, in all its lanes. A row has a teacher where an entry is not
+// minus infinity; a NaN or plus infinity among them makes every p a NaN, which goes into both sums (only p = 0 is left out of them).
 template <typename T>
 __device__ __forceinline__ float take_teacher(const DistillArgs& A, int t, const T* z, Teacher& sh) {
   const int lane = threadIdx.x & 63;
@@ -136,14 +137,17 @@ __device__ __forceinline__ float take_teacher(const DistillArgs& A, int t, const
   const int32_t* idx = A.top_idx + (int64_t)t * A.K;
   const float* u = A.top_logits + (int64_t)t * A.K;
   float top = -INFINITY, sum = 0.f, plogp = 0.f;
+  bool some = false;
   for (int j = lane; j < A.K; j += 64) {
     const int i = idx[j];
     const bool ok = (uint32_t)i < (uint32_t)A.V;
     sh.idx[j] = ok ? i : -1;
     sh.p[j] = ok ? u[j] : -INFINITY;
     sh.z[j] = ok ? (float)z[i] : 0.f;
+    some |= ok && u[j] != -INFINITY;
     top = ok ? fmaxf(top, u[j]) : top;
   }
+  const bool any = __ballot(some) != 0;
   top = wave_max(top);
   const float o = origin(top);
   for (int j = lane; j < A.K; j += 64) {
@@ -154,10 +158,10 @@ __device__ __forceinline__ float take_teacher(const DistillArgs& A, int t, const
   const float log_sum = __builtin_amdgcn_logf(sum) * kLn2;
   for (int j = lane; j < A.K; j += 64) {
     const float lp = (sh.p[j] - o) * it - log_sum, p = __builtin_amdgcn_exp2f(lp * kLog2e);
-    plogp += p > 0.f ? p * lp : 0.f;
-    sh.p[j] = top == -INFINITY ? 0.f : p;
+    plogp += p != 0.f ? p * lp : 0.f;
+    sh.p[j] = any ? p : 0.f;
   }
-  if (lane == 0) sh.any = top != -INFINITY;
+  if (lane == 0) sh.any = any;
   return wave_sum(plogp);
 }
 // The loss from there, by the first wavefront: w tau^2 (sum p log p - sum p ((z_j - m) / tau - log S)).
@@ -165,7 +169,7 @@ __device__ __forceinline__ float row_loss(const DistillArgs& A, const Teacher& s
   const float it = 1.f / A.temperature, o = origin(st.m), log_s = __builtin_amdgcn_logf(st.s) * kLn2;
   float cross = 0.f;
   for (int j = threadIdx.x & 63; j < A.K; j += 64)
-    if (sh.p[j] > 0.f) cross += sh.z[j] == -INFINITY ? -INFINITY : sh.p[j] * ((sh.z[j] - o) * it - log_s);
+    if (sh.p[j] != 0.f) cross += sh.z[j] == -INFINITY ? -INFINITY : sh.p[j] * ((sh.z[j] - o) * it - log_s);
   cross = wave_sum(cross);
   return sh.any && w != 0.f ? w * A.temperature * A.temperature * (plogp - cross) : 0.f;
 }

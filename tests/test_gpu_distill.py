@@ -226,3 +226,41 @@ def test_rows_of_every_form(T, vectors, rest, kind):
     if T > 100:
         z[100], w[100] = float("-inf"), 0
     check_all(z, idx, u, 2.0, w, put=lambda t: strided(t, 3, 1))
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("T,V", [(9, 300), (9, 100000), (520, 900)])      # rows in registers, in chunks, many of them
+def test_a_teacher_that_is_not_finite_is_seen(T, V, kind):
+    """softmax(u / tau) of entries that hold a NaN or plus infinity is NaN in every entry: so are the loss, and the gradient at the indices.
+    Only rows without an entry or of minus infinities alone, and rows without weight, have neither."""
+    rng = rng_of("teacher", T, V, kind)
+    z = torch.from_numpy(rng.normal(size=(T, V)) * 2.5).to(TYPES[kind])
+    K, nan, inf = 6, float("nan"), float("inf")
+    idx, u = teacher(rng, z, K)
+    w = torch.from_numpy(rng.random(T) + 0.5).float()
+    clean = u.clone()
+    u[0, 2] = nan
+    u[1, 4] = inf
+    u[2] = nan
+    u[3] = inf
+    u[4, :3], u[4, 3:] = -inf, nan                         # nothing else beside the NaN
+    u[5, 0], idx[5, 0] = nan, V                            # no entry: not seen
+    u[6], w[6] = nan, 0.0                                  # no weight
+    u[7] = -inf                                            # no probability
+    z[8, idx[8, 0].long()], u[8, 0] = -inf, nan            # ... where the student has no probability either
+    bad, none = [0, 1, 2, 3, 4, 8], [6, 7]
+    zg, ig, ug, wg, one = (t.to(DEV) for t in (z, idx, u, w, torch.ones(T)))
+    loss, lse = moeq.moe_distill_forward(zg, ig, ug, temperature=2.0, weight=wg)
+    both, dz = moeq.moe_distill_loss_grad(zg, ig, ug, temperature=2.0, weight=wg)
+    dz1 = moeq.moe_distill_backward(zg, ig, ug, lse, one, temperature=2.0, weight=wg)
+    want_loss, want = moeq.moe_distill_loss_grad(zg, ig, clean.to(DEV), temperature=2.0, weight=wg)
+    at = torch.zeros((T, V), dtype=torch.bool)
+    at[torch.arange(T)[:, None].expand(T, K)[idx < V], idx[idx < V].long()] = True
+    for l in (loss, both):
+        assert l[bad].isnan().all() and (l[none] == 0).all() and l.isnan().sum().item() == len(bad)
+        assert torch.equal(l[9:], want_loss[9:])
+    for d in (dz, dz1):
+        d = d.cpu()
+        assert d[bad][at[bad]].isnan().all() and d[bad][~at[bad]].isfinite().all()
+        assert (d[none] == 0).all() and d.isnan().sum().item() == int(at[bad].sum())
+    assert torch.equal(dz.cpu()[bad][~at[bad]], want.cpu()[bad][~at[bad]])      # (the student's part is what it was)
