@@ -410,8 +410,8 @@ def _load():
         _build.build()
     from . import _calls
     names = ("moe_sort_bytes", "moe_sort_pairs", "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward",
-             "moe_adapters_forward", "moe_adapters_backward", "moe_distill_workspace_bytes", "moe_distill_forward",
-             "moe_distill_backward", "moe_distill_loss_grad")
+             "moe_adapters_workspace_bytes", "moe_adapters_forward", "moe_adapters_backward", "moe_distill_workspace_bytes",
+             "moe_distill_forward", "moe_distill_backward", "moe_distill_loss_grad")
     _calls.bind(MoeqError, lambda: _stream(None), *[C.cast(getattr(L, n), C.c_void_p).value for n in names])
     _native = _calls
     return _calls
@@ -480,33 +480,27 @@ class Adapters:
         self.n_adapters, self.rank, self.d_in, self.d_out, self.dtype = n, r, d_in, b.shape[1], a.dtype
         self._desc = moeq_adapters(n, r, d_in, self.d_out, _DTYPES[a.dtype], a.data_ptr(), b.data_ptr(), scale.data_ptr())
         self.handle = C.addressof(self._desc)
-        self._ws, self._ready, self._outgrown = None, {}, []
+        self._ws = None               # the last call's own workspace, held until the next one
 
     def workspace_bytes(self, max_tokens, backward=False):
         return int(lib().moe_adapters_workspace_bytes(self.handle, max_tokens, int(backward)))
 
-    def workspace(self, n_tokens, backward=False):
-        ws = self._ready.get((n_tokens, backward))
-        if ws is None:
-            need = max(self.workspace_bytes(n_tokens, backward), 16)
-            if self._ws is None or self._ws.numel() < need:
-                # (a captured graph or another stream may still use the one before: it is kept, and twice as large a one taken)
-                if self._ws is not None:
-                    self._outgrown.append(self._ws)
-                    need = max(need, 2 * self._ws.numel())
-                self._ws, self._ready = torch.empty(need, dtype=torch.uint8, device=self.a.device), {}
-            ws = self._ready[(n_tokens, backward)] = self._ws
-        return ws
+    def workspace(self, max_tokens, backward=False):
+        """A workspace for calls of up to max_tokens rows, for callers who pass one (`ws`) and order the calls that share it."""
+        return torch.empty(max(self.workspace_bytes(max_tokens, backward), 16), dtype=torch.uint8, device=self.a.device)
 
 
 def moe_adapters_forward(adapters, x, ids, base=None, y=None, ws=None, stream=None):
     """y[t] = base[t] + scale_a B_a A_a x[t] with a = ids[t] (int32; outside [0, n): no adapter). base: [T][d_out] or None
-    (zeros), may be y itself. y: in the adapters' dtype or fp32 (default: the base's, or the adapters'). Calls that share a workspace
-    (the adapters' own unless one is passed) have to be ordered."""
+    (zeros), may be y itself. y: in the adapters' dtype or fp32 (default: the base's, or the adapters'). ws: a workspace that the
+    caller keeps; calls that share one have to be ordered. Without it a call has its own."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return moe_adapters_forward(adapters, x, ids, base, y, ws)
-    return (_native or _load()).adapters_forward(adapters.handle, x, ids, base, y, adapters.workspace(len(x)) if ws is None else ws)
+    y, used = (_native or _load()).adapters_forward(adapters.handle, x, ids, base, y, ws)
+    if ws is None:
+        adapters._ws = used
+    return y
 
 
 def moe_adapters_backward(adapters, x, ids, dy, dx_base=None, dx=None, want_dx=True, ws=None, stream=None):
@@ -515,8 +509,10 @@ def moe_adapters_backward(adapters, x, ids, dy, dx_base=None, dx=None, want_dx=T
     if stream is not None:
         with torch.cuda.stream(stream):
             return moe_adapters_backward(adapters, x, ids, dy, dx_base, dx, want_dx, ws)
-    return (_native or _load()).adapters_backward(adapters.handle, x, ids, dy, dx_base, dx, bool(want_dx),
-                                                  adapters.workspace(len(x), True) if ws is None else ws)
+    dx, dA, dB, used = (_native or _load()).adapters_backward(adapters.handle, x, ids, dy, dx_base, dx, bool(want_dx), ws)
+    if ws is None:
+        adapters._ws = used
+    return dx, dA, dB
 
 
 def moe_distill_forward(logits, top_idx, top_logits, temperature=1.0, weight=None, stream=None):

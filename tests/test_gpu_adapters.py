@@ -1,5 +1,7 @@
 """Low-rank adapters of many requests and their gradient against plain arithmetic in 64 bits on the host: one row to many, every rank
 class, widths that end inside a vector or tile, rows without an adapter, adapters without rows, every pair of types."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -286,3 +288,87 @@ def test_long_calls(T, n, r, d_in, d_out, how, kind, out):
     again = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], dx_base=g["dx_base"])
     assert torch.equal(moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"]), y)
     assert all(torch.equal(a, b) for a, b in zip(again, (dx, dA, dB)))
+
+
+def mixed_calls(n_calls, seed):
+    """Adapters, and calls of different rows and lengths on them, with what each gives when it runs alone."""
+    rng = rng_of("calls", seed)
+    n, r, d = 6, 16, 256
+    m = make(rng, 2000, n, r, d, d, torch.bfloat16, torch.bfloat16)
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    calls = []
+    for T in rng.integers(65, 2000, size=n_calls).tolist():
+        ids = torch.from_numpy(ids_of(rng, T, n, "mixed")).to(DEV)
+        x, dy = g["x"][:T], g["dy"][-T:]
+        calls.append(lambda x=x, dy=dy, ids=ids, **kw: [moeq.moe_adapters_forward(ad, x, ids, **kw), *moeq.moe_adapters_backward(ad, x, ids, dy, **kw)])
+    want = []
+    for c in calls:
+        want.append(c())
+        torch.cuda.synchronize()
+    return ad, calls, want
+
+
+def test_calls_on_two_streams_have_workspaces_of_their_own():
+    ad, calls, want = mixed_calls(16, "streams")
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    places = []
+    for s in streams:
+        calls[0](stream=s)
+        places.append(ad._ws)                             # (held: the allocator cannot give the same place twice)
+    assert places[0].data_ptr() != places[1].data_ptr()
+    torch.cuda.synchronize()
+    for s in streams:
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(20_000_000)                 # both queues fill up before either runs
+    got = [c(stream=streams[i % 2]) for i, c in enumerate(calls)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+
+
+def test_calls_of_two_threads_have_workspaces_of_their_own():
+    """On the same stream: the launches of their calls may come between each other."""
+    ad, calls, want = mixed_calls(12, "threads")
+    got = {}
+
+    def work(k):
+        for turn in range(20):
+            for i in range(k, len(calls), 2):
+                got[turn, i] = calls[i]()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    [t.start() for t in threads]
+    [t.join(60) for t in threads]
+    torch.cuda.synchronize()
+    assert len(got) == 20 * len(calls)
+    assert all(torch.equal(a, b) for (_, i), g in got.items() for a, b in zip(g, want[i]))
+
+
+def test_a_workspace_is_not_given_away_while_its_stream_works():
+    ad, calls, want = mixed_calls(2, "dropped")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    got = calls[1](stream=side)
+    size = ad._ws.numel()
+    ad._ws = None                                         # the last reference
+    others = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want[1])) and all(bool((t == 255).all()) for t in others)
+
+
+def test_a_graph_and_calls_beside_it():
+    """A graph has the workspace of its capture to itself: calls on another stream run beside its replays."""
+    ad, calls, want = mixed_calls(8, "graph")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = calls[0]()
+    side = torch.cuda.Stream()
+    for i in range(1, 8):
+        for h in held:
+            h.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        got = calls[i](stream=side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want[0])) and all(torch.equal(a, b) for a, b in zip(got, want[i]))
