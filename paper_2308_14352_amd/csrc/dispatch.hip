@@ -1,6 +1,7 @@
 // (Token, choice) pairs sorted by expert, the tokens' rows copied into that order, and expert rows combined back into tokens with
 // the gradient of that. Pair i = token * k + choice; order[p] is the pair in place p, slot[i] the place of pair i; pairs without an
 // expert (an index outside [0, E)) come last, as ~pair and ~place, have rows of zeros and add nothing.
+#include <algorithm>
 #include <type_traits>
 
 #include "sort_core.h"
@@ -91,7 +92,7 @@ __device__ __forceinline__ void for_pieces(int d, F&& f) {
 
 template <typename T, int G, int KB>
 __global__ __launch_bounds__(256) void k_gather_rows(RowsArgs A) {
-  const int t = blockIdx.x * (256 / G) + threadIdx.x / G;
+  const int t = A.first + blockIdx.x * (256 / G) + threadIdx.x / G;
   if (t >= A.T) return;
   const T* x = (const T*)A.a + (int64_t)t * A.a_stride;
   for (int j0 = 0; j0 < A.k; j0 += KB) {
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(256) void k_gather_rows(RowsArgs A) {
 // y[t] = sum of gate * row over the token's choices, in their order, in fp32.
 template <typename T, typename Y, int G, int KB>
 __global__ __launch_bounds__(256) void k_combine_rows(RowsArgs A) {
-  const int t = blockIdx.x * (256 / G) + threadIdx.x / G;
+  const int t = A.first + blockIdx.x * (256 / G) + threadIdx.x / G;
   if (t >= A.T) return;
   Choice ch[KB];
   take_choices(A, t, 0, ch);
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(256) void k_combine_rows(RowsArgs A) {
 template <typename T, typename Y, int G, int KB>
 __global__ __launch_bounds__(256) void k_combine_grad(RowsArgs A) {
   __shared__ float part[4][KB];
-  const int t = blockIdx.x * (256 / G) + threadIdx.x / G, me = threadIdx.x % G;
+  const int t = A.first + blockIdx.x * (256 / G) + threadIdx.x / G, me = threadIdx.x % G;
   if (t >= A.T) return;                       // (G = 256: the whole workgroup)
   const Y* dy = (const Y*)A.dy + (int64_t)t * A.dy_stride;
   for (int j0 = 0; j0 < A.k; j0 += KB) {
@@ -217,6 +218,18 @@ hipError_t by_width(int d, int k, int ve, F&& f) {
   return with_k(std::integral_constant<int, 256>{});
 }
 
+// The tokens of a call, `per` a workgroup of 256 threads: f(arguments, workgroups) for every launch.
+template <typename F>
+hipError_t in_launches(RowsArgs a, int per, F&& f) {
+  for (a.first = 0; a.first < a.T;) {
+    const int groups = std::min((a.T - a.first + per - 1) / per, launch_groups(256));
+    f(a, groups);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    a.first += groups * per;
+  }
+  return hipSuccess;
+}
+
 }  // namespace
 
 size_t sort_ws_bytes(int64_t pairs, int32_t experts) {
@@ -245,8 +258,9 @@ hipError_t launch_gather_rows(const RowsArgs& a, int32_t dtype, hipStream_t st) 
     using T = decltype(tag);
     return by_width(a.d, a.k, 16 / sizeof(T), [&](auto g, auto kb) {
       constexpr int G = decltype(g)::value, KB = decltype(kb)::value;
-      hipLaunchKernelGGL((k_gather_rows<T, G, KB>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
-      return hipGetLastError();
+      return in_launches(a, 256 / G, [&](const RowsArgs& b, int groups) {
+        hipLaunchKernelGGL((k_gather_rows<T, G, KB>), dim3(groups), dim3(256), 0, st, b);
+      });
     });
   });
 }
@@ -265,8 +279,9 @@ hipError_t launch_combine_rows(const RowsArgs& a, int32_t dtype, int32_t y_dtype
     using Y = decltype(ytag);
     return by_width(a.d, a.k, 16 / sizeof(T), [&](auto g, auto kb) {
       constexpr int G = decltype(g)::value, KB = decltype(kb)::value;
-      hipLaunchKernelGGL((k_combine_rows<T, Y, G, KB>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
-      return hipGetLastError();
+      return in_launches(a, 256 / G, [&](const RowsArgs& b, int groups) {
+        hipLaunchKernelGGL((k_combine_rows<T, Y, G, KB>), dim3(groups), dim3(256), 0, st, b);
+      });
     });
   });
 }
@@ -277,8 +292,9 @@ hipError_t launch_combine_rows_backward(const RowsArgs& a, int32_t dtype, int32_
     using Y = decltype(ytag);
     return by_width(a.d, a.k, 16 / sizeof(T), [&](auto g, auto kb) {
       constexpr int G = decltype(g)::value, KB = decltype(kb)::value;
-      hipLaunchKernelGGL((k_combine_grad<T, Y, G, KB>), dim3((a.T + 256 / G - 1) / (256 / G)), dim3(256), 0, st, a);
-      return hipGetLastError();
+      return in_launches(a, 256 / G, [&](const RowsArgs& b, int groups) {
+        hipLaunchKernelGGL((k_combine_grad<T, Y, G, KB>), dim3(groups), dim3(256), 0, st, b);
+      });
     });
   });
 }

@@ -358,22 +358,13 @@ bool by_rows(int32_t T, int32_t V, int32_t dtype, bool gradient) {
   return all <= 8192 || (gradient && all <= 16384 && T >= 128);
 }
 
-template <typename T>
-hipError_t launch_rows(const DistillArgs& a, hipStream_t st) {
-  const int all = a.V / (16 / (int)sizeof(T));
-  if (all <= 1024) hipLaunchKernelGGL((k_distill_row<T, 256, 4>), dim3(a.T), dim3(256), 0, st, a);
-  else if (all <= 4096) hipLaunchKernelGGL((k_distill_row<T, 512, 8>), dim3(a.T), dim3(512), 0, st, a);
-  else if (all <= 8192) hipLaunchKernelGGL((k_distill_row<T, 1024, 8>), dim3(a.T), dim3(1024), 0, st, a);
-  else hipLaunchKernelGGL((k_distill_row<T, 1024, 16>), dim3(a.T), dim3(1024), 0, st, a);
-  return hipGetLastError();
-}
 // Rows of one launch of the chunked kernels (the grid's second dimension).
 constexpr int32_t kRowsOfLaunch = 65535;
 template <typename F>
-hipError_t in_launches(DistillArgs a, F&& f) {
+hipError_t in_launches(DistillArgs a, int32_t most, F&& f) {
   while (a.T > 0) {
     DistillArgs b = a;
-    b.T = a.T < kRowsOfLaunch ? a.T : kRowsOfLaunch;
+    b.T = std::min(a.T, most);
     if (hipError_t e = f(b); e != hipSuccess) return e;
     const int64_t sz = dtype_bytes(a.dtype), k = b.T;
     a.T -= b.T;
@@ -389,6 +380,18 @@ hipError_t in_launches(DistillArgs a, F&& f) {
   return hipSuccess;
 }
 
+template <typename T>
+hipError_t launch_rows(const DistillArgs& a, hipStream_t st) {
+  const int all = a.V / (16 / (int)sizeof(T)), threads = all <= 1024 ? 256 : all <= 4096 ? 512 : 1024;
+  return in_launches(a, launch_groups(threads), [&](const DistillArgs& b) {
+    if (all <= 1024) hipLaunchKernelGGL((k_distill_row<T, 256, 4>), dim3(b.T), dim3(256), 0, st, b);
+    else if (all <= 4096) hipLaunchKernelGGL((k_distill_row<T, 512, 8>), dim3(b.T), dim3(512), 0, st, b);
+    else if (all <= 8192) hipLaunchKernelGGL((k_distill_row<T, 1024, 8>), dim3(b.T), dim3(1024), 0, st, b);
+    else hipLaunchKernelGGL((k_distill_row<T, 1024, 16>), dim3(b.T), dim3(1024), 0, st, b);
+    return hipGetLastError();
+  });
+}
+
 }  // namespace
 
 size_t distill_ws_bytes(int32_t T, int32_t V, int32_t dtype) {
@@ -401,7 +404,7 @@ hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t st) {
     using T = decltype(tag);
     if (by_rows(a.T, a.V, a.dtype, false)) return launch_rows<T>(a, st);
     const Chunks k = chunks_of(a.T, a.V, a.dtype);
-    return in_launches(a, [&](const DistillArgs& b) {
+    return in_launches(a, kRowsOfLaunch, [&](const DistillArgs& b) {
       hipLaunchKernelGGL(k_distill_stat<T>, dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per);
       hipLaunchKernelGGL(k_distill_join<T>, dim3(b.T), dim3(64), 0, st, b, k.n);
       return hipGetLastError();
@@ -413,7 +416,7 @@ hipError_t launch_distill_backward(const DistillArgs& a, hipStream_t st) {
   return with_type(a.dtype, [&](auto tag) {
     using T = decltype(tag);
     const Chunks k = chunks_of(a.T, a.V, a.dtype);
-    return in_launches(a, [&](const DistillArgs& b) {
+    return in_launches(a, kRowsOfLaunch, [&](const DistillArgs& b) {
       hipLaunchKernelGGL((k_distill_grad<T, true>), dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per, k.n);
       return hipGetLastError();
     });
@@ -425,7 +428,7 @@ hipError_t launch_distill_loss_grad(const DistillArgs& a, hipStream_t st) {
     using T = decltype(tag);
     if (by_rows(a.T, a.V, a.dtype, true)) return launch_rows<T>(a, st);
     const Chunks k = chunks_of(a.T, a.V, a.dtype);
-    return in_launches(a, [&](const DistillArgs& b) {
+    return in_launches(a, kRowsOfLaunch, [&](const DistillArgs& b) {
       hipLaunchKernelGGL(k_distill_stat<T>, dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per);
       hipLaunchKernelGGL((k_distill_grad<T, false>), dim3(k.n, b.T), dim3(kChunkThreads), 0, st, b, k.per, k.n);
       return hipGetLastError();

@@ -9,6 +9,8 @@
 namespace moeq {
 
 inline int dtype_bytes(int32_t t) { return t == MOEQ_F32 ? 4 : 2; }
+// Workgroups of a launch: the threads of a dimension of the grid have to be fewer than 2^32. Calls of more are several launches.
+constexpr int32_t launch_groups(int32_t threads) { return (int32_t)(0xffffffffu / (uint32_t)threads); }
 
 // ---- dispatch.hip ----
 constexpr int32_t kSortMaxExperts = 1024;
@@ -19,6 +21,7 @@ struct RowsArgs {
   const int32_t* slot;      // [T][k]
   const float* gate;        // [T][k] or null (ones)
   int32_t T, k, d;
+  int32_t first;            // token of the launch's first thread
   const void* a;            // gather: x; combine: rows; backward: rows
   int64_t a_stride;
   const void* dy;           // backward only

@@ -208,3 +208,43 @@ def test_sort_around_the_chunks(T, k, E):
     s = moeq.moe_sort_pairs(torch.from_numpy(idx).to(DEV), E)
     for got, want in zip((s.offsets, s.order, s.slot), sorted_on_host(idx, E)):
         assert np.array_equal(got.cpu().numpy(), want)
+
+
+def order_backwards(T):
+    """A sort of one choice a token whose places run backwards, without the sort itself."""
+    slot = torch.arange(T - 1, -1, -1, dtype=torch.int32, device=DEV)
+    return moeq.PairSort(torch.tensor([0, T], dtype=torch.int32, device=DEV), slot, slot, T, 1, 1)
+
+
+def test_as_many_pairs_as_there_may_be():
+    """2^28 rows of one element: 2^32 threads, more than a launch may have."""
+    T = 1 << 28
+    sort = order_backwards(T)
+    x = torch.randn(T, device=DEV).to(torch.float16)[:, None]
+    rows = moeq.moe_gather_rows(sort, x)
+    assert torch.equal(rows, x.flip(0))
+    assert torch.equal(moeq.moe_combine_rows(sort, rows), x)
+    drows, dgate = moeq.moe_combine_rows_backward(sort, x, rows)
+    assert torch.equal(drows, rows) and torch.equal(dgate, x.float() ** 2)
+    torch.cuda.empty_cache()
+
+
+def test_as_many_wide_rows_as_pass_a_launch():
+    """2^24 rows of a workgroup each: outputs of 34 GB from inputs whose rows are all one."""
+    T, d = 1 << 24, 1025
+    sort = order_backwards(T)
+    one = torch.randn((1, d), device=DEV).to(torch.bfloat16)
+    buf = torch.zeros((T, d), dtype=torch.bfloat16, device=DEV)
+    same = lambda: all(bool((part == one).all()) for part in buf.split(1 << 21))
+    moeq.moe_gather_rows(sort, one.expand(T, d), rows=buf)
+    assert same()
+    buf.zero_()
+    moeq.moe_combine_rows(sort, one.expand(T, d), y=buf)
+    assert same()
+    buf.zero_()
+    _, dgate = moeq.moe_combine_rows_backward(sort, one.expand(T, d), one.expand(T, d), drows=buf)
+    assert same() and bool((dgate == dgate[0]).all())
+    # 1025 squares of positive sum: a chain of at most 1025 / 256 + 16 roundings
+    assert abs(dgate[0].item() / (one.double() ** 2).sum().item() - 1) < (1025 / 256 + 16) * 2.0**-24
+    del buf
+    torch.cuda.empty_cache()

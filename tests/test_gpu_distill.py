@@ -264,3 +264,18 @@ def test_a_teacher_that_is_not_finite_is_seen(T, V, kind):
         assert d[bad][at[bad]].isnan().all() and d[bad][~at[bad]].isfinite().all()
         assert (d[none] == 0).all() and d.isnan().sum().item() == int(at[bad].sum())
     assert torch.equal(dz.cpu()[bad][~at[bad]], want.cpu()[bad][~at[bad]])      # (the student's part is what it was)
+
+
+def test_as_many_rows_as_there_may_be():
+    """2^24 rows of 256 threads, more than a launch may have: the same bits as in two calls of half of them."""
+    T, V = 1 << 24, 8
+    z = torch.randn((T, V), device=DEV).to(torch.bfloat16)
+    idx = torch.randint(0, V, (T, 1), dtype=torch.int32, device=DEV)
+    u, w = torch.randn((T, 1), device=DEV), torch.rand(T, device=DEV)
+    a, b = slice(0, T // 2), slice(T // 2, T)
+    for call in (lambda s: moeq.moe_distill_forward(z[s], idx[s], u[s], temperature=2.0, weight=w[s]),
+                 lambda s: moeq.moe_distill_loss_grad(z[s], idx[s], u[s], temperature=2.0, weight=w[s])):
+        for whole, first, last in zip(call(slice(0, T)), call(a), call(b)):
+            assert torch.equal(whole[a], first) and torch.equal(whole[b], last)
+    with pytest.raises(moeq.MoeqError):
+        moeq.moe_distill_forward(z[:1].expand(T + 1, V), idx[:1].repeat(T + 1, 1), u[:1].repeat(T + 1, 1))
