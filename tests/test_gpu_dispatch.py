@@ -248,3 +248,50 @@ def test_as_many_wide_rows_as_pass_a_launch():
     assert abs(dgate[0].item() / (one.double() ** 2).sum().item() - 1) < (1025 / 256 + 16) * 2.0**-24
     del buf
     torch.cuda.empty_cache()
+
+
+# chunks of 4096 pairs on both sides of where their counts are scanned ahead, and as many as make adding them up in every chunk too long
+@pytest.mark.parametrize("P,E,drop", [(96 * 4096, 8, 0.02), (96 * 4096 + 1, 8, 0.02), (19 * 4096, 256, 0.0), (19 * 4096 + 5, 256, 0.1),
+                                      (4 * 4096, 1024, 0.02), (4 * 4096 + 1, 1024, 0.02), (1000001, 63, 0.3), (5000003, 1024, 0.0)])
+def test_sort_of_many_chunks(P, E, drop):
+    rng = rng_of("many", P, E, drop)
+    idx = rng.integers(0, E, size=(P, 1)).astype(np.int32)
+    idx[rng.random((P, 1)) < drop] = -1
+    s = moeq.moe_sort_pairs(torch.from_numpy(idx).to(DEV), E)
+    for got, want in zip((s.offsets, s.order, s.slot), sorted_on_host(idx, E)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_sort_takes_time_in_proportion_to_its_pairs():
+    """16 times the pairs, 4.2 million to 67 million of 256 experts: some 16 times the time, where counts that every chunk adds up for
+    itself would take 256 times."""
+    def least(P):
+        idx = torch.randint(0, 256, (P, 1), dtype=torch.int32, device=DEV)
+        times = []
+        for _ in range(4):
+            a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+            a.record()
+            moeq.moe_sort_pairs(idx, 256)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    assert least(1 << 26) < 64 * least(1 << 22)
+
+
+def test_sort_of_as_many_pairs_as_there_may_be():
+    P, E = 1 << 28, 5
+    idx = torch.randint(-1, E, (P // 2, 2), dtype=torch.int32, device=DEV)
+    s = moeq.moe_sort_pairs(idx, E)
+    key = torch.where(idx < 0, E, idx).flatten().to(torch.int8)
+    counts = [int((key == e).sum()) for e in range(E)]
+    assert s.offsets.tolist() == [sum(counts[:e]) for e in range(E + 1)]
+    order = torch.where(s.order < 0, ~s.order, s.order)
+    got = key[order.long()]
+    assert bool((got[1:] >= got[:-1]).all()) and bool(((got == E) == (s.order < 0)).all())
+    assert bool(((order[1:] > order[:-1]) | (got[1:] > got[:-1])).all())           # stable, and so every pair once
+    place = torch.where(s.slot < 0, ~s.slot, s.slot)
+    assert bool((place[order.long()] == torch.arange(P, dtype=torch.int32, device=DEV)).all()) and bool(((s.slot < 0) == (key == E)).all())
+    del order, got, place, key
+    torch.cuda.empty_cache()
