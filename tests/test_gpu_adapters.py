@@ -372,3 +372,36 @@ def test_a_graph_and_calls_beside_it():
         got = calls[i](stream=side)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, want[0])) and all(torch.equal(a, b) for a, b in zip(got, want[i]))
+
+
+# columns that several workgroups share: in the backward pass two shares from 993 fp32 or 1985 16-bit columns of the narrower side, four
+# from twice as many, eight from four times; in the forward pass, by d_in, eight from 4065 fp32 or 8129 16-bit columns
+SHARED = [("f32", "f32", 70, 5, 992, 1500), ("f32", "f32", 70, 5, 993, 1500), ("f32", "f32", 300, 17, 1501, 994), ("f32", "f32", 130, 40, 2049, 1987),
+          ("f32", "f32", 33, 16, 4001, 4099), ("bf16", "bf16", 70, 3, 1984, 2500), ("bf16", "bf16", 200, 33, 1985, 2500),
+          ("bf16", "f32", 90, 16, 2505, 1986), ("bf16", "bf16", 1100, 32, 4096, 4097), ("bf16", "bf16", 40, 64, 8000, 7937), ("f16", "f16", 70, 8, 2047, 1984),
+          ("f16", "f16", 70, 20, 2047, 1985), ("f16", "f32", 160, 50, 1985, 4096), ("f16", "f16", 520, 1, 4096, 4096), ("bf16", "bf16", 9, 16, 8128, 64),
+          ("bf16", "bf16", 9, 16, 8129, 64), ("bf16", "f32", 66, 48, 8129, 72), ("f16", "f16", 64, 7, 8200, 40), ("f32", "f32", 64, 20, 4064, 64),
+          ("f32", "f32", 64, 20, 4065, 64), ("f32", "f32", 150, 64, 4070, 33), ("bf16", "bf16", 5, 9, 32768, 64), ("bf16", "bf16", 70, 9, 64, 32768), ("f32", "f32", 40, 33, 4064, 4500), ("f32", "f32", 40, 33, 4500, 4065),
+          ("bf16", "bf16", 100, 64, 8129, 8150), ("bf16", "f32", 35, 8, 8200, 8129), ("f16", "f16", 80, 24, 8128, 8300), ("f16", "f32", 80, 24, 8300, 8129)]
+
+
+@pytest.mark.parametrize("kind,out,T,r,d_in,d_out", SHARED)
+def test_columns_shared_among_workgroups(kind, out, T, r, d_in, d_out):
+    n = 3
+    rng = rng_of("shared", kind, out, T, r, d_in, d_out)
+    m = make(rng, T, n, r, d_in, d_out, TYPES[kind], TYPES[out])
+    ids = ids_of(rng, T, n, "mixed")
+    want = reference(m, ids, n)
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ids = torch.from_numpy(ids).to(DEV)
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    y = moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"])
+    check(y, *want["y"], d_in + r)
+    dx, dA, dB = moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], dx_base=g["dx_base"])
+    check(dx, *want["dx"], d_out + r)
+    check(dA, *want["dA"], d_out + T)
+    check(dB, *want["dB"], d_in + T)
+    s = {k: strided(g[k], 3, 1) for k in ("x", "dy", "base", "dx_base")}
+    y2 = moeq.moe_adapters_forward(ad, s["x"], ids, base=s["base"], y=s["base"])
+    again = moeq.moe_adapters_backward(ad, s["x"], ids, s["dy"], dx_base=s["dx_base"], dx=s["dx_base"])
+    assert torch.equal(y, y2) and all(torch.equal(a, b) for a, b in zip(again, (dx, dA, dB)))
