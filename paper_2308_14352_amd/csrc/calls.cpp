@@ -208,8 +208,9 @@ CALL(combine_rows_backward, 7) {
 // (Past the dispatcher, which at::empty goes through: 0.4 us less of a call of nine rows of the host's time.)
 Tensor workspace(PyObject* o, const moeq_adapters* L, int64_t T, bool backward, const Tensor& like) {
   if (o == Py_None) {
+    static at::Allocator* const memory = empty({1}, at::kByte, like).storage().allocator();      // (that of torch's own tensors)
     const int64_t bytes = std::max<int64_t>(lib.adapters_workspace_bytes(L, size32(T), backward), 16);
-    return Tensor(at::detail::empty_generic({bytes}, c10::GetAllocator(like.device().type()), c10::DispatchKeySet(c10::DispatchKey::CUDA), at::kByte, c10::nullopt));
+    return Tensor(at::detail::empty_generic({bytes}, memory, c10::DispatchKeySet(c10::DispatchKey::CUDA), at::kByte, c10::nullopt));
   }
   const Tensor& ws = tensor(o);
   need(ws.is_cuda() && ws.is_contiguous() && ws.scalar_type() == at::kByte);

@@ -316,7 +316,7 @@ def test_calls_on_two_streams_have_workspaces_of_their_own():
     for s in streams:
         calls[0](stream=s)
         places.append(ad._ws)                             # (held: the allocator cannot give the same place twice)
-    assert places[0].data_ptr() != places[1].data_ptr()
+    assert places[0].data_ptr() != places[1].data_ptr() and all(t.device == ad.a.device for t in places)
     torch.cuda.synchronize()
     for s in streams:
         with torch.cuda.stream(s):
