@@ -402,6 +402,13 @@ _DTYPES = {torch.float32: MOEQ_F32, torch.bfloat16: MOEQ_BF16, torch.float16: MO
 _native = None
 
 
+def _stream_on(device):
+    """The handle of the current stream, where `device` (that of a call's tensors) is the current one."""
+    if torch._C._cuda_getDevice() != device:
+        raise MoeqError(MOEQ_EINVAL, "tensors on a device that is not the current one")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _load():
     global _native
     L = lib()
@@ -412,7 +419,7 @@ def _load():
     names = ("moe_sort_bytes", "moe_sort_pairs", "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward",
              "moe_adapters_workspace_bytes", "moe_adapters_forward", "moe_adapters_backward", "moe_distill_workspace_bytes",
              "moe_distill_forward", "moe_distill_backward", "moe_distill_loss_grad")
-    _calls.bind(MoeqError, lambda: _stream(None), *[C.cast(getattr(L, n), C.c_void_p).value for n in names])
+    _calls.bind(MoeqError, _stream_on, *[C.cast(getattr(L, n), C.c_void_p).value for n in names])
     _native = _calls
     return _calls
 
@@ -475,7 +482,7 @@ class Adapters:
         _need(a.dim() == 3 and b.dim() == 3 and scale.dim() == 1 and a.dtype in _DTYPES and b.dtype is a.dtype, what)
         n, r, d_in = a.shape
         _need(b.shape[0] == n and b.shape[2] == r and scale.shape[0] == n and scale.dtype is torch.float32, what)
-        _need(all(t.is_cuda and t.is_contiguous() for t in (a, b, scale)), what)
+        _need(all(t.is_cuda and t.is_contiguous() and t.device == a.device for t in (a, b, scale)), what)
         self.a, self.b, self.scale = a, b, scale
         self.n_adapters, self.rank, self.d_in, self.d_out, self.dtype = n, r, d_in, b.shape[1], a.dtype
         self._desc = moeq_adapters(n, r, d_in, self.d_out, _DTYPES[a.dtype], a.data_ptr(), b.data_ptr(), scale.data_ptr())
@@ -497,7 +504,7 @@ def moe_adapters_forward(adapters, x, ids, base=None, y=None, ws=None, stream=No
     if stream is not None:
         with torch.cuda.stream(stream):
             return moe_adapters_forward(adapters, x, ids, base, y, ws)
-    y, used = (_native or _load()).adapters_forward(adapters.handle, x, ids, base, y, ws)
+    y, used = (_native or _load()).adapters_forward(adapters.handle, x, ids, base, y, ws, adapters.a)
     if ws is None:
         adapters._ws = used
     return y
@@ -509,7 +516,7 @@ def moe_adapters_backward(adapters, x, ids, dy, dx_base=None, dx=None, want_dx=T
     if stream is not None:
         with torch.cuda.stream(stream):
             return moe_adapters_backward(adapters, x, ids, dy, dx_base, dx, want_dx, ws)
-    dx, dA, dB, used = (_native or _load()).adapters_backward(adapters.handle, x, ids, dy, dx_base, dx, bool(want_dx), ws)
+    dx, dA, dB, used = (_native or _load()).adapters_backward(adapters.handle, x, ids, dy, dx_base, dx, bool(want_dx), ws, adapters.a)
     if ws is None:
         adapters._ws = used
     return dx, dA, dB

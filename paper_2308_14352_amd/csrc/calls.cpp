@@ -10,6 +10,7 @@
 #include <ATen/ops/empty.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "moeq.h"
 
@@ -30,7 +31,7 @@ struct Entry {
   decltype(&moe_distill_loss_grad) distill_loss_grad;
 } lib;
 PyObject* error_class = nullptr;      // binding.MoeqError(status, what)
-PyObject* current_stream = nullptr;   // () -> the handle of torch's current stream
+PyObject* current_stream = nullptr;   // index of a device -> the handle of torch's current stream there; raises MoeqError if another is current
 
 using at::Tensor;
 
@@ -77,11 +78,17 @@ inline int32_t whole32(PyObject* o) {
   return (int32_t)v;
 }
 inline void* address(PyObject* o) { return (void*)whole(o); }
-inline void* stream_now() {
-  PyObject* s = PyObject_CallNoArgs(current_stream);
+// The current stream of the device that a call's tensors are on: all of them (those that are there) on one, which has to be the current
+// device, for the launches go to that.
+inline void* stream_of(const Tensor& t, std::initializer_list<const Tensor*> others) {
+  for (const Tensor* o : others) need(!o || !o->defined() || o->device() == t.device());
+  PyObject* index = PyLong_FromLong(t.get_device());
+  PyObject* s = index ? PyObject_CallFunctionObjArgs(current_stream, index, nullptr) : nullptr;
+  Py_XDECREF(index);
   if (!s) throw python_error();
   const long long v = PyLong_AsLongLong(s);
   Py_DECREF(s);
+  if (v == -1 && PyErr_Occurred()) throw python_error();
   return (void*)v;
 }
 inline void* data(const Tensor& t) { return t.data_ptr(); }
@@ -151,7 +158,7 @@ CALL(sort_pairs, 2) {
   const size_t ws = lib.sort_bytes(size32(T), size32(k), (int32_t)E);
   const Tensor buf = empty({E + 1 + 2 * P + (int64_t)ws / 4}, at::kInt, idx);
   int32_t* at = (int32_t*)data(buf);
-  void* stream = stream_now();
+  void* stream = stream_of(idx, {});
   run([&] { return lib.sort_pairs((const int32_t*)data(idx), (int32_t)T, (int32_t)k, (int32_t)E, at, at + E + 1, at + E + 1 + P, at + E + 1 + 2 * P, ws, stream); });
   return give_tuple(give(buf.narrow(0, 0, E + 1)), give(buf.narrow(0, E + 1, P)), give(buf.narrow(0, E + 1 + P, P)), PyLong_FromLongLong(T), PyLong_FromLongLong(k), again(a[1]));
 }
@@ -165,7 +172,7 @@ CALL(gather_rows, 5) {
   plain(slot, {T * k}, at::kInt);
   const Tensor rows = a[4] == Py_None ? empty({T * k, d}, x.scalar_type(), x) : tensor(a[4]);
   need(rows.scalar_type() == x.scalar_type());
-  void* stream = stream_now();
+  void* stream = stream_of(slot, {&x, &rows});
   run([&] { return lib.gather_rows((const int32_t*)data(slot), (int32_t)T, (int32_t)k, size32(d), type_of(x.scalar_type()), data(x), xs, data(rows), matrix(rows, T * k, d), stream); });
   return a[4] == Py_None ? give(rows) : again(a[4]);
 }
@@ -181,7 +188,7 @@ CALL(combine_rows, 7) {
   const at::ScalarType type = a[5] != Py_None ? ((THPDtype*)a[5])->scalar_type : a[6] != Py_None ? tensor(a[6]).scalar_type() : rows.scalar_type();
   const Tensor y = a[6] == Py_None ? empty({T, d}, type, rows) : tensor(a[6]);
   need(y.scalar_type() == type);
-  void* stream = stream_now();
+  void* stream = stream_of(slot, {&rows, gate, &y});
   run([&] { return lib.combine_rows((const int32_t*)data(slot), data<const float>(gate), (int32_t)T, (int32_t)k, size32(d), type_of(rows.scalar_type()), data(rows), rs, type_of(type),
                         data(y), matrix(y, T, d), stream); });
   return a[6] == Py_None ? give(y) : again(a[6]);
@@ -197,7 +204,7 @@ CALL(combine_rows_backward, 7) {
   if (gate) plain(*gate, {T, k}, at::kFloat);
   const Tensor drows = a[6] == Py_None ? empty({T * k, d}, rows.scalar_type(), rows) : tensor(a[6]), dgate = empty({T, k}, at::kFloat, rows);
   need(drows.scalar_type() == rows.scalar_type());
-  void* stream = stream_now();
+  void* stream = stream_of(slot, {&dy, &rows, gate, &drows});
   run([&] { return lib.combine_rows_backward((const int32_t*)data(slot), data<const float>(gate), (int32_t)T, (int32_t)k, size32(d), type_of(rows.scalar_type()), data(rows), rs,
                                  type_of(dy.scalar_type()), data(dy), ys, data(drows), matrix(drows, T * k, d), (float*)data(dgate), stream); });
   return give_tuple(a[6] == Py_None ? give(drows) : again(a[6]), give(dgate));
@@ -217,26 +224,26 @@ Tensor workspace(PyObject* o, const moeq_adapters* L, int64_t T, bool backward, 
   return ws;
 }
 
-// handle, x, ids, base or None, y or None, ws or None -> y, ws
-CALL(adapters_forward, 6) {
+// handle, x, ids, base or None, y or None, ws or None, the adapters' weights -> y, ws
+CALL(adapters_forward, 7) {
   const moeq_adapters* L = (const moeq_adapters*)address(a[0]);
-  const Tensor &x = tensor(a[1]), &ids = tensor(a[2]), *base = tensor_or_none(a[3]);
+  const Tensor &x = tensor(a[1]), &ids = tensor(a[2]), *base = tensor_or_none(a[3]), &weights = tensor(a[6]);
   need(x.dim() == 2 && type_of(x.scalar_type()) == L->dtype);
   const int64_t T = x.size(0), xs = matrix(x, T, L->d_in);
   plain(ids, {T}, at::kInt);
   const Tensor ws = workspace(a[5], L, T, false, x);
   const Tensor y = a[4] != Py_None ? tensor(a[4]) : empty({T, L->d_out}, base ? base->scalar_type() : x.scalar_type(), x);
   need(!base || base->scalar_type() == y.scalar_type());
-  void* stream = stream_now();
+  void* stream = stream_of(x, {&weights, &ids, base, &ws, &y});
   run([&] { return lib.adapters_forward(L, data(x), xs, (const int32_t*)data(ids), size32(T), data<const void>(base), base ? matrix(*base, T, L->d_out) : 0, type_of(y.scalar_type()), data(y),
                             matrix(y, T, L->d_out), data(ws), ws.numel(), stream); });
   return give_tuple(a[4] == Py_None ? give(y) : again(a[4]), give(ws));
 }
 
-// handle, x, ids, dy, dx_base or None, dx or None, whether dx is wanted, ws or None -> dx or None, dA, dB, ws
-CALL(adapters_backward, 8) {
+// handle, x, ids, dy, dx_base or None, dx or None, whether dx is wanted, ws or None, the adapters' weights -> dx or None, dA, dB, ws
+CALL(adapters_backward, 9) {
   const moeq_adapters* L = (const moeq_adapters*)address(a[0]);
-  const Tensor &x = tensor(a[1]), &ids = tensor(a[2]), &dy = tensor(a[3]), *base = tensor_or_none(a[4]);
+  const Tensor &x = tensor(a[1]), &ids = tensor(a[2]), &dy = tensor(a[3]), *base = tensor_or_none(a[4]), &weights = tensor(a[8]);
   need(x.dim() == 2 && type_of(x.scalar_type()) == L->dtype);
   const int64_t T = x.size(0), xs = matrix(x, T, L->d_in), ys = matrix(dy, T, L->d_out);
   plain(ids, {T}, at::kInt);
@@ -246,7 +253,7 @@ CALL(adapters_backward, 8) {
   need(!dx.defined() || dx.scalar_type() == dy.scalar_type());
   need(!base || base->scalar_type() == dy.scalar_type());
   const Tensor dA = empty({L->n_adapters, L->rank, L->d_in}, at::kFloat, x), dB = empty({L->n_adapters, L->d_out, L->rank}, at::kFloat, x);
-  void* stream = stream_now();
+  void* stream = stream_of(x, {&weights, &ids, &dy, base, &ws, &dx});
   run([&] { return lib.adapters_backward(L, data(x), xs, (const int32_t*)data(ids), size32(T), type_of(dy.scalar_type()), data(dy), ys, data<const void>(base), base ? matrix(*base, T, L->d_in) : 0,
                              dx.defined() ? data(dx) : nullptr, dx.defined() ? matrix(dx, T, L->d_in) : 0, (float*)data(dA), (float*)data(dB), data(ws), ws.numel(), stream); });
   return give_tuple(mine ? give(dx) : again(a[5]), give(dA), give(dB), give(ws));
@@ -274,7 +281,7 @@ CALL(distill_forward, 5) {
   const size_t ws = lib.distill_workspace_bytes(t.T, t.V, t.type);
   const Tensor buf = empty({2 * t.T + (int64_t)(ws + 3) / 4 + 1}, at::kFloat, *t.logits);      // (loss, lse, and the workspace at the next 8 bytes)
   float *at = (float*)data(buf), *scratch = at + (2 * t.T + 1) / 2 * 2;
-  void* stream = stream_now();
+  void* stream = stream_of(*t.logits, {t.idx, t.top, t.weight});
   run([&] { return lib.distill_forward(data(*t.logits), t.stride, t.type, t.T, t.V, (const int32_t*)data(*t.idx), (const float*)data(*t.top), t.K, t.temperature, data<const float>(t.weight), at,
                            at + t.T, scratch, ws, stream); });
   return give_tuple(give(buf.narrow(0, 0, t.T)), give(buf.narrow(0, t.T, t.T)));
@@ -288,7 +295,7 @@ CALL(distill_backward, 8) {
   plain(dloss, {t.T}, at::kFloat);
   const Tensor dz = a[7] == Py_None ? empty({t.T, t.V}, t.logits->scalar_type(), *t.logits) : tensor(a[7]);
   need(dz.scalar_type() == t.logits->scalar_type());
-  void* stream = stream_now();
+  void* stream = stream_of(*t.logits, {t.idx, t.top, t.weight, &lse, &dloss, &dz});
   run([&] { return lib.distill_backward(data(*t.logits), t.stride, t.type, t.T, t.V, (const int32_t*)data(*t.idx), (const float*)data(*t.top), t.K, t.temperature, data<const float>(t.weight),
                             (const float*)data(lse), (const float*)data(dloss), data(dz), matrix(dz, t.T, t.V), stream); });
   return a[7] == Py_None ? give(dz) : again(a[7]);
@@ -302,13 +309,13 @@ CALL(distill_loss_grad, 6) {
   const Tensor dz = a[5] == Py_None ? empty({t.T, t.V}, t.logits->scalar_type(), *t.logits) : tensor(a[5]);
   need(dz.scalar_type() == t.logits->scalar_type());
   float *at = (float*)data(buf), *scratch = at + (t.T + 1) / 2 * 2;
-  void* stream = stream_now();
+  void* stream = stream_of(*t.logits, {t.idx, t.top, t.weight, &dz});
   run([&] { return lib.distill_loss_grad(data(*t.logits), t.stride, t.type, t.T, t.V, (const int32_t*)data(*t.idx), (const float*)data(*t.top), t.K, t.temperature, data<const float>(t.weight), at,
                              data(dz), matrix(dz, t.T, t.V), scratch, ws, stream); });
   return give_tuple(give(buf.narrow(0, 0, t.T)), a[5] == Py_None ? give(dz) : again(a[5]));
 }
 
-// MoeqError, the function that gives the current stream, then the addresses of the library's entry points in the order of Entry.
+// MoeqError, the function that gives the current stream of a device, then the addresses of the library's entry points in the order of Entry.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   constexpr int kEntries = sizeof(Entry) / sizeof(void*);

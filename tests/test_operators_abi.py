@@ -122,3 +122,12 @@ def test_binding_refuses_tensors_that_are_not_on_the_device_or_of_another_form()
         with pytest.raises(moeq.MoeqError) as e:
             call_()
         assert e.value.status == INVALID
+
+
+def test_binding_takes_the_stream_of_the_current_device_only(monkeypatch):
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device)
+    assert B._stream_on(1) == 101
+    with pytest.raises(moeq.MoeqError) as e:
+        B._stream_on(0)
+    assert e.value.status == INVALID
