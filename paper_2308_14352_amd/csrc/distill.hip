@@ -137,17 +137,14 @@ __device__ __forceinline__ float take_teacher(const DistillArgs& A, int t, const
   const int32_t* idx = A.top_idx + (int64_t)t * A.K;
   const float* u = A.top_logits + (int64_t)t * A.K;
   float top = -INFINITY, sum = 0.f, plogp = 0.f;
-  bool some = false;
   for (int j = lane; j < A.K; j += 64) {
     const int i = idx[j];
     const bool ok = (uint32_t)i < (uint32_t)A.V;
     sh.idx[j] = ok ? i : -1;
     sh.p[j] = ok ? u[j] : -INFINITY;
     sh.z[j] = ok ? (float)z[i] : 0.f;
-    some |= ok && u[j] != -INFINITY;
     top = ok ? fmaxf(top, u[j]) : top;
   }
-  const bool any = __ballot(some) != 0;
   top = wave_max(top);
   const float o = origin(top);
   for (int j = lane; j < A.K; j += 64) {
@@ -155,6 +152,7 @@ __device__ __forceinline__ float take_teacher(const DistillArgs& A, int t, const
     sum += e;
   }
   sum = wave_sum(sum);
+  const bool any = sum != 0.f;      // (0: no entry, or minus infinities alone; the largest finite one adds 1)
   const float log_sum = __builtin_amdgcn_logf(sum) * kLn2;
   for (int j = lane; j < A.K; j += 64) {
     const float lp = (sh.p[j] - o) * it - log_sum, p = __builtin_amdgcn_exp2f(lp * kLog2e);
