@@ -283,7 +283,8 @@ moeq_status moe_unprepare_in(const void *stream_buf, int64_t rows, int64_t cols,
  *   - All pointers are device pointers; calls enqueue on `stream` and return, allocate nothing and can be captured into a
  *     graph. Elements are fp32, bf16 or fp16 (moeq_dtype); sums are held in fp32.
  *   - Matrices have contiguous rows and a row stride in elements, at any alignment of an element. An input whose rows are all
- *     the same one may have stride 0. Outputs must not overlap inputs, unless it is said.
+ *     the same one may have stride 0. Outputs that overlap inputs or each other are refused, unless it is said. A workspace
+ *     is memory of its own: that it overlaps nothing is not checked.
  *   - Indices that come with the call (experts, slots, adapter ids, a teacher's indices) are data: one that is out of its range
  *     means "none" and never leads to an access. */
 

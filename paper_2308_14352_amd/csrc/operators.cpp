@@ -1,6 +1,8 @@
 // Host side of the operators beside the layer: argument checks (all before the first HIP call) and launches.
 #include "operators.h"
 
+#include <initializer_list>
+
 using namespace moeq;
 
 namespace {
@@ -21,6 +23,18 @@ bool overlap(const Block& a, const Block& b) {
   if (pitch > 0 && pitch == b.stride * eb) {
     const int64_t at = ((int64_t)(y - x) % pitch + pitch) % pitch;      // where b's rows begin in a's
     return at < a.width * ea || at + b.width * eb > pitch;
+  }
+  return true;
+}
+// n contiguous elements of 4 bytes.
+inline Block vec(const void* p, int64_t n) { return Block{p, n > 0, n, n, MOEQ_F32}; }
+// Whether the outputs share no byte with the inputs or with each other (those that are null, or of no rows, with none).
+bool apart(std::initializer_list<Block> out, std::initializer_list<Block> in) {
+  for (const Block* o = out.begin(); o != out.end(); ++o) {
+    for (const Block& i : in)
+      if (overlap(i, *o)) return false;
+    for (const Block* p = o + 1; p != out.end(); ++p)
+      if (overlap(*p, *o)) return false;
   }
   return true;
 }
@@ -52,6 +66,9 @@ moeq_status adapters_ok(const moeq_adapters* a, int32_t n_tokens, int32_t out_dt
   return MOEQ_OK;
 }
 
+inline Block a_of(const moeq_adapters& L) { return Block{L.a, (int64_t)L.n_adapters * L.rank, L.d_in, L.d_in, L.dtype}; }
+inline Block b_of(const moeq_adapters& L) { return Block{L.b, (int64_t)L.n_adapters * L.d_out, L.rank, L.rank, L.dtype}; }
+
 AdapterArgs adapter_args(const moeq_adapters* a, int32_t n_tokens, int32_t out_dtype) {
   AdapterArgs p = {};
   p.n = a->n_adapters, p.rank = a->rank, p.d_in = a->d_in, p.d_out = a->d_out, p.dtype = a->dtype, p.out_dtype = out_dtype;
@@ -66,8 +83,11 @@ moeq_status distill_ok(const DistillArgs& a, const void* ws, size_t ws_bytes, bo
   if (a.T == 0) return MOEQ_OK;
   if (!matrix_ok(a.logits, a.T, a.stride, a.V, a.dtype, true)) return MOEQ_EINVAL;
   if (!a.top_idx || !a.top_logits || !aligned(a.top_idx, 4) || !aligned(a.top_logits, 4) || !aligned(a.weight, 4)) return MOEQ_EINVAL;
-  if (grad && (!matrix_ok(a.dlogits, a.T, a.dstride, a.V, a.dtype, false) ||
-               overlap({a.logits, a.T, a.stride, a.V, a.dtype}, {a.dlogits, a.T, a.dstride, a.V, a.dtype})))
+  if (grad && !matrix_ok(a.dlogits, a.T, a.dstride, a.V, a.dtype, false)) return MOEQ_EINVAL;
+  const int64_t entries = (int64_t)a.T * a.K;
+  if (!apart({{a.dlogits, a.T, a.dstride, a.V, a.dtype}, vec(a.loss, a.T), vec(a.lse, a.T)},
+             {{a.logits, a.T, a.stride, a.V, a.dtype}, vec(a.top_idx, entries), vec(a.top_logits, entries), vec(a.weight, a.T),
+              vec(a.lse_in, a.T), vec(a.dloss, a.T)}))
     return MOEQ_EINVAL;
   if (stats) {
     const size_t need = distill_ws_bytes(a.T, a.V, a.dtype);
@@ -100,6 +120,7 @@ moeq_status moe_sort_pairs(const int32_t* idx, int32_t n_tokens, int32_t top_k, 
   if (n_tokens && (!idx || !order || !slot || !aligned(idx, 4) || !aligned(order, 4) || !aligned(slot, 4))) return MOEQ_EINVAL;
   const int64_t pairs = (int64_t)n_tokens * top_k;
   if (n_experts > kSortMaxExperts || pairs > kMaxPairs) return MOEQ_EUNSUPPORTED;
+  if (!apart({vec(offsets, n_experts + 1), vec(order, pairs), vec(slot, pairs)}, {vec(idx, pairs)})) return MOEQ_EINVAL;
   const size_t need = sort_ws_bytes(pairs, n_experts);
   if (need && (!ws || ws_bytes < need)) return MOEQ_EWORKSPACE;
   if (need && !aligned(ws, 4)) return MOEQ_EINVAL;
@@ -111,7 +132,8 @@ moeq_status moe_gather_rows(const int32_t* slot, int32_t n_tokens, int32_t top_k
   if (moeq_status s = rows_ok(slot, n_tokens, top_k, d); s != MOEQ_OK) return s;
   if (!type_ok(dtype) || !matrix_ok(x, n_tokens, x_stride, d, dtype, true)) return MOEQ_EINVAL;
   if (!matrix_ok(rows, (int64_t)n_tokens * top_k, rows_stride, d, dtype, false)) return MOEQ_EINVAL;
-  if (overlap({x, n_tokens, x_stride, d, dtype}, {rows, (int64_t)n_tokens * top_k, rows_stride, d, dtype})) return MOEQ_EINVAL;
+  const int64_t pairs = (int64_t)n_tokens * top_k;
+  if (!apart({{rows, pairs, rows_stride, d, dtype}}, {{x, n_tokens, x_stride, d, dtype}, vec(slot, pairs)})) return MOEQ_EINVAL;
   if (n_tokens == 0) return MOEQ_OK;
   RowsArgs a = {};
   a.slot = slot, a.T = n_tokens, a.k = top_k, a.d = d, a.a = x, a.a_stride = x_stride, a.out = rows, a.out_stride = rows_stride;
@@ -124,7 +146,8 @@ moeq_status moe_combine_rows(const int32_t* slot, const float* gate_opt, int32_t
   if (!type_ok(dtype) || (y_dtype != dtype && y_dtype != MOEQ_F32) || !aligned(gate_opt, 4)) return MOEQ_EINVAL;
   if (!matrix_ok(rows, (int64_t)n_tokens * top_k, rows_stride, d, dtype, true)) return MOEQ_EINVAL;
   if (!matrix_ok(y, n_tokens, y_stride, d, y_dtype, false)) return MOEQ_EINVAL;
-  if (overlap({rows, (int64_t)n_tokens * top_k, rows_stride, d, dtype}, {y, n_tokens, y_stride, d, y_dtype})) return MOEQ_EINVAL;
+  const int64_t pairs = (int64_t)n_tokens * top_k;
+  if (!apart({{y, n_tokens, y_stride, d, y_dtype}}, {{rows, pairs, rows_stride, d, dtype}, vec(slot, pairs), vec(gate_opt, pairs)})) return MOEQ_EINVAL;
   if (n_tokens == 0) return MOEQ_OK;
   RowsArgs a = {};
   a.slot = slot, a.gate = gate_opt, a.T = n_tokens, a.k = top_k, a.d = d, a.a = rows, a.a_stride = rows_stride, a.out = y, a.out_stride = y_stride;
@@ -139,8 +162,9 @@ moeq_status moe_combine_rows_backward(const int32_t* slot, const float* gate_opt
   const int64_t pairs = (int64_t)n_tokens * top_k;
   if (dgate_opt && !matrix_ok(rows, pairs, rows_stride, d, dtype, true)) return MOEQ_EINVAL;
   if (!matrix_ok(dy, n_tokens, dy_stride, d, dy_dtype, true) || !matrix_ok(drows, pairs, drows_stride, d, dtype, false)) return MOEQ_EINVAL;
-  const Block out{drows, pairs, drows_stride, d, dtype};
-  if ((dgate_opt && overlap({rows, pairs, rows_stride, d, dtype}, out)) || overlap({dy, n_tokens, dy_stride, d, dy_dtype}, out)) return MOEQ_EINVAL;
+  if (!apart({{drows, pairs, drows_stride, d, dtype}, vec(dgate_opt, pairs)},
+             {{dgate_opt ? rows : nullptr, pairs, rows_stride, d, dtype}, {dy, n_tokens, dy_stride, d, dy_dtype}, vec(slot, pairs), vec(gate_opt, pairs)}))
+    return MOEQ_EINVAL;
   if (n_tokens == 0) return MOEQ_OK;
   RowsArgs a = {};
   a.slot = slot, a.gate = gate_opt, a.T = n_tokens, a.k = top_k, a.d = d, a.a = rows, a.a_stride = rows_stride, a.dy = dy, a.dy_stride = dy_stride;
@@ -164,7 +188,8 @@ moeq_status moe_adapters_forward(const moeq_adapters* adapters, const void* x, i
     return MOEQ_EINVAL;
   if (base_opt && !matrix_ok(base_opt, n_tokens, base_stride, L.d_out, y_dtype, true)) return MOEQ_EINVAL;
   const Block out{y, n_tokens, y_stride, L.d_out, y_dtype};
-  if (overlap({x, n_tokens, x_stride, L.d_in, L.dtype}, out) || !apart_or_same({base_opt, n_tokens, base_stride, L.d_out, y_dtype}, out))
+  if (!apart({out}, {{x, n_tokens, x_stride, L.d_in, L.dtype}, vec(ids, n_tokens), a_of(L), b_of(L), vec(L.scale, L.n_adapters)}) ||
+      !apart_or_same({base_opt, n_tokens, base_stride, L.d_out, y_dtype}, out))
     return MOEQ_EINVAL;
   AdapterArgs p = adapter_args(adapters, n_tokens, y_dtype);
   p.x = x, p.x_stride = x_stride, p.ids = ids, p.base = base_opt, p.base_stride = base_stride, p.out = y, p.out_stride = y_stride, p.ws = ws;
@@ -185,11 +210,13 @@ moeq_status moe_adapters_backward(const moeq_adapters* adapters, const void* x, 
   if (dx_opt) {
     if (!matrix_ok(dx_opt, n_tokens, dx_stride, L.d_in, dy_dtype, false)) return MOEQ_EINVAL;
     if (dx_base_opt && !matrix_ok(dx_base_opt, n_tokens, dx_base_stride, L.d_in, dy_dtype, true)) return MOEQ_EINVAL;
-    const Block out{dx_opt, n_tokens, dx_stride, L.d_in, dy_dtype};
-    if (overlap({x, n_tokens, x_stride, L.d_in, L.dtype}, out) || overlap({dy, n_tokens, dy_stride, L.d_out, dy_dtype}, out) ||
-        !apart_or_same({dx_base_opt, n_tokens, dx_base_stride, L.d_in, dy_dtype}, out))
-      return MOEQ_EINVAL;
   }
+  const Block dx{dx_opt, n_tokens, dx_stride, L.d_in, dy_dtype}, base{dx_opt ? dx_base_opt : nullptr, n_tokens, dx_base_stride, L.d_in, dy_dtype};
+  const Block da = vec(dA, (int64_t)L.n_adapters * L.rank * L.d_in), db = vec(dB, (int64_t)L.n_adapters * L.rank * L.d_out);
+  if (!apart({dx, da, db}, {{x, n_tokens, x_stride, L.d_in, L.dtype}, {dy, n_tokens, dy_stride, L.d_out, dy_dtype}, vec(ids, n_tokens), a_of(L), b_of(L),
+                            vec(L.scale, L.n_adapters)}) ||
+      overlap(base, da) || overlap(base, db) || !apart_or_same(base, dx))
+    return MOEQ_EINVAL;
   AdapterArgs p = adapter_args(adapters, n_tokens, dy_dtype);
   p.x = x, p.x_stride = x_stride, p.ids = ids, p.dy = dy, p.dy_stride = dy_stride, p.base = dx_base_opt, p.base_stride = dx_base_stride;
   p.out = dx_opt, p.out_stride = dx_stride, p.dA = dA, p.dB = dB, p.ws = ws;
@@ -208,10 +235,10 @@ moeq_status moe_distill_forward(const void* logits, int64_t stride, int32_t dtyp
                                 const int32_t* top_idx, const float* top_logits, int32_t top, float temperature,
                                 const float* weight_opt, float* loss, float* lse_opt, void* ws, size_t ws_bytes, void* stream) {
   DistillArgs a = distill_args(logits, stride, dtype, n_tokens, vocab, top_idx, top_logits, top, temperature, weight_opt);
+  a.loss = loss, a.lse = lse_opt, a.ws = ws;
   if (moeq_status s = distill_ok(a, ws, ws_bytes, false, true); s != MOEQ_OK) return s;
   if (n_tokens == 0) return MOEQ_OK;
   if (!loss || !aligned(loss, 4) || !aligned(lse_opt, 4)) return MOEQ_EINVAL;
-  a.loss = loss, a.lse = lse_opt, a.ws = ws;
   return done(launch_distill_forward(a, (hipStream_t)stream));
 }
 
@@ -220,11 +247,10 @@ moeq_status moe_distill_backward(const void* logits, int64_t stride, int32_t dty
                                  const float* weight_opt, const float* lse, const float* dloss, void* dlogits, int64_t dstride,
                                  void* stream) {
   DistillArgs a = distill_args(logits, stride, dtype, n_tokens, vocab, top_idx, top_logits, top, temperature, weight_opt);
-  a.dlogits = dlogits, a.dstride = dstride;
+  a.dlogits = dlogits, a.dstride = dstride, a.lse_in = lse, a.dloss = dloss;
   if (moeq_status s = distill_ok(a, nullptr, 0, true, false); s != MOEQ_OK) return s;
   if (n_tokens == 0) return MOEQ_OK;
   if (!lse || !dloss || !aligned(lse, 4) || !aligned(dloss, 4)) return MOEQ_EINVAL;
-  a.lse_in = lse, a.dloss = dloss;
   return done(launch_distill_backward(a, (hipStream_t)stream));
 }
 
@@ -233,11 +259,10 @@ moeq_status moe_distill_loss_grad(const void* logits, int64_t stride, int32_t dt
                                   const float* weight_opt, float* loss, void* dlogits, int64_t dstride, void* ws, size_t ws_bytes,
                                   void* stream) {
   DistillArgs a = distill_args(logits, stride, dtype, n_tokens, vocab, top_idx, top_logits, top, temperature, weight_opt);
-  a.dlogits = dlogits, a.dstride = dstride;
+  a.dlogits = dlogits, a.dstride = dstride, a.loss = loss, a.ws = ws;
   if (moeq_status s = distill_ok(a, ws, ws_bytes, true, true); s != MOEQ_OK) return s;
   if (n_tokens == 0) return MOEQ_OK;
   if (!loss || !aligned(loss, 4)) return MOEQ_EINVAL;
-  a.loss = loss, a.ws = ws;
   return done(launch_distill_loss_grad(a, (hipStream_t)stream));
 }
 

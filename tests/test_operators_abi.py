@@ -131,3 +131,37 @@ def test_binding_takes_the_stream_of_the_current_device_only(monkeypatch):
     with pytest.raises(moeq.MoeqError) as e:
         B._stream_on(0)
     assert e.value.status == INVALID
+
+
+# outputs that are no matrices: each over an input, or over another output, by its last element
+GOOD_SORT, GOOD_GRAD = dict(SORT, T=4), dict(COMBINE_GRAD, dgate=P + (1 << 19))
+
+
+@pytest.mark.parametrize("name,good,bad", [
+    ("moe_sort_pairs", GOOD_SORT, dict(offsets=P - 32)), ("moe_sort_pairs", GOOD_SORT, dict(order=P + 12)),
+    ("moe_sort_pairs", GOOD_SORT, dict(slot=Q + 4096 + 12)), ("moe_sort_pairs", GOOD_SORT, dict(offsets=Q + 4096 - 32)),
+    ("moe_gather_rows", GATHER, dict(rows=P - 7 * 32)), ("moe_combine_rows", COMBINE, dict(gate=R + 3 * 32)),
+    ("moe_combine_rows", COMBINE, dict(y=P + 7 * 4)), ("moe_combine_rows_backward", GOOD_GRAD, dict(dgate=Q + 8 * 16 - 4)),
+    ("moe_combine_rows_backward", GOOD_GRAD, dict(dgate=P + 7 * 4)), ("moe_combine_rows_backward", GOOD_GRAD, dict(dgate=R - 7 * 4)),
+    ("moe_combine_rows_backward", GOOD_GRAD, dict(gate=P + (1 << 19))), ("moe_combine_rows_backward", GOOD_GRAD, dict(dgate=Q + 4096 - 28)),
+    ("moe_distill_forward", DISTILL, dict(loss=Q + 4 * 400 - 4)), ("moe_distill_forward", DISTILL, dict(loss=P + 4 * 12 - 4)),
+    ("moe_distill_forward", DISTILL, dict(lse=R + 12)), ("moe_distill_forward", DISTILL, dict(weight=R - 12)),
+    ("moe_distill_forward", DISTILL, dict(lse=P - 12)), ("moe_distill_backward", DISTILL_GRAD, dict(lse=R + 4 * 400 - 4)),
+    ("moe_distill_backward", DISTILL_GRAD, dict(dloss=R - 12)), ("moe_distill_backward", DISTILL_GRAD, dict(dlogits=P - 3 * 400)),
+])
+def test_refusals_of_outputs_that_overlap(name, good, bad):
+    assert call(name, good, **bad) == INVALID
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dA=Q + 5 * 64 * 2 - 4), dict(dA=Q + 65536 - 4 * (3 * 8 * 64 - 1)), dict(dB=P + 4 * 4), dict(dA=R + (1 << 20) + 4 * 3 * 8 * 32 - 4),
+    dict(dx=R + 65536 - 4), dict(dx_base=R + 65536 - 4), dict(dx=P - 4 * 4 * 64)])
+def test_refusals_of_gradients_that_overlap(bad):
+    d = desc(a=P + (1 << 16), b=P + (1 << 18), scale=P + (1 << 12))
+    a = dict(x=Q, ids=P, dy=Q + 65536, dx_base=None, dx=R, dA=R + 65536, dB=R + (1 << 20))
+    a.update(bad)
+    assert B.lib().moe_adapters_backward(C.addressof(d), a["x"], 64, a["ids"], 5, F32, a["dy"], 32, a["dx_base"], 64, a["dx"], 64, a["dA"], a["dB"],
+                                         P + (1 << 19), 1 << 24, None) == INVALID
+    for over in (dict(a=R - 2), dict(b=R + 4), dict(scale=R - 8)):
+        e = desc(**dict(dict(a=P + (1 << 16), b=P + (1 << 18), scale=P + (1 << 12)), **over))
+        assert B.lib().moe_adapters_forward(C.addressof(e), Q, 64, P, 5, None, 0, F32, R, 32, P + (1 << 19), 1 << 24, None) == INVALID
