@@ -349,7 +349,8 @@ moeq_status moe_adapters_backward(const moeq_adapters *adapters, const void *x, 
  * Rows of weight 0, and rows whose teacher's entries have no index or are all minus infinity, have loss 0 and gradient 0
  * whatever their logits hold; a NaN or plus infinity among a teacher's entries makes the loss, and the gradient at the row's
  * indices, NaN. A student's logit of minus infinity has probability 0 (a teacher's entry there makes the loss infinite). top <= 1024, n_tokens <= 2^24. */
-size_t moe_distill_workspace_bytes(int32_t n_tokens, int32_t vocab, int32_t dtype);
+/* Workspace of a call of up to max_tokens tokens; 0 where none is needed. */
+size_t moe_distill_workspace_bytes(int32_t max_tokens, int32_t vocab, int32_t dtype);
 /* loss [n_tokens] and, if wanted, lse [n_tokens] (of every row, whatever its weight). */
 moeq_status moe_distill_forward(const void *logits, int64_t stride, int32_t dtype, int32_t n_tokens, int32_t vocab,
                                 const int32_t *top_idx, const float *top_logits, int32_t top, float temperature,

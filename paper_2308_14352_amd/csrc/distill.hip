@@ -340,10 +340,13 @@ __global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, i
 // Vectors of a chunk and their number in a row: full chunks, or shorter ones (of a vector a thread or more) where the rows are too few
 // to give every compute unit four workgroups.
 struct Chunks { int per, n; };
+constexpr int64_t kFewChunks = 1024;      // of all rows
+int64_t vectors_of(int32_t V, int32_t dtype) { return std::max<int64_t>(1, V / (16 / dtype_bytes(dtype))); }
+int64_t full_chunks(int64_t vectors) { return (vectors + kChunkThreads * kChunkVectors - 1) / (kChunkThreads * kChunkVectors); }
 Chunks chunks_of(int32_t T, int32_t V, int32_t dtype) {
-  const int64_t all = std::max<int64_t>(1, V / (16 / dtype_bytes(dtype)));
-  int64_t n = (all + kChunkThreads * kChunkVectors - 1) / (kChunkThreads * kChunkVectors);
-  while (n * T < 1024 && all / (2 * n) >= kChunkThreads) n *= 2;
+  const int64_t all = vectors_of(V, dtype);
+  int64_t n = full_chunks(all);
+  while (n * T < kFewChunks && all / (2 * n) >= kChunkThreads) n *= 2;
   const int64_t per = (all + n - 1) / n;
   return Chunks{(int)per, (int)((all + per - 1) / per)};
 }
@@ -394,7 +397,8 @@ hipError_t launch_rows(const DistillArgs& a, hipStream_t st) {
 
 size_t distill_ws_bytes(int32_t T, int32_t V, int32_t dtype) {
   if (T <= 0 || by_rows(T, V, dtype, false)) return 0;
-  return (size_t)(T < kRowsOfLaunch ? T : kRowsOfLaunch) * chunks_of(T, V, dtype).n * sizeof(Stat);
+  // (room for as many rows and for any fewer: those in shorter chunks have less than twice kFewChunks of them)
+  return (size_t)std::max<int64_t>(std::min(T, kRowsOfLaunch) * full_chunks(vectors_of(V, dtype)), 2 * kFewChunks) * sizeof(Stat);
 }
 
 hipError_t launch_distill_forward(const DistillArgs& a, hipStream_t st) {

@@ -226,9 +226,9 @@ moeq_status moe_adapters_backward(const moeq_adapters* adapters, const void* x, 
   return done(launch_adapters_backward(p, (hipStream_t)stream));
 }
 
-size_t moe_distill_workspace_bytes(int32_t n_tokens, int32_t vocab, int32_t dtype) {
-  if (n_tokens <= 0 || vocab <= 0 || !type_ok(dtype)) return 0;
-  return distill_ws_bytes(n_tokens, vocab, dtype);
+size_t moe_distill_workspace_bytes(int32_t max_tokens, int32_t vocab, int32_t dtype) {
+  if (max_tokens <= 0 || vocab <= 0 || !type_ok(dtype)) return 0;
+  return distill_ws_bytes(max_tokens, vocab, dtype);
 }
 
 moeq_status moe_distill_forward(const void* logits, int64_t stride, int32_t dtype, int32_t n_tokens, int32_t vocab,

@@ -165,3 +165,17 @@ def test_refusals_of_gradients_that_overlap(bad):
     for over in (dict(a=R - 2), dict(b=R + 4), dict(scale=R - 8)):
         e = desc(**dict(dict(a=P + (1 << 16), b=P + (1 << 18), scale=P + (1 << 12)), **over))
         assert B.lib().moe_adapters_forward(C.addressof(e), Q, 64, P, 5, None, 0, F32, R, 32, P + (1 << 19), 1 << 24, None) == INVALID
+
+
+@pytest.mark.parametrize("dtype", (F32, BF16, F16))
+@pytest.mark.parametrize("vocab", (100, 32000, 40000, 70001, 131072, 1000003))
+def test_workspace_of_many_rows_serves_fewer(vocab, dtype):
+    sizes = [B.lib().moe_distill_workspace_bytes(T, vocab, dtype) for T in [*range(1, 2100), 5000, 65535, 65536, 1 << 20, 1 << 24]]
+    assert sizes == sorted(sizes)
+    # what calls in shorter chunks need: those of as many rows as leave a compute unit less than four workgroups
+    ve, step = 4 if dtype == F32 else 8, 256 * 8
+    for T in [t for t in range(1, 2100) if sizes[0]]:
+        n = -(-(vocab // ve) // step)
+        while n * T < 1024 and vocab // ve // (2 * n) >= 256:
+            n *= 2
+        assert sizes[T - 1] >= 8 * T * -(-(vocab // ve) // -(-(vocab // ve) // n))
