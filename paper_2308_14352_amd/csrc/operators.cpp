@@ -12,15 +12,16 @@ inline bool type_ok(int32_t t) { return t == MOEQ_F32 || t == MOEQ_BF16 || t == 
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 // A strided matrix in memory, for the checks of outputs against inputs.
 struct Block { const void* p; int64_t rows, stride, width; int32_t dtype; };
-// Whether two may share a byte. Slices of the columns of one buffer (the same stride in bytes) are compared within a row.
+// Whether two may share a byte. Slices of the columns of one buffer (the same stride in bytes, or a single row) are compared within a row.
 bool overlap(const Block& a, const Block& b) {
   if (!a.p || !b.p || a.rows == 0 || b.rows == 0) return false;
   const int64_t ea = dtype_bytes(a.dtype), eb = dtype_bytes(b.dtype);
   const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
   if (!(x < y + (uintptr_t)(((b.rows - 1) * b.stride + b.width) * eb) && y < x + (uintptr_t)(((a.rows - 1) * a.stride + a.width) * ea)))
     return false;
-  const int64_t pitch = a.stride * ea;
-  if (pitch > 0 && pitch == b.stride * eb) {
+  // (the stride of a single row says nothing)
+  const int64_t pitch = a.rows > 1 ? a.stride * ea : b.rows > 1 ? b.stride * eb : 0;
+  if (pitch > 0 && (b.rows == 1 || pitch == b.stride * eb)) {
     const int64_t at = ((int64_t)(y - x) % pitch + pitch) % pitch;      // where b's rows begin in a's
     return at < a.width * ea || at + b.width * eb > pitch;
   }
@@ -40,13 +41,13 @@ bool apart(std::initializer_list<Block> out, std::initializer_list<Block> in) {
 }
 // Whether an input may be used beside an output that it may also be itself.
 inline bool apart_or_same(const Block& in, const Block& out) {
-  return !overlap(in, out) || (in.p == out.p && in.stride == out.stride && in.dtype == out.dtype);
+  return !overlap(in, out) || (in.p == out.p && (in.rows == 1 || in.stride == out.stride) && in.dtype == out.dtype);
 }
-// A matrix of n rows: there, aligned to its elements, its rows either apart or (inputs only) all the same one.
+// A matrix of n rows: there, aligned to its elements, its rows either apart or (inputs only) all the same one; a single row has any stride.
 inline bool matrix_ok(const void* p, int64_t rows, int64_t stride, int64_t width, int32_t dtype, bool input) {
   if (rows == 0) return true;
-  return p && aligned(p, dtype_bytes(dtype)) && (stride >= width || rows == 1 || (input && stride == 0)) && stride >= 0 &&
-         stride <= (int64_t)1 << 32;
+  return p && aligned(p, dtype_bytes(dtype)) &&
+         (rows == 1 || ((stride >= width || (input && stride == 0)) && stride <= (int64_t)1 << 32));
 }
 constexpr int64_t kMaxPairs = (int64_t)1 << 28;
 

@@ -295,3 +295,34 @@ def test_sort_of_as_many_pairs_as_there_may_be():
     assert bool((place[order.long()] == torch.arange(P, dtype=torch.int32, device=DEV)).all()) and bool(((s.slot < 0) == (key == E)).all())
     del order, got, place, key
     torch.cuda.empty_cache()
+
+
+def test_a_single_row_may_have_any_stride():
+    """The stride of a single row says nothing: torch gives it what the row was cut out of."""
+    x = torch.randn((1, 40), device=DEV)
+    far, sort = torch.as_strided(x, (1, 40), (1 << 40, 1)), moeq.moe_sort_pairs(torch.zeros((1, 1), dtype=torch.int32, device=DEV), 3)
+    assert torch.equal(moeq.moe_gather_rows(sort, far), x)
+    assert torch.equal(moeq.moe_combine_rows(sort, far, y=torch.as_strided(torch.empty_like(x), (1, 40), (1 << 40, 1))), x)
+    ids, top = torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.zeros((1, 1), device=DEV)
+    for a, b in zip(moeq.moe_distill_loss_grad(far, ids, top), moeq.moe_distill_loss_grad(x, ids, top)):
+        assert torch.equal(a, b)
+    ad = moeq.Adapters(torch.randn((1, 4, 40), device=DEV), torch.randn((1, 24, 4), device=DEV), torch.ones(1, device=DEV))
+    assert torch.equal(moeq.moe_adapters_forward(ad, far, ids[0]), moeq.moe_adapters_forward(ad, x, ids[0]))
+
+
+@pytest.mark.parametrize("kind,dy_kind", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")])
+@pytest.mark.parametrize("T,k,d", [(1, 1, 3), (37, 2, 100), (65, 3, 1025), (9, 8, 4096), (5, 5, 16)])
+def test_gradient_of_the_rows_alone(T, k, d, kind, dy_kind):
+    """The C call without dgate, whose rows are not read: the same gradient of the rows."""
+    rng = rng_of("alone", T, k, d, kind)
+    sort = moeq.moe_sort_pairs(torch.from_numpy(routing(rng, T, k, 8, 0.2)).to(DEV), 8)
+    dy, gate = torch.randn((T, d), device=DEV).to(TYPES[dy_kind]), torch.rand((T, k), device=DEV)
+    rows = torch.randn((T * k, d), device=DEV).to(TYPES[kind])
+    B = moeq.binding
+    for g in (gate, None):
+        want, _ = moeq.moe_combine_rows_backward(sort, dy, rows, g)
+        got = torch.full_like(rows, float("nan"))
+        assert B.lib().moe_combine_rows_backward(sort.slot.data_ptr(), None if g is None else g.data_ptr(), T, k, d, B._DTYPES[TYPES[kind]], None, 0,
+                                                 B._DTYPES[TYPES[dy_kind]], dy.data_ptr(), d, got.data_ptr(), d, None, B._stream(None)) == B.MOEQ_OK
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
