@@ -162,14 +162,15 @@ __device__ __forceinline__ float take_teacher(const DistillArgs& A, int t, const
   if (lane == 0) sh.any = any;
   return wave_sum(plogp);
 }
-// The loss from there, by the first wavefront: w tau^2 (sum p log p - sum p ((z_j - m) / tau - log S)).
+// The loss from there, by the first wavefront: w tau^2 (sum p log p - sum p ((z_j - m) / tau - log S)). The temperature is multiplied twice: its
+// square is no fp32 number below 1e-19.
 __device__ __forceinline__ float row_loss(const DistillArgs& A, const Teacher& sh, Stat st, float w, float plogp) {
   const float it = 1.f / A.temperature, o = origin(st.m), log_s = __builtin_amdgcn_logf(st.s) * kLn2;
   float cross = 0.f;
   for (int j = threadIdx.x & 63; j < A.K; j += 64)
     if (sh.p[j] != 0.f) cross += sh.z[j] == -INFINITY ? -INFINITY : sh.p[j] * ((sh.z[j] - o) * it - log_s);
   cross = wave_sum(cross);
-  return sh.any && w != 0.f ? w * A.temperature * A.temperature * (plogp - cross) : 0.f;
+  return sh.any && w != 0.f ? w * (A.temperature * (A.temperature * (plogp - cross))) : 0.f;
 }
 // The teacher's elements of a gradient in columns [c0, c1): scale * (q - p), q = exp2((z - o) c) * inv.
 template <typename T>

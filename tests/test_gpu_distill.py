@@ -279,3 +279,19 @@ def test_as_many_rows_as_there_may_be():
             assert torch.equal(whole[a], first) and torch.equal(whole[b], last)
     with pytest.raises(moeq.MoeqError):
         moeq.moe_distill_forward(z[:1].expand(T + 1, V), idx[:1].repeat(T + 1, 1), u[:1].repeat(T + 1, 1))
+
+
+@pytest.mark.parametrize("tau", (1e-15, 1e-20, 1e-25, 1e-30))
+@pytest.mark.parametrize("V", (4, 70000))
+def test_temperatures_whose_square_is_no_fp32_number(V, tau):
+    """Logits 0, 1, 2, 3 (and minus infinity) with the teacher at the first: s = z / tau lies so far apart that log sum exp(s) = 3 / tau, and the loss
+    tau^2 (3 / tau - 0) = 3 tau; the gradient is tau at the last and -tau at the first."""
+    z = torch.full((1, V), float("-inf"), device=DEV)
+    z[0, :4] = torch.arange(4.0, device=DEV)
+    idx, u = torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.zeros((1, 1), device=DEV)
+    loss, lse = moeq.moe_distill_forward(z, idx, u, temperature=tau)
+    both, dz = moeq.moe_distill_loss_grad(z, idx, u, temperature=tau)
+    # (the quotient by tau, two factors of it, tau itself: a step each)
+    for got, want in ((loss, 3 * tau), (both, 3 * tau), (lse, 3 / tau), (dz[0, 3], tau), (-dz[0, 0], tau)):
+        assert abs(got.item() / want - 1) < 8 * 2.0**-24
+    assert (dz[0, 1:3] == 0).all() and (dz[0, 4:] == 0).all()
