@@ -56,6 +56,9 @@ def heal(adapted, head, batches, temperature=1.0, lr=1e-3):
     params = [torch.nn.Parameter(t.float()) for t in (ad.a, ad.b)]
     opt = torch.optim.Adam(params, lr=lr)
     for x, top_idx, top_logits in batches:
+        if x.shape[0] == 0:
+            yield torch.zeros((), device=x.device)      # (nothing to learn from, and no mean)
+            continue
         loss, dA, dB = loss_and_gradients(adapted, head, x, top_idx, top_logits, temperature)
         for p, g, t in zip(params, (dA, dB), (ad.a, ad.b)):
             p.grad = g / x.shape[0]

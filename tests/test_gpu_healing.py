@@ -72,3 +72,14 @@ def test_graph_of_a_training_step():
         torch.cuda.synchronize()
         for a, b in zip(held, step()):
             assert torch.allclose(a, b, rtol=1e-3, atol=1e-4)       # (the library's products may take another form in a capture)
+
+
+def test_a_batch_without_tokens_changes_nothing():
+    _, adapted, head, _, (x, idx, top) = setup(20)
+    ad = adapted.adapters
+    before = ad.a.clone(), ad.b.clone()
+    assert [loss.item() for loss in healing.heal(adapted, head, [(x[:0], idx[:0], top[:0])])] == [0.0]
+    assert torch.equal(ad.a, before[0]) and torch.equal(ad.b, before[1])
+    losses = [loss.item() for loss in healing.heal(adapted, head, [(x, idx, top), (x[:0], idx[:0], top[:0]), (x, idx, top)])]
+    assert losses[1] == 0.0 and 0 < losses[2] < losses[0] and not torch.equal(ad.b, before[1])
+    assert ad.a.isfinite().all() and ad.b.isfinite().all()
