@@ -41,6 +41,7 @@ constexpr int kInlineTokens = 64;
 // alone / in chunks: 12288 rows of 8 adapters 92 / 88, 16384 of 64 128 / 118, of 1024 columns 58 / 47 (8192 ids, the sort by itself: 9.1 /
 // 8.9).
 constexpr int kPlanOne = 8192;
+static_assert(kPlanOne <= kSortKept);
 
 // ---- operands of the matrix instructions: eight elements as they lie in memory, 4 words (16-bit types) or 8 ----
 template <typename T> constexpr int kPieces = sizeof(T) == 4 ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;

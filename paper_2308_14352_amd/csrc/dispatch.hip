@@ -12,6 +12,7 @@ namespace {
 // Pairs that one workgroup sorts alone; beyond, they go in chunks, and a kernel that counts goes ahead. us alone / in chunks:
 // 4096 pairs of 8 experts 5.9 / 8.3, of 128 8.1 / 10.6; 6144 7.5 / 8.6 and 10.6 / 11.5; 8192 9.1 / 8.9 and 13.0 / 11.7; 32768 36 / 9.1.
 constexpr int64_t kSortOne = 6144;
+static_assert(kSortOne <= kSortKept);
 
 __global__ __launch_bounds__(1024) void k_sort_one(const int32_t* __restrict__ idx, int pairs, int run, int E,
                                                    int32_t* __restrict__ offsets, int32_t* __restrict__ order, int32_t* __restrict__ slot) {

@@ -117,20 +117,6 @@ __device__ __forceinline__ void stream_n(T* p, const float (&v)[N]) {
     store_n(p, v);
   }
 }
-// The same where only `n` of them (possibly none) exist.
-template <int N, typename T>
-__device__ __forceinline__ void load_some(float (&v)[N], const T* p, int n) {
-  if (n >= N) return load_n(v, p);
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = i < n ? (float)p[i] : 0.f;
-}
-template <int N, typename T>
-__device__ __forceinline__ void store_some(T* p, const float (&v)[N], int n) {
-  if (n >= N) return store_n(p, v);
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (i < n) p[i] = (T)v[i];
-}
 #endif
 
 }  // namespace moeq

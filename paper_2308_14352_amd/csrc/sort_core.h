@@ -10,8 +10,8 @@ namespace {
 // runs before, and those before it in the run (64 at a time, by ballots on the bits of the bin). All counts are integers, so the
 // order never depends on timing. The run is gone through twice by the same loop, once to count and once to place: what a launch
 // executes once costs some 200 cycles per 64 bytes of code, so that loops unrolled to keep what was counted in registers took longer.
-// A pair's number in its run and bin is kept in LDS for the second time where there is room; beyond, the ballots are taken again.
-constexpr int kSortKept = 8192;          // pairs
+// A pair's number in its run and bin is kept in LDS for the second time.
+constexpr int kSortKept = 8192;          // pairs of a workgroup, at most
 struct SortShared {
   int cnt[4112];                         // 16 wavefronts x 257 bins, 8 x 513 or 4 x 1025
   uint16_t number[kSortKept];
@@ -52,14 +52,13 @@ __device__ __forceinline__ void sort_scan(int E, int* v) {
   }
 }
 
-// The pairs idx[0, n) of a workgroup, `run` of them a wavefront. After counting, totals(bin, count) is called for every bin by one
+// The pairs idx[0, n) of a workgroup, n <= kSortKept, `run` of them a wavefront. After counting, totals(bin, count) is called for every bin by one
 // thread, then starts() by all (with barriers before and behind), then put(pair, number, bin) for every pair with its number in the bin.
 template <typename Totals, typename Starts, typename Put>
 __device__ __forceinline__ void sort_pairs(const int32_t* idx, int n, int run, int E, SortShared& sh, Totals&& totals, Starts&& starts, Put&& put) {
   const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, bits = 32 - __builtin_clz(E);
   const int a = wave * run, b = min(a + run, n);
   int *cnt = sh.cnt, *mine = cnt + wave * (E + 1);
-  const bool keep = n <= kSortKept;
   constexpr int kNext = 4;                      // 64 pairs that are on their way ahead of those worked on
   int next[kNext];
   auto request = [&](int i) { return idx[min(i + lane, n - 1)]; };
@@ -75,7 +74,7 @@ __device__ __forceinline__ void sort_pairs(const int32_t* idx, int n, int run, i
 #pragma unroll
       for (int j = 0; j + 1 < kNext; ++j) next[j] = next[j + 1];
       next[kNext - 1] = request(i0 + 64 * kNext);
-      if (placing && keep) {
+      if (placing) {
         if (in) put(i, mine[key] + sh.number[i], key);
         continue;
       }
@@ -91,8 +90,7 @@ __device__ __forceinline__ void sort_pairs(const int32_t* idx, int n, int run, i
         const int rank = __popcll(same & ((1ull << lane) - 1)), at = mine[key] + rank;
         __builtin_amdgcn_wave_barrier();                 // every lane has read before the first of the bin counts on
         if (rank == 0) mine[key] = at + __popcll(same);
-        if (placing) put(i, at, key);
-        else if (keep) sh.number[i] = (uint16_t)at;
+        sh.number[i] = (uint16_t)at;
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -118,6 +116,7 @@ __device__ __forceinline__ void sort_pairs(const int32_t* idx, int n, int run, i
 // Sorts of several workgroups: a chunk's pairs of every bin (counts [chunks][E + 1]), and from those, a bin's pairs in all chunks and in
 // the ones ahead of `me`.
 constexpr int64_t kSortChunk = 4096;     // pairs
+static_assert(kSortChunk <= kSortKept);
 __global__ __launch_bounds__(1024) void k_sort_count(const int32_t* __restrict__ idx, int64_t pairs, int E, int32_t* __restrict__ counts) {
   __shared__ int cnt[kSortMaxExperts + 1];
   for (int e = threadIdx.x; e <= E; e += blockDim.x) cnt[e] = 0;
