@@ -42,7 +42,10 @@ __device__ __forceinline__ float wave_sum(float v) { return fold(v, 0.f, [](floa
 // A maximum of logits and the sum of exp2((z - max) c) that belongs to it; minus infinity counts from 0.
 struct Stat { float m, s; };
 __device__ __forceinline__ float origin(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ float rescale(Stat a, float m, float c) { return a.s * __builtin_amdgcn_exp2f((origin(a.m) - origin(m)) * c); }
+// The sum from another maximum on. That of nothing but minus infinities is 0 (NaNs: NaN) from any: not times exp2 of how far 0 is above m.
+__device__ __forceinline__ float rescale(Stat a, float m, float c) {
+  return a.m == -INFINITY ? a.s : a.s * __builtin_amdgcn_exp2f((a.m - m) * c);
+}
 
 // ---- a row as vectors of 16 bytes that lie on a multiple of 16 in the gradient (in the logits, where there is none), with single
 // elements before the first and behind the last: rows of an odd length begin anywhere, and a store across two lines is two of them ----

@@ -295,3 +295,18 @@ def test_temperatures_whose_square_is_no_fp32_number(V, tau):
     for got, want in ((loss, 3 * tau), (both, 3 * tau), (lse, 3 / tau), (dz[0, 3], tau), (-dz[0, 0], tau)):
         assert abs(got.item() / want - 1) < 8 * 2.0**-24
     assert (dz[0, 1:3] == 0).all() and (dz[0, 4:] == 0).all()
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("T,V,K", [(3, 3, 2), (4, 300, 5), (9, 1537, 20), (200, 2100, 7), (4, 40000, 20), (5, 140001, 64)])
+def test_low_logits_beside_nothing(T, V, K, kind):
+    """Rows whose largest logit is far below 0, of which wavefronts or whole pieces have no element, or minus infinities alone."""
+    rng = rng_of("low", T, V, K, kind)
+    z = torch.from_numpy(rng.normal(size=(T, V)) * 2.5 - rng.choice([100.0, 300.0, 2000.0], size=(T, 1))).to(TYPES[kind])
+    keep = max(K, V // 9)
+    z[0, keep:] = float("-inf")                            # all but the first ninth masked, the last, one in the middle
+    z[1, :V - keep] = float("-inf")
+    z[2, :V // 2 - keep // 2], z[2, V // 2 - keep // 2 + keep:] = float("-inf"), float("-inf")
+    idx, u = teacher(rng, torch.where(torch.isfinite(z), z, torch.full_like(z, -1e4)), K)
+    check_all(z, idx, u, 1.0, None)
+    check_all(z, idx, u, 0.5, torch.from_numpy(rng.random(T) + 0.5).float(), put=lambda t: strided(t, 3, 1))
