@@ -326,9 +326,9 @@ typedef struct {
 size_t moe_adapters_workspace_bytes(const moeq_adapters *adapters, int32_t max_tokens, int32_t backward);
 
 /* y[t] = base[t] + scale_a B_a A_a x[t], a = ids[t]; a row whose id is outside [0, n_adapters) has no adapter: y = base.
- * base_opt NULL: zeros; base may be y itself. base and y are y_dtype: dtype or MOEQ_F32. At most 65535 tokens. Products are
- * of the operands' full bits (fp32 as sums of three bf16 pieces, fp16 of two where it meets another type), sums and A x in fp32. An
- * infinity in a row's x, A or B may come out as a NaN. */
+ * base_opt NULL: zeros; base may be y itself. base and y are y_dtype: dtype or MOEQ_F32. At most 65535 rows, as many as a layer
+ * takes pairs (and a launch has in its grid's second dimension). Products are of the operands' full bits (fp32 as sums of three bf16
+ * pieces, fp16 of two where it meets another type), sums and A x in fp32. An infinity in a row's x, A or B may come out as a NaN. */
 moeq_status moe_adapters_forward(const moeq_adapters *adapters, const void *x, int64_t x_stride, const int32_t *ids,
                                  int32_t n_tokens, const void *base_opt, int64_t base_stride, int32_t y_dtype, void *y,
                                  int64_t y_stride, void *ws, size_t ws_bytes, void *stream);
@@ -356,7 +356,8 @@ moeq_status moe_distill_forward(const void *logits, int64_t stride, int32_t dtyp
                                 const int32_t *top_idx, const float *top_logits, int32_t top, float temperature,
                                 const float *weight_opt, float *loss, float *lse_opt, void *ws, size_t ws_bytes,
                                 void *stream);
-/* dlogits [n_tokens][vocab] in dtype, times dloss [n_tokens], from the forward's lse. */
+/* dlogits [n_tokens][vocab] in dtype, times dloss [n_tokens], from the forward's lse: probabilities are exp(z / tau - lse), off by
+ * some 2^-23 |lse| of themselves up to |lse| = 4096, and taken from the logits anew beyond. */
 moeq_status moe_distill_backward(const void *logits, int64_t stride, int32_t dtype, int32_t n_tokens, int32_t vocab,
                                  const int32_t *top_idx, const float *top_logits, int32_t top, float temperature,
                                  const float *weight_opt, const float *lse, const float *dloss, void *dlogits,

@@ -9,8 +9,10 @@
 // Memory bounds it: 4096 rows of 32000 bf16 logits to loss and gradient 105 us, 5.0 TB/s of one reading and one writing; the gradient of
 // 1000 rows of 50257 fp16 logits, a fifth of them masked, 33.4 us, 5.4 TB/s; the losses of 2048 bf16 rows of 32000 26 us, 5.0 TB/s. Few
 // rows are latency: 13 of 131072 fp32 logits take 4.7 us for the chunks and 3.8 for their join (the teacher's entries, one wavefront).
-// Differences z - max are taken before the scaling, so that a probability's error does not grow with the size of the logits. The
-// gradient is written without the teacher's part first; its K elements are written again behind a barrier.
+// Differences z - max are taken before the scaling, so that where the row's maximum is known (the loss, and the gradient that comes with
+// it) a probability's error does not grow with the size of the logits. The gradient from a saved log-sum-exp takes that for the origin, an
+// fp32 number, for which a probability is off by some 2^-23 |lse|: beyond kFarLse the row's maximum and sum are taken again. The gradient is
+// written without the teacher's part first; its K elements are written again behind a barrier.
 #include <algorithm>
 #include <type_traits>
 
@@ -253,6 +255,24 @@ __global__ __launch_bounds__(THREADS) void k_distill_row(DistillArgs A) {
   put_teacher(A, teacher, dz, 0, A.V, o, c, inv, scale);
 }
 
+// A saved log-sum-exp beyond which it is not used: 2^-23 |lse| is half a step of the 16-bit types there. In rows of the type's lowest value
+// alone it cannot tell log V, and below temperature 1 it may be no finite number.
+constexpr float kFarLse = 4096.f;
+// The statistics of a whole row, by a workgroup (rows of that kind are rare, and every chunk's workgroup goes through all of theirs).
+template <typename T>
+__device__ __forceinline__ Stat row_stat(const T* z, int V, float c, Stat* sh) {
+  float m = -INFINITY, s = 0.f;
+#pragma unroll 1
+  for (int64_t i = threadIdx.x; i < V; i += blockDim.x) m = fmaxf(m, (float)z[i]);
+  m = wave_max(m);
+#pragma unroll 1
+  for (int64_t i = threadIdx.x; i < V; i += blockDim.x) s += __builtin_amdgcn_exp2f(((float)z[i] - origin(m)) * c);
+  s = wave_sum(s);
+  if (threadIdx.x % 64 == 0) sh[threadIdx.x / 64] = Stat{m, s};
+  __syncthreads();
+  return join(sh, blockDim.x / 64, c);
+}
+
 // ---- rows in chunks of a workgroup: vectors [chunk * per, ...); the single elements with the last chunk ----
 constexpr int kChunkThreads = 256, kChunkVectors = 8;
 
@@ -291,7 +311,7 @@ __global__ __launch_bounds__(64) void k_distill_join(DistillArgs A, int chunks) 
 template <typename T, bool SAVED>
 __global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, int per, int chunks) {
   __shared__ Teacher teacher;
-  __shared__ Stat sh;
+  __shared__ Stat sh[SAVED ? kChunkThreads / 64 : 1];
   const int t = blockIdx.y;
   const T* z = (const T*)A.logits + (int64_t)t * A.stride;
   T* dz = (T*)A.dlogits + (int64_t)t * A.dstride;
@@ -312,7 +332,7 @@ __global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, i
     const float plogp = take_teacher(A, t, z, teacher);
     if constexpr (!SAVED) {
       const Stat st = join((const Stat*)A.ws + (int64_t)t * chunks, chunks, c);
-      if (threadIdx.x == 0) sh = st;
+      if (threadIdx.x == 0) sh[0] = st;
       if (blockIdx.x == 0) {
         const float loss = row_loss(A, teacher, st, w, plogp);
         if (threadIdx.x == 0) A.loss[t] = loss;
@@ -324,11 +344,15 @@ __global__ __launch_bounds__(kChunkThreads) void k_distill_grad(DistillArgs A, i
   float o, inv, scale = w * A.temperature;
   if constexpr (SAVED) {
     // exp(z / tau - lse): the sum's logarithm as an origin of the logits, and nothing left to divide by
-    o = A.lse_in[t] * A.temperature, inv = 1.f;
+    const float lse = A.lse_in[t];
+    o = lse * A.temperature, inv = 1.f;
     scale *= A.dloss[t];
-    if (A.lse_in[t] == -INFINITY) o = 0.f;
+    if (fabsf(lse) > kFarLse) {
+      const Stat st = row_stat(z, A.V, c, sh);
+      o = origin(st.m), inv = st.s == 0.f ? 0.f : 1.f / st.s;
+    }
   } else {
-    o = origin(sh.m), inv = sh.s == 0.f ? 0.f : 1.f / sh.s;
+    o = origin(sh[0].m), inv = sh[0].s == 0.f ? 0.f : 1.f / sh[0].s;
   }
   put_piece(held, dz + at, n, kChunkThreads, rest, last, dz + single, o, c, inv * scale);
   stores_done();

@@ -310,3 +310,35 @@ def test_low_logits_beside_nothing(T, V, K, kind):
     idx, u = teacher(rng, torch.where(torch.isfinite(z), z, torch.full_like(z, -1e4)), K)
     check_all(z, idx, u, 1.0, None)
     check_all(z, idx, u, 0.5, torch.from_numpy(rng.random(T) + 0.5).float(), put=lambda t: strided(t, 3, 1))
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("T,V", [(5, 300), (5, 70001), (300, 4000)])
+def test_gradient_from_a_saved_sum_of_far_rows(T, V, kind):
+    """Rows of the type's lowest value alone, and rows far from zero, where a log-sum-exp in fp32 says little of its row."""
+    t, rng = TYPES[kind], rng_of("far", T, V, kind)
+    z = torch.from_numpy(rng.normal(size=(T, V)) * 2.5).to(t)
+    z[0] = torch.finfo(t).min
+    z[1] = (z[1].float() * 200 + (1e5 if kind == "f32" else 3e4)).to(t)
+    z[2] = (z[2].float() * 200 - (1e7 if kind == "f32" else 3e4)).to(t)
+    z[3] = torch.finfo(t).max
+    z[3, 1:] = 0
+    K = 3
+    idx = torch.tensor([[0, V // 2, V - 1]], dtype=torch.int32).repeat(T, 1)
+    u = torch.from_numpy(rng.normal(size=(T, K))).float()
+    for tau in (1.0, 0.5, 3.0):
+        zg, ig, ug = z.to(DEV), idx.to(DEV), u.to(DEV)
+        lse = moeq.moe_distill_forward(zg, ig, ug, temperature=tau)[1]
+        dz = moeq.moe_distill_backward(zg, ig, ug, lse, torch.ones(T, device=DEV), temperature=tau).double().cpu().numpy()
+        z64, p = z.double().numpy() / tau, np.exp(u.double().numpy() / tau)
+        q = np.exp(z64 - z64.max(1, keepdims=True))
+        q /= q.sum(1, keepdims=True)
+        p /= p.sum(1, keepdims=True)
+        want = tau * q
+        for j in range(K):
+            want[:, idx[0, j]] -= tau * p[:, j]
+        # differences of logits up to 600 / tau where q is not 0: 2^-22 of them each, the sum's own 2^-22 + (V / 256 + 16) 2^-24, p as much, the type's
+        # half step, and for the near rows 2^-23 of an lse of 30 / tau
+        rel = (600 / tau + 60 / tau + 8) * 2.0**-22 + (V / 256 + 16) * 2.0**-24
+        tol = rel * tau * (q + (np.abs(want - tau * q) > 0)) + torch.finfo(t).eps / 2 * np.abs(want) * 1.001 + (2.0**-25 if kind == "f16" else 2.0**-120)
+        assert (np.abs(dz - want) <= tol).all(), (tau, (np.abs(dz - want) / tol).max(1)[:6])
