@@ -396,7 +396,8 @@ def moe_layer_forward_routed(layer, x, idx, gate, y=None, ws=None, stream=None):
 
 # ---- operators beside the layer ----------------------------------------------------------------------------------------------
 # The checks of their tensors, the memory of their outputs and the C ABI calls are in the extension module _calls (csrc/calls.cpp):
-# most of these calls are a kernel or two of a few microseconds.
+# most of these calls are a kernel or two of a few microseconds. Nothing is recorded for autograd: tensors that require gradients are taken as
+# they are, and gradients come from the backward calls.
 
 _DTYPES = {torch.float32: MOEQ_F32, torch.bfloat16: MOEQ_BF16, torch.float16: MOEQ_F16}
 _native = None

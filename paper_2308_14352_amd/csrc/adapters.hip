@@ -800,7 +800,11 @@ struct Setup {
 
 // Rows of a segment of the weights' gradients, as a power of two: 1024, fewer where that leaves too few workgroups for the chip (but not
 // in calls that are one segment, which need no sums to be joined: a launch less), more in long calls (the partial sums are
-// rank x (d_in + d_out) floats a segment).
+// rank x (d_in + d_out) floats a segment). us of the gradient with segments of 256 / 512 / 1024 rows, rank 16: one adapter, 2048 rows of 256
+// columns 24.2 / 26.0 / 31.8, of 1024 29.4 / 31.4 / 36.7, 4096 rows of 1024 36.1 / 36.3 / 41.0, four adapters 42.3 / 42.7 / 48.8 (rank 32): few
+// columns want more workgroups. Of eight adapters whose rows are hardly more than a segment each the sums to join cost more: 2048 rows of
+// 2048 columns 38.9 / 37.1 / 36.8, of 4096 (rank 32) 56.1 / 51.4 / 51.1, 4096 rows 77.3 / 77.9 / 70.9. The rule goes by the columns alone:
+// how the rows spread is not known on the host.
 int segment_shift(const AdapterArgs& a) {
   const int64_t slices = (a.d_in + 127) / 128 + (a.d_out + 127) / 128;
   int k = 10;
@@ -813,7 +817,9 @@ int segment_shift(const AdapterArgs& a) {
 // compute unit. A row's units of 128 bytes fall on 4 k wavefronts and what reads the result adds k sums, so k grows as the square root of
 // the units: 2 of 1024 bf16 columns, 4 of 4096, 8 of 8192 and more. us of a forward call with one share more in the doubling / this /
 // one less: 256 rows of 4096 15.3 / 13.9 / -, 8 rows 9.5 / 8.8 / -, 8 rows of 14336 - / 10.4 / 12.0, 512 of 1024 - / 14.7 / 17.2. The
-// backward pass has a launch that adds the shares, none where there is one: up to 1024 columns.
+// backward pass has a launch that adds the shares, none where there is one, and twice the workgroups, for it takes both products. us of the
+// gradient with two or more shares by this rule / with one: 777 rows of 4096 31.0 / 33.4, 4096 rows 77.5 / 80.6, 8192 115.1 / 117.8; 2048 rows
+// of 2048 39.3 / 35.6, 4096 55.5 / 54.6, 12000 rows of 4096 163 / 154; up to 1024 columns one.
 inline int column_splits(const AdapterArgs& a, int d, int tiles, bool backward) {
   const int units = a.dtype == MOEQ_F32 ? (d + 31) / 32 : (d + 63) / 64;
   int k = 1;
@@ -842,7 +848,7 @@ Setup set_up(const AdapterArgs& a, bool backward) {
     // Rows of a tile: as many as share the weights that are read for them, unless that is mostly padding or leaves compute units without
     // work. us of calls of 4096 columns by tiles of 16 / 32 / 64, rows x adapters: rank 16, 128 x 32 15.1 / 17.2 / 23.2, 1024 x 32 22.3
     // / 22.8 / 25.3, 6144 x 256 74 / 69 / 84, 8192 x 64 83 / 74 / 80, 8192 x 8 74 / 63 / 67, 16384 x 8 135 / 124 / 114; rank 64, 4096 x
-    // 8 81 / 70 / 92, 8192 x 8 126 / 115 / 110. Backward, 8192 x 8 - / 101 / 104, 16384 x 64 - / 213 / 215, 32768 x 8 - / 400 / 392.
+    // 8 81 / 70 / 92, 8192 x 8 126 / 115 / 110 (one line for all ranks: 8192 rows lose 4 us at rank 16 and gain 5 at 64). Backward, 8192 x 8 - / 101 / 104, 16384 x 64 - / 213 / 215, 32768 x 8 - / 400 / 392.
     // The narrowing products take 16 MT rows at a time, two or four times their rank at most.
     s.TP = backward ? (a.T >= 16384 && a.T >= 512 * (int64_t)a.n ? 64 : 32)
                     : a.T < 64 * (int64_t)a.n && a.T < 4096 ? 16 : a.T < 256 * (int64_t)a.n || a.T < 8192 ? 32 : 64;
