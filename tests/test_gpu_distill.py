@@ -342,3 +342,47 @@ def test_gradient_from_a_saved_sum_of_far_rows(T, V, kind):
         rel = (600 / tau + 60 / tau + 8) * 2.0**-22 + (V / 256 + 16) * 2.0**-24
         tol = rel * tau * (q + (np.abs(want - tau * q) > 0)) + torch.finfo(t).eps / 2 * np.abs(want) * 1.001 + (2.0**-25 if kind == "f16" else 2.0**-120)
         assert (np.abs(dz - want) <= tol).all(), (tau, (np.abs(dz - want) / tol).max(1)[:6])
+
+
+@pytest.mark.parametrize("T,V,kind", [(70000, 8, "bf16"), (65537, 33000, "f32")])
+def test_more_rows_than_a_launch_has_in_pieces(T, V, kind):
+    """The gradient from a saved log-sum-exp, and rows too long for a workgroup, take their rows from the grid's second dimension."""
+    z = torch.empty((T, V), dtype=TYPES[kind], device=DEV).normal_(std=2.0)
+    idx = torch.randint(0, V, (T, 3), dtype=torch.int32, device=DEV)
+    u, w, dloss = torch.randn((T, 3), device=DEV), torch.rand(T, device=DEV), torch.rand(T, device=DEV)
+    a, b = slice(0, T // 2), slice(T // 2, T)
+
+    def call(s):
+        loss, lse = moeq.moe_distill_forward(z[s], idx[s], u[s], temperature=2.0, weight=w[s])
+        return loss, lse, moeq.moe_distill_backward(z[s], idx[s], u[s], lse, dloss[s], temperature=2.0, weight=w[s])
+
+    for whole, first, last in zip(call(slice(0, T)), call(a), call(b)):
+        assert torch.equal(whole[a], first) and torch.equal(whole[b], last)
+    del z
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T,V", [(7, 500), (7, 70000)])
+def test_losses_alone(T, V):
+    """The C call without lse: rows without weight are not read."""
+    rng = rng_of("alone", T, V)
+    z = torch.from_numpy(rng.normal(size=(T, V))).float()
+    idx, u = teacher(rng, z, 9)
+    w = torch.rand(T)
+    w[2], z[2] = 0.0, float("nan")
+    z, idx, u, w = z.to(DEV), idx.to(DEV), u.to(DEV), w.to(DEV)
+    want, _ = moeq.moe_distill_forward(z, idx, u, temperature=2.0, weight=w)
+    B, loss = moeq.binding, torch.full((T,), float("nan"), device=DEV)
+    ws = torch.empty(B.lib().moe_distill_workspace_bytes(T, V, B.MOEQ_F32) + 16, dtype=torch.uint8, device=DEV).fill_(255)
+    assert B.lib().moe_distill_forward(z.data_ptr(), V, B.MOEQ_F32, T, V, idx.data_ptr(), u.data_ptr(), 9, 2.0, w.data_ptr(), loss.data_ptr(), None,
+                                       ws.data_ptr(), ws.numel(), B._stream(None)) == B.MOEQ_OK
+    torch.cuda.synchronize()
+    assert torch.equal(loss, want) and loss[2] == 0
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+def test_more_entries_of_the_teacher_than_columns(kind):
+    rng = rng_of("entries", kind)
+    z = torch.from_numpy(rng.normal(size=(6, 3))).to(TYPES[kind])
+    idx = torch.from_numpy(rng.integers(-1, 4, size=(6, 130)).astype(np.int32))
+    check_all(z, idx, torch.from_numpy(rng.normal(size=(6, 130))).float(), 1.0, None)
