@@ -405,3 +405,26 @@ def test_columns_shared_among_workgroups(kind, out, T, r, d_in, d_out):
     y2 = moeq.moe_adapters_forward(ad, s["x"], ids, base=s["base"], y=s["base"])
     again = moeq.moe_adapters_backward(ad, s["x"], ids, s["dy"], dx_base=s["dx_base"], dx=s["dx_base"])
     assert torch.equal(y, y2) and all(torch.equal(a, b) for a, b in zip(again, (dx, dA, dB)))
+
+
+def test_replays_of_a_graph_with_shared_columns():
+    """The gradient whose pieces come from shares joined in the workspace."""
+    rng = rng_of("graph of shares")
+    T, n, r, d = 200, 3, 24, 4096
+    m = make(rng, T, n, r, d, d, torch.bfloat16, torch.bfloat16)
+    g = {k: v.to(DEV) for k, v in m.items()}
+    ids = torch.from_numpy(ids_of(rng, T, n, "mixed")).to(DEV)
+    ad = moeq.Adapters(g["A"], g["B"], g["scale"])
+    step = lambda: [moeq.moe_adapters_forward(ad, g["x"], ids, base=g["base"]), *moeq.moe_adapters_backward(ad, g["x"], ids, g["dy"], dx_base=g["dx_base"])]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for how in ("mixed", "one", "none", "sorted"):
+        g["x"].normal_()
+        g["dy"].normal_()
+        ids.copy_(torch.from_numpy(ids_of(rng, T, n, how)).to(DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))

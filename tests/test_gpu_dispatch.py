@@ -326,3 +326,24 @@ def test_gradient_of_the_rows_alone(T, k, d, kind, dy_kind):
                                                  B._DTYPES[TYPES[dy_kind]], dy.data_ptr(), d, got.data_ptr(), d, None, B._stream(None)) == B.MOEQ_OK
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def test_replays_of_a_graph_with_scanned_counts():
+    rng = rng_of("graph of chunks")
+    P, E = 20 * 4096, 300
+    idx = torch.empty((P, 1), dtype=torch.int32, device=DEV)
+    fill = lambda n: idx.copy_(torch.from_numpy(np.sort(rng.integers(-1, E - 40 * n, size=(P, 1)), axis=0 if n == 2 else 1).astype(np.int32)))
+    step = lambda: (lambda s: [s.offsets, s.order, s.slot])(moeq.moe_sort_pairs(idx, E))
+    fill(0)
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = step()
+    for n in range(4):
+        fill(n)
+        g.replay()
+        torch.cuda.synchronize()
+        want = sorted_on_host(idx.cpu().numpy(), E)
+        assert all(np.array_equal(a.cpu().numpy(), w) for a, w in zip(held, want))
+        assert all(torch.equal(a, b) for a, b in zip(held, step()))
