@@ -279,7 +279,8 @@ moeq_status moe_unprepare_in(const void *stream_buf, int64_t rows, int64_t cols,
 /* ---- operators beside the layer ------------------------------------------------------------
  *
  * Sorting the (token, choice) pairs of a routing by expert and back, low-rank adapters of many requests (or of the experts)
- * beside a shared projection, and distillation from a teacher's top logits, with their gradients.
+ * beside a shared projection, and distillation from a teacher's top logits, with their gradients; the norms around a block with
+ * gate and residual, a dense gated feed-forward block, both with their gradients, tensors kept in 8 bits, products in 8-bit integers.
  *   - All pointers are device pointers; calls enqueue on `stream` and return, allocate nothing and can be captured into a
  *     graph. Elements are fp32, bf16 or fp16 (moeq_dtype); sums are held in fp32.
  *   - Matrices have contiguous rows and a row stride in elements, at any alignment of an element. An input whose rows are all
@@ -367,6 +368,83 @@ moeq_status moe_distill_loss_grad(const void *logits, int64_t stride, int32_t dt
                                   const int32_t *top_idx, const float *top_logits, int32_t top, float temperature,
                                   const float *weight_opt, float *loss, void *dlogits, int64_t dstride, void *ws,
                                   size_t ws_bytes, void *stream);
+
+/* The norms around a block, with its gate and residual. Of a row with the branch's output f, the residual r, gate g and weights w:
+ *     N(v; w) = v / sqrt(mean v^2 + eps) w,   y = residual_scale r + g N(f; w_after),   n = N(y; w_before)
+ * gate_opt [n_tokens], w_after_opt [d], w_before_opt [d] are fp32; without a gate it is one, without w_after f itself is added,
+ * without w_before there is no n. f, r (and y) and n are each of one and the same 16-bit type or fp32. n is the norm of y before its
+ * rounding. y may be r itself, n may be f itself. d <= 16384. */
+moeq_status moe_block_norms_forward(int32_t n_tokens, int32_t d, float residual_scale, float eps, int32_t f_dtype, const void *f,
+                                    int64_t f_stride, int32_t r_dtype, const void *r, int64_t r_stride, const float *gate_opt,
+                                    const float *w_after_opt, const float *w_before_opt, void *y, int64_t y_stride,
+                                    int32_t n_dtype, void *n, int64_t n_stride, void *stream);
+
+/* Its gradient from f, the y that the forward pass left, dy (of y, of r's type) and dn (of n): df in f's type, dr in r's, dgate
+ * [n_tokens], dw_after [d] and dw_before [d] in fp32 (sums over the rows; zeros where there are none). What belongs to a weight or
+ * gate that is not there is not touched, and y and dn are not read without w_before. The sums' order does not depend on timing.
+ * ws: moe_block_norms_workspace_bytes, needed where there is a weight. */
+size_t moe_block_norms_workspace_bytes(int32_t max_tokens, int32_t d);
+moeq_status moe_block_norms_backward(int32_t n_tokens, int32_t d, float residual_scale, float eps, int32_t f_dtype, const void *f,
+                                     int64_t f_stride, int32_t r_dtype, const void *y, int64_t y_stride, const void *dy,
+                                     int64_t dy_stride, int32_t n_dtype, const void *dn, int64_t dn_stride, const float *gate_opt,
+                                     const float *w_after_opt, const float *w_before_opt, void *df, int64_t df_stride, void *dr,
+                                     int64_t dr_stride, float *dgate, float *dw_after, float *dw_before, void *ws, size_t ws_bytes,
+                                     void *stream);
+
+/* Tensors kept in 8 bits. Blocks of 32 columns of a row share a power of two: e = floor(log2(largest |x|)) - 6, at least -126 (fp16:
+ * -24), code = rint(x 2^-e) in [-127, 127], value = code 2^e, which dtype holds exactly. codes [rows][d] int8, exps
+ * [rows][ceil(d / 32)] int8, contiguous. A block that holds a NaN or an infinity comes back as NaN (exponent -128). */
+moeq_status moe_pack8(const void *x, int64_t x_stride, int32_t dtype, int32_t rows, int32_t d, int8_t *codes, int8_t *exps,
+                      void *stream);
+moeq_status moe_unpack8(const int8_t *codes, const int8_t *exps, int32_t rows, int32_t d, int32_t dtype, void *x, int64_t x_stride,
+                        void *stream);
+
+/* A gated feed-forward block: w_in and w_gate [d_ff][d_model], w_out [d_model][d_ff] in dtype, contiguous device memory that the
+ * caller keeps. Widths <= 65536. */
+typedef struct {
+  int32_t d_model, d_ff, dtype;
+  const void *w_in, *w_gate, *w_out;
+} moeq_gated_ffn;
+
+/* How the products a = x w_in^T and b = x w_gate^T are kept for the backward pass: not; ab [2][n_tokens][d_ff] in dtype; as packed
+ * codes [2][n_tokens][d_ff] with ab_exps [2][n_tokens][ceil(d_ff / 32)] (moe_pack8's form). */
+#define MOEQ_KEEP_NONE 0
+#define MOEQ_KEEP_OWN 1
+#define MOEQ_KEEP_8 8
+
+/* Workspace of a call of up to max_tokens tokens; that of a backward pass says whether x comes packed, and how a and b were kept.
+ * 0 for an invalid description. Calls that share one must be ordered. */
+size_t moe_gated_ffn_workspace_bytes(const moeq_gated_ffn *ffn, int32_t max_tokens, int32_t backward, int32_t x_packed, int32_t keep);
+
+/* y = base + (silu(x w_in^T) * (x w_gate^T)) w_out^T, silu(a) = a / (1 + exp(-a)). base_opt NULL: zeros; base may be y itself; base and
+ * y are y_dtype: dtype or MOEQ_F32. Sums are held in fp32, the rows between the products are rounded to dtype (fp16: infinite past
+ * 65504). An infinity in an operand may come out as a NaN. */
+moeq_status moe_gated_ffn_forward(const moeq_gated_ffn *ffn, const void *x, int64_t x_stride, int32_t n_tokens, const void *base_opt,
+                                  int64_t base_stride, int32_t y_dtype, void *y, int64_t y_stride, int32_t keep, void *ab,
+                                  int8_t *ab_exps, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient: dx (dx_opt NULL: not wanted) and dw_in, dw_gate, dw_out (the weights' shapes, contiguous), all in dtype; base's is dy.
+ * x: rows in dtype, or x_codes and x_exps as moe_pack8 leaves them (x NULL). keep, ab, ab_exps: as the forward pass left them;
+ * MOEQ_KEEP_NONE computes a and b again. No rows: the weights' gradients are zeros. The sums' order does not depend on timing. */
+moeq_status moe_gated_ffn_backward(const moeq_gated_ffn *ffn, const void *x, int64_t x_stride, const int8_t *x_codes,
+                                   const int8_t *x_exps, int32_t n_tokens, const void *dy, int64_t dy_stride, int32_t keep,
+                                   const void *ab, const int8_t *ab_exps, void *dx_opt, int64_t dx_stride, void *dw_in, void *dw_gate,
+                                   void *dw_out, void *ws, size_t ws_bytes, void *stream);
+
+/* Rows in 8-bit integers with a scale each: scale = max |x| / 127 (at least 2^-126), code = rint(x / scale), the quotient in fp32; a
+ * row with a NaN or an infinity has scale NaN and codes 0. codes [rows][moe_q8_pitch(d)] int8, zeros behind column d (the pitch is d
+ * up to a multiple of 128), 16-byte aligned; scale [rows] fp32. d <= 65536. */
+int64_t moe_q8_pitch(int32_t d);
+moeq_status moe_quantize_rows(const void *x, int64_t x_stride, int32_t dtype, int32_t rows, int32_t d, int8_t *codes, float *scale,
+                              void *stream);
+
+/* y[t][n] = base[t][n] + x_scale[t] w_scale[n] sum over k of x[t][k] w[n][k], x [n_tokens] and w [n_out] rows of k codes in the form
+ * above (any int8, also -128; what lies behind column k has to be zero). The sums are exact. base_opt NULL: zeros; base may be y
+ * itself; both are dtype. ws: moe_matmul_q8_workspace_bytes (may be 0), 16-byte aligned. */
+size_t moe_matmul_q8_workspace_bytes(int32_t max_tokens, int32_t n_out, int32_t k);
+moeq_status moe_matmul_q8(const int8_t *x, const float *x_scale, int32_t n_tokens, const int8_t *w, const float *w_scale, int32_t n_out,
+                          int32_t k, const void *base_opt, int64_t base_stride, int32_t dtype, void *y, int64_t y_stride, void *ws,
+                          size_t ws_bytes, void *stream);
 
 /* Measurement aid, per layer. While `which` names a kernel, every moe_layer_forward call on THIS
  * layer records start_event just before and stop_event just after that kernel on the call's stream

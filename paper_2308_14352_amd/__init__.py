@@ -11,4 +11,6 @@ from .binding import (MOEQ_ACT_RELU, MOEQ_ACT_SWIGLU, MOEQ_BF16, MOEQ_F16, MOEQ_
                       moe_quantize_pack, moe_router_topk, moe_unpack_codes, moe_unprepare_out,
                       Adapters, PairSort, moe_adapters_backward, moe_adapters_forward, moe_combine_rows,
                       moe_combine_rows_backward, moe_distill_backward, moe_distill_forward, moe_distill_loss_grad,
-                      moe_gather_rows, moe_sort_pairs)
+                      moe_gather_rows, moe_sort_pairs, GatedFfn, Packed8, QuantRows, moe_block_norms_backward,
+                      moe_block_norms_forward, moe_gated_ffn_backward, moe_gated_ffn_forward, moe_matmul_q8, moe_pack8,
+                      moe_quantize_rows, moe_unpack8)

@@ -17,6 +17,7 @@ MOEQ_ACT_RELU, MOEQ_ACT_SWIGLU = 0, 1
 MOEQ_F32, MOEQ_BF16, MOEQ_F16 = 0, 1, 2
 MOEQ_OUT_CANONICAL, MOEQ_OUT_COLUMNS = 0, 1
 MOEQ_IN_CANONICAL, MOEQ_IN_STREAM = 0, 1
+MOEQ_KEEP_NONE, MOEQ_KEEP_OWN, MOEQ_KEEP_8 = 0, 1, 8
 
 
 class MoeqError(RuntimeError):
@@ -44,6 +45,11 @@ class moeq_layer_desc(C.Structure):
 class moeq_adapters(C.Structure):
     _fields_ = [("n_adapters", C.c_int32), ("rank", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32), ("dtype", C.c_int32),
                 ("a", C.c_void_p), ("b", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class moeq_gated_ffn(C.Structure):
+    _fields_ = [("d_model", C.c_int32), ("d_ff", C.c_int32), ("dtype", C.c_int32),
+                ("w_in", C.c_void_p), ("w_gate", C.c_void_p), ("w_out", C.c_void_p)]
 
 
 _lib = None
@@ -115,7 +121,20 @@ def lib():
             ("moe_distill_workspace_bytes", sz, [i32, i32, i32]),
             ("moe_distill_forward", C.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, vp, sz, vp]),
             ("moe_distill_backward", C.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, vp, i64, vp]),
-            ("moe_distill_loss_grad", C.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp, sz, vp])):
+            ("moe_distill_loss_grad", C.c_int, [vp, i64, i32, i32, i32, vp, vp, i32, f32, vp, vp, vp, i64, vp, sz, vp]),
+            ("moe_block_norms_forward", C.c_int, [i32, i32, f32, f32, i32, vp, i64, i32, vp, i64, vp, vp, vp, vp, i64, i32, vp, i64, vp]),
+            ("moe_block_norms_workspace_bytes", sz, [i32, i32]),
+            ("moe_block_norms_backward", C.c_int, [i32, i32, f32, f32, i32, vp, i64, i32, vp, i64, vp, i64, i32, vp, i64, vp, vp, vp, vp, i64,
+                                                   vp, i64, vp, vp, vp, vp, sz, vp]),
+            ("moe_pack8", C.c_int, [vp, i64, i32, i32, i32, vp, vp, vp]),
+            ("moe_unpack8", C.c_int, [vp, vp, i32, i32, i32, vp, i64, vp]),
+            ("moe_gated_ffn_workspace_bytes", sz, [vp, i32, i32, i32, i32]),
+            ("moe_gated_ffn_forward", C.c_int, [vp, vp, i64, i32, vp, i64, i32, vp, i64, i32, vp, vp, vp, sz, vp]),
+            ("moe_gated_ffn_backward", C.c_int, [vp, vp, i64, vp, vp, i32, vp, i64, i32, vp, vp, vp, i64, vp, vp, vp, vp, sz, vp]),
+            ("moe_q8_pitch", i64, [i32]),
+            ("moe_quantize_rows", C.c_int, [vp, i64, i32, i32, i32, vp, vp, vp]),
+            ("moe_matmul_q8_workspace_bytes", sz, [i32, i32, i32]),
+            ("moe_matmul_q8", C.c_int, [vp, vp, i32, vp, vp, i32, i32, vp, i64, i32, vp, i64, vp, sz, vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = res, args
     _lib = L
@@ -128,7 +147,10 @@ EXPORTS = ["moe_status_str", "moe_layer_profile_kernel", "moe_layer_table_bytes"
            "moe_unprepare_out", "moe_prepare_in", "moe_unprepare_in", "moe_stream_bytes",
            "moe_sort_bytes", "moe_sort_pairs", "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward",
            "moe_adapters_workspace_bytes", "moe_adapters_forward", "moe_adapters_backward",
-           "moe_distill_workspace_bytes", "moe_distill_forward", "moe_distill_backward", "moe_distill_loss_grad"]
+           "moe_distill_workspace_bytes", "moe_distill_forward", "moe_distill_backward", "moe_distill_loss_grad",
+           "moe_block_norms_forward", "moe_block_norms_workspace_bytes", "moe_block_norms_backward", "moe_pack8", "moe_unpack8",
+           "moe_gated_ffn_workspace_bytes", "moe_gated_ffn_forward", "moe_gated_ffn_backward", "moe_q8_pitch", "moe_quantize_rows",
+           "moe_matmul_q8_workspace_bytes", "moe_matmul_q8"]
 
 
 def status_str(st):
@@ -419,7 +441,10 @@ def _load():
     from . import _calls
     names = ("moe_sort_bytes", "moe_sort_pairs", "moe_gather_rows", "moe_combine_rows", "moe_combine_rows_backward",
              "moe_adapters_workspace_bytes", "moe_adapters_forward", "moe_adapters_backward", "moe_distill_workspace_bytes",
-             "moe_distill_forward", "moe_distill_backward", "moe_distill_loss_grad")
+             "moe_distill_forward", "moe_distill_backward", "moe_distill_loss_grad", "moe_block_norms_forward",
+             "moe_block_norms_workspace_bytes", "moe_block_norms_backward", "moe_pack8", "moe_unpack8", "moe_gated_ffn_workspace_bytes",
+             "moe_gated_ffn_forward", "moe_gated_ffn_backward", "moe_q8_pitch", "moe_quantize_rows", "moe_matmul_q8_workspace_bytes",
+             "moe_matmul_q8")
     _calls.bind(MoeqError, _stream_on, *[C.cast(getattr(L, n), C.c_void_p).value for n in names])
     _native = _calls
     return _calls
@@ -546,3 +571,159 @@ def moe_distill_loss_grad(logits, top_idx, top_logits, temperature=1.0, weight=N
         with torch.cuda.stream(stream):
             return moe_distill_loss_grad(logits, top_idx, top_logits, temperature, weight, dlogits)
     return (_native or _load()).distill_loss_grad(logits, top_idx, top_logits, temperature, weight, dlogits)
+
+
+def moe_block_norms_forward(f, r, gate=None, w_after=None, w_before=None, residual_scale=1.0, eps=1e-5, dtype=None, y=None, n=None,
+                            stream=None):
+    """The norms around a block: y = residual_scale r + gate N(f; w_after) and n = N(y; w_before) with N(v; w) = v / sqrt(mean v^2 + eps) w
+    over the rows of f (the block's output) and r (the residual), [T][d]: (y in r's dtype, n in `dtype`, r's by default). gate [T],
+    w_after [d] and w_before [d] are fp32; without w_after f itself is added, without w_before n is None. y may be r, n may be f."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_block_norms_forward(f, r, gate, w_after, w_before, residual_scale, eps, dtype, y, n)
+    return (_native or _load()).block_norms_forward(f, r, gate, w_after, w_before, residual_scale, eps, dtype, y, n)
+
+
+def moe_block_norms_backward(f, y, dy, dn=None, gate=None, w_after=None, w_before=None, residual_scale=1.0, eps=1e-5, df=None, dr=None,
+                             stream=None):
+    """The gradient of moe_block_norms_forward from f, the forward's y and the gradients of y and n (y and dn may be None without
+    w_before): (df, dr, dgate [T], dw_after [d], dw_before [d]), the last three fp32 and None where their input is."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_block_norms_backward(f, y, dy, dn, gate, w_after, w_before, residual_scale, eps, df, dr)
+    return (_native or _load()).block_norms_backward(f, y, dy, dn, gate, w_after, w_before, residual_scale, eps, df, dr)
+
+
+class Packed8:
+    """A tensor kept in 8 bits: codes int8 [..., d] and exps int8 [..., ceil(d / 32)], one power of two for 32 columns of a row;
+    dtype: of the tensor it was."""
+
+    __slots__ = ("codes", "exps", "dtype")
+
+    def __init__(self, codes, exps, dtype):
+        self.codes, self.exps, self.dtype = codes, exps, dtype
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+    def nbytes(self):
+        return self.codes.numel() + self.exps.numel()
+
+
+def moe_pack8(x, packed=None, stream=None):
+    """x [T][d] -> Packed8, 33/64 of the bytes of 16-bit elements. A block with a NaN or an infinity comes back as NaN. packed: a
+    Packed8 of this shape and dtype that is written again."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_pack8(x, packed)
+    _need(packed is None or packed.dtype is x.dtype, "moe_pack8")
+    codes, exps = (_native or _load()).pack8(x, packed and packed.codes, packed and packed.exps)
+    return packed or Packed8(codes, exps, x.dtype)
+
+
+def moe_unpack8(packed, x=None, stream=None):
+    """The tensor in its dtype: the values that the codes stand for, exactly. x: rows [T][d] to write to."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_unpack8(packed, x)
+    return (_native or _load()).unpack8(packed.codes, packed.exps, packed.dtype, x)
+
+
+class GatedFfn:
+    """The weights of a gated feed-forward block, w_in and w_gate [d_ff][d_model] and w_out [d_model][d_ff] of one dtype: device
+    tensors that are borrowed, not copied, so that an update in place is seen by the next call."""
+
+    def __init__(self, w_in, w_gate, w_out):
+        what = "GatedFfn"
+        _need(all(t.dim() == 2 and t.dtype in _DTYPES and t.dtype is w_in.dtype for t in (w_in, w_gate, w_out)), what)
+        f, d = w_in.shape
+        _need(tuple(w_gate.shape) == (f, d) and tuple(w_out.shape) == (d, f) and f > 0 and d > 0, what)
+        _need(all(t.is_cuda and t.is_contiguous() and t.device == w_in.device for t in (w_in, w_gate, w_out)), what)
+        self.w_in, self.w_gate, self.w_out = w_in, w_gate, w_out
+        self.d_model, self.d_ff, self.dtype = d, f, w_in.dtype
+        self._desc = moeq_gated_ffn(d, f, _DTYPES[w_in.dtype], w_in.data_ptr(), w_gate.data_ptr(), w_out.data_ptr())
+        self.handle = C.addressof(self._desc)
+
+    def workspace_bytes(self, max_tokens, backward=False, x_packed=False, keep=None):
+        return int(lib().moe_gated_ffn_workspace_bytes(self.handle, max_tokens, int(backward), int(x_packed), _keep(keep)))
+
+    def workspace(self, max_tokens, backward=False, x_packed=False, keep=None):
+        """A workspace for calls of up to max_tokens rows, for callers who pass one (`ws`) and order the calls that share it."""
+        return torch.empty(max(self.workspace_bytes(max_tokens, backward, x_packed, keep), 16), dtype=torch.uint8, device=self.w_in.device)
+
+
+def _keep(keep):
+    _need(keep is None or keep == "own" or keep == 8, "keep: None, \"own\" or 8")
+    return MOEQ_KEEP_NONE if keep is None else MOEQ_KEEP_OWN if keep == "own" else MOEQ_KEEP_8
+
+
+def moe_gated_ffn_forward(ffn, x, keep=None, base=None, dtype=None, y=None, ws=None, stream=None):
+    """y = base + (silu(x w_in^T) * (x w_gate^T)) w_out^T, x [T][d_model] in the weights' dtype. base: [T][d_model] or None (zeros), may
+    be y itself; y in the weights' dtype or fp32 (`dtype`; default: the base's, or the weights'). keep: what the backward pass finds of
+    the products a = x w_in^T and b = x w_gate^T: None (y alone is returned), "own" ((y, ab [2][T][d_ff])) or 8 ((y, ab as Packed8))."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_gated_ffn_forward(ffn, x, keep, base, dtype, y, ws)
+    y, ab, exps = (_native or _load()).gated_ffn_forward(ffn.handle, x, base, dtype, y, _keep(keep), ws, ffn.w_in)
+    if keep is None:
+        return y
+    return y, ab if keep == "own" else Packed8(ab, exps, x.dtype)
+
+
+def moe_gated_ffn_backward(ffn, x, dy, ab=None, dx=None, want_dx=True, ws=None, stream=None):
+    """The gradient of moe_gated_ffn_forward: (dx [T][d_model], dw_in, dw_gate, dw_out) in the weights' dtype. x: the forward's, or a
+    Packed8 of it. ab: what the forward pass kept (a tensor or a Packed8), None: computed again."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_gated_ffn_backward(ffn, x, dy, ab, dx, want_dx, ws)
+    x8, ab8 = isinstance(x, Packed8), isinstance(ab, Packed8)
+    _need((not x8 or x.dtype is ffn.dtype) and (not ab8 or ab.dtype is ffn.dtype), "moe_gated_ffn_backward")
+    keep = MOEQ_KEEP_NONE if ab is None else MOEQ_KEEP_8 if ab8 else MOEQ_KEEP_OWN
+    return (_native or _load()).gated_ffn_backward(ffn.handle, x.codes if x8 else x, x.exps if x8 else None, dy, keep, ab.codes if ab8 else ab,
+                                                   ab.exps if ab8 else None, dx, bool(want_dx), ws, ffn.w_in)
+
+
+class QuantRows:
+    """Rows of k codes int8 with a scale each (value = code * scale): codes [n][pitch], pitch = k up to a multiple of 128 with zeros
+    behind column k, scale [n] fp32. Codes [n][k] of another pitch are copied into such rows once, here; with the right one they are
+    borrowed."""
+
+    def __init__(self, codes, scale, k=None):
+        what = "QuantRows"
+        _need(codes.dim() == 2 and codes.dtype is torch.int8 and scale.dim() == 1 and scale.dtype is torch.float32, what)
+        _need(codes.is_cuda and scale.is_cuda and scale.is_contiguous() and scale.device == codes.device, what)
+        n, width = codes.shape
+        k = width if k is None else k
+        pitch = (k + 127) // 128 * 128
+        _need(scale.shape[0] == n and k > 0 and width in (k, pitch), what)
+        if width != pitch or not codes.is_contiguous() or codes.data_ptr() % 16:
+            wide = torch.zeros((n, pitch), dtype=torch.int8, device=codes.device)
+            wide[:, :k] = codes[:, :k]
+            codes = wide
+        self.codes, self.scale, self.k = codes, scale, k
+
+    @classmethod
+    def _of(cls, codes, scale, k):
+        rows = cls.__new__(cls)
+        rows.codes, rows.scale, rows.k = codes, scale, k
+        return rows
+
+
+def moe_quantize_rows(x, stream=None):
+    """x [T][k] -> QuantRows: scale = max |x[t]| / 127, code = rint(x / scale). A row with a NaN or an infinity has the scale NaN."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_quantize_rows(x)
+    codes, scale = (_native or _load()).quantize_rows(x)
+    return QuantRows._of(codes, scale, x.shape[1])
+
+
+def moe_matmul_q8(rows, weights, base=None, dtype=None, y=None, stream=None):
+    """y[t][n] = base[t][n] + the product of row t of `rows` and row n of `weights` (both QuantRows of the same k): whole numbers summed
+    exactly, times both scales. base: [T][n] or None (zeros), may be y itself; y in `dtype` (default: the base's, or fp32)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return moe_matmul_q8(rows, weights, base, dtype, y)
+    _need(rows.k == weights.k, "moe_matmul_q8")
+    return (_native or _load()).matmul_q8(rows.k, rows.codes, rows.scale, weights.codes, weights.scale, base, dtype, y)

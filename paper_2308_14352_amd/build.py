@@ -10,7 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoeq.so")
 CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["api.cpp", "router.hip", "ffn_decode.hip", "decode_fused.hip", "decode_small.hip", "decode_stream.hip", "decode_batch.hip", "prefill.hip", "group_gemm.hip", "quant.hip",
-           "operators.cpp", "dispatch.hip", "adapters.hip", "distill.hip"]
+           "operators.cpp", "dispatch.hip", "adapters.hip", "distill.hip",
+           "block_norms.hip", "rows8.hip", "gated_ffn.hip", "gated_ffn_f16.hip", "gated_ffn_f32.hip", "matmul_q8.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          # packed-fp32 instructions are kept off on this target: some of their forms have given wrong results
@@ -39,7 +40,8 @@ def stale():
         return True
     t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = sources() + [os.path.join(CSRC, "calls.cpp"), os.path.join(CSRC, "moeq_internal.h"), os.path.join(CSRC, "decode_core.h"),
-                        os.path.join(CSRC, "small_split.h"), os.path.join(CSRC, "operators.h"), os.path.join(CSRC, "sort_core.h"), os.path.join(ROOT, "include", "moeq.h")]
+                        os.path.join(CSRC, "small_split.h"), os.path.join(CSRC, "operators.h"), os.path.join(CSRC, "sort_core.h"),
+                        os.path.join(CSRC, "tiles.h"), os.path.join(CSRC, "ffn_core.h"), os.path.join(ROOT, "include", "moeq.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

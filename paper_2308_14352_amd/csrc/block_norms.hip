@@ -1,0 +1,306 @@
+// The norms around a block, with its gate and its residual. Of a row with branch f and residual r, gate g and weights w:
+//   N(v; w) = v / sqrt(mean v^2 + eps) w,   y = alpha r + g N(f; w_after),   n = N(y; w_before)
+// (without w_after: g f; without w_before: no n). Backward, with a unit row u(v) = v / sqrt(mean v^2 + eps), b = 1 / sqrt(mean y^2 + eps):
+//   dY = dy + b (dn w_before - u(y) mean(dn w_before u(y))),  dr = alpha dY,  dgate = S = dY . N(f; w_after),
+//   df = (dY g w_after - u(f) g S / d) / sqrt(mean f^2 + eps),  dw_before = sum over rows of dn u(y),  dw_after = of dY g u(f).
+//
+// Memory bounds both: a row is read once into registers and the sums over it (three together, then S) are joined between the wavefronts
+// that share it. n is the norm of y before its rounding; the backward pass takes the y that the forward pass left. The weights' gradients
+// are sums over rows: a stream of rows keeps its columns' sums in registers, and a second kernel adds the streams in their order, so that
+// the same call gives the same bits. All in fp32.
+#include <algorithm>
+
+#include "operators.h"
+
+namespace moeq {
+namespace {
+
+constexpr int VE = 8;
+
+template <typename T>
+__device__ __forceinline__ void load_part(float (&v)[VE], const T* row, int c, int d) {
+  if (c + VE <= d) {
+    load_n(v, row + c);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = c + i < d ? (float)row[c + i] : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* row, const float (&v)[VE], int c, int d) {
+  if (c + VE <= d) {
+    stream_n(row + c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VE; ++i)
+      if (c + i < d) row[c + i] = (T)v[i];
+  }
+}
+
+// Sums over a row's threads: of a wavefront, or of W by LDS (one barrier: two sets of places take turns).
+template <int W>
+struct RowSum {
+  float (*sh)[W][4];
+  int turn = 0;
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&s)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+    if constexpr (W > 1) {
+      if (threadIdx.x % 64 == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sh[turn][threadIdx.x / 64][i] = s[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) s[i] += sh[turn][w][i];
+      }
+      turn ^= 1;
+    }
+  }
+};
+
+template <int W> constexpr int kThreadsOf = W == 1 ? 256 : 64 * W;
+template <int W> constexpr int kRowsOf = W == 1 ? 4 : 1;
+
+template <typename F, typename R, typename N, int W, int NV>
+__global__ __launch_bounds__(kThreadsOf<W>) void k_norms_forward(NormsArgs a) {
+  __shared__ float sh[2][W][4];
+  RowSum<W> sum{sh};
+  const int at = W == 1 ? threadIdx.x % 64 : threadIdx.x, d = a.d;
+  const float by_d = 1.f / (float)d;
+  for (int64_t row = (int64_t)blockIdx.x * kRowsOf<W> + (W == 1 ? threadIdx.x / 64 : 0); row < a.T; row += (int64_t)gridDim.x * kRowsOf<W>) {
+    const F* f = (const F*)a.f + row * a.f_stride;
+    const R* r = (const R*)a.r + row * a.r_stride;
+    float v[NV][VE], y[NV][VE];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_part(v[i], f, (at + i * 64 * W) * VE, d);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_part(y[i], r, (at + i * 64 * W) * VE, d);
+    const float g = a.gate ? a.gate[row] : 1.f;
+    float by = 1.f;
+    if (a.w_after) {
+      float s[1] = {0.f};
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < VE; ++j) s[0] += v[i][j] * v[i][j];
+      sum(s);
+      by = 1.f / sqrtf(s[0] * by_d + a.eps);
+    }
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (at + i * 64 * W) * VE;
+      if (a.w_after) {
+        float w[VE];
+        load_part(w, a.w_after, c, d);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) v[i][j] = v[i][j] * by * w[j];
+      }
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        y[i][j] = a.alpha * y[i][j] + (a.gate ? v[i][j] * g : v[i][j]);
+        s[0] += y[i][j] * y[i][j];
+      }
+      store_part((R*)a.out_y + row * a.out_y_stride, y[i], c, d);
+    }
+    if (!a.w_before) continue;
+    sum(s);
+    by = 1.f / sqrtf(s[0] * by_d + a.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (at + i * 64 * W) * VE;
+      float w[VE];
+      load_part(w, a.w_before, c, d);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) w[j] *= y[i][j] * by;
+      store_part((N*)a.out_n + row * a.out_n_stride, w, c, d);
+    }
+  }
+}
+
+// A stream of rows: stream, stream + streams, ...
+template <typename F, typename R, typename N, int W, int NV>
+__global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, int streams) {
+  __shared__ float sh[2][W][4];
+  RowSum<W> sum{sh};
+  const int at = W == 1 ? threadIdx.x % 64 : threadIdx.x, d = a.d;
+  const int stream = blockIdx.x * kRowsOf<W> + (W == 1 ? threadIdx.x / 64 : 0);
+  if (stream >= streams) return;
+  const float by_d = 1.f / (float)d;
+  float sum_after[NV][VE] = {}, sum_before[NV][VE] = {};
+  for (int64_t row = stream; row < a.T; row += streams) {
+    float f[NV][VE], y[NV][VE], dn[NV][VE], dy[NV][VE];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (at + i * 64 * W) * VE;
+      load_part(f[i], (const F*)a.f + row * a.f_stride, c, d);
+      load_part(dy[i], (const R*)a.dy + row * a.dy_stride, c, d);
+      if (a.w_before) {
+        load_part(y[i], (const R*)a.y + row * a.y_stride, c, d);
+        load_part(dn[i], (const N*)a.dn + row * a.dn_stride, c, d);
+      }
+    }
+    const float g = a.gate ? a.gate[row] : 1.f;
+    float s[3] = {0.f, 0.f, 0.f};      // y . y, (dn w) . y, f . f
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (a.w_before) {
+        float w[VE];
+        load_part(w, a.w_before, (at + i * 64 * W) * VE, d);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) s[0] += y[i][j] * y[i][j], s[1] += dn[i][j] * w[j] * y[i][j];
+      }
+#pragma unroll
+      for (int j = 0; j < VE; ++j) s[2] += f[i][j] * f[i][j];
+    }
+    sum(s);
+    const float by = 1.f / sqrtf(s[0] * by_d + a.eps), mean = s[1] * by * by_d;      // of y; of dn w u(y)
+    const float bf = a.w_after ? 1.f / sqrtf(s[2] * by_d + a.eps) : 1.f;
+    float t[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (at + i * 64 * W) * VE;
+      if (a.w_before) {
+        float w[VE];
+        load_part(w, a.w_before, c, d);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+          const float u = y[i][j] * by;
+          sum_before[i][j] += dn[i][j] * u;
+          dy[i][j] += by * (dn[i][j] * w[j] - u * mean);
+        }
+      }
+      float w[VE];
+      if (a.w_after) load_part(w, a.w_after, c, d);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        t[0] += dy[i][j] * (a.w_after ? f[i][j] * bf * w[j] : f[i][j]);
+        y[i][j] = a.alpha * dy[i][j];
+      }
+      store_part((R*)a.out_y + row * a.out_y_stride, y[i], c, d);
+    }
+    if (a.gate || a.w_after) sum(t);
+    if (a.gate && at == 0) a.dgate[row] = t[0];
+    const float back = g * t[0] * by_d;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (at + i * 64 * W) * VE;
+      float w[VE];
+      if (a.w_after) load_part(w, a.w_after, c, d);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        float v = a.gate ? dy[i][j] * g : dy[i][j];
+        if (a.w_after) {
+          const float u = f[i][j] * bf;
+          sum_after[i][j] += v * u;
+          v = bf * (v * w[j] - u * back);
+        }
+        w[j] = v;
+      }
+      store_part((F*)a.out_n + row * a.out_n_stride, w, c, d);
+    }
+  }
+  float* part = a.ws + (int64_t)stream * 2 * d;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (at + i * 64 * W) * VE;
+#pragma unroll
+    for (int j = 0; j < VE; ++j)
+      if (c + j < d) {
+        if (a.w_after) part[c + j] = sum_after[i][j];
+        if (a.w_before) part[d + c + j] = sum_before[i][j];
+      }
+  }
+}
+
+// The weights' gradients from the streams': 64 columns a workgroup, 16 shares of the streams.
+__global__ __launch_bounds__(1024) void k_norms_join(NormsArgs a, int streams) {
+  __shared__ float sh[16][64];
+  float* out = blockIdx.y ? a.dw_before : a.dw_after;
+  if (!out) return;
+  const int c = blockIdx.x * 64 + threadIdx.x % 64, share = threadIdx.x / 64;
+  float s = 0.f;
+  if (c < a.d)
+    for (int i = share; i < streams; i += 16) s += a.ws[((int64_t)i * 2 + blockIdx.y) * a.d + c];
+  sh[share][threadIdx.x % 64] = s;
+  __syncthreads();
+  if (share || c >= a.d) return;
+  for (int i = 1; i < 16; ++i) s += sh[i][threadIdx.x];
+  out[c] = s;
+}
+
+// Streams of a backward call: enough to fill the card, few enough that their sums are little beside the rows.
+int streams_of(int32_t T, int32_t d) { return std::min(T, d <= 1024 ? 2048 : 512); }
+
+// Wavefronts and vectors of a row.
+template <typename F>
+hipError_t by_width(int32_t d, F&& f) {
+  using std::integral_constant;
+  auto go = [&](auto w, auto nv) { return f(w, nv); };
+  if (d <= 512) return go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+  if (d <= 1024) return go(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  if (d <= 2048) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+  if (d <= 4096) return go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  if (d <= 8192) return go(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+  return go(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+}
+// The types: each the call's 16-bit one, or fp32.
+template <typename F>
+hipError_t by_types(const NormsArgs& a, F&& f) {
+  const int32_t h = a.f_dtype != MOEQ_F32 ? a.f_dtype : a.r_dtype != MOEQ_F32 ? a.r_dtype : a.n_dtype;
+  return with_type(h, [&](auto t) {
+    using H = decltype(t);
+    if constexpr (std::is_same<H, float>::value) {
+      return f(0.f, 0.f, 0.f);
+    } else {
+      const int which = (a.f_dtype == MOEQ_F32) * 4 + (a.r_dtype == MOEQ_F32) * 2 + (a.n_dtype == MOEQ_F32);
+      switch (which) {
+        case 0: return f(t, t, t);
+        case 1: return f(t, t, 0.f);
+        case 2: return f(t, 0.f, t);
+        case 3: return f(t, 0.f, 0.f);
+        case 4: return f(0.f, t, t);
+        case 5: return f(0.f, t, 0.f);
+        default: return f(0.f, 0.f, t);
+      }
+    }
+  });
+}
+
+}  // namespace
+
+size_t norms_ws_bytes(int32_t T, int32_t d) { return (size_t)streams_of(T, d) * 2 * d * 4; }
+
+hipError_t launch_norms_forward(const NormsArgs& a, hipStream_t st) {
+  return by_types(a, [&](auto f, auto r, auto n) {
+    return by_width(a.d, [&](auto w, auto nv) {
+      constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
+      const int64_t groups = ((int64_t)a.T + kRowsOf<W> - 1) / kRowsOf<W>;
+      k_norms_forward<decltype(f), decltype(r), decltype(n), W, NV><<<(uint32_t)std::min<int64_t>(groups, 1 << 20), kThreadsOf<W>, 0, st>>>(a);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t launch_norms_backward(const NormsArgs& a, hipStream_t st) {
+  const int streams = streams_of(a.T, a.d);
+  if (a.T > 0) {
+    const hipError_t e = by_types(a, [&](auto f, auto r, auto n) {
+      return by_width(a.d, [&](auto w, auto nv) {
+        constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
+        k_norms_backward<decltype(f), decltype(r), decltype(n), W, NV><<<(streams + kRowsOf<W> - 1) / kRowsOf<W>, kThreadsOf<W>, 0, st>>>(a, streams);
+        return hipGetLastError();
+      });
+    });
+    if (e != hipSuccess) return e;
+  }
+  if (!a.dw_after && !a.dw_before) return hipSuccess;
+  k_norms_join<<<dim3((a.d + 63) / 64, 2), 1024, 0, st>>>(a, streams);
+  return hipGetLastError();
+}
+
+}  // namespace moeq

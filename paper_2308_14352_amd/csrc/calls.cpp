@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <initializer_list>
+#include <vector>
 
 #include "moeq.h"
 
@@ -29,6 +30,18 @@ struct Entry {
   decltype(&moe_distill_forward) distill_forward;
   decltype(&moe_distill_backward) distill_backward;
   decltype(&moe_distill_loss_grad) distill_loss_grad;
+  decltype(&moe_block_norms_forward) block_norms_forward;
+  decltype(&moe_block_norms_workspace_bytes) block_norms_workspace_bytes;
+  decltype(&moe_block_norms_backward) block_norms_backward;
+  decltype(&moe_pack8) pack8;
+  decltype(&moe_unpack8) unpack8;
+  decltype(&moe_gated_ffn_workspace_bytes) gated_ffn_workspace_bytes;
+  decltype(&moe_gated_ffn_forward) gated_ffn_forward;
+  decltype(&moe_gated_ffn_backward) gated_ffn_backward;
+  decltype(&moe_q8_pitch) q8_pitch;
+  decltype(&moe_quantize_rows) quantize_rows;
+  decltype(&moe_matmul_q8_workspace_bytes) matmul_q8_workspace_bytes;
+  decltype(&moe_matmul_q8) matmul_q8;
 } lib;
 PyObject* error_class = nullptr;      // binding.MoeqError(status, what)
 PyObject* current_stream = nullptr;   // index of a device -> the handle of torch's current stream there; raises MoeqError if another is current
@@ -315,6 +328,189 @@ CALL(distill_loss_grad, 6) {
   return give_tuple(give(buf.narrow(0, 0, t.T)), a[5] == Py_None ? give(dz) : again(a[5]));
 }
 
+inline float real(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw python_error();
+  return (float)v;
+}
+inline at::ScalarType type_or(PyObject* o, at::ScalarType otherwise) {
+  need(o == Py_None || THPDtype_Check(o));
+  return o == Py_None ? otherwise : ((THPDtype*)o)->scalar_type;
+}
+inline const float* vector(const Tensor* t, int64_t n) {      // fp32 [n], or none
+  if (t) plain(*t, {n}, at::kFloat);
+  return data<const float>(t);
+}
+// What a call writes for itself between its kernels, from the allocator on the stream of the call; the smallest for calls that need none.
+inline Tensor scratch(size_t bytes, const Tensor& like) { return empty({(int64_t)std::max<size_t>(bytes, 16)}, at::kByte, like); }
+
+// f, r, gate, w_after, w_before (each or None), residual_scale, eps, dtype of n or None, y or None, n or None -> y, n or None
+CALL(block_norms_forward, 10) {
+  const Tensor &f = tensor(a[0]), &r = tensor(a[1]), *gate = tensor_or_none(a[2]), *after = tensor_or_none(a[3]), *before = tensor_or_none(a[4]);
+  need(f.dim() == 2 && (before || a[9] == Py_None));
+  const int64_t T = f.size(0), d = f.size(1), fs = matrix(f, T, d), rs = matrix(r, T, d);
+  const at::ScalarType type = type_or(a[7], a[9] != Py_None ? tensor(a[9]).scalar_type() : r.scalar_type());
+  const Tensor y = a[8] == Py_None ? empty({T, d}, r.scalar_type(), f) : tensor(a[8]);
+  const Tensor n = a[9] != Py_None ? tensor(a[9]) : before ? empty({T, d}, type, f) : Tensor();
+  need(y.scalar_type() == r.scalar_type() && (!n.defined() || n.scalar_type() == type));
+  const float scale = real(a[5]), eps = real(a[6]), *g = vector(gate, T), *wa = vector(after, d), *wb = vector(before, d);
+  void* stream = stream_of(f, {&r, gate, after, before, &y, &n});
+  run([&] {
+    return lib.block_norms_forward(size32(T), size32(d), scale, eps, type_of(f.scalar_type()), data(f), fs, type_of(r.scalar_type()), data(r), rs, g, wa, wb, data(y), matrix(y, T, d), type_of(type), n.defined() ? data(n) : nullptr, n.defined() ? matrix(n, T, d) : 0, stream);
+  });
+  return give_tuple(a[8] == Py_None ? give(y) : again(a[8]), a[9] == Py_None && before ? give(n) : again(a[9]));
+}
+
+// f, y or None, dy, dn or None, gate, w_after, w_before (each or None), residual_scale, eps, df or None, dr or None -> df, dr, dgate, dw_after, dw_before (each of the last or None)
+CALL(block_norms_backward, 11) {
+  const Tensor &f = tensor(a[0]), *y = tensor_or_none(a[1]), &dy = tensor(a[2]), *dn = tensor_or_none(a[3]);
+  const Tensor *gate = tensor_or_none(a[4]), *after = tensor_or_none(a[5]), *before = tensor_or_none(a[6]);
+  need(f.dim() == 2 && (!before || (y && dn && y->scalar_type() == dy.scalar_type())));
+  const int64_t T = f.size(0), d = f.size(1), fs = matrix(f, T, d), ds = matrix(dy, T, d);
+  if (!before) y = dn = nullptr;      // (not read)
+  const Tensor df = a[9] == Py_None ? empty({T, d}, f.scalar_type(), f) : tensor(a[9]), dr = a[10] == Py_None ? empty({T, d}, dy.scalar_type(), f) : tensor(a[10]);
+  need(df.scalar_type() == f.scalar_type() && dr.scalar_type() == dy.scalar_type());
+  const Tensor dgate = gate ? empty({T}, at::kFloat, f) : Tensor(), da = after ? empty({d}, at::kFloat, f) : Tensor(), db = before ? empty({d}, at::kFloat, f) : Tensor();
+  const size_t bytes = after || before ? lib.block_norms_workspace_bytes(size32(T), size32(d)) : 0;
+  const Tensor ws = scratch(bytes, f);
+  const int64_t ys = y ? matrix(*y, T, d) : 0, ns = dn ? matrix(*dn, T, d) : 0;
+  const float scale = real(a[7]), eps = real(a[8]), *g = vector(gate, T), *wa = vector(after, d), *wb = vector(before, d);
+  const auto at = [](const Tensor& t) { return t.defined() ? (float*)t.data_ptr() : nullptr; };
+  void* stream = stream_of(f, {y, &dy, dn, gate, after, before, &df, &dr});
+  run([&] {
+    return lib.block_norms_backward(size32(T), size32(d), scale, eps, type_of(f.scalar_type()), data(f), fs, type_of(dy.scalar_type()), data<const void>(y), ys, data(dy), ds,
+                                    dn ? type_of(dn->scalar_type()) : type_of(dy.scalar_type()), data<const void>(dn), ns, g, wa, wb, data(df), matrix(df, T, d), data(dr), matrix(dr, T, d),
+                                    at(dgate), at(da), at(db), data(ws), ws.numel(), stream);
+  });
+  const auto some = [](const Tensor& t) { return t.defined() ? give(t) : again(Py_None); };
+  return give_tuple(a[9] == Py_None ? give(df) : again(a[9]), a[10] == Py_None ? give(dr) : again(a[10]), some(dgate), some(da), some(db));
+}
+
+inline int64_t pack_blocks(int64_t d) { return (d + 31) / 32; }
+
+// x, codes or None, exps or None -> codes, exps
+CALL(pack8, 3) {
+  const Tensor& x = tensor(a[0]);
+  need(x.dim() == 2 && (a[1] == Py_None) == (a[2] == Py_None));
+  const int64_t T = x.size(0), d = x.size(1), xs = matrix(x, T, d);
+  const Tensor codes = a[1] == Py_None ? empty({T, d}, at::kChar, x) : tensor(a[1]), exps = a[2] == Py_None ? empty({T, pack_blocks(d)}, at::kChar, x) : tensor(a[2]);
+  plain(codes, {T, d}, at::kChar);
+  plain(exps, {T, pack_blocks(d)}, at::kChar);
+  void* stream = stream_of(x, {&codes, &exps});
+  run([&] { return lib.pack8(data(x), xs, type_of(x.scalar_type()), size32(T), size32(d), (int8_t*)data(codes), (int8_t*)data(exps), stream); });
+  return give_tuple(a[1] == Py_None ? give(codes) : again(a[1]), a[2] == Py_None ? give(exps) : again(a[2]));
+}
+
+// codes [..., d], exps [..., blocks], dtype, x or None -> x
+CALL(unpack8, 4) {
+  const Tensor &codes = tensor(a[0]), &exps = tensor(a[1]);
+  need(codes.dim() >= 1 && THPDtype_Check(a[2]));
+  const int64_t d = codes.size(-1), T = d > 0 ? codes.numel() / d : 0;
+  plain(codes, codes.sizes(), at::kChar);
+  std::vector<int64_t> shape = codes.sizes().vec();
+  shape.back() = pack_blocks(d);
+  plain(exps, shape, at::kChar);
+  const at::ScalarType type = ((THPDtype*)a[2])->scalar_type;
+  const Tensor x = a[3] == Py_None ? empty(codes.sizes(), type, codes) : tensor(a[3]);
+  need(x.scalar_type() == type && (a[3] == Py_None || x.dim() == 2));
+  const int64_t xs = a[3] == Py_None ? d : matrix(x, T, d);
+  void* stream = stream_of(codes, {&exps, &x});
+  run([&] { return lib.unpack8((const int8_t*)data(codes), (const int8_t*)data(exps), size32(T), size32(d), type_of(type), data(x), xs, stream); });
+  return a[3] == Py_None ? give(x) : again(a[3]);
+}
+
+// handle, x, base or None, dtype of y or None, y or None, keep, ws or None, a weight -> y, what is kept of a and b or None, its exponents or None
+CALL(gated_ffn_forward, 8) {
+  const moeq_gated_ffn* L = (const moeq_gated_ffn*)address(a[0]);
+  const Tensor &x = tensor(a[1]), *base = tensor_or_none(a[2]), &weight = tensor(a[7]);
+  const int32_t keep = whole32(a[5]);
+  need(x.dim() == 2 && type_of(x.scalar_type()) == L->dtype);
+  const int64_t T = x.size(0), xs = matrix(x, T, L->d_model), F = L->d_ff;
+  const at::ScalarType type = type_or(a[3], a[4] != Py_None ? tensor(a[4]).scalar_type() : base ? base->scalar_type() : x.scalar_type());
+  const Tensor y = a[4] != Py_None ? tensor(a[4]) : empty({T, L->d_model}, type, x);
+  need(y.scalar_type() == type && (!base || base->scalar_type() == type));
+  const Tensor ab = keep == MOEQ_KEEP_NONE ? Tensor() : empty({2, T, F}, keep == MOEQ_KEEP_8 ? at::kChar : x.scalar_type(), x);
+  const Tensor exps = keep == MOEQ_KEEP_8 ? empty({2, T, pack_blocks(F)}, at::kChar, x) : Tensor();
+  const Tensor ws = a[6] != Py_None ? tensor(a[6]) : scratch(lib.gated_ffn_workspace_bytes(L, size32(T), 0, 0, keep), x);
+  need(ws.is_contiguous() && ws.scalar_type() == at::kByte);
+  const int64_t bs = base ? matrix(*base, T, L->d_model) : 0, ys = matrix(y, T, L->d_model);
+  void* stream = stream_of(x, {base, &y, &ws, &weight});
+  run([&] {
+    return lib.gated_ffn_forward(L, data(x), xs, size32(T), data<const void>(base), bs, type_of(type), data(y), ys, keep, ab.defined() ? data(ab) : nullptr,
+                                 exps.defined() ? (int8_t*)data(exps) : nullptr, data(ws), ws.numel(), stream);
+  });
+  const auto some = [](const Tensor& t) { return t.defined() ? give(t) : again(Py_None); };
+  return give_tuple(a[4] == Py_None ? give(y) : again(a[4]), some(ab), some(exps));
+}
+
+// handle, x or its codes, None or its exponents, dy, keep, ab or codes or None, exponents or None, dx or None, whether dx is wanted, ws or None, a weight
+// -> dx or None, dw_in, dw_gate, dw_out
+CALL(gated_ffn_backward, 11) {
+  const moeq_gated_ffn* L = (const moeq_gated_ffn*)address(a[0]);
+  const Tensor &x = tensor(a[1]), *xe = tensor_or_none(a[2]), &dy = tensor(a[3]), *ab = tensor_or_none(a[5]), *abe = tensor_or_none(a[6]), &weight = tensor(a[10]);
+  const int32_t keep = whole32(a[4]);
+  need(dy.dim() == 2 && type_of(dy.scalar_type()) == L->dtype);
+  const int64_t T = dy.size(0), D = L->d_model, F = L->d_ff, ds = matrix(dy, T, D);
+  int64_t xs = 0;
+  if (xe) {
+    plain(x, {T, D}, at::kChar);
+    plain(*xe, {T, pack_blocks(D)}, at::kChar);
+  } else {
+    need(x.scalar_type() == dy.scalar_type());
+    xs = matrix(x, T, D);
+  }
+  need((ab != nullptr) == (keep != MOEQ_KEEP_NONE) && (abe != nullptr) == (keep == MOEQ_KEEP_8));
+  if (ab) plain(*ab, {2, T, F}, keep == MOEQ_KEEP_8 ? at::kChar : dy.scalar_type());
+  if (abe) plain(*abe, {2, T, pack_blocks(F)}, at::kChar);
+  const bool mine = a[7] == Py_None && a[8] == Py_True;
+  const Tensor dx = a[7] != Py_None ? tensor(a[7]) : mine ? empty({T, D}, dy.scalar_type(), dy) : Tensor();
+  need(!dx.defined() || dx.scalar_type() == dy.scalar_type());
+  const Tensor d_in = empty({F, D}, dy.scalar_type(), dy), d_gate = empty({F, D}, dy.scalar_type(), dy), d_out = empty({D, F}, dy.scalar_type(), dy);
+  const Tensor ws = a[9] != Py_None ? tensor(a[9]) : scratch(lib.gated_ffn_workspace_bytes(L, size32(T), 1, xe != nullptr, keep), dy);
+  need(ws.is_contiguous() && ws.scalar_type() == at::kByte);
+  const int64_t dxs = dx.defined() ? matrix(dx, T, D) : 0;
+  void* stream = stream_of(dy, {&x, xe, ab, abe, &dx, &ws, &weight});
+  run([&] {
+    return lib.gated_ffn_backward(L, xe ? nullptr : data(x), xs, xe ? (const int8_t*)data(x) : nullptr, data<const int8_t>(xe), size32(T), data(dy), ds, keep, data<const void>(ab),
+                                  data<const int8_t>(abe), dx.defined() ? data(dx) : nullptr, dxs, data(d_in), data(d_gate), data(d_out), data(ws), ws.numel(), stream);
+  });
+  return give_tuple(mine ? give(dx) : again(a[7]), give(d_in), give(d_gate), give(d_out));
+}
+
+// x -> codes [T][pitch], scale
+CALL(quantize_rows, 1) {
+  const Tensor& x = tensor(a[0]);
+  need(x.dim() == 2 && x.size(1) > 0);
+  const int64_t T = x.size(0), d = x.size(1), xs = matrix(x, T, d);
+  const Tensor codes = empty({T, lib.q8_pitch(size32(d))}, at::kChar, x), scale = empty({T}, at::kFloat, x);
+  void* stream = stream_of(x, {});
+  run([&] { return lib.quantize_rows(data(x), xs, type_of(x.scalar_type()), size32(T), (int32_t)d, (int8_t*)data(codes), (float*)data(scale), stream); });
+  return give_tuple(give(codes), give(scale));
+}
+
+// k, codes and scale of x, codes and scale of w, base or None, dtype or None, y or None -> y
+CALL(matmul_q8, 8) {
+  const int32_t k = whole32(a[0]);
+  const Tensor &x = tensor(a[1]), &xs = tensor(a[2]), &w = tensor(a[3]), &ws = tensor(a[4]), *base = tensor_or_none(a[5]);
+  need(k > 0 && x.dim() == 2 && w.dim() == 2);
+  const int64_t T = x.size(0), N = w.size(0), pitch = lib.q8_pitch(k);
+  plain(x, {T, pitch}, at::kChar);
+  plain(w, {N, pitch}, at::kChar);
+  plain(xs, {T}, at::kFloat);
+  plain(ws, {N}, at::kFloat);
+  const at::ScalarType type = type_or(a[6], a[7] != Py_None ? tensor(a[7]).scalar_type() : base ? base->scalar_type() : at::kFloat);
+  const Tensor y = a[7] != Py_None ? tensor(a[7]) : empty({T, N}, type, x);
+  need(y.scalar_type() == type && (!base || base->scalar_type() == type));
+  const Tensor room = scratch(lib.matmul_q8_workspace_bytes(size32(T), size32(N), k), x);
+  const int64_t bs = base ? matrix(*base, T, N) : 0, ys = matrix(y, T, N);
+  void* stream = stream_of(x, {&xs, &w, &ws, base, &y});
+  run([&] {
+    return lib.matmul_q8((const int8_t*)data(x), (const float*)data(xs), (int32_t)T, (const int8_t*)data(w), (const float*)data(ws), (int32_t)N, k, data<const void>(base), bs, type_of(type),
+                         data(y), ys, data(room), room.numel(), stream);
+  });
+  return a[7] == Py_None ? give(y) : again(a[7]);
+}
+
 // MoeqError, the function that gives the current stream of a device, then the addresses of the library's entry points in the order of Entry.
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -335,7 +531,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(sort_pairs), METHOD(gather_rows), METHOD(combine_rows), METHOD(combine_rows_backward), METHOD(adapters_forward), METHOD(adapters_backward),
-                         METHOD(distill_forward), METHOD(distill_backward), METHOD(distill_loss_grad), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(distill_forward), METHOD(distill_backward), METHOD(distill_loss_grad), METHOD(block_norms_forward), METHOD(block_norms_backward), METHOD(pack8), METHOD(unpack8), METHOD(gated_ffn_forward),
+                         METHOD(gated_ffn_backward), METHOD(quantize_rows), METHOD(matmul_q8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

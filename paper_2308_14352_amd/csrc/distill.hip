@@ -23,24 +23,6 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-// ---- folds over a wavefront, by moves between lanes that are part of the operation ----
-template <int CTRL, int ROWS>
-__device__ __forceinline__ float from_lane(float v, float none) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
-}
-template <typename Op>
-__device__ __forceinline__ float fold(float v, float none, Op op) {
-  v = op(v, from_lane<0x111, 0xf>(v, none));
-  v = op(v, from_lane<0x112, 0xf>(v, none));
-  v = op(v, from_lane<0x114, 0xf>(v, none));
-  v = op(v, from_lane<0x118, 0xf>(v, none));
-  v = op(v, from_lane<0x142, 0xa>(v, none));      // the last lane of rows 0 and 2 to rows 1 and 3
-  v = op(v, from_lane<0x143, 0xc>(v, none));      // lane 31 to rows 2 and 3
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-}
-__device__ __forceinline__ float wave_max(float v) { return fold(v, -INFINITY, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ float wave_sum(float v) { return fold(v, 0.f, [](float a, float b) { return a + b; }); }
-
 // A maximum of logits and the sum of exp2((z - max) c) that belongs to it; minus infinity counts from 0.
 struct Stat { float m, s; };
 __device__ __forceinline__ float origin(float m) { return m == -INFINITY ? 0.f : m; }

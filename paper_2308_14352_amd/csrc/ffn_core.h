@@ -1,0 +1,230 @@
+// A gated feed-forward block. With a = x w_in^T, b = x w_gate^T:
+//   forward    h = silu(a) b,  y = base + h w_out^T
+//   backward   dh = dy w_out,  s = sigmoid(a),  da = dh b s (1 + a (1 - s)),  db = dh a s,  h again
+//              dx = da w_in + db w_gate,  dw_in = da^T x,  dw_gate = db^T x,  dw_out = dy^T h
+// Four products' worth of work forward and backward are matrix products (tiles.h); what stands between them happens on their sums:
+// the product of x with both weights takes their rows in turns of 32, so that a and b of an element meet in one lane; that of dy leaves da,
+// db and h. h, da and db are rounded to the type (as a program in that type holds them): an output has that rounding and its own. They lie
+// in the workspace, rows of a multiple of 64 elements, zeros behind the last column and in rows up to a multiple of 64, which later
+// products sum over; da and db of a row side by side, so that dx is one product through both weights.
+#pragma once
+#include <algorithm>
+
+#include "tiles.h"
+
+namespace moeq {
+namespace tiles {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+template <typename T>
+__device__ __forceinline__ float sigmoid(float a) {
+  if constexpr (std::is_same<T, float>::value) return 1.f / (1.f + expf(-a));
+  else return 1.f / (1.f + __builtin_amdgcn_exp2f(-a * kLog2e));
+}
+
+__device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
+// 32 columns of a row (16 of them here, the rest in lane ^ 32) to codes and their exponent, as k_pack8 does.
+template <typename T>
+__device__ __forceinline__ int to_codes(const f32x16& c, int n, int half, int N, int8_t (&code)[16]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float v = column(n, half, i / 4) + i % 4 < N ? c[i] : 0.f;
+    top = max(top, __builtin_bit_cast(uint32_t, v) & 0x7fffffffu);
+  }
+  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  const bool nan = top >= 0x7f800000u;
+  const int e = max((int)(top >> 23) - 127 - 6, std::is_same<T, _Float16>::value ? -24 : -126);
+  const float up = nan ? 0.f : power(-e);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) code[i] = nan ? 0 : (int8_t)fminf(fmaxf(rintf(c[i] * up), -127.f), 127.f);
+  return nan ? kPackNan : e;
+}
+
+// From a and b: h to the workspace (if wanted), a and b kept.
+template <typename T>
+struct Up {
+  T* h;
+  int64_t pitch;            // of h
+  int32_t T_, F, Tp, Fp;
+  int32_t keep;
+  T* ab;                    // MOEQ_KEEP_OWN
+  int8_t *codes, *exps;     // MOEQ_KEEP_8
+  __device__ __forceinline__ void keep8(int which, int m, int f, int half, const f32x16& c) const {
+    int8_t code[16];
+    const int e = to_codes<T>(c, f, half, F, code);      // (lanes of every row, also behind the last: lanes exchange)
+    if (m >= T_ || f >= F) return;
+    const int64_t row = (int64_t)which * T_ + m;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = column(f, half, q);
+      if (at + 4 <= F) {
+        __builtin_memcpy(codes + row * F + at, code + 4 * q, 4);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (at + i < F) codes[row * F + at + i] = code[4 * q + i];
+      }
+    }
+    if (half == 0) exps[row * ((F + kPackBlock - 1) / kPackBlock) + f / kPackBlock] = (int8_t)e;
+  }
+  __device__ __forceinline__ void pair(int m, int f, int half, const f32x16& a, const f32x16& b) const {
+    if (keep == MOEQ_KEEP_8) keep8(0, m, f, half, a), keep8(1, m, f, half, b);
+    if (m >= Tp) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = column(f, half, q);
+      if (at >= Fp) continue;
+      float u[4], v[4], w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u[i] = a[4 * q + i], v[i] = b[4 * q + i];
+        w[i] = m < T_ && at + i < F ? u[i] * sigmoid<T>(u[i]) * v[i] : 0.f;
+      }
+      if (h) store_n(h + m * pitch + at, w);
+      if (keep == MOEQ_KEEP_OWN && m < T_ && at < F) {
+        store4(ab + (int64_t)m * F, at, F, u);
+        store4(ab + ((int64_t)T_ + m) * F, at, F, v);
+      }
+    }
+  }
+};
+
+// From dh, a and b: da, db and h.
+template <typename T>
+struct Act {
+  const T* ab;
+  const int8_t *codes, *exps;      // in ab's place
+  T *dab, *h;                      // [Tp][2 Fp], [Tp][Fp]
+  int32_t T_, F, Tp, Fp;
+  __device__ __forceinline__ void get(int which, int m, int at, float unit, float (&v)[4]) const {
+    const int64_t row = (int64_t)which * T_ + m;
+    if (!codes) return load4(v, ab + row * F, at, F);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = at + i < F ? (float)codes[row * F + at + i] * unit : 0.f;
+  }
+  __device__ __forceinline__ void block(int, int m, int f, int half, const f32x16& c) const {
+    if (m >= Tp) return;
+    float unit[2] = {1.f, 1.f};
+    if (codes && m < T_ && f < F) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int e = exps[((int64_t)w * T_ + m) * ((F + kPackBlock - 1) / kPackBlock) + f / kPackBlock];
+        unit[w] = e == kPackNan ? __builtin_nanf("") : power(e);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = column(f, half, q);
+      if (at >= Fp) continue;
+      float da[4] = {}, db[4] = {}, hh[4] = {};
+      if (m < T_ && at < F) {
+        float a[4], b[4];
+        get(0, m, at, unit[0], a);
+        get(1, m, at, unit[1], b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (at + i >= F) continue;
+          const float s = sigmoid<T>(a[i]), g = a[i] * s, dh = c[4 * q + i];
+          da[i] = dh * b[i] * (s + g * (1.f - s)), db[i] = dh * g, hh[i] = g * b[i];
+        }
+      }
+      store_n(dab + (int64_t)m * 2 * Fp + at, da);
+      store_n(dab + (int64_t)m * 2 * Fp + Fp + at, db);
+      store_n(h + (int64_t)m * Fp + at, hh);
+    }
+  }
+};
+
+inline int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
+// The workspace's parts, each at a multiple of 256 bytes.
+struct FfnPlan {
+  int64_t Tp, Fp, Dp;
+  size_t h, dab, x, ab, bytes;
+  FfnPlan(const FfnArgs& a, bool backward) : Tp(padded(a.T)), Fp(padded(a.F)), Dp(padded(a.D)) {
+    const size_t e = dtype_bytes(a.dtype);
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t here = at; at += (n + 255) / 256 * 256; return here; };
+    h = take(Tp * Fp * e);
+    dab = x = ab = at;
+    if (backward) {
+      dab = take(Tp * 2 * Fp * e);
+      if (a.x_codes) x = take((size_t)a.T * Dp * e);
+      if (a.keep == MOEQ_KEEP_NONE) ab = take((size_t)2 * a.T * a.F * e);
+    }
+    bytes = at;
+  }
+};
+
+template <typename T>
+Side side(const void* p, int64_t stride, int32_t n, int32_t k, const void* q = nullptr) {
+  return Side{{(const char*)p, (const char*)(q ? q : p)}, stride * (int64_t)sizeof(T), n, k};
+}
+template <typename T> int32_t steps_of(int64_t k) { return (int32_t)((k + kStep<T> - 1) / kStep<T>); }
+
+template <typename T>
+hipError_t up(const FfnArgs& a, const void* x, int64_t x_stride, const Up<T>& epi, hipStream_t st) {
+  Product p = {side<T>(x, x_stride, a.T, a.D), side<T>(a.w_in, a.D, a.F, a.D, a.w_gate), steps_of<T>(a.D), 0};
+  return launch_tile<T, true, true, 128, 128, 2, 2, kOne, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, epi, st);
+}
+
+template <typename T>
+hipError_t ffn_forward(const FfnArgs& a, hipStream_t st) {
+  const FfnPlan plan(a, false);
+  T* h = (T*)((char*)a.ws + plan.h);
+  Up<T> e = {h, plan.Fp, a.T, a.F, (int32_t)plan.Tp, (int32_t)plan.Fp, a.keep, (T*)a.ab, (int8_t*)a.ab, a.ab_exps};
+  if (hipError_t s = up<T>(a, a.x, a.x_stride, e, st); s != hipSuccess) return s;
+  Product p = {side<T>(h, plan.Fp, (int32_t)plan.Tp, (int32_t)plan.Fp), side<T>(a.w_out, a.F, a.D, a.F), steps_of<T>(a.F), 0};
+  auto down = [&](auto o) {
+    using O = decltype(o);
+    Store<O> out = {{(O*)a.y, nullptr}, a.y_stride, (const O*)a.base, a.base_stride, a.T, a.D};
+    return launch_tile<T, true, true, 128, 128, 2, 2, kOne, kOne>(p, a.T, a.D, 1, out, st);
+  };
+  if (a.y_dtype == a.dtype) return down(T{});
+  return down(0.f);
+}
+
+template <typename T>
+hipError_t ffn_backward(const FfnArgs& a, hipStream_t st) {
+  const FfnPlan plan(a, true);
+  char* ws = (char*)a.ws;
+  T *h = (T*)(ws + plan.h), *dab = (T*)(ws + plan.dab);
+  const int32_t Tp = (int32_t)plan.Tp, Fp = (int32_t)plan.Fp;
+  const void* x = a.x;
+  int64_t x_stride = a.x_stride;
+  if (a.T > 0) {
+    if (a.x_codes) {
+      Rows8Args r = {};
+      r.T = a.T, r.d = a.D, r.dtype = a.dtype, r.codes = (int8_t*)a.x_codes, r.exps = (int8_t*)a.x_exps, r.out = ws + plan.x, r.out_stride = plan.Dp;
+      if (hipError_t s = launch_unpack8(r, st); s != hipSuccess) return s;
+      x = r.out, x_stride = plan.Dp;
+    }
+    const T* ab = (const T*)a.ab;
+    if (a.keep == MOEQ_KEEP_NONE) {
+      T* made = (T*)(ws + plan.ab);
+      Up<T> e = {nullptr, 0, a.T, a.F, Tp, Fp, MOEQ_KEEP_OWN, made, nullptr, nullptr};
+      if (hipError_t s = up<T>(a, x, x_stride, e, st); s != hipSuccess) return s;
+      ab = made;
+    }
+    const bool eight = a.keep == MOEQ_KEEP_8;
+    Act<T> e = {eight ? nullptr : ab, eight ? (const int8_t*)a.ab : nullptr, a.ab_exps, dab, h, a.T, a.F, Tp, Fp};
+    Product p = {side<T>(a.dy, a.dy_stride, a.T, a.D), side<T>(a.w_out, a.F, a.F, a.D), steps_of<T>(a.D), 0};
+    if (hipError_t s = launch_tile<T, true, false, 128, 128, 2, 2, kOne, kOne>(p, Tp, Fp, 1, e, st); s != hipSuccess) return s;
+    if (a.dx) {
+      Product q = {side<T>(dab, 2 * plan.Fp, Tp, 2 * Fp), side<T>(a.w_in, a.D, a.D, a.F, a.w_gate), 2 * steps_of<T>(Fp), steps_of<T>(Fp)};
+      Store<T> out = {{(T*)a.dx, nullptr}, a.dx_stride, nullptr, 0, a.T, a.D};
+      if (hipError_t s = launch_tile<T, true, false, 128, 128, 2, 2, kOne, kBehind>(q, a.T, a.D, 1, out, st); s != hipSuccess) return s;
+    }
+  }
+  // (the workspace's rows are zero from row T on, those of x and dy end there)
+  Product p = {side<T>(dab, 2 * plan.Fp, a.F, Tp, dab + Fp), side<T>(x, x_stride, a.D, a.T), steps_of<T>(a.T), 0};
+  Store<T> out = {{(T*)a.dw_in, (T*)a.dw_gate}, a.D, nullptr, 0, a.F, a.D};
+  if (hipError_t s = launch_tile<T, false, false, 128, 128, 2, 2, kOne, kOne>(p, a.F, a.D, 2, out, st); s != hipSuccess) return s;
+  p.a = side<T>(a.dy, a.dy_stride, a.D, a.T), p.b = side<T>(h, plan.Fp, a.F, Tp);
+  out = {{(T*)a.dw_out, nullptr}, a.F, nullptr, 0, a.D, a.F};
+  return launch_tile<T, false, false, 128, 128, 2, 2, kOne, kOne>(p, a.D, a.F, 1, out, st);
+}
+
+}  // namespace tiles
+}  // namespace moeq

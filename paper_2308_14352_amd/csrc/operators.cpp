@@ -49,6 +49,8 @@ inline bool matrix_ok(const void* p, int64_t rows, int64_t stride, int64_t width
   return p && aligned(p, dtype_bytes(dtype)) &&
          (rows == 1 || ((stride >= width || (input && stride == 0)) && stride <= (int64_t)1 << 32));
 }
+// n contiguous bytes.
+inline Block codes_of(const void* p, int64_t n) { return Block{p, n > 0, n, n, kByteType}; }
 constexpr int64_t kMaxPairs = (int64_t)1 << 28;
 
 moeq_status rows_ok(const int32_t* slot, int32_t n_tokens, int32_t top_k, int32_t d) {
@@ -105,6 +107,47 @@ DistillArgs distill_args(const void* logits, int64_t stride, int32_t dtype, int3
   a.temperature = temperature, a.weight = weight;
   return a;
 }
+
+moeq_status norms_ok(const NormsArgs& a) {
+  if (a.T < 0 || a.d <= 0 || !type_ok(a.f_dtype) || !type_ok(a.r_dtype) || !type_ok(a.n_dtype)) return MOEQ_EINVAL;
+  if (!(a.eps >= 0.f) || a.eps > 1e30f || !(a.alpha >= -1e30f && a.alpha <= 1e30f)) return MOEQ_EINVAL;
+  int32_t half = MOEQ_F32;
+  for (int32_t t : {a.f_dtype, a.r_dtype, a.n_dtype}) {
+    if (t == MOEQ_F32) continue;
+    if (half != MOEQ_F32 && half != t) return MOEQ_EINVAL;
+    half = t;
+  }
+  if (a.d > kNormsMaxWidth) return MOEQ_EUNSUPPORTED;
+  if (!aligned(a.gate, 4) || !aligned(a.w_after, 4) || !aligned(a.w_before, 4)) return MOEQ_EINVAL;
+  return matrix_ok(a.f, a.T, a.f_stride, a.d, a.f_dtype, true) ? MOEQ_OK : MOEQ_EINVAL;
+}
+
+moeq_status ffn_ok(const moeq_gated_ffn* f, int32_t n_tokens, int32_t keep) {
+  if (!f || f->d_model <= 0 || f->d_ff <= 0 || !type_ok(f->dtype) || n_tokens < 0) return MOEQ_EINVAL;
+  if (keep != MOEQ_KEEP_NONE && keep != MOEQ_KEEP_OWN && keep != MOEQ_KEEP_8) return MOEQ_EINVAL;
+  if (f->d_model > kFfnMaxWidth || f->d_ff > kFfnMaxWidth || n_tokens > kProductMaxRows) return MOEQ_EUNSUPPORTED;
+  const size_t e = dtype_bytes(f->dtype);
+  if (!f->w_in || !f->w_gate || !f->w_out || !aligned(f->w_in, e) || !aligned(f->w_gate, e) || !aligned(f->w_out, e)) return MOEQ_EINVAL;
+  return MOEQ_OK;
+}
+FfnArgs ffn_args(const moeq_gated_ffn* f, int32_t n_tokens, int32_t keep) {
+  FfnArgs a = {};
+  a.T = n_tokens, a.D = f->d_model, a.F = f->d_ff, a.dtype = f->dtype, a.w_in = f->w_in, a.w_gate = f->w_gate, a.w_out = f->w_out, a.keep = keep;
+  return a;
+}
+// What is kept of a and b, and of one of them the exponents.
+Block ab_of(const FfnArgs& a, const void* ab) {
+  const int64_t n = (int64_t)2 * a.T * a.F;
+  return a.keep == MOEQ_KEEP_NONE ? Block{} : a.keep == MOEQ_KEEP_8 ? codes_of(ab, n) : Block{ab, n > 0, n, n, a.dtype};
+}
+Block exps_of(const FfnArgs& a, const void* exps) {
+  return a.keep == MOEQ_KEEP_8 ? codes_of(exps, (int64_t)2 * a.T * ((a.F + kPackBlock - 1) / kPackBlock)) : Block{};
+}
+bool kept_ok(const FfnArgs& a, const void* ab, const void* exps) {
+  if (a.T == 0 || a.keep == MOEQ_KEEP_NONE) return true;
+  return ab && (a.keep == MOEQ_KEEP_8 ? exps != nullptr : aligned(ab, dtype_bytes(a.dtype)));
+}
+inline Block weight_of(const FfnArgs& a, const void* w) { return Block{w, 1, (int64_t)a.D * a.F, (int64_t)a.D * a.F, a.dtype}; }
 
 }  // namespace
 
@@ -265,6 +308,173 @@ moeq_status moe_distill_loss_grad(const void* logits, int64_t stride, int32_t dt
   if (n_tokens == 0) return MOEQ_OK;
   if (!loss || !aligned(loss, 4)) return MOEQ_EINVAL;
   return done(launch_distill_loss_grad(a, (hipStream_t)stream));
+}
+
+moeq_status moe_block_norms_forward(int32_t n_tokens, int32_t d, float residual_scale, float eps, int32_t f_dtype, const void* f,
+                                    int64_t f_stride, int32_t r_dtype, const void* r, int64_t r_stride, const float* gate_opt,
+                                    const float* w_after_opt, const float* w_before_opt, void* y, int64_t y_stride, int32_t n_dtype,
+                                    void* n, int64_t n_stride, void* stream) {
+  NormsArgs a = {};
+  a.T = n_tokens, a.d = d, a.alpha = residual_scale, a.eps = eps, a.f_dtype = f_dtype, a.r_dtype = r_dtype, a.n_dtype = n_dtype;
+  a.f = f, a.f_stride = f_stride, a.r = r, a.r_stride = r_stride, a.gate = gate_opt, a.w_after = w_after_opt, a.w_before = w_before_opt;
+  a.out_y = y, a.out_y_stride = y_stride, a.out_n = w_before_opt ? n : nullptr, a.out_n_stride = n_stride;
+  if (moeq_status s = norms_ok(a); s != MOEQ_OK) return s;
+  if (!matrix_ok(r, n_tokens, r_stride, d, r_dtype, true) || !matrix_ok(y, n_tokens, y_stride, d, r_dtype, false)) return MOEQ_EINVAL;
+  if (w_before_opt && !matrix_ok(n, n_tokens, n_stride, d, n_dtype, false)) return MOEQ_EINVAL;
+  const Block by{y, n_tokens, y_stride, d, r_dtype}, bn{a.out_n, n_tokens, n_stride, d, n_dtype}, bf{f, n_tokens, f_stride, d, f_dtype},
+      br{r, n_tokens, r_stride, d, r_dtype};
+  if (!apart({by, bn}, {vec(gate_opt, n_tokens), vec(w_after_opt, d), vec(w_before_opt, d)}) || overlap(bf, by) || overlap(br, bn) ||
+      !apart_or_same(br, by) || !apart_or_same(bf, bn))
+    return MOEQ_EINVAL;
+  if (n_tokens == 0) return MOEQ_OK;
+  return done(launch_norms_forward(a, (hipStream_t)stream));
+}
+
+size_t moe_block_norms_workspace_bytes(int32_t max_tokens, int32_t d) {
+  return max_tokens <= 0 || d <= 0 || d > kNormsMaxWidth ? 0 : norms_ws_bytes(max_tokens, d);
+}
+
+moeq_status moe_block_norms_backward(int32_t n_tokens, int32_t d, float residual_scale, float eps, int32_t f_dtype, const void* f,
+                                     int64_t f_stride, int32_t r_dtype, const void* y, int64_t y_stride, const void* dy,
+                                     int64_t dy_stride, int32_t n_dtype, const void* dn, int64_t dn_stride, const float* gate_opt,
+                                     const float* w_after_opt, const float* w_before_opt, void* df, int64_t df_stride, void* dr,
+                                     int64_t dr_stride, float* dgate, float* dw_after, float* dw_before, void* ws, size_t ws_bytes,
+                                     void* stream) {
+  NormsArgs a = {};
+  a.T = n_tokens, a.d = d, a.alpha = residual_scale, a.eps = eps, a.f_dtype = f_dtype, a.r_dtype = r_dtype, a.n_dtype = n_dtype;
+  a.f = f, a.f_stride = f_stride, a.y = w_before_opt ? y : nullptr, a.y_stride = y_stride, a.dy = dy, a.dy_stride = dy_stride;
+  a.dn = w_before_opt ? dn : nullptr, a.dn_stride = dn_stride, a.gate = gate_opt, a.w_after = w_after_opt, a.w_before = w_before_opt;
+  a.out_y = dr, a.out_y_stride = dr_stride, a.out_n = df, a.out_n_stride = df_stride;
+  a.dgate = gate_opt ? dgate : nullptr, a.dw_after = w_after_opt ? dw_after : nullptr, a.dw_before = w_before_opt ? dw_before : nullptr, a.ws = (float*)ws;
+  if (moeq_status s = norms_ok(a); s != MOEQ_OK) return s;
+  if (!matrix_ok(dy, n_tokens, dy_stride, d, r_dtype, true) || !matrix_ok(df, n_tokens, df_stride, d, f_dtype, false) ||
+      !matrix_ok(dr, n_tokens, dr_stride, d, r_dtype, false))
+    return MOEQ_EINVAL;
+  if (w_before_opt && (!matrix_ok(y, n_tokens, y_stride, d, r_dtype, true) || !matrix_ok(dn, n_tokens, dn_stride, d, n_dtype, true))) return MOEQ_EINVAL;
+  if ((gate_opt && n_tokens && !a.dgate) || (w_after_opt && !a.dw_after) || (w_before_opt && !a.dw_before)) return MOEQ_EINVAL;
+  if (!aligned(a.dgate, 4) || !aligned(a.dw_after, 4) || !aligned(a.dw_before, 4)) return MOEQ_EINVAL;
+  if (!apart({{df, n_tokens, df_stride, d, f_dtype}, {dr, n_tokens, dr_stride, d, r_dtype}, vec(a.dgate, n_tokens), vec(a.dw_after, d), vec(a.dw_before, d)},
+             {{f, n_tokens, f_stride, d, f_dtype}, {a.y, n_tokens, y_stride, d, r_dtype}, {dy, n_tokens, dy_stride, d, r_dtype},
+              {a.dn, n_tokens, dn_stride, d, n_dtype}, vec(gate_opt, n_tokens), vec(w_after_opt, d), vec(w_before_opt, d)}))
+    return MOEQ_EINVAL;
+  if (n_tokens && (w_after_opt || w_before_opt)) {
+    if (!ws || ws_bytes < norms_ws_bytes(n_tokens, d)) return MOEQ_EWORKSPACE;
+    if (!aligned(ws, 4)) return MOEQ_EINVAL;
+  }
+  return done(launch_norms_backward(a, (hipStream_t)stream));
+}
+
+moeq_status moe_pack8(const void* x, int64_t x_stride, int32_t dtype, int32_t rows, int32_t d, int8_t* codes, int8_t* exps, void* stream) {
+  if (rows < 0 || d <= 0 || !type_ok(dtype) || !matrix_ok(x, rows, x_stride, d, dtype, true) || (rows && (!codes || !exps))) return MOEQ_EINVAL;
+  const Block c = codes_of(codes, (int64_t)rows * d), e = codes_of(exps, (int64_t)rows * ((d + kPackBlock - 1) / kPackBlock));
+  if (!apart({c, e}, {{x, rows, x_stride, d, dtype}})) return MOEQ_EINVAL;
+  if (rows == 0) return MOEQ_OK;
+  Rows8Args a = {};
+  a.T = rows, a.d = d, a.dtype = dtype, a.x = x, a.x_stride = x_stride, a.codes = codes, a.exps = exps;
+  return done(launch_pack8(a, (hipStream_t)stream));
+}
+
+moeq_status moe_unpack8(const int8_t* codes, const int8_t* exps, int32_t rows, int32_t d, int32_t dtype, void* x, int64_t x_stride, void* stream) {
+  if (rows < 0 || d <= 0 || !type_ok(dtype) || !matrix_ok(x, rows, x_stride, d, dtype, false) || (rows && (!codes || !exps))) return MOEQ_EINVAL;
+  if (!apart({{x, rows, x_stride, d, dtype}},
+             {codes_of(codes, (int64_t)rows * d), codes_of(exps, (int64_t)rows * ((d + kPackBlock - 1) / kPackBlock))}))
+    return MOEQ_EINVAL;
+  if (rows == 0) return MOEQ_OK;
+  Rows8Args a = {};
+  a.T = rows, a.d = d, a.dtype = dtype, a.out = x, a.out_stride = x_stride, a.codes = (int8_t*)codes, a.exps = (int8_t*)exps;
+  return done(launch_unpack8(a, (hipStream_t)stream));
+}
+
+size_t moe_gated_ffn_workspace_bytes(const moeq_gated_ffn* ffn, int32_t max_tokens, int32_t backward, int32_t x_packed, int32_t keep) {
+  if (ffn_ok(ffn, max_tokens, keep) != MOEQ_OK || max_tokens == 0) return 0;
+  FfnArgs a = ffn_args(ffn, max_tokens, keep);
+  a.x_codes = x_packed ? (const int8_t*)ffn : nullptr;      // (whether there are any is all that counts)
+  return ffn_ws_bytes(a, backward != 0);
+}
+
+moeq_status moe_gated_ffn_forward(const moeq_gated_ffn* ffn, const void* x, int64_t x_stride, int32_t n_tokens, const void* base_opt,
+                                  int64_t base_stride, int32_t y_dtype, void* y, int64_t y_stride, int32_t keep, void* ab, int8_t* ab_exps,
+                                  void* ws, size_t ws_bytes, void* stream) {
+  if (moeq_status s = ffn_ok(ffn, n_tokens, keep); s != MOEQ_OK) return s;
+  if (y_dtype != ffn->dtype && y_dtype != MOEQ_F32) return MOEQ_EINVAL;
+  if (n_tokens == 0) return MOEQ_OK;
+  FfnArgs a = ffn_args(ffn, n_tokens, keep);
+  a.x = x, a.x_stride = x_stride, a.base = base_opt, a.base_stride = base_stride, a.y_dtype = y_dtype, a.y = y, a.y_stride = y_stride, a.ws = ws;
+  if (keep != MOEQ_KEEP_NONE) a.ab = ab, a.ab_exps = keep == MOEQ_KEEP_8 ? ab_exps : nullptr;
+  if (!matrix_ok(x, n_tokens, x_stride, a.D, a.dtype, true) || !matrix_ok(y, n_tokens, y_stride, a.D, y_dtype, false) || !kept_ok(a, ab, ab_exps)) return MOEQ_EINVAL;
+  if (base_opt && !matrix_ok(base_opt, n_tokens, base_stride, a.D, y_dtype, true)) return MOEQ_EINVAL;
+  const Block out{y, n_tokens, y_stride, a.D, y_dtype}, base{base_opt, n_tokens, base_stride, a.D, y_dtype}, kab = ab_of(a, ab), kexps = exps_of(a, ab_exps);
+  if (!apart({out, kab, kexps}, {{x, n_tokens, x_stride, a.D, a.dtype}, weight_of(a, a.w_in), weight_of(a, a.w_gate), weight_of(a, a.w_out)}) ||
+      !apart_or_same(base, out) || overlap(base, kab) || overlap(base, kexps))
+    return MOEQ_EINVAL;
+  if (!ws || ws_bytes < ffn_ws_bytes(a, false)) return MOEQ_EWORKSPACE;
+  if (!aligned(ws, 256)) return MOEQ_EINVAL;
+  return done(launch_ffn_forward(a, (hipStream_t)stream));
+}
+
+moeq_status moe_gated_ffn_backward(const moeq_gated_ffn* ffn, const void* x, int64_t x_stride, const int8_t* x_codes, const int8_t* x_exps,
+                                   int32_t n_tokens, const void* dy, int64_t dy_stride, int32_t keep, const void* ab, const int8_t* ab_exps,
+                                   void* dx_opt, int64_t dx_stride, void* dw_in, void* dw_gate, void* dw_out, void* ws, size_t ws_bytes,
+                                   void* stream) {
+  if (moeq_status s = ffn_ok(ffn, n_tokens, keep); s != MOEQ_OK) return s;
+  FfnArgs a = ffn_args(ffn, n_tokens, keep);
+  const size_t e = dtype_bytes(a.dtype);
+  a.x = x, a.x_stride = x_stride, a.x_codes = x_codes, a.x_exps = x_exps, a.dy = dy, a.dy_stride = dy_stride, a.dx = dx_opt, a.dx_stride = dx_stride;
+  if (keep != MOEQ_KEEP_NONE) a.ab = (void*)ab, a.ab_exps = keep == MOEQ_KEEP_8 ? (int8_t*)ab_exps : nullptr;
+  a.dw_in = dw_in, a.dw_gate = dw_gate, a.dw_out = dw_out, a.ws = ws;
+  if (!dw_in || !dw_gate || !dw_out || !aligned(dw_in, e) || !aligned(dw_gate, e) || !aligned(dw_out, e)) return MOEQ_EINVAL;
+  if (n_tokens && ((x != nullptr) == (x_codes != nullptr) || (x_codes && !x_exps))) return MOEQ_EINVAL;
+  if ((x && !matrix_ok(x, n_tokens, x_stride, a.D, a.dtype, true)) || !matrix_ok(dy, n_tokens, dy_stride, a.D, a.dtype, true) || !kept_ok(a, ab, ab_exps)) return MOEQ_EINVAL;
+  if (dx_opt && !matrix_ok(dx_opt, n_tokens, dx_stride, a.D, a.dtype, false)) return MOEQ_EINVAL;
+  const int64_t blocks = (a.D + kPackBlock - 1) / kPackBlock;
+  if (!apart({{dx_opt, n_tokens, dx_stride, a.D, a.dtype}, weight_of(a, dw_in), weight_of(a, dw_gate), weight_of(a, dw_out)},
+             {{x, n_tokens, x_stride, a.D, a.dtype}, codes_of(x_codes, (int64_t)n_tokens * a.D), codes_of(x_exps, n_tokens * blocks),
+              {dy, n_tokens, dy_stride, a.D, a.dtype}, ab_of(a, ab), exps_of(a, ab_exps), weight_of(a, a.w_in), weight_of(a, a.w_gate), weight_of(a, a.w_out)}))
+    return MOEQ_EINVAL;
+  if (n_tokens) {
+    if (!ws || ws_bytes < ffn_ws_bytes(a, true)) return MOEQ_EWORKSPACE;
+    if (!aligned(ws, 256)) return MOEQ_EINVAL;
+  }
+  return done(launch_ffn_backward(a, (hipStream_t)stream));
+}
+
+int64_t moe_q8_pitch(int32_t d) { return d <= 0 ? 0 : q8_pitch(d); }
+
+moeq_status moe_quantize_rows(const void* x, int64_t x_stride, int32_t dtype, int32_t rows, int32_t d, int8_t* codes, float* scale, void* stream) {
+  if (rows < 0 || d <= 0 || !type_ok(dtype) || !matrix_ok(x, rows, x_stride, d, dtype, true)) return MOEQ_EINVAL;
+  if (d > kQuantMaxWidth) return MOEQ_EUNSUPPORTED;
+  if (rows && (!codes || !scale || !aligned(codes, 16) || !aligned(scale, 4))) return MOEQ_EINVAL;
+  if (!apart({codes_of(codes, rows * q8_pitch(d)), vec(scale, rows)}, {{x, rows, x_stride, d, dtype}})) return MOEQ_EINVAL;
+  if (rows == 0) return MOEQ_OK;
+  Rows8Args a = {};
+  a.T = rows, a.d = d, a.dtype = dtype, a.x = x, a.x_stride = x_stride, a.codes = codes, a.scale = scale;
+  return done(launch_quantize_rows(a, (hipStream_t)stream));
+}
+
+size_t moe_matmul_q8_workspace_bytes(int32_t max_tokens, int32_t n_out, int32_t k) {
+  if (max_tokens <= 0 || n_out <= 0 || k <= 0 || k > kQuantMaxWidth || max_tokens > kProductMaxRows || n_out > kProductMaxRows / 8) return 0;
+  return q8_ws_bytes(max_tokens, n_out, k);
+}
+
+moeq_status moe_matmul_q8(const int8_t* x, const float* x_scale, int32_t n_tokens, const int8_t* w, const float* w_scale, int32_t n_out,
+                          int32_t k, const void* base_opt, int64_t base_stride, int32_t dtype, void* y, int64_t y_stride, void* ws,
+                          size_t ws_bytes, void* stream) {
+  if (n_tokens < 0 || n_out <= 0 || k <= 0 || !type_ok(dtype) || !w || !w_scale || !aligned(w, 16) || !aligned(w_scale, 4)) return MOEQ_EINVAL;
+  if (k > kQuantMaxWidth || n_tokens > kProductMaxRows || n_out > kProductMaxRows / 8) return MOEQ_EUNSUPPORTED;
+  if (n_tokens == 0) return MOEQ_OK;
+  if (!x || !x_scale || !aligned(x, 16) || !aligned(x_scale, 4) || !matrix_ok(y, n_tokens, y_stride, n_out, dtype, false)) return MOEQ_EINVAL;
+  if (base_opt && !matrix_ok(base_opt, n_tokens, base_stride, n_out, dtype, true)) return MOEQ_EINVAL;
+  const Block out{y, n_tokens, y_stride, n_out, dtype};
+  if (!apart({out}, {codes_of(x, n_tokens * q8_pitch(k)), vec(x_scale, n_tokens), codes_of(w, n_out * q8_pitch(k)), vec(w_scale, n_out)}) ||
+      !apart_or_same({base_opt, n_tokens, base_stride, n_out, dtype}, out))
+    return MOEQ_EINVAL;
+  const size_t need = q8_ws_bytes(n_tokens, n_out, k);
+  if (need && (!ws || ws_bytes < need)) return MOEQ_EWORKSPACE;
+  if (need && !aligned(ws, 16)) return MOEQ_EINVAL;
+  Q8Args a = {};
+  a.T = n_tokens, a.N = n_out, a.K = k, a.dtype = dtype, a.x = x, a.w = w, a.x_scale = x_scale, a.w_scale = w_scale;
+  a.base = base_opt, a.base_stride = base_stride, a.y = y, a.y_stride = y_stride, a.ws = ws;
+  return done(launch_matmul_q8(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

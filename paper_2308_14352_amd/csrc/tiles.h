@@ -1,0 +1,268 @@
+// Matrix products out[m][n] = sum over k of a(m, k) b(n, k) on the matrix cores, for the operators beside the layer (gated_ffn.hip,
+// matmul_q8.hip): one tile of the output a workgroup, an epilogue of the operator's own on the sums.
+//
+// A step is 128 bytes of the sum's length: 64 elements of 16 bits, 32 of fp32, 128 of 8 bits. A side (a or b) lies in memory with its sum
+// contiguous (rows) or its rows contiguous (columns: weights in a backward pass, and everything in a weight's gradient). In LDS it lies as
+// in memory, swizzled so that neither the writes of 16 bytes nor the reads of operands meet on banks:
+//   rows     [tile row][128 bytes]: piece c (16 bytes) of row r at c ^ (r / 2 % 8). An operand is one read of 16 bytes.
+//   columns  [k][tile row]: 64-byte unit u of k at u ^ k % 4 (tiles of 64: u ^ k / 2 % 2); 16-bit operands by reads that transpose
+//            (16 lanes read 4 k of 16 rows and each gets 4 k of its row), fp32 ones by four reads of 4 bytes.
+// An operand is 16 bytes a lane whatever its type, lane / 32 choosing one half of 32 bytes of the sum: v_mfma_*_32x32x16 of 16 bits,
+// v_mfma_i32_32x32x32_i8, or four v_mfma_f32_32x32x2_f32. The matrix instruction takes b first, so that a lane has one row m and four
+// consecutive n in every four sums.
+#pragma once
+#include <type_traits>
+
+#include "operators.h"
+
+namespace moeq {
+namespace tiles {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kStepBytes = 128;
+template <typename T> constexpr int kStep = kStepBytes / (int)sizeof(T);
+template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);
+template <typename T> using Sums = std::conditional_t<std::is_same<T, int8_t>::value, i32x16, f32x16>;
+
+// How a side is made of its two matrices: one; rows by 32 from the one and the other in turn (n: of each); the sum through the one, then
+// the other (k: of each).
+enum Made { kOne, kTurns, kBehind };
+struct Side {
+  const char* p[2];
+  int64_t stride;      // bytes
+  int32_t n, k;
+};
+struct Product {
+  Side a, b;
+  int32_t steps, first_steps;      // of the sum; of the first matrix (kBehind)
+  int32_t tiles_m, tiles_n;
+};
+
+__device__ __forceinline__ void mma(Sums<float>& c, i32x4 b, i32x4 a, __bf16) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(Sums<float>& c, i32x4 b, i32x4 a, _Float16) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(Sums<float>& c, i32x4 b, i32x4 a, float) {
+  const f32x4 u = __builtin_bit_cast(f32x4, b), v = __builtin_bit_cast(f32x4, a);      // (a bit cast of a vector's element takes its first)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(u[i], v[i], c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(Sums<int8_t>& c, i32x4 b, i32x4 a, int8_t) { c = __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, c, 0, 0, 0); }
+
+// Where 16 bytes of a tile of R rows lie in LDS: piece `at` of tile row `row` (rows), or of k `row` (columns).
+template <typename T, bool ROWS, int R>
+__device__ __forceinline__ int place(int row, int at) {
+  if constexpr (ROWS) return row * kStepBytes + ((at ^ (row >> 1 & 7)) << 4);
+  else if constexpr (sizeof(T) == 4) return row * R * 4 + at * 16;
+  else return row * R * 2 + (((at >> 2) ^ (R >= 128 ? row & 3 : row >> 1 & 1)) << 6) + (at & 3) * 16;
+}
+
+// 16 bytes of a row of `limit` elements from element `at` on, at any alignment; zeros behind its end.
+template <typename T>
+__device__ __forceinline__ uint4 piece(const char* row, int at, int limit) {
+  uint4 v = {0, 0, 0, 0};
+  const T* p = (const T*)row + at;
+  if (at + kPiece<T> <= limit) {
+    __builtin_memcpy(&v, p, 16);
+  } else {
+    T t[kPiece<T>];
+#pragma unroll
+    for (int i = 0; i < kPiece<T>; ++i) t[i] = at + i < limit ? p[i] : (T)0;
+    __builtin_memcpy(&v, t, 16);
+  }
+  return v;
+}
+
+// A tile of a side on its way through registers: for operands at any alignment and of any length.
+template <typename T, bool ROWS, int R, int NT, Made MADE>
+struct Through {
+  static constexpr int kPieces = R * 8 / NT, kWide = ROWS ? 8 : R / kPiece<T>;      // a thread's pieces; those of a row in LDS
+  uint4 r[kPieces];
+  __device__ __forceinline__ void load(const Side& s, int z, int n0, int step, int first_steps) {
+    const int which = MADE == kBehind ? step >= first_steps : z;
+    const int k0 = (MADE == kBehind && which ? step - first_steps : step) * kStep<T>;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int c = threadIdx.x + j * NT, row = c / kWide, at = c % kWide * kPiece<T>;
+      if constexpr (ROWS) {
+        const int w = MADE == kTurns ? row / 32 % 2 : which, n = MADE == kTurns ? n0 / 2 + row / 64 * 32 + row % 32 : n0 + row;
+        r[j] = piece<T>(s.p[w] + min(n, s.n - 1) * s.stride, k0 + at, s.k);
+      } else {
+        r[j] = k0 + row < s.k ? piece<T>(s.p[which] + (k0 + row) * s.stride, n0 + at, s.n) : uint4{0, 0, 0, 0};
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int c = threadIdx.x + j * NT;
+      *(uint4*)(lds + place<T, ROWS, R>(c / kWide, c % kWide)) = r[j];
+    }
+  }
+};
+
+// The operand of 32 rows from `base` on and the slice's 32 bytes of the sum.
+template <typename T, bool ROWS, int R>
+__device__ __forceinline__ i32x4 operand(const char* lds, int base, int slice) {
+  const int lane = threadIdx.x % 64, half = lane / 32;
+  if constexpr (ROWS) {
+    return *(const i32x4*)(lds + place<T, true, R>(base + lane % 32, slice * 2 + half));
+  } else if constexpr (sizeof(T) == 4) {
+    i32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *(const int*)(lds + ((slice * 8 + half * 4 + i) * R + base + lane % 32) * 4);
+    return v;
+  } else {
+    typedef __attribute__((address_space(3))) i16x4* at_lds;
+    const int k = slice * 16 + half * 8 + lane % 16 / 4, col = base + lane / 16 % 2 * 16 + lane % 4 * 4;      // (of what this lane reads)
+    const char* p = lds + place<T, false, R>(k, col / 8) + col % 8 * 2;
+    i16x4 v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds)p), __builtin_amdgcn_ds_read_tr16_b64_v4i16((at_lds)(p + 4 * R * 2))};
+    return __builtin_bit_cast(i32x4, v);
+  }
+}
+
+// Workgroups of an XCD (every eighth of a launch) take tiles that lie together: eight tiles of m by as many of n as it comes to.
+__device__ __forceinline__ void tile_of(const Product& p, int& tm, int& tn) {
+  const int n = p.tiles_m * p.tiles_n, x = blockIdx.x % 8, i = blockIdx.x / 8;
+  const int t = x * (n / 8) + min(x, n % 8) + i;
+  const int g = t / (8 * p.tiles_n), rows = min(8, p.tiles_m - g * 8), in = t - g * 8 * p.tiles_n;
+  tm = g * 8 + in % rows;
+  tn = in / rows;
+}
+
+// One tile: BM x BN by WM x WN wavefronts. blockIdx.y: the matrix of a (kOne), blockIdx.z of gridDim.z: the share of the sum.
+template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, class Epi>
+__global__ __launch_bounds__(64 * WM * WN) void k_tile(Product p, Epi epi) {
+  constexpr int NT = 64 * WM * WN, MB = BM / WM / 32, NB = BN / WN / 32, kBuffer = (BM + BN) * kStepBytes;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  int tm, tn;
+  tile_of(p, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN, z = blockIdx.y;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  const int share = (p.steps + gridDim.z - 1) / gridDim.z, from = blockIdx.z * share, to = min(from + share, p.steps);
+  Sums<T> acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = Sums<T>{};
+  Through<T, A_ROWS, BM, NT, A_MADE> a;
+  Through<T, B_ROWS, BN, NT, B_MADE> b;
+  if (from < to) {
+    a.load(p.a, z, m0, from, p.first_steps);
+    b.load(p.b, 0, n0, from, p.first_steps);
+    a.store(lds);
+    b.store(lds + BM * kStepBytes);
+  }
+  __syncthreads();
+  for (int step = from; step < to; ++step) {
+    const char* at = lds + (step - from) % 2 * kBuffer;
+    char* next = lds + (step - from + 1) % 2 * kBuffer;
+    if (step + 1 < to) {
+      a.load(p.a, z, m0, step + 1, p.first_steps);
+      b.load(p.b, 0, n0, step + 1, p.first_steps);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      i32x4 u[MB], v[NB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) u[i] = operand<T, A_ROWS, BM>(at, wm + i * 32, s);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) v[j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, s);
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) mma(acc[i][j], v[j], u[i], T{});
+    }
+    if (step + 1 < to) {
+      a.store(next);
+      b.store(next + BM * kStepBytes);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const int m = m0 + wm + i * 32 + lane % 32;
+    if constexpr (B_MADE == kTurns) {
+#pragma unroll
+      for (int j = 0; j < NB; j += 2) epi.pair(m, (n0 + wn + j * 32) / 2, lane / 32, acc[i][j], acc[i][j + 1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) epi.block(z, m, n0 + wn + j * 32, lane / 32, acc[i][j]);
+    }
+  }
+}
+
+// The n of a lane's sums 4 q to 4 q + 3.
+__device__ __forceinline__ int column(int n, int half, int q) { return n + q * 8 + half * 4; }
+
+// Four consecutive elements of a row that ends at `limit`.
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int at, int limit, const float (&v)[4]) {
+  if (at + 4 <= limit) {
+    store_n(row + at, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + i < limit) row[at + i] = (T)v[i];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void load4(float (&v)[4], const T* row, int at, int limit) {
+  if (at + 4 <= limit) {
+    load_n(v, row + at);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = at + i < limit ? (float)row[at + i] : 0.f;
+  }
+}
+
+// out[z][m][n] = base[m][n] + sums, in O.
+template <typename O>
+struct Store {
+  O* out[2];
+  int64_t stride;
+  const O* base;
+  int64_t base_stride;
+  int32_t M, N;
+  __device__ __forceinline__ void block(int z, int m, int n, int half, const f32x16& c) const {
+    if (m >= M) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = column(n, half, q);
+      if (at >= N) continue;
+      float v[4] = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+      if (base) {
+        float b[4];
+        load4(b, base + m * base_stride, at, N);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += b[i];
+      }
+      store4(out[z] + m * stride, at, N, v);
+    }
+  }
+};
+
+template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, class Epi>
+hipError_t launch_tile(Product p, int M, int N, int batch, const Epi& epi, hipStream_t st) {
+  constexpr int kLds = 2 * (BM + BN) * kStepBytes;
+  const auto kernel = k_tile<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
+  if constexpr (kLds > 64 * 1024) {
+    static const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+    if (e != hipSuccess) return e;
+  }
+  p.tiles_m = (M + BM - 1) / BM, p.tiles_n = (N + BN - 1) / BN;
+  kernel<<<dim3(p.tiles_m * p.tiles_n, batch), 64 * WM * WN, kLds, st>>>(p, epi);
+  return hipGetLastError();
+}
+
+}  // namespace tiles
+}  // namespace moeq

@@ -1,0 +1,182 @@
+"""Tensors kept in 8 bits and products in 8-bit integers against plain arithmetic in 64 bits on the host."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2308_14352_amd as moeq
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def strided(t, pad, shift):
+    buf = torch.full((t.shape[0] * (t.shape[1] + pad) + shift,), float("nan"), dtype=t.dtype, device=t.device)
+    v = buf[shift:].view(t.shape[0], t.shape[1] + pad)[:, :t.shape[1]]
+    v.copy_(t)
+    return v
+
+
+def rows(T, d, kind, by=1.0):
+    g = np.random.default_rng([T, d])
+    return torch.from_numpy(g.normal(size=(T, d)) * np.exp(g.normal(size=(T, 1))) * by).to(TYPES[kind])
+
+
+def packed(x, kind):
+    """(codes, exponents, values) by blocks of 32 columns, in 64 bits."""
+    v = x.double().numpy()
+    T, d = v.shape
+    codes, exps = np.zeros((T, d)), np.zeros((T, (d + 31) // 32), int)
+    for b in range(exps.shape[1]):
+        part = v[:, b * 32:b * 32 + 32]
+        e = np.frexp(np.abs(part).max(1))[1] - 7
+        exps[:, b] = np.maximum(np.where(np.abs(part).max(1) == 0, -10**6, e), -24 if kind == "f16" else -126)
+        codes[:, b * 32:b * 32 + 32] = np.clip(np.rint(np.ldexp(part, -exps[:, b:b + 1])), -127, 127)
+    return codes, exps, np.ldexp(codes, np.repeat(exps, 32, 1)[:, :d])
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("T,d,pad", [(1, 1, 0), (1, 31, 0), (3, 32, 0), (5, 33, 7), (64, 100, 0), (9, 1000, 1), (130, 256, 8), (2, 14336, 0), (1000, 40, 3)])
+def test_packed_values_are_exact(T, d, pad, kind):
+    x = rows(T, d, kind)
+    p = moeq.moe_pack8(strided(x.to(DEV), pad, pad))
+    codes, exps, values = packed(x, kind)
+    assert np.array_equal(p.codes.cpu().numpy(), codes) and np.array_equal(p.exps.cpu().numpy(), exps)
+    out = moeq.moe_unpack8(p)
+    assert out.dtype == TYPES[kind] and np.array_equal(out.cpu().double().numpy(), values)
+    # a value is off by half a unit, 2^-7 of the block's largest; where that rounds up to 128, by a unit
+    top = np.repeat(np.stack([np.abs(x.double().numpy()[:, b * 32:b * 32 + 32]).max(1) for b in range(exps.shape[1])], 1), 32, 1)[:, :d]
+    assert (np.abs(values - x.double().numpy()) <= top * 2.0**-6).all()
+    wide = torch.full((T, d + 5), 9.0, dtype=TYPES[kind], device=DEV)
+    moeq.moe_unpack8(p, wide[:, :d])
+    assert torch.equal(wide[:, :d], out) and (wide[:, d:] == 9.0).all()
+    again = moeq.moe_pack8(out)
+    assert np.array_equal(moeq.moe_unpack8(again).cpu().double().numpy(), values)      # (what is packed already stays)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+def test_packed_ends_of_the_range(kind):
+    info = torch.finfo(TYPES[kind])
+    x = torch.zeros((8, 64), dtype=TYPES[kind])
+    x[1, 3], x[2, :32], x[3, 40], x[4, 0] = info.max, info.smallest_normal, -info.max, 1.0
+    x[4, 1:32] = 1 / 128                                   # half a unit: to even
+    x[5, 5], x[6, 33], x[7, 63] = float("nan"), float("inf"), -float("inf")
+    p = moeq.moe_pack8(x.to(DEV))
+    out = moeq.moe_unpack8(p).cpu()
+    ok = x.clone()
+    ok[5:] = 0
+    assert np.array_equal(out[:5].double().numpy(), packed(ok, kind)[2][:5]) and out[:5].isfinite().all()
+    assert out[5, :32].isnan().all() and (out[5, 32:] == 0).all() and out[6, 32:].isnan().all() and (out[6, :32] == 0).all() and out[7, 32:].isnan().all()
+
+
+def test_packed_outputs_given_and_leading_dimensions():
+    x = rows(12, 70, "bf16").to(DEV)
+    p = moeq.moe_pack8(x)
+    q = moeq.Packed8(torch.zeros_like(p.codes), torch.zeros_like(p.exps), x.dtype)
+    assert moeq.moe_pack8(x, packed=q) is q and torch.equal(q.codes, p.codes) and torch.equal(q.exps, p.exps)
+    three = moeq.Packed8(p.codes.view(2, 6, 70), p.exps.view(2, 6, 3), x.dtype)
+    assert torch.equal(moeq.moe_unpack8(three), moeq.moe_unpack8(p).view(2, 6, 70)) and three.shape == (2, 6, 70) and three.nbytes() == 12 * 73
+    assert moeq.moe_unpack8(moeq.moe_pack8(x[:0])).shape == (0, 70)
+    with pytest.raises(moeq.MoeqError):
+        moeq.moe_pack8(x.float(), packed=q)
+
+
+def quantized(x):
+    """A row's scale, and codes from fp32 quotients."""
+    v = x.float().numpy()
+    scale = np.maximum(np.abs(v).max(1) / np.float32(127), np.float32(2.0**-126)).astype(np.float32)
+    return np.rint(v / scale[:, None]), scale
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("T,d,pad", [(1, 1, 0), (3, 127, 1), (2, 128, 0), (5, 129, 0), (4, 513, 3), (2, 1100, 0), (3, 2049, 0), (2, 4100, 0), (2, 8200, 0),
+                                     (1, 16400, 0), (1, 40000, 0), (1, 65536, 0)])
+def test_quantized_rows(T, d, pad, kind):
+    x = rows(T, d, kind)
+    x[0, 0] = 0
+    q = moeq.moe_quantize_rows(strided(x.to(DEV), pad, pad))
+    codes, scale = quantized(x)
+    assert q.k == d and q.codes.shape == (T, (d + 127) // 128 * 128)
+    assert np.array_equal(q.scale.cpu().numpy(), scale) and np.array_equal(q.codes[:, :d].cpu().numpy(), codes) and (q.codes[:, d:] == 0).all()
+
+
+def test_quantized_rows_without_a_size():
+    x = torch.zeros((4, 200))
+    x[1, 7], x[2, 199], x[3, 0] = float("nan"), float("inf"), 2.0**-140
+    q = moeq.moe_quantize_rows(x.to(DEV))
+    assert (q.codes == 0).all() and q.scale[0] == 2.0**-126 and q.scale[1].isnan() and q.scale[2].isnan() and q.scale[3] == 2.0**-126
+
+
+# one token to several tiles of each kind, widths that end inside a step, a vector or a tile
+SHAPES = [(1, 1, 1), (1, 128, 64), (2, 100, 33), (3, 4096, 130), (7, 129, 517), (16, 640, 72), (17, 256, 129), (33, 1000, 200), (65, 384, 96), (100, 2000, 260),
+          (130, 512, 300), (256, 128, 256), (300, 1200, 520), (520, 640, 700)]
+
+
+@pytest.mark.parametrize("T,k,n", SHAPES)
+@pytest.mark.parametrize("kind,base", [("f32", False), ("bf16", True), ("f16", True), ("bf16", False), ("f32", True)])
+def test_products(T, k, n, kind, base):
+    product(T, k, n, kind, base)
+
+
+@pytest.mark.parametrize("T,k,n", [(1, 14336, 4100), (5, 65536, 40), (12, 6000, 5000), (40, 9000, 1030), (1030, 3000, 1030), (2100, 256, 4000)])
+def test_larger_products(T, k, n):
+    product(T, k, n, "bf16", True)
+
+
+def product(T, k, n, kind, base):
+    g = np.random.default_rng([T, k, n])
+    t = TYPES[kind]
+    x = rows(T, k, "f32")
+    w = g.integers(-128, 128, size=(n, k)).astype(np.int8)
+    ws = (g.random(n) + 0.5).astype(np.float32) / 127
+    b = torch.from_numpy(g.normal(size=(T, n))).to(t)
+    q = moeq.moe_quantize_rows(x.to(DEV))
+    weights = moeq.QuantRows(torch.from_numpy(w).to(DEV), torch.from_numpy(ws).to(DEV))
+    dev = strided(b.to(DEV), 3, 1) if base else None
+    y = moeq.moe_matmul_q8(q, weights, base=dev, dtype=t)
+    codes, scale = quantized(x)
+    p = (codes @ w.T.astype(np.float64)) * (scale[:, None].astype(np.float64) * ws)
+    want = p + (b.double().numpy() if base else 0.0)
+    got = y.cpu().double().numpy()
+    # the sum as fp32, the two scales' product, its product with the sum: three roundings; the addition to the base; the output's own
+    tol = np.abs(p) * 3 * 2.0**-24 + (np.abs(want) * 2.0**-24 if base else 0) + np.abs(want) * torch.finfo(t).eps / 2 * (1 + 2.0**-8) + (2.0**-25 if kind == "f16" else 0)
+    assert y.dtype == t and (np.abs(got - want) <= tol).all(), np.argwhere(np.abs(got - want) > tol)[:5]
+    if base:
+        out = b.to(DEV).clone()
+        assert moeq.moe_matmul_q8(q, weights, base=out, y=out) is out and torch.equal(out, y)
+
+
+def test_products_refuse_other_lengths_and_leave_other_rows():
+    q = moeq.moe_quantize_rows(torch.randn((5, 300), device=DEV))
+    w = moeq.moe_quantize_rows(torch.randn((70, 300), device=DEV))
+    buf = torch.full((7, 80), 5.0, device=DEV)
+    y = moeq.moe_matmul_q8(q, w, y=buf[1:6, :70])
+    assert torch.equal(y, moeq.moe_matmul_q8(q, w)) and (buf[0] == 5).all() and (buf[6] == 5).all() and (buf[:, 70:] == 5).all()
+    with pytest.raises(moeq.MoeqError):
+        moeq.moe_matmul_q8(q, moeq.moe_quantize_rows(torch.randn((70, 301), device=DEV)))
+    assert moeq.moe_matmul_q8(moeq.moe_quantize_rows(torch.zeros((0, 300), device=DEV)), w).shape == (0, 70)
+
+
+def test_products_of_a_row_of_nan():
+    x = torch.randn((40, 500), device=DEV)
+    w = moeq.moe_quantize_rows(torch.randn((90, 500), device=DEV))
+    want = moeq.moe_matmul_q8(moeq.moe_quantize_rows(x), w)
+    x[7, 3] = float("nan")
+    y = moeq.moe_matmul_q8(moeq.moe_quantize_rows(x), w)
+    assert y[7].isnan().all() and torch.equal(y[:7], want[:7]) and torch.equal(y[8:], want[8:])
+
+
+def test_graphs_of_packing_and_products():
+    x, w = torch.randn((37, 1000), device=DEV), moeq.moe_quantize_rows(torch.randn((300, 1000), device=DEV))
+    run = lambda: (moeq.moe_unpack8(moeq.moe_pack8(x)), moeq.moe_matmul_q8(moeq.moe_quantize_rows(x), w))
+    want = run()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = run()
+    for _ in range(3):
+        for t in got:
+            t.fill_(3.0)
+        g.replay()
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
