@@ -5,8 +5,8 @@
 // Four products' worth of work forward and backward are matrix products (tiles.h); what stands between them happens on their sums:
 // the product of x with both weights takes their rows in turns of 32, so that a and b of an element meet in one lane; that of dy leaves da,
 // db and h. h, da and db are rounded to the type (as a program in that type holds them): an output has that rounding and its own. They lie
-// in the workspace, rows of a multiple of 64 elements, zeros behind the last column and in rows up to a multiple of 64, which later
-// products sum over; da and db of a row side by side, so that dx is one product through both weights.
+// in the workspace, rows of whole steps (64 elements, 32 of fp32), zeros behind the last column and in rows up to a multiple of 64,
+// which later products sum over; da and db of a row side by side, so that dx is one product through both weights.
 #pragma once
 #include <algorithm>
 
@@ -137,13 +137,14 @@ struct Act {
   }
 };
 
-inline int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
+inline int64_t up_to(int64_t n, int64_t by) { return (n + by - 1) / by * by; }
 // The workspace's parts, each at a multiple of 256 bytes.
 struct FfnPlan {
   int64_t Tp, Fp, Dp;
   size_t h, dab, x, ab, bytes;
-  FfnPlan(const FfnArgs& a, bool backward) : Tp(padded(a.T)), Fp(padded(a.F)), Dp(padded(a.D)) {
+  FfnPlan(const FfnArgs& a, bool backward) : Tp(up_to(a.T, 64)) {
     const size_t e = dtype_bytes(a.dtype);
+    Fp = up_to(a.F, kStepBytes / e), Dp = up_to(a.D, kStepBytes / e);      // (whole steps, each with a column that there is)
     size_t at = 0;
     auto take = [&](size_t n) { const size_t here = at; at += (n + 255) / 256 * 256; return here; };
     h = take(Tp * Fp * e);
@@ -166,7 +167,7 @@ template <typename T> int32_t steps_of(int64_t k) { return (int32_t)((k + kStep<
 template <typename T>
 hipError_t up(const FfnArgs& a, const void* x, int64_t x_stride, const Up<T>& epi, hipStream_t st) {
   Product p = {side<T>(x, x_stride, a.T, a.D), side<T>(a.w_in, a.D, a.F, a.D, a.w_gate), steps_of<T>(a.D), 0};
-  return launch_tile<T, true, true, 128, 128, 2, 2, kOne, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, epi, st);
+  return launch_tile<T, true, true, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, epi, st);
 }
 
 template <typename T>
@@ -179,7 +180,7 @@ hipError_t ffn_forward(const FfnArgs& a, hipStream_t st) {
   auto down = [&](auto o) {
     using O = decltype(o);
     Store<O> out = {{(O*)a.y, nullptr}, a.y_stride, (const O*)a.base, a.base_stride, a.T, a.D};
-    return launch_tile<T, true, true, 128, 128, 2, 2, kOne, kOne>(p, a.T, a.D, 1, out, st);
+    return launch_tile<T, true, true, kOne>(p, a.T, a.D, 1, out, st);
   };
   if (a.y_dtype == a.dtype) return down(T{});
   return down(0.f);
@@ -210,20 +211,20 @@ hipError_t ffn_backward(const FfnArgs& a, hipStream_t st) {
     const bool eight = a.keep == MOEQ_KEEP_8;
     Act<T> e = {eight ? nullptr : ab, eight ? (const int8_t*)a.ab : nullptr, a.ab_exps, dab, h, a.T, a.F, Tp, Fp};
     Product p = {side<T>(a.dy, a.dy_stride, a.T, a.D), side<T>(a.w_out, a.F, a.F, a.D), steps_of<T>(a.D), 0};
-    if (hipError_t s = launch_tile<T, true, false, 128, 128, 2, 2, kOne, kOne>(p, Tp, Fp, 1, e, st); s != hipSuccess) return s;
+    if (hipError_t s = launch_tile<T, true, false, kOne>(p, Tp, Fp, 1, e, st); s != hipSuccess) return s;
     if (a.dx) {
       Product q = {side<T>(dab, 2 * plan.Fp, Tp, 2 * Fp), side<T>(a.w_in, a.D, a.D, a.F, a.w_gate), 2 * steps_of<T>(Fp), steps_of<T>(Fp)};
       Store<T> out = {{(T*)a.dx, nullptr}, a.dx_stride, nullptr, 0, a.T, a.D};
-      if (hipError_t s = launch_tile<T, true, false, 128, 128, 2, 2, kOne, kBehind>(q, a.T, a.D, 1, out, st); s != hipSuccess) return s;
+      if (hipError_t s = launch_tile<T, true, false, kBehind>(q, a.T, a.D, 1, out, st); s != hipSuccess) return s;
     }
   }
   // (the workspace's rows are zero from row T on, those of x and dy end there)
   Product p = {side<T>(dab, 2 * plan.Fp, a.F, Tp, dab + Fp), side<T>(x, x_stride, a.D, a.T), steps_of<T>(a.T), 0};
   Store<T> out = {{(T*)a.dw_in, (T*)a.dw_gate}, a.D, nullptr, 0, a.F, a.D};
-  if (hipError_t s = launch_tile<T, false, false, 128, 128, 2, 2, kOne, kOne>(p, a.F, a.D, 2, out, st); s != hipSuccess) return s;
+  if (hipError_t s = launch_tile<T, false, false, kOne>(p, a.F, a.D, 2, out, st); s != hipSuccess) return s;
   p.a = side<T>(a.dy, a.dy_stride, a.D, a.T), p.b = side<T>(h, plan.Fp, a.F, Tp);
   out = {{(T*)a.dw_out, nullptr}, a.F, nullptr, 0, a.D, a.F};
-  return launch_tile<T, false, false, 128, 128, 2, 2, kOne, kOne>(p, a.D, a.F, 1, out, st);
+  return launch_tile<T, false, false, kOne>(p, a.D, a.F, 1, out, st);
 }
 
 }  // namespace tiles

@@ -201,6 +201,186 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(Product p, Epi epi) {
   }
 }
 
+constexpr int kLdsDone = 0xc07f;      // s_waitcnt lgkmcnt(0), no wait for the others
+
+// ---- straight to LDS: sides whose rows begin at multiples of 16 bytes, whole pieces of 16 bytes long ----
+__device__ const uint4 kZeros[1] = {};
+
+// A tile's way to LDS (global_load_lds: a wavefront's 64 pieces to 1 KB in a row, so the swizzle is in which piece a lane asks for). The
+// step that a tile begins with is fetched with a whole address for each lane, so that pieces behind the end of the sum are zeros; the
+// others are whole, at one scalar address and a lane's offset.
+template <typename T, bool ROWS, int R, int NT, Made MADE>
+struct Fetch {
+  static constexpr int kPieces = R * 8 / NT, kWide = ROWS ? 8 : R / kPiece<T>;
+  uint32_t off[kPieces];
+  const char* base[2];
+  int64_t by;            // bytes from a step to the next
+  uint32_t lds;          // of this wavefront's first piece
+  int k;
+  __device__ __forceinline__ static int row(int j) { return (threadIdx.x + j * NT) / kWide; }
+  __device__ __forceinline__ static int at(int j) {      // which piece of its row lies in a lane's place
+    const int pos = (threadIdx.x + j * NT) % kWide, r = row(j);
+    if constexpr (ROWS) return pos ^ (r >> 1 & 7);
+    else if constexpr (sizeof(T) == 4) return pos;
+    else return ((pos >> 2) ^ (R >= 128 ? r & 3 : r >> 1 & 1)) << 2 | (pos & 3);
+  }
+  __device__ __forceinline__ void init(const Side& s, int z, int n0, uint32_t lds_base) {
+    k = s.k;
+    by = ROWS ? kStepBytes : kStep<T> * s.stride;
+    lds = lds_base + threadIdx.x / 64 * 1024;
+    const int first = MADE == kTurns ? n0 / 2 : n0;      // of this side's rows
+    const int64_t skip = ROWS ? first * s.stride : first * (int64_t)sizeof(T);
+    base[0] = s.p[MADE == kOne ? z : 0] + skip;
+    base[1] = s.p[1] + skip;
+    const int last = ROWS ? s.n - 1 - first : (s.n - first) / kPiece<T> - 1;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const int r = MADE == kTurns ? row(j) / 64 * 32 + row(j) % 32 : row(j);
+      off[j] = ROWS ? (uint32_t)min(r, last) * (uint32_t)s.stride + at(j) * 16 : (uint32_t)r * (uint32_t)s.stride + min(at(j), last) * 16;
+    }
+  }
+  __device__ __forceinline__ const char* start(int which, int step) const { return base[which] + step * by; }
+  static __device__ __forceinline__ int matrix(int j, int which) { return MADE == kTurns ? row(j) / 32 % 2 : which; }
+  // The step that comes first.
+  __device__ __forceinline__ void first(const Side& s, int step, int first_steps, int buffer) {
+    const int which = MADE == kBehind && step >= first_steps, k0 = (which ? step - first_steps : step) * kStep<T>;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+      const bool there = k0 + (ROWS ? at(j) * kPiece<T> : row(j)) < k;
+      const char* p = there ? base[matrix(j, which)] + (which ? step - first_steps : step) * by + off[j] : (const char*)kZeros;
+      asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(p), "s"(lds + buffer + j * NT * 16) : "memory");
+    }
+  }
+  // Piece j of a whole step that begins at `from` (of the matrix that this piece is of).
+  __device__ __forceinline__ void piece(int j, const char* from, int buffer) const {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off[j]), "s"(from), "s"(lds + buffer + j * NT * 16) : "memory");
+  }
+  // Offsets of a step whose rows end before it does (columns, behind which the other side has zeros): its last row again.
+  __device__ __forceinline__ void rows_to(const Side& s, int n0, int rows) {
+    const int last = (s.n - n0) / kPiece<T> - 1;
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) off[j] = (uint32_t)min(row(j), rows - 1) * (uint32_t)s.stride + min(at(j), last) * 16;
+  }
+};
+
+// As k_tile. Two steps are in LDS: while one is multiplied, the pieces of the next are on their way. A slice's operands are read while
+// the slice before is multiplied; the last slice of a step stands around the one barrier, so that the reads behind it and the requests
+// into the step that is now done have matrix instructions to hide behind. Steps run from the last to the first.
+template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, class Epi>
+__global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
+  constexpr int NT = 64 * WM * WN, MB = BM / WM / 32, NB = BN / WN / 32, kBuffer = (BM + BN) * kStepBytes;
+  using FA = Fetch<T, A_ROWS, BM, NT, A_MADE>;
+  using FB = Fetch<T, B_ROWS, BN, NT, B_MADE>;
+  constexpr int LA = FA::kPieces, L = LA + FB::kPieces, kEach = (MB + NB + MB - 1) / MB;      // requests of a step; operands read with a row of products
+  constexpr int kAsk = (L + 2 * MB - 2) / (2 * MB - 1);      // requests with a row of products: all of them within the first 2 MB - 1 rows behind the barrier
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  int tm, tn;
+  tile_of(p, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN, z = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  const int share = (p.steps + gridDim.z - 1) / gridDim.z, from = blockIdx.z * share, to = min(from + share, p.steps);
+  Sums<T> acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = Sums<T>{};
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  FA a;
+  FB b;
+  a.init(p.a, z, m0, __builtin_amdgcn_readfirstlane(lds_base));
+  b.init(p.b, 0, n0, __builtin_amdgcn_readfirstlane(lds_base + BM * kStepBytes));
+  a.lds = __builtin_amdgcn_readfirstlane(a.lds), b.lds = __builtin_amdgcn_readfirstlane(b.lds);
+  i32x4 u[2][MB], v[2][NB];
+  // Where step `step`'s requests go: its scalar addresses, computed once.
+  const char *ask_a = nullptr, *ask_b[2] = {nullptr, nullptr};
+  auto aim = [&](int step) {
+    ask_a = a.start(0, step);
+    if constexpr (B_MADE == kBehind) {
+      const int which = step >= p.first_steps, in = which ? step - p.first_steps : step;
+      ask_b[0] = b.start(which, in);
+      const int rows = b.k - in * kStep<T>;
+      if (rows < kStep<T>) b.rows_to(p.b, n0, rows);
+      else if (rows < 2 * kStep<T>) b.rows_to(p.b, n0, kStep<T>);      // (behind such a step: whole ones again)
+    } else {
+      ask_b[0] = b.start(0, step), ask_b[1] = b.start(1, step);
+    }
+  };
+  auto ask = [&](int r, int buffer) {      // the requests that go with row r of products behind the barrier
+#pragma unroll
+    for (int j = r * kAsk; j < (r + 1) * kAsk && j < L; ++j) {
+      if (j < LA) a.piece(j, ask_a, buffer);
+      else b.piece(j - LA, ask_b[B_MADE == kTurns ? (j - LA) * (NT / 8) / 32 % 2 : 0], buffer);
+    }
+  };
+  auto read = [&](int set, int r, const char* at, int slice) {      // the operands that are read with row r of products: those of b first
+#pragma unroll
+    for (int j = r * kEach; j < (r + 1) * kEach && j < MB + NB; ++j) {
+      if (j < NB) v[set][j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice);
+      else u[set][j - NB] = operand<T, A_ROWS, BM>(at, wm + (j - NB) * 32, slice);
+    }
+  };
+  if (from < to) {
+    int step = to - 1, buffer = 0;
+    a.first(p.a, step, p.first_steps, 0);
+    b.first(p.b, step, p.first_steps, 0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (step > from) {
+      aim(step - 1);
+#pragma unroll
+      for (int r = 0; r < MB - 1; ++r) ask(r, kBuffer);
+    }
+#pragma unroll
+    for (int r = 0; r < MB; ++r) read(0, r, lds, 0);
+    auto multiply = [&](auto more_) {      // (a step's last one apart: what waits for which reads is then known without a branch between)
+      constexpr bool more = decltype(more_)::value;
+      const char *here = lds + buffer * kBuffer, *next = lds + (buffer ^ 1) * kBuffer;
+      const bool after = step - 1 > from;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int cur = s % 2;
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (s < 3) {
+            read(cur ^ 1, i, here, s + 1);
+            if (s < 2 && more) ask(s * MB + i + MB - 1, (buffer ^ 1) * kBuffer);
+          } else if (more) {
+            if (i == 1) {
+              __builtin_amdgcn_s_waitcnt(kLdsDone);      // (this wavefront's reads of the buffer that is asked into next)
+              asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+              __builtin_amdgcn_s_barrier();
+              asm volatile("" ::: "memory");
+              if (after) aim(step - 2);
+            }
+            if (i >= 1) {
+              read(0, i - 1, next, 0);
+              if (i == MB - 1) read(0, MB - 1, next, 0);
+              if (after) ask(i - 1, buffer * kBuffer);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < NB; ++j) mma(acc[i][j], v[cur][j], u[cur][i], T{});
+        }
+      }
+    };
+    for (; step > from; --step, buffer ^= 1) multiply(std::true_type{});
+    multiply(std::false_type{});
+  }
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const int m = m0 + wm + i * 32 + lane % 32;
+    if constexpr (B_MADE == kTurns) {
+#pragma unroll
+      for (int j = 0; j < NB; j += 2) epi.pair(m, (n0 + wn + j * 32) / 2, lane / 32, acc[i][j], acc[i][j + 1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) epi.block(z, m, n0 + wn + j * 32, lane / 32, acc[i][j]);
+    }
+  }
+}
+
 // The n of a lane's sums 4 q to 4 q + 3.
 __device__ __forceinline__ int column(int n, int half, int q) { return n + q * 8 + half * 4; }
 
@@ -251,10 +431,20 @@ struct Store {
   }
 };
 
-template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, class Epi>
-hipError_t launch_tile(Product p, int M, int N, int batch, const Epi& epi, hipStream_t st) {
+// Whether a side can go straight to LDS: every row that is read (rows of the product or of the sum) at a multiple of 16 bytes and whole
+// pieces of them long, the rows of a tile within 2^31 bytes.
+template <typename T>
+bool straight(const Side& s, bool rows, Made made) {
+  const int32_t count = rows ? s.n : s.k, length = rows ? s.k : s.n;
+  return (uintptr_t)s.p[0] % 16 == 0 && (made == kOne || (uintptr_t)s.p[1] % 16 == 0) && length % kPiece<T> == 0 && (count == 1 || (s.stride % 16 == 0 && s.stride < 1 << 23));
+}
+
+template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, bool DIRECT, class Epi>
+hipError_t launch_as(Product p, int M, int N, int batch, const Epi& epi, hipStream_t st) {
   constexpr int kLds = 2 * (BM + BN) * kStepBytes;
-  const auto kernel = k_tile<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
+  void (*kernel)(Product, Epi);
+  if constexpr (DIRECT) kernel = k_direct<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
+  else kernel = k_tile<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
   if constexpr (kLds > 64 * 1024) {
     static const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (e != hipSuccess) return e;
@@ -262,6 +452,19 @@ hipError_t launch_tile(Product p, int M, int N, int batch, const Epi& epi, hipSt
   p.tiles_m = (M + BM - 1) / BM, p.tiles_n = (N + BN - 1) / BN;
   kernel<<<dim3(p.tiles_m * p.tiles_n, batch), 64 * WM * WN, kLds, st>>>(p, epi);
   return hipGetLastError();
+}
+
+// M x N outputs of each of `batch` products.
+template <typename T, bool A_ROWS, bool B_ROWS, Made B_MADE, class Epi>
+hipError_t launch_tile(Product p, int M, int N, int batch, const Epi& epi, hipStream_t st) {
+  if (p.a.n == 1 && A_ROWS) p.a.stride = 0;      // (of a single row: any)
+  if (p.a.k == 1 && !A_ROWS) p.a.stride = 0;
+  if (p.b.k == 1 && !B_ROWS) p.b.stride = 0;
+  const bool direct = straight<T>(p.a, A_ROWS, batch == 2 ? kTurns : kOne) && straight<T>(p.b, B_ROWS, B_MADE);
+  if (!direct) return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, kOne, B_MADE, false>(p, M, N, batch, epi, st);
+  const int64_t large = (int64_t)((M + 255) / 256) * ((N + 255) / 256) * batch;
+  if (large >= 96) return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 2, kOne, B_MADE, true>(p, M, N, batch, epi, st);
+  return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, kOne, B_MADE, true>(p, M, N, batch, epi, st);
 }
 
 }  // namespace tiles
