@@ -24,21 +24,19 @@ __device__ __forceinline__ float sigmoid(float a) {
 }
 
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
-// 32 columns of a row (16 of them here, the rest in lane ^ 32) to codes and their exponent, as k_pack8 does.
+// Eight columns of a block of 32, whose others the lanes of a quad have, to codes and their exponent, as k_pack8 does.
 template <typename T>
-__device__ __forceinline__ int to_codes(const f32x16& c, int n, int half, int N, int8_t (&code)[16]) {
+__device__ __forceinline__ int to_codes(const float (&v)[8], int n, int N, int8_t (&code)[8]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float v = column(n, half, i / 4) + i % 4 < N ? c[i] : 0.f;
-    top = max(top, __builtin_bit_cast(uint32_t, v) & 0x7fffffffu);
-  }
-  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  for (int i = 0; i < 8; ++i) top = max(top, n + i < N ? __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu : 0u);
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
   const bool nan = top >= 0x7f800000u;
   const int e = max((int)(top >> 23) - 127 - 6, std::is_same<T, _Float16>::value ? -24 : -126);
   const float up = nan ? 0.f : power(-e);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) code[i] = nan ? 0 : (int8_t)fminf(fmaxf(rintf(c[i] * up), -127.f), 127.f);
+  for (int i = 0; i < 8; ++i) code[i] = nan ? 0 : (int8_t)fminf(fmaxf(rintf(v[i] * up), -127.f), 127.f);
   return nan ? kPackNan : e;
 }
 
@@ -51,42 +49,34 @@ struct Up {
   int32_t keep;
   T* ab;                    // MOEQ_KEEP_OWN
   int8_t *codes, *exps;     // MOEQ_KEEP_8
-  __device__ __forceinline__ void keep8(int which, int m, int f, int half, const f32x16& c) const {
-    int8_t code[16];
-    const int e = to_codes<T>(c, f, half, F, code);      // (lanes of every row, also behind the last: lanes exchange)
+  struct Beside {};
+  __device__ __forceinline__ void ask(Beside&, int, int) const {}
+  __device__ __forceinline__ void keep8(int which, int m, int f, const float (&v)[8]) const {
+    int8_t code[8];
+    const int e = to_codes<T>(v, f, F, code);      // (by every lane, also of rows behind the last: lanes exchange)
     if (m >= T_ || f >= F) return;
     const int64_t row = (int64_t)which * T_ + m;
+    if (f + 8 <= F) {
+      __builtin_memcpy(codes + row * F + f, code, 8);
+    } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int at = column(f, half, q);
-      if (at + 4 <= F) {
-        __builtin_memcpy(codes + row * F + at, code + 4 * q, 4);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (at + i < F) codes[row * F + at + i] = code[4 * q + i];
-      }
+      for (int i = 0; i < 8; ++i)
+        if (f + i < F) codes[row * F + f + i] = code[i];
     }
-    if (half == 0) exps[row * ((F + kPackBlock - 1) / kPackBlock) + f / kPackBlock] = (int8_t)e;
+    if (f % kPackBlock == 0) exps[row * ((F + kPackBlock - 1) / kPackBlock) + f / kPackBlock] = (int8_t)e;
   }
-  __device__ __forceinline__ void pair(int m, int f, int half, const f32x16& a, const f32x16& b) const {
-    if (keep == MOEQ_KEEP_8) keep8(0, m, f, half, a), keep8(1, m, f, half, b);
-    if (m >= Tp) return;
+  __device__ __forceinline__ void pair(const Beside&, int m, int f, const float (&a)[8], const float (&b)[8]) const {
+    if (keep == MOEQ_KEEP_8) keep8(0, m, f, a), keep8(1, m, f, b);
+    if (m >= Tp || f >= Fp) return;
+    if (h) {
+      float w[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int at = column(f, half, q);
-      if (at >= Fp) continue;
-      float u[4], v[4], w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        u[i] = a[4 * q + i], v[i] = b[4 * q + i];
-        w[i] = m < T_ && at + i < F ? u[i] * sigmoid<T>(u[i]) * v[i] : 0.f;
-      }
-      if (h) store_n(h + m * pitch + at, w);
-      if (keep == MOEQ_KEEP_OWN && m < T_ && at < F) {
-        store4(ab + (int64_t)m * F, at, F, u);
-        store4(ab + ((int64_t)T_ + m) * F, at, F, v);
-      }
+      for (int i = 0; i < 8; ++i) w[i] = m < T_ && f + i < F ? a[i] * sigmoid<T>(a[i]) * b[i] : 0.f;
+      store_n(h + m * pitch + f, w);
+    }
+    if (keep == MOEQ_KEEP_OWN && m < T_ && f < F) {
+      store8(ab + (int64_t)m * F, f, F, a);
+      store8(ab + ((int64_t)T_ + m) * F, f, F, b);
     }
   }
 };
@@ -98,42 +88,52 @@ struct Act {
   const int8_t *codes, *exps;      // in ab's place
   T *dab, *h;                      // [Tp][2 Fp], [Tp][Fp]
   int32_t T_, F, Tp, Fp;
-  __device__ __forceinline__ void get(int which, int m, int at, float unit, float (&v)[4]) const {
-    const int64_t row = (int64_t)which * T_ + m;
-    if (!codes) return load4(v, ab + row * F, at, F);
+  struct Beside {
+    T ab[2][8];
+    int8_t codes[2][8], exps[2];
+  };
+  template <typename E>
+  __device__ __forceinline__ void get(E (&v)[8], const E* row, int f) const {
+    if (f + 8 <= F) {
+      __builtin_memcpy(v, row + f, sizeof(v));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = at + i < F ? (float)codes[row * F + at + i] * unit : 0.f;
+      for (int i = 0; i < 8; ++i) v[i] = f + i < F ? row[f + i] : (E)0;
+    }
   }
-  __device__ __forceinline__ void block(int, int m, int f, int half, const f32x16& c) const {
-    if (m >= Tp) return;
-    float unit[2] = {1.f, 1.f};
-    if (codes && m < T_ && f < F) {
+  __device__ __forceinline__ void ask(Beside& s, int m, int f) const {
+    if (m >= T_ || f >= F) return;
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const int e = exps[((int64_t)w * T_ + m) * ((F + kPackBlock - 1) / kPackBlock) + f / kPackBlock];
-        unit[w] = e == kPackNan ? __builtin_nanf("") : power(e);
+    for (int w = 0; w < 2; ++w) {
+      const int64_t row = (int64_t)w * T_ + m;
+      if (codes) {
+        get(s.codes[w], codes + row * F, f);
+        s.exps[w] = exps[row * ((F + kPackBlock - 1) / kPackBlock) + f / kPackBlock];
+      } else {
+        get(s.ab[w], ab + row * F, f);
       }
     }
+  }
+  __device__ __forceinline__ void row(const Beside& s, int, int m, int f, const float (&c)[8]) const {
+    if (m >= Tp || f >= Fp) return;
+    float da[8] = {}, db[8] = {}, hh[8] = {};
+    if (m < T_ && f < F) {
+      float unit[2] = {1.f, 1.f};
+      if (codes) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int at = column(f, half, q);
-      if (at >= Fp) continue;
-      float da[4] = {}, db[4] = {}, hh[4] = {};
-      if (m < T_ && at < F) {
-        float a[4], b[4];
-        get(0, m, at, unit[0], a);
-        get(1, m, at, unit[1], b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (at + i >= F) continue;
-          const float s = sigmoid<T>(a[i]), g = a[i] * s, dh = c[4 * q + i];
-          da[i] = dh * b[i] * (s + g * (1.f - s)), db[i] = dh * g, hh[i] = g * b[i];
-        }
+        for (int w = 0; w < 2; ++w) unit[w] = s.exps[w] == kPackNan ? __builtin_nanf("") : power(s.exps[w]);
       }
-      store_n(dab + (int64_t)m * 2 * Fp + at, da);
-      store_n(dab + (int64_t)m * 2 * Fp + Fp + at, db);
-      store_n(h + (int64_t)m * Fp + at, hh);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (f + i >= F) continue;
+        const float a = codes ? (float)s.codes[0][i] * unit[0] : (float)s.ab[0][i], b = codes ? (float)s.codes[1][i] * unit[1] : (float)s.ab[1][i];
+        const float sg = sigmoid<T>(a), g = a * sg, dh = c[i];
+        da[i] = dh * b * (sg + g * (1.f - sg)), db[i] = dh * g, hh[i] = g * b;
+      }
     }
+    store_n(dab + (int64_t)m * 2 * Fp + f, da);
+    store_n(dab + (int64_t)m * 2 * Fp + Fp + f, db);
+    store_n(h + (int64_t)m * Fp + f, hh);
   }
 };
 

@@ -16,23 +16,22 @@ struct Scaled {
   int64_t base_stride;
   const float *xs, *ws;
   int32_t T, N;
-  __device__ __forceinline__ void block(int, int m, int n, int half, const i32x16& c) const {
-    if (m >= T) return;
-    const float s = xs[m];
+  struct Beside { float x, w[8], base[8]; };
+  __device__ __forceinline__ void ask(Beside& b, int m, int n) const {
+    if (m >= T || n >= N) return;
+    b.x = xs[m];
+    load8(b.w, ws, n, N);
+    if (base) load8(b.base, base + m * base_stride, n, N);
+  }
+  __device__ __forceinline__ void row(const Beside& b, int, int m, int n, const int32_t (&c)[8]) const {
+    if (m >= T || n >= N) return;
+    float v[8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int at = column(n, half, q);
-      if (at >= N) continue;
-      float v[4], w[4], b[4] = {};
-      load4(w, ws, at, N);
-      if (base) load4(b, base + m * base_stride, at, N);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = (float)c[4 * q + i] * (s * w[i]);
-        v[i] = base ? b[i] + p : p;
-      }
-      store4(y + m * stride, at, N, v);
+    for (int i = 0; i < 8; ++i) {
+      const float p = (float)c[i] * (b.x * b.w[i]);
+      v[i] = base ? b.base[i] + p : p;
     }
+    store8(y + m * stride, n, N, v);
   }
 };
 

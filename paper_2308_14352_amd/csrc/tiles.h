@@ -139,6 +139,100 @@ __device__ __forceinline__ void tile_of(const Product& p, int& tm, int& tn) {
   tn = in / rows;
 }
 
+// Eight consecutive elements of a row that ends at `limit`, from or to any alignment of an element.
+template <typename T>
+__device__ __forceinline__ void load8(float (&v)[8], const T* row, int at, int limit) {
+  if (at + 8 <= limit) {
+    load_n(v, row + at);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = at + i < limit ? (float)row[at + i] : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* row, int at, int limit, const float (&v)[8]) {
+  if (at + 8 <= limit) {
+    store_n(row + at, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (at + i < limit) row[at + i] = (T)v[i];
+  }
+}
+
+// out[z][m][n] = base[m][n] + sums, in O.
+template <typename O>
+struct Store {
+  O* out[2];
+  int64_t stride;
+  const O* base;
+  int64_t base_stride;
+  int32_t M, N;
+  struct Beside { float base[8]; };
+  __device__ __forceinline__ void ask(Beside& b, int m, int n) const {
+    if (base && m < M && n < N) load8(b.base, base + m * base_stride, n, N);
+  }
+  __device__ __forceinline__ void row(const Beside& b, int z, int m, int n, float (&v)[8]) const {
+    if (m >= M || n >= N) return;
+    if (base) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += b.base[i];
+    }
+    store8(out[z] + m * stride, n, N, v);
+  }
+};
+
+// The sums to the operator's epilogue, by each wavefront for itself: 32 rows at a time through LDS, so that a lane has eight consecutive
+// columns of a row and consecutive lanes consecutive pieces (16 bytes of 16-bit elements; straight from the sums a store is 8 bytes of each
+// of 32 rows: the gradient through the activation spent as long on its stores as on the product). What the epilogue reads beside the sums
+// is asked for four pieces at a time.
+constexpr int finish_bytes(int nb) { return 32 * (nb * 32 + 4) * 4; }      // of a wavefront (rows 16 bytes apart on the banks)
+template <typename T, int MB, int NB, Made MADE, class Epi>
+__device__ __forceinline__ void finish(const Sums<T> (&acc)[MB][NB], char* lds, int wave, int z, int m0, int n0, const Epi& epi) {
+  constexpr int kRow = NB * 32 + 4, kWide = NB * 32 / 8 / (MADE == kTurns ? 2 : 1), kPieces = 32 * kWide / 64, kGroup = kPieces < 4 ? kPieces : 4;
+  using Word = std::conditional_t<std::is_same<T, int8_t>::value, int32_t, float>;
+  Word* at = (Word*)(lds + wave * finish_bytes(NB));
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const Word w[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        __builtin_memcpy(__builtin_assume_aligned(at + lane % 32 * kRow + j * 32 + q * 8 + lane / 32 * 4, 16), w, 16);
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int g = 0; g < kPieces; g += kGroup) {
+      typename Epi::Beside beside[kGroup];
+      int m[kGroup], n[kGroup], row[kGroup], col[kGroup];
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) {
+        const int c = (g + e) * 64 + lane, piece = c % kWide;
+        row[e] = c / kWide;
+        m[e] = m0 + i * 32 + row[e];
+        col[e] = MADE == kTurns ? piece / 4 * 64 + piece % 4 * 8 : piece * 8;
+        n[e] = MADE == kTurns ? n0 / 2 + piece * 8 : n0 + piece * 8;
+        epi.ask(beside[e], m[e], n[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) {
+        Word v[8];
+        __builtin_memcpy(v, __builtin_assume_aligned(at + row[e] * kRow + col[e], 16), 32);
+        if constexpr (MADE == kTurns) {
+          Word w[8];
+          __builtin_memcpy(w, __builtin_assume_aligned(at + row[e] * kRow + col[e] + 32, 16), 32);
+          epi.pair(beside[e], m[e], n[e], v, w);
+        } else {
+          epi.row(beside[e], z, m[e], n[e], v);
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // One tile: BM x BN by WM x WN wavefronts. blockIdx.y: the matrix of a (kOne), blockIdx.z of gridDim.z: the share of the sum.
 template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, class Epi>
 __global__ __launch_bounds__(64 * WM * WN) void k_tile(Product p, Epi epi) {
@@ -188,17 +282,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(Product p, Epi epi) {
     }
     __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int m = m0 + wm + i * 32 + lane % 32;
-    if constexpr (B_MADE == kTurns) {
-#pragma unroll
-      for (int j = 0; j < NB; j += 2) epi.pair(m, (n0 + wn + j * 32) / 2, lane / 32, acc[i][j], acc[i][j + 1]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < NB; ++j) epi.block(z, m, n0 + wn + j * 32, lane / 32, acc[i][j]);
-    }
-  }
+  __syncthreads();
+  finish<T, MB, NB, B_MADE>(acc, lds, wave, z, m0 + wm, n0 + wn, epi);
 }
 
 constexpr int kLdsDone = 0xc07f;      // s_waitcnt lgkmcnt(0), no wait for the others
@@ -264,15 +349,17 @@ struct Fetch {
 };
 
 // As k_tile. Two steps are in LDS: while one is multiplied, the pieces of the next are on their way. A slice's operands are read while
-// the slice before is multiplied; the last slice of a step stands around the one barrier, so that the reads behind it and the requests
-// into the step that is now done have matrix instructions to hide behind. Steps run from the last to the first.
+// the slice before is multiplied, one between two matrix instructions, and so are the next step's pieces asked for, in the last slice
+// of a step, behind the one barrier, and in the first of the next. Steps run from the last to the first. Lines asked for into L2 four
+// steps ahead, by a dword of each, cost more than they saved (sum of 28672, 256 tiles: 844 us, without 817).
 template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, class Epi>
 __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   constexpr int NT = 64 * WM * WN, MB = BM / WM / 32, NB = BN / WN / 32, kBuffer = (BM + BN) * kStepBytes;
   using FA = Fetch<T, A_ROWS, BM, NT, A_MADE>;
   using FB = Fetch<T, B_ROWS, BN, NT, B_MADE>;
-  constexpr int LA = FA::kPieces, L = LA + FB::kPieces, kEach = (MB + NB + MB - 1) / MB;      // requests of a step; operands read with a row of products
-  constexpr int kAsk = (L + 2 * MB - 2) / (2 * MB - 1);      // requests with a row of products: all of them within the first 2 MB - 1 rows behind the barrier
+  constexpr int LA = FA::kPieces, L = LA + FB::kPieces, kSlots = MB * NB;      // requests of a step; matrix instructions of a slice
+  constexpr int kGap = kSlots >= 2 * (MB + NB) ? 2 : 1;      // where there is room, a read and a request go with instructions of their own
+  static_assert(2 * (kSlots / kGap) >= L && kSlots / kGap >= MB + NB, "a step's requests go with two slices, a slice's reads with one");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int tm, tn;
   tile_of(p, tm, tn);
@@ -305,19 +392,13 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
       ask_b[0] = b.start(0, step), ask_b[1] = b.start(1, step);
     }
   };
-  auto ask = [&](int r, int buffer) {      // the requests that go with row r of products behind the barrier
-#pragma unroll
-    for (int j = r * kAsk; j < (r + 1) * kAsk && j < L; ++j) {
-      if (j < LA) a.piece(j, ask_a, buffer);
-      else b.piece(j - LA, ask_b[B_MADE == kTurns ? (j - LA) * (NT / 8) / 32 % 2 : 0], buffer);
-    }
+  auto ask = [&](int j, int buffer) {      // one request
+    if (j < LA) a.piece(j, ask_a, buffer);
+    else if (j < L) b.piece(j - LA, ask_b[B_MADE == kTurns ? (j - LA) * (NT / 8) / 32 % 2 : 0], buffer);
   };
-  auto read = [&](int set, int r, const char* at, int slice) {      // the operands that are read with row r of products: those of b first
-#pragma unroll
-    for (int j = r * kEach; j < (r + 1) * kEach && j < MB + NB; ++j) {
-      if (j < NB) v[set][j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice);
-      else u[set][j - NB] = operand<T, A_ROWS, BM>(at, wm + (j - NB) * 32, slice);
-    }
+  auto read = [&](int set, int j, const char* at, int slice) {      // one operand: those of b first
+    if (j < NB) v[set][j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice);
+    else if (j < NB + MB) u[set][j - NB] = operand<T, A_ROWS, BM>(at, wm + (j - NB) * 32, slice);
   };
   if (from < to) {
     int step = to - 1, buffer = 0;
@@ -329,10 +410,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
     if (step > from) {
       aim(step - 1);
 #pragma unroll
-      for (int r = 0; r < MB - 1; ++r) ask(r, kBuffer);
+      for (int j = 0; j < kSlots / kGap; ++j) ask(j, kBuffer);
     }
 #pragma unroll
-    for (int r = 0; r < MB; ++r) read(0, r, lds, 0);
+    for (int j = 0; j < NB + MB; ++j) read(0, j, lds, 0);
     auto multiply = [&](auto more_) {      // (a step's last one apart: what waits for which reads is then known without a branch between)
       constexpr bool more = decltype(more_)::value;
       const char *here = lds + buffer * kBuffer, *next = lds + (buffer ^ 1) * kBuffer;
@@ -341,95 +422,35 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
       for (int s = 0; s < 4; ++s) {
         const int cur = s % 2;
 #pragma unroll
-        for (int i = 0; i < MB; ++i) {
+        for (int t = 0; t < kSlots; ++t) {
           __builtin_amdgcn_sched_barrier(0);
+          const int turn = t / kGap;
+          const bool reads = t % kGap == 0, asks = t % kGap == kGap - 1;
           if (s < 3) {
-            read(cur ^ 1, i, here, s + 1);
-            if (s < 2 && more) ask(s * MB + i + MB - 1, (buffer ^ 1) * kBuffer);
+            if (reads) read(cur ^ 1, turn, here, s + 1);
+            if (s == 0 && more && asks) ask(kSlots / kGap + turn, (buffer ^ 1) * kBuffer);
           } else if (more) {
-            if (i == 1) {
+            if (t == 0) {
               __builtin_amdgcn_s_waitcnt(kLdsDone);      // (this wavefront's reads of the buffer that is asked into next)
               asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
               __builtin_amdgcn_s_barrier();
               asm volatile("" ::: "memory");
               if (after) aim(step - 2);
             }
-            if (i >= 1) {
-              read(0, i - 1, next, 0);
-              if (i == MB - 1) read(0, MB - 1, next, 0);
-              if (after) ask(i - 1, buffer * kBuffer);
-            }
+            if (reads) read(0, turn, next, 0);
+            if (asks && after) ask(turn, buffer * kBuffer);
           }
-#pragma unroll
-          for (int j = 0; j < NB; ++j) mma(acc[i][j], v[cur][j], u[cur][i], T{});
+          mma(acc[t / NB][t % NB], v[cur][t % NB], u[cur][t / NB], T{});
         }
       }
     };
     for (; step > from; --step, buffer ^= 1) multiply(std::true_type{});
     multiply(std::false_type{});
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
-#pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int m = m0 + wm + i * 32 + lane % 32;
-    if constexpr (B_MADE == kTurns) {
-#pragma unroll
-      for (int j = 0; j < NB; j += 2) epi.pair(m, (n0 + wn + j * 32) / 2, lane / 32, acc[i][j], acc[i][j + 1]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < NB; ++j) epi.block(z, m, n0 + wn + j * 32, lane / 32, acc[i][j]);
-    }
-  }
+  __syncthreads();
+  finish<T, MB, NB, B_MADE>(acc, lds, wave, z, m0 + wm, n0 + wn, epi);
 }
-
-// The n of a lane's sums 4 q to 4 q + 3.
-__device__ __forceinline__ int column(int n, int half, int q) { return n + q * 8 + half * 4; }
-
-// Four consecutive elements of a row that ends at `limit`.
-template <typename T>
-__device__ __forceinline__ void store4(T* row, int at, int limit, const float (&v)[4]) {
-  if (at + 4 <= limit) {
-    store_n(row + at, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (at + i < limit) row[at + i] = (T)v[i];
-  }
-}
-template <typename T>
-__device__ __forceinline__ void load4(float (&v)[4], const T* row, int at, int limit) {
-  if (at + 4 <= limit) {
-    load_n(v, row + at);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = at + i < limit ? (float)row[at + i] : 0.f;
-  }
-}
-
-// out[z][m][n] = base[m][n] + sums, in O.
-template <typename O>
-struct Store {
-  O* out[2];
-  int64_t stride;
-  const O* base;
-  int64_t base_stride;
-  int32_t M, N;
-  __device__ __forceinline__ void block(int z, int m, int n, int half, const f32x16& c) const {
-    if (m >= M) return;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int at = column(n, half, q);
-      if (at >= N) continue;
-      float v[4] = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-      if (base) {
-        float b[4];
-        load4(b, base + m * base_stride, at, N);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += b[i];
-      }
-      store4(out[z] + m * stride, at, N, v);
-    }
-  }
-};
 
 // Whether a side can go straight to LDS: every row that is read (rows of the product or of the sum) at a multiple of 16 bytes and whole
 // pieces of them long, the rows of a tile within 2^31 bytes.
@@ -442,6 +463,7 @@ bool straight(const Side& s, bool rows, Made made) {
 template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, bool DIRECT, class Epi>
 hipError_t launch_as(Product p, int M, int N, int batch, const Epi& epi, hipStream_t st) {
   constexpr int kLds = 2 * (BM + BN) * kStepBytes;
+  static_assert(WM * WN * finish_bytes(BN / WN / 32) <= 2 * (BM + BN) * kStepBytes, "the epilogue's rows");
   void (*kernel)(Product, Epi);
   if constexpr (DIRECT) kernel = k_direct<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
   else kernel = k_tile<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
