@@ -167,6 +167,7 @@ template <typename T> int32_t steps_of(int64_t k) { return (int32_t)((k + kStep<
 template <typename T>
 hipError_t up(const FfnArgs& a, const void* x, int64_t x_stride, const Up<T>& epi, hipStream_t st) {
   Product p = {side<T>(x, x_stride, a.T, a.D), side<T>(a.w_in, a.D, a.F, a.D, a.w_gate), steps_of<T>(a.D), 0};
+  if (a.T <= kFewRows) return launch_few<T, kTurns>(p, epi, st);
   return launch_tile<T, true, true, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, epi, st);
 }
 
@@ -176,10 +177,11 @@ hipError_t ffn_forward(const FfnArgs& a, hipStream_t st) {
   T* h = (T*)((char*)a.ws + plan.h);
   Up<T> e = {h, plan.Fp, a.T, a.F, (int32_t)plan.Tp, (int32_t)plan.Fp, a.keep, (T*)a.ab, (int8_t*)a.ab, a.ab_exps};
   if (hipError_t s = up<T>(a, a.x, a.x_stride, e, st); s != hipSuccess) return s;
-  Product p = {side<T>(h, plan.Fp, (int32_t)plan.Tp, (int32_t)plan.Fp), side<T>(a.w_out, a.F, a.D, a.F), steps_of<T>(a.F), 0};
+  Product p = {side<T>(h, plan.Fp, a.T <= kFewRows ? a.T : (int32_t)plan.Tp, (int32_t)plan.Fp), side<T>(a.w_out, a.F, a.D, a.F), steps_of<T>(a.F), 0};
   auto down = [&](auto o) {
     using O = decltype(o);
     Store<O> out = {{(O*)a.y, nullptr}, a.y_stride, (const O*)a.base, a.base_stride, a.T, a.D};
+    if (a.T <= kFewRows) return launch_few<T, kOne>(p, out, st);
     return launch_tile<T, true, true, kOne>(p, a.T, a.D, 1, out, st);
   };
   if (a.y_dtype == a.dtype) return down(T{});

@@ -452,6 +452,157 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   finish<T, MB, NB, B_MADE>(acc, lds, wave, z, m0 + wm, n0 + wn, epi);
 }
 
+// ---- few rows of a: b is read once, from memory to registers ----
+// A workgroup has RB blocks of 16 rows of b (kTurns: 32 rows of each matrix) and all rows of a (NG groups of 16); its W wavefronts share
+// the sum, line by line (128 bytes of a row) in turn, and join in LDS. The matrix instructions are of 16 x 16: their operand is 16 bytes a
+// lane as above, lane / 16 choosing one quarter of 64 bytes. Memory bounds it; a line of each of a block's rows is asked for by two loads
+// next to each other, kDeep lines ahead.
+__device__ __forceinline__ void mma16(f32x4& c, i32x4 b, i32x4 a, __bf16) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(f32x4& c, i32x4 b, i32x4 a, _Float16) {
+  c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, b), __builtin_bit_cast(f16x8, a), c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(f32x4& c, i32x4 b, i32x4 a, float) {
+  const f32x4 u = __builtin_bit_cast(f32x4, b), v = __builtin_bit_cast(f32x4, a);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(u[i], v[i], c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16(i32x4& c, i32x4 b, i32x4 a, int8_t) { c = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0); }
+
+constexpr int kDeep = 4;
+template <typename T, int RB, int NG, int W, Made MADE, class Epi>
+__global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
+  using Word = std::conditional_t<std::is_same<T, int8_t>::value, int32_t, float>;
+  using Acc = std::conditional_t<std::is_same<T, int8_t>::value, i32x4, f32x4>;
+  constexpr int kRows = RB * 16;
+  __shared__ __attribute__((aligned(16))) Word sums[W][NG * 16][kRows + 4];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, at = lane / 16 * kPiece<T>;
+  const int n0 = blockIdx.x * (MADE == kTurns ? kRows / 2 : kRows);
+  const char *bp[RB], *ap[NG];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    const int n = MADE == kTurns ? n0 + r % (RB / 2) * 16 + row : n0 + r * 16 + row;
+    bp[r] = p.b.p[MADE == kTurns ? r / (RB / 2) : 0] + min(n, p.b.n - 1) * p.b.stride;
+  }
+#pragma unroll
+  for (int g = 0; g < NG; ++g) ap[g] = p.a.p[0] + min(g * 16 + row, p.a.n - 1) * p.a.stride;
+  Acc acc[RB][NG];
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int g = 0; g < NG; ++g) acc[r][g] = Acc{};
+  const int k = p.b.k, whole = k / kStep<T>;
+  struct Line { i32x4 b[RB][2], a[NG][2]; };
+  auto load = [&](Line& l, int step) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int r = 0; r < RB; ++r) __builtin_memcpy(&l.b[r][h], (const T*)bp[r] + step * kStep<T> + h * (kStep<T> / 2) + at, 16);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) __builtin_memcpy(&l.a[g][h], (const T*)ap[g] + step * kStep<T> + h * (kStep<T> / 2) + at, 16);
+    }
+  };
+  auto multiply = [&](const Line& l) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) mma16(acc[r][g], l.b[r][h], l.a[g][h], T{});
+  };
+  Line line[kDeep];
+#pragma unroll
+  for (int i = 0; i < kDeep; ++i)
+    if (wave + i * W < whole) load(line[i], wave + i * W);
+  int step = wave;
+  for (; step + (2 * kDeep - 1) * W < whole; step += kDeep * W) {
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) {
+      multiply(line[i]);
+      load(line[i], step + (kDeep + i) * W);
+    }
+  }
+  // the last of the lines, up to two of each place: those behind the ones in hand are asked for as these are multiplied
+#pragma unroll
+  for (int i = 0; i < kDeep; ++i) {
+    if (step + i * W < whole) multiply(line[i]);
+    if (step + (kDeep + i) * W < whole) load(line[i], step + (kDeep + i) * W);
+  }
+#pragma unroll
+  for (int i = 0; i < kDeep; ++i)
+    if (step + (kDeep + i) * W < whole) multiply(line[i]);
+  if (whole * kStep<T> < k && whole % W == wave) {      // a line that ends before its 128 bytes do
+    Line l;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int from = whole * kStep<T> + h * (kStep<T> / 2) + at;
+#pragma unroll
+      for (int r = 0; r < RB; ++r) l.b[r][h] = __builtin_bit_cast(i32x4, piece<T>(bp[r], from, k));
+#pragma unroll
+      for (int g = 0; g < NG; ++g) l.a[g][h] = __builtin_bit_cast(i32x4, piece<T>(ap[g], from, k));
+    }
+    multiply(l);
+  }
+#pragma unroll
+  for (int r = 0; r < RB; ++r)
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const Word w[4] = {acc[r][g][0], acc[r][g][1], acc[r][g][2], acc[r][g][3]};
+      __builtin_memcpy(__builtin_assume_aligned(&sums[wave][g * 16 + row][r * 16 + lane / 16 * 4], 16), w, 16);
+    }
+  __syncthreads();
+  constexpr int kQuads = kRows / 4;
+  for (int i = threadIdx.x; i < NG * 16 * kQuads; i += 64 * W) {      // (the wavefronts' sums in their order)
+    Word* to = &sums[0][i / kQuads][i % kQuads * 4];
+    Word s[4];
+    __builtin_memcpy(s, to, 16);
+#pragma unroll
+    for (int w = 1; w < W; ++w)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += sums[w][i / kQuads][i % kQuads * 4 + j];
+    __builtin_memcpy(to, s, 16);
+  }
+  __syncthreads();
+  constexpr int kPieces = kRows / 8 / (MADE == kTurns ? 2 : 1);
+  for (int i = threadIdx.x; i < NG * 16 * kPieces; i += 64 * W) {
+    const int m = i / kPieces, n = i % kPieces * 8;
+    typename Epi::Beside beside;
+    epi.ask(beside, m, n0 + n);
+    Word v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = sums[0][m][n + j];
+    if constexpr (MADE == kTurns) {
+      Word w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = sums[0][m][kRows / 2 + n + j];
+      epi.pair(beside, m, n0 + n, v, w);
+    } else {
+      epi.row(beside, 0, m, n0 + n, v);
+    }
+  }
+}
+constexpr int kFewRows = 32;
+
+template <typename T, int RB, int NG, int W, Made MADE, class Epi>
+hipError_t few_as(const Product& p, const Epi& epi, hipStream_t st) {
+  constexpr int kRows = MADE == kTurns ? RB * 8 : RB * 16;
+  k_few<T, RB, NG, W, MADE, Epi><<<(p.b.n + kRows - 1) / kRows, 64 * W, 0, st>>>(p, epi);
+  return hipGetLastError();
+}
+// a.n <= kFewRows; b and a by rows, at any alignment.
+template <typename T, Made MADE, class Epi>
+hipError_t launch_few(const Product& p, const Epi& epi, hipStream_t st) {
+  constexpr int kRB = MADE == kTurns ? 4 : 1;
+  auto go = [&](auto ng, auto w) { return few_as<T, kRB, decltype(ng)::value, decltype(w)::value, MADE>(p, epi, st); };
+  using std::integral_constant;
+  const bool short_sum = p.b.k <= 16 * kStep<T>;
+  if (p.a.n <= 16) return short_sum ? go(integral_constant<int, 1>{}, integral_constant<int, 4>{}) : go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+  // (64 rows of b and 32 of a: eight wavefronts' sums would be 70 KB)
+  if (short_sum || MADE == kTurns) return go(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+  return go(integral_constant<int, 2>{}, integral_constant<int, MADE == kTurns ? 4 : 8>{});
+}
+
 // Whether a side can go straight to LDS: every row that is read (rows of the product or of the sum) at a multiple of 16 bytes and whole
 // pieces of them long, the rows of a tile within 2^31 bytes.
 template <typename T>
