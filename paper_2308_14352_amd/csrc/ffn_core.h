@@ -49,6 +49,7 @@ struct Up {
   int32_t keep;
   T* ab;                    // MOEQ_KEEP_OWN
   int8_t *codes, *exps;     // MOEQ_KEEP_8
+  static constexpr bool kRaw = false;
   struct Beside {};
   __device__ __forceinline__ void ask(Beside&, int, int) const {}
   __device__ __forceinline__ void keep8(int which, int m, int f, const float (&v)[8]) const {
@@ -88,6 +89,7 @@ struct Act {
   const int8_t *codes, *exps;      // in ab's place
   T *dab, *h;                      // [Tp][2 Fp], [Tp][Fp]
   int32_t T_, F, Tp, Fp;
+  static constexpr bool kRaw = false;
   struct Beside {
     T ab[2][8];
     int8_t codes[2][8], exps[2];
@@ -141,7 +143,7 @@ inline int64_t up_to(int64_t n, int64_t by) { return (n + by - 1) / by * by; }
 // The workspace's parts, each at a multiple of 256 bytes.
 struct FfnPlan {
   int64_t Tp, Fp, Dp;
-  size_t h, dab, x, ab, bytes;
+  size_t h, dab, x, ab, room, bytes;
   FfnPlan(const FfnArgs& a, bool backward) : Tp(up_to(a.T, 64)) {
     const size_t e = dtype_bytes(a.dtype);
     Fp = up_to(a.F, kStepBytes / e), Dp = up_to(a.D, kStepBytes / e);      // (whole steps, each with a column that there is)
@@ -154,6 +156,7 @@ struct FfnPlan {
       if (a.x_codes) x = take((size_t)a.T * Dp * e);
       if (a.keep == MOEQ_KEEP_NONE) ab = take((size_t)2 * a.T * a.F * e);
     }
+    room = take(std::max(room_bytes(Tp, 2 * Fp), room_bytes(a.T, a.D)));
     bytes = at;
   }
 };
@@ -165,10 +168,10 @@ Side side(const void* p, int64_t stride, int32_t n, int32_t k, const void* q = n
 template <typename T> int32_t steps_of(int64_t k) { return (int32_t)((k + kStep<T> - 1) / kStep<T>); }
 
 template <typename T>
-hipError_t up(const FfnArgs& a, const void* x, int64_t x_stride, const Up<T>& epi, hipStream_t st) {
+hipError_t up(const FfnArgs& a, const void* x, int64_t x_stride, const Up<T>& epi, void* room, hipStream_t st) {
   Product p = {side<T>(x, x_stride, a.T, a.D), side<T>(a.w_in, a.D, a.F, a.D, a.w_gate), steps_of<T>(a.D), 0};
   if (a.T <= kFewRows) return launch_few<T, kTurns>(p, epi, st);
-  return launch_tile<T, true, true, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, epi, st);
+  return launch_tile<T, true, true, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, room, epi, st);
 }
 
 template <typename T>
@@ -176,13 +179,13 @@ hipError_t ffn_forward(const FfnArgs& a, hipStream_t st) {
   const FfnPlan plan(a, false);
   T* h = (T*)((char*)a.ws + plan.h);
   Up<T> e = {h, plan.Fp, a.T, a.F, (int32_t)plan.Tp, (int32_t)plan.Fp, a.keep, (T*)a.ab, (int8_t*)a.ab, a.ab_exps};
-  if (hipError_t s = up<T>(a, a.x, a.x_stride, e, st); s != hipSuccess) return s;
+  if (hipError_t s = up<T>(a, a.x, a.x_stride, e, (char*)a.ws + plan.room, st); s != hipSuccess) return s;
   Product p = {side<T>(h, plan.Fp, a.T <= kFewRows ? a.T : (int32_t)plan.Tp, (int32_t)plan.Fp), side<T>(a.w_out, a.F, a.D, a.F), steps_of<T>(a.F), 0};
   auto down = [&](auto o) {
     using O = decltype(o);
     Store<O> out = {{(O*)a.y, nullptr}, a.y_stride, (const O*)a.base, a.base_stride, a.T, a.D};
     if (a.T <= kFewRows) return launch_few<T, kOne>(p, out, st);
-    return launch_tile<T, true, true, kOne>(p, a.T, a.D, 1, out, st);
+    return launch_tile<T, true, true, kOne>(p, a.T, a.D, 1, (char*)a.ws + plan.room, out, st);
   };
   if (a.y_dtype == a.dtype) return down(T{});
   return down(0.f);
@@ -207,26 +210,26 @@ hipError_t ffn_backward(const FfnArgs& a, hipStream_t st) {
     if (a.keep == MOEQ_KEEP_NONE) {
       T* made = (T*)(ws + plan.ab);
       Up<T> e = {nullptr, 0, a.T, a.F, Tp, Fp, MOEQ_KEEP_OWN, made, nullptr, nullptr};
-      if (hipError_t s = up<T>(a, x, x_stride, e, st); s != hipSuccess) return s;
+      if (hipError_t s = up<T>(a, x, x_stride, e, ws + plan.room, st); s != hipSuccess) return s;
       ab = made;
     }
     const bool eight = a.keep == MOEQ_KEEP_8;
     Act<T> e = {eight ? nullptr : ab, eight ? (const int8_t*)a.ab : nullptr, a.ab_exps, dab, h, a.T, a.F, Tp, Fp};
     Product p = {side<T>(a.dy, a.dy_stride, a.T, a.D), side<T>(a.w_out, a.F, a.F, a.D), steps_of<T>(a.D), 0};
-    if (hipError_t s = launch_tile<T, true, false, kOne>(p, Tp, Fp, 1, e, st); s != hipSuccess) return s;
+    if (hipError_t s = launch_tile<T, true, false, kOne>(p, Tp, Fp, 1, ws + plan.room, e, st); s != hipSuccess) return s;
     if (a.dx) {
       Product q = {side<T>(dab, 2 * plan.Fp, Tp, 2 * Fp), side<T>(a.w_in, a.D, a.D, a.F, a.w_gate), 2 * steps_of<T>(Fp), steps_of<T>(Fp)};
       Store<T> out = {{(T*)a.dx, nullptr}, a.dx_stride, nullptr, 0, a.T, a.D};
-      if (hipError_t s = launch_tile<T, true, false, kBehind>(q, a.T, a.D, 1, out, st); s != hipSuccess) return s;
+      if (hipError_t s = launch_tile<T, true, false, kBehind>(q, a.T, a.D, 1, ws + plan.room, out, st); s != hipSuccess) return s;
     }
   }
   // (the workspace's rows are zero from row T on, those of x and dy end there)
   Product p = {side<T>(dab, 2 * plan.Fp, a.F, Tp, dab + Fp), side<T>(x, x_stride, a.D, a.T), steps_of<T>(a.T), 0};
   Store<T> out = {{(T*)a.dw_in, (T*)a.dw_gate}, a.D, nullptr, 0, a.F, a.D};
-  if (hipError_t s = launch_tile<T, false, false, kOne>(p, a.F, a.D, 2, out, st); s != hipSuccess) return s;
+  if (hipError_t s = launch_tile<T, false, false, kOne>(p, a.F, a.D, 2, nullptr, out, st); s != hipSuccess) return s;
   p.a = side<T>(a.dy, a.dy_stride, a.D, a.T), p.b = side<T>(h, plan.Fp, a.F, Tp);
   out = {{(T*)a.dw_out, nullptr}, a.F, nullptr, 0, a.D, a.F};
-  return launch_tile<T, false, false, kOne>(p, a.D, a.F, 1, out, st);
+  return launch_tile<T, false, false, kOne>(p, a.D, a.F, 1, nullptr, out, st);
 }
 
 }  // namespace tiles

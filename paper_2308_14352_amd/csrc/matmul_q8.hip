@@ -16,6 +16,7 @@ struct Scaled {
   int64_t base_stride;
   const float *xs, *ws;
   int32_t T, N;
+  static constexpr bool kRaw = false;
   struct Beside { float x, w[8], base[8]; };
   __device__ __forceinline__ void ask(Beside& b, int m, int n) const {
     if (m >= T || n >= N) return;
@@ -37,7 +38,7 @@ struct Scaled {
 
 }  // namespace
 
-size_t q8_ws_bytes(int32_t, int32_t, int32_t) { return 0; }
+size_t q8_ws_bytes(int32_t T, int32_t N, int32_t) { return T <= kFewRows ? 0 : room_bytes(T, N); }
 
 hipError_t launch_matmul_q8(const Q8Args& a, hipStream_t st) {
   return with_type(a.dtype, [&](auto o) {
@@ -46,7 +47,7 @@ hipError_t launch_matmul_q8(const Q8Args& a, hipStream_t st) {
     Product p = {Side{{(const char*)a.x, nullptr}, pitch, a.T, pitch}, Side{{(const char*)a.w, nullptr}, pitch, a.N, pitch}, pitch / kStepBytes, 0};
     Scaled<O> e = {(O*)a.y, a.y_stride, (const O*)a.base, a.base_stride, a.x_scale, a.w_scale, a.T, a.N};
     if (a.T <= kFewRows) return launch_few<int8_t, kOne>(p, e, st);
-    return launch_tile<int8_t, true, true, kOne>(p, a.T, a.N, 1, e, st);
+    return launch_tile<int8_t, true, true, kOne>(p, a.T, a.N, 1, a.ws, e, st);
   });
 }
 

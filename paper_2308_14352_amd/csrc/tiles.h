@@ -11,6 +11,7 @@
 // v_mfma_i32_32x32x32_i8, or four v_mfma_f32_32x32x2_f32. The matrix instruction takes b first, so that a lane has one row m and four
 // consecutive n in every four sums.
 #pragma once
+#include <algorithm>
 #include <type_traits>
 
 #include "operators.h"
@@ -168,6 +169,7 @@ struct Store {
   const O* base;
   int64_t base_stride;
   int32_t M, N;
+  static constexpr bool kRaw = false;
   struct Beside { float base[8]; };
   __device__ __forceinline__ void ask(Beside& b, int m, int n) const {
     if (base && m < M && n < N) load8(b.base, base + m * base_stride, n, N);
@@ -283,10 +285,15 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(Product p, Epi epi) {
     __syncthreads();
   }
   __syncthreads();
-  finish<T, MB, NB, B_MADE>(acc, lds, wave, z, m0 + wm, n0 + wn, epi);
+  finish<T, MB, NB, Epi::kRaw ? kOne : B_MADE>(acc, lds, wave, z, m0 + wm, n0 + wn, epi);
 }
 
 constexpr int kLdsDone = 0xc07f;      // s_waitcnt lgkmcnt(0), no wait for the others
+template <int N>
+__device__ __forceinline__ void landed() {      // all but the N youngest of this wavefront's requests
+  static_assert(N < 64, "six bits");
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
 
 // ---- straight to LDS: sides whose rows begin at multiples of 16 bytes, whole pieces of 16 bytes long ----
 __device__ const uint4 kZeros[1] = {};
@@ -348,18 +355,19 @@ struct Fetch {
   }
 };
 
-// As k_tile. Two steps are in LDS: while one is multiplied, the pieces of the next are on their way. A slice's operands are read while
+// As k_tile. S steps are in LDS: while one is multiplied, the pieces of the next ones are on their way. A slice's operands are read while
 // the slice before is multiplied, one between two matrix instructions, and so are the next step's pieces asked for, in the last slice
 // of a step, behind the one barrier, and in the first of the next. Steps run from the last to the first. Lines asked for into L2 four
 // steps ahead, by a dword of each, cost more than they saved (sum of 28672, 256 tiles: 844 us, without 817).
-template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, class Epi>
+template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, int S, Made A_MADE, Made B_MADE, class Epi>
 __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   constexpr int NT = 64 * WM * WN, MB = BM / WM / 32, NB = BN / WN / 32, kBuffer = (BM + BN) * kStepBytes;
   using FA = Fetch<T, A_ROWS, BM, NT, A_MADE>;
   using FB = Fetch<T, B_ROWS, BN, NT, B_MADE>;
   constexpr int LA = FA::kPieces, L = LA + FB::kPieces, kSlots = MB * NB;      // requests of a step; matrix instructions of a slice
   constexpr int kGap = kSlots >= 2 * (MB + NB) ? 2 : 1;      // where there is room, a read and a request go with instructions of their own
-  static_assert(2 * (kSlots / kGap) >= L && kSlots / kGap >= MB + NB, "a step's requests go with two slices, a slice's reads with one");
+  constexpr int kTurnsOf = kSlots / kGap, kReads = (MB + NB + kTurnsOf - 1) / kTurnsOf, kAsks = (L + 2 * kTurnsOf - 1) / (2 * kTurnsOf);      // (a step's requests go with two slices, a slice's reads with one)
+  constexpr int kAtOnce = kTurnsOf * kAsks < L ? kTurnsOf * kAsks : L;      // requests with the first of them
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int tm, tn;
   tile_of(p, tm, tn);
@@ -400,24 +408,36 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
     if (j < NB) v[set][j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice);
     else if (j < NB + MB) u[set][j - NB] = operand<T, A_ROWS, BM>(at, wm + (j - NB) * 32, slice);
   };
+  auto ask_some = [&](int turn, int buffer) {
+#pragma unroll
+    for (int j = turn * kAsks; j < (turn + 1) * kAsks; ++j) ask(j, buffer * kBuffer);
+  };
+  auto read_some = [&](int set, int turn, const char* at, int slice) {
+#pragma unroll
+    for (int j = turn * kReads; j < (turn + 1) * kReads; ++j) read(set, j, at, slice);
+  };
   if (from < to) {
     int step = to - 1, buffer = 0;
     a.first(p.a, step, p.first_steps, 0);
     b.first(p.b, step, p.first_steps, 0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int q = 1; q < S; ++q)
+      if (step - q >= from) {
+        aim(step - q);
+#pragma unroll
+        for (int j = 0; j < (q < S - 1 ? L : kAtOnce); ++j) ask(j, q * kBuffer);
+      }
+    if (step - (S - 1) >= from) landed<(S - 2) * L + kAtOnce>();
+    else landed<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (step > from) {
-      aim(step - 1);
-#pragma unroll
-      for (int j = 0; j < kSlots / kGap; ++j) ask(j, kBuffer);
-    }
 #pragma unroll
     for (int j = 0; j < NB + MB; ++j) read(0, j, lds, 0);
     auto multiply = [&](auto more_) {      // (a step's last one apart: what waits for which reads is then known without a branch between)
       constexpr bool more = decltype(more_)::value;
-      const char *here = lds + buffer * kBuffer, *next = lds + (buffer ^ 1) * kBuffer;
-      const bool after = step - 1 > from;
+      const int following = buffer + 1 == S ? 0 : buffer + 1, freed = buffer == 0 ? S - 1 : buffer - 1;
+      const char *here = lds + buffer * kBuffer, *next = lds + following * kBuffer;
+      const int left = step - from;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const int cur = s % 2;
@@ -427,29 +447,34 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
           const int turn = t / kGap;
           const bool reads = t % kGap == 0, asks = t % kGap == kGap - 1;
           if (s < 3) {
-            if (reads) read(cur ^ 1, turn, here, s + 1);
-            if (s == 0 && more && asks) ask(kSlots / kGap + turn, (buffer ^ 1) * kBuffer);
+            if (reads) read_some(cur ^ 1, turn, here, s + 1);
+            if (s == 0 && more && asks && left >= S - 1) ask_some(kTurnsOf + turn, freed);
           } else if (more) {
             if (t == 0) {
               __builtin_amdgcn_s_waitcnt(kLdsDone);      // (this wavefront's reads of the buffer that is asked into next)
-              asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+              if (S >= 3 && left >= S - 1) landed<(S - 2) * L>();      // (all but the requests of the steps behind the next)
+              else if (S == 4 && left == 2) landed<L>();
+              else landed<0>();
               __builtin_amdgcn_s_barrier();
               asm volatile("" ::: "memory");
-              if (after) aim(step - 2);
+              if (left >= S) aim(step - S);
             }
-            if (reads) read(0, turn, next, 0);
-            if (asks && after) ask(turn, buffer * kBuffer);
+            if (reads) read_some(0, turn, next, 0);
+            if (asks && left >= S) ask_some(turn, buffer);
           }
           mma(acc[t / NB][t % NB], v[cur][t % NB], u[cur][t / NB], T{});
         }
       }
     };
-    for (; step > from; --step, buffer ^= 1) multiply(std::true_type{});
+    while (step > from) {
+      multiply(std::true_type{});
+      --step, buffer = buffer + 1 == S ? 0 : buffer + 1;
+    }
     multiply(std::false_type{});
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    landed<0>();
   }
   __syncthreads();
-  finish<T, MB, NB, B_MADE>(acc, lds, wave, z, m0 + wm, n0 + wn, epi);
+  finish<T, MB, NB, Epi::kRaw ? kOne : B_MADE>(acc, lds, wave, z, m0 + wm, n0 + wn, epi);
 }
 
 // ---- few rows of a: b is read once, from memory to registers ----
@@ -611,33 +636,116 @@ bool straight(const Side& s, bool rows, Made made) {
   return (uintptr_t)s.p[0] % 16 == 0 && (made == kOne || (uintptr_t)s.p[1] % 16 == 0) && length % kPiece<T> == 0 && (count == 1 || (s.stride % 16 == 0 && s.stride < 1 << 23));
 }
 
-template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, Made A_MADE, Made B_MADE, bool DIRECT, class Epi>
-hipError_t launch_as(Product p, int M, int N, int batch, const Epi& epi, hipStream_t st) {
-  constexpr int kLds = 2 * (BM + BN) * kStepBytes;
-  static_assert(WM * WN * finish_bytes(BN / WN / 32) <= 2 * (BM + BN) * kStepBytes, "the epilogue's rows");
+// The tile of a product, by the time it would take. A step's time is what was measured (bf16, us at the clock that the card keeps under
+// it), with as many workgroups a compute unit as their LDS leaves room for; a share has its beginning and end besides.
+enum Tile { kTile256, kTile128x256, kTile128, kTile128Two, kTile64 };
+struct Choice { Tile tile; int shares; };
+constexpr int kMaxShares = 8;
+constexpr size_t kRoomMost = (size_t)48 << 20;      // of the sums of shares
+inline int64_t part_pitch(int64_t N) { return (N + 63) / 64 * 64; }
+inline size_t room_bytes(int64_t M, int64_t N) { return std::min((size_t)(kMaxShares * M * part_pitch(N) * 4), kRoomMost); }
+inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bool room) {
+  struct Form { Tile tile; int bm, bn, at_once; float step, ends; };
+  static constexpr Form kStraight[] = {{kTile256, 256, 256, 1, 1.75f, 8.f}, {kTile128x256, 128, 256, 1, 1.1f, 5.f}, {kTile128, 128, 128, 1, 0.7f, 4.f},
+                                       {kTile128Two, 128, 128, 2, 1.2f, 5.f}, {kTile64, 64, 128, 2, 0.8f, 4.f}};
+  static constexpr Form kThrough[] = {{kTile128, 128, 128, 2, 2.0f, 6.f}, {kTile64, 64, 128, 3, 2.0f, 5.f}};
+  Choice best = {kTile128, 1};
+  float least = 1e30f;
+  const auto look = [&](const Form& f) {
+    for (int shares = 1; shares <= (room && batch == 1 ? kMaxShares : 1); ++shares) {
+      if (shares > 1 && (steps < 4 * shares || shares * M * part_pitch(N) * 4 > (int64_t)kRoomMost)) break;
+      const int64_t tiles = (M + f.bm - 1) / f.bm * ((N + f.bn - 1) / f.bn) * batch * shares, rounds = (tiles + 256 * f.at_once - 1) / (256 * f.at_once);
+      const float join = shares == 1 ? 0.f : 4.f + (float)(shares * M * N) * 8.f / 4e6f;      // (written and read at 4 TB/s)
+      const float time = (float)rounds * ((float)((steps + shares - 1) / shares) * f.step + f.ends) + join;
+      if (time < least) least = time, best = {f.tile, shares};
+    }
+  };
+  if (direct) for (const Form& f : kStraight) look(f);
+  else for (const Form& f : kThrough) look(f);
+  return best;
+}
+
+// ---- a sum in shares: workgroups leave theirs in the workspace, and a second kernel adds them in their order ----
+template <typename T> using WordOf = std::conditional_t<std::is_same<T, int8_t>::value, int32_t, float>;
+template <typename Word>
+struct Part {
+  Word* out;           // [shares][M][pitch], columns as the tiles have them
+  int64_t pitch;
+  int32_t M;
+  static constexpr bool kRaw = true;
+  struct Beside {};
+  __device__ __forceinline__ void ask(Beside&, int, int) const {}
+  __device__ __forceinline__ void row(const Beside&, int, int m, int n, const Word (&v)[8]) const {
+    if (m < M && n < pitch) __builtin_memcpy(__builtin_assume_aligned(out + ((int64_t)blockIdx.z * M + m) * pitch + n, 16), v, 32);
+  }
+};
+template <typename Word, Made MADE, class Epi>
+__global__ __launch_bounds__(256) void k_join(Part<Word> p, int shares, int pieces, Epi epi) {
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+  const int m = i / (uint32_t)pieces, n = (i - m * (uint32_t)pieces) * 8;      // (the lanes of a quad have a block of 32 columns: pieces are a multiple of 4)
+  typename Epi::Beside beside;
+  epi.ask(beside, m, n);
+  Word v[MADE == kTurns ? 2 : 1][8] = {};
+  const Word* from = p.out + (int64_t)min(m, p.M - 1) * p.pitch + (MADE == kTurns ? n / 32 * 64 + n % 32 : n);
+  for (int s = 0; s < shares; ++s) {
+#pragma unroll
+    for (int w = 0; w < (MADE == kTurns ? 2 : 1); ++w) {
+      Word t[8];
+      __builtin_memcpy(t, __builtin_assume_aligned(from + s * p.M * p.pitch + w * 32, 16), 32);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[w][j] += t[j];
+    }
+  }
+  if constexpr (MADE == kTurns) epi.pair(beside, m, n, v[0], v[1]);
+  else epi.row(beside, 0, m, n, v[0]);
+}
+
+// S: the steps in LDS of a side that goes there straight; 0: through registers.
+template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, int S, Made B_MADE, class Epi>
+hipError_t launch_one(Product p, int M, int N, int batch, int shares, const Epi& epi, hipStream_t st) {
+  constexpr int kLds = (S ? S : 2) * (BM + BN) * kStepBytes;
+  static_assert(WM * WN * finish_bytes(BN / WN / 32) <= kLds && kLds <= 160 * 1024, "the epilogue's rows; a compute unit's LDS");
   void (*kernel)(Product, Epi);
-  if constexpr (DIRECT) kernel = k_direct<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
-  else kernel = k_tile<T, A_ROWS, B_ROWS, BM, BN, WM, WN, A_MADE, B_MADE, Epi>;
+  if constexpr (S > 0) kernel = k_direct<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, kOne, B_MADE, Epi>;
+  else kernel = k_tile<T, A_ROWS, B_ROWS, BM, BN, WM, WN, kOne, B_MADE, Epi>;
   if constexpr (kLds > 64 * 1024) {
     static const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (e != hipSuccess) return e;
   }
   p.tiles_m = (M + BM - 1) / BM, p.tiles_n = (N + BN - 1) / BN;
-  kernel<<<dim3(p.tiles_m * p.tiles_n, batch), 64 * WM * WN, kLds, st>>>(p, epi);
+  kernel<<<dim3(p.tiles_m * p.tiles_n, batch, shares), 64 * WM * WN, kLds, st>>>(p, epi);
+  return hipGetLastError();
+}
+template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, int S, Made B_MADE, class Epi>
+hipError_t launch_as(const Product& p, int M, int N, int batch, int shares, void* room, const Epi& epi, hipStream_t st) {
+  if (shares == 1) return launch_one<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, B_MADE>(p, M, N, batch, 1, epi, st);
+  using Word = WordOf<T>;
+  const Part<Word> part = {(Word*)room, part_pitch(N), M};
+  if (hipError_t e = launch_one<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, B_MADE>(p, M, N, 1, shares, part, st); e != hipSuccess) return e;
+  const int pieces = (int)part.pitch / (B_MADE == kTurns ? 16 : 8);
+  k_join<Word, B_MADE, Epi><<<(uint32_t)(((int64_t)M * pieces + 255) / 256), 256, 0, st>>>(part, shares, pieces, epi);
   return hipGetLastError();
 }
 
-// M x N outputs of each of `batch` products.
+// M x N outputs of each of `batch` products. `room`: room_bytes(M, N) bytes for the sums of shares.
 template <typename T, bool A_ROWS, bool B_ROWS, Made B_MADE, class Epi>
-hipError_t launch_tile(Product p, int M, int N, int batch, const Epi& epi, hipStream_t st) {
+hipError_t launch_tile(Product p, int M, int N, int batch, void* room, const Epi& epi, hipStream_t st) {
   if (p.a.n == 1 && A_ROWS) p.a.stride = 0;      // (of a single row: any)
   if (p.a.k == 1 && !A_ROWS) p.a.stride = 0;
   if (p.b.k == 1 && !B_ROWS) p.b.stride = 0;
   const bool direct = straight<T>(p.a, A_ROWS, batch == 2 ? kTurns : kOne) && straight<T>(p.b, B_ROWS, B_MADE);
-  if (!direct) return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, kOne, B_MADE, false>(p, M, N, batch, epi, st);
-  const int64_t large = (int64_t)((M + 255) / 256) * ((N + 255) / 256) * batch;
-  if (large >= 96) return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 2, kOne, B_MADE, true>(p, M, N, batch, epi, st);
-  return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, kOne, B_MADE, true>(p, M, N, batch, epi, st);
+  const Choice c = choose(M, N, batch, p.steps, direct, room != nullptr);
+  if (!direct) {
+    if (c.tile == kTile64) return launch_as<T, A_ROWS, B_ROWS, 64, 128, 2, 2, 0, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 0, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+  }
+  switch (c.tile) {
+    case kTile256: return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 2, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    case kTile128x256: return launch_as<T, A_ROWS, B_ROWS, 128, 256, 2, 2, 3, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    case kTile128: return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 4, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    case kTile128Two: return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    default: return launch_as<T, A_ROWS, B_ROWS, 64, 128, 2, 2, 3, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+  }
 }
 
 }  // namespace tiles
