@@ -740,7 +740,7 @@ hipError_t launch_tile(Product p, int M, int N, int batch, void* room, const Epi
     return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 0, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
   }
   switch (c.tile) {
-    case kTile256: return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 2, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    case kTile256: return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 4, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
     case kTile128x256: return launch_as<T, A_ROWS, B_ROWS, 128, 256, 2, 2, 3, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
     case kTile128: return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 4, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
     case kTile128Two: return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
