@@ -402,7 +402,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   };
   auto ask = [&](int j, int buffer) {      // one request
     if (j < LA) a.piece(j, ask_a, buffer);
-    else if (j < L) b.piece(j - LA, ask_b[B_MADE == kTurns ? (j - LA) * (NT / 8) / 32 % 2 : 0], buffer);
+    else if (j < L) b.piece(j - LA, B_MADE == kTurns && ((j - LA) * (NT / 8) + wave * 8) / 32 % 2 ? ask_b[1] : ask_b[0], buffer);
   };
   auto read = [&](int set, int j, const char* at, int slice) {      // one operand: those of b first
     if (j < NB) v[set][j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice);
