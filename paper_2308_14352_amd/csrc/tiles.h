@@ -324,6 +324,14 @@ struct Fetch {
     const int64_t skip = ROWS ? first * s.stride : first * (int64_t)sizeof(T);
     base[0] = s.p[MADE == kOne ? z : 0] + skip;
     base[1] = s.p[1] + skip;
+    if constexpr (MADE == kTurns) {      // 32 rows a piece of 256 threads: the matrices in turn; 64 of 512: half of the wavefronts each
+      static_assert(ROWS && (NT == 256 || NT == 512), "which matrix a wavefront's rows are of");
+      if (NT == 512) {
+        const uint64_t own = (uint64_t)(threadIdx.x / 256 ? base[1] : base[0]);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)own), hi = __builtin_amdgcn_readfirstlane((uint32_t)(own >> 32));
+        base[0] = base[1] = (const char*)((uint64_t)hi << 32 | lo);
+      }
+    }
     const int last = ROWS ? s.n - 1 - first : (s.n - first) / kPiece<T> - 1;
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
@@ -402,7 +410,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   };
   auto ask = [&](int j, int buffer) {      // one request
     if (j < LA) a.piece(j, ask_a, buffer);
-    else if (j < L) b.piece(j - LA, B_MADE == kTurns && ((j - LA) * (NT / 8) + wave * 8) / 32 % 2 ? ask_b[1] : ask_b[0], buffer);
+    else if (j < L) b.piece(j - LA, ask_b[B_MADE == kTurns && NT == 256 ? (j - LA) % 2 : 0], buffer);
   };
   auto read = [&](int set, int j, const char* at, int slice) {      // one operand: those of b first
     if (j < NB) v[set][j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice);
