@@ -382,7 +382,7 @@ moeq_status moe_block_norms_forward(int32_t n_tokens, int32_t d, float residual_
 /* Its gradient from f, the y that the forward pass left, dy (of y, of r's type) and dn (of n): df in f's type, dr in r's, dgate
  * [n_tokens], dw_after [d] and dw_before [d] in fp32 (sums over the rows; zeros where there are none). What belongs to a weight or
  * gate that is not there is not touched, and y and dn are not read without w_before. The sums' order does not depend on timing.
- * ws: moe_block_norms_workspace_bytes, needed where there is a weight. */
+ * ws: moe_block_norms_workspace_bytes, 16-byte aligned, needed where there is a weight. */
 size_t moe_block_norms_workspace_bytes(int32_t max_tokens, int32_t d);
 moeq_status moe_block_norms_backward(int32_t n_tokens, int32_t d, float residual_scale, float eps, int32_t f_dtype, const void *f,
                                      int64_t f_stride, int32_t r_dtype, const void *y, int64_t y_stride, const void *dy,

@@ -65,12 +65,32 @@ struct RowSum {
 template <int W> constexpr int kThreadsOf = W == 1 ? 256 : 64 * W;
 template <int W> constexpr int kRowsOf = W == 1 ? 4 : 1;
 
+// A row's vectors as they lie in memory: 8 elements of each of NV places.
+template <typename T, int NV>
+struct Raw {
+  T v[NV][VE];
+  __device__ __forceinline__ void load(const T* row, int at, int step, int d) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (at + i * step) * VE;
+      if (c + VE <= d) {
+        __builtin_memcpy(v[i], row + c, sizeof(v[i]));
+      } else {
+#pragma unroll
+        for (int j = 0; j < VE; ++j) v[i][j] = c + j < d ? row[c + j] : (T)0.f;
+      }
+    }
+  }
+};
+
 template <typename F, typename R, typename N, int W, int NV>
 __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_forward(NormsArgs a) {
+  constexpr bool kHeld = NV <= 2;      // the weights in registers, asked for together with the row
   __shared__ float sh[2][W][4];
   RowSum<W> sum{sh};
   const int at = W == 1 ? threadIdx.x % 64 : threadIdx.x, d = a.d;
   const float by_d = 1.f / (float)d;
+  Raw<float, kHeld ? NV : 1> after, before;
   for (int64_t row = (int64_t)blockIdx.x * kRowsOf<W> + (W == 1 ? threadIdx.x / 64 : 0); row < a.T; row += (int64_t)gridDim.x * kRowsOf<W>) {
     const F* f = (const F*)a.f + row * a.f_stride;
     const R* r = (const R*)a.r + row * a.r_stride;
@@ -79,6 +99,10 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_forward(NormsArgs a) {
     for (int i = 0; i < NV; ++i) load_part(v[i], f, (at + i * 64 * W) * VE, d);
 #pragma unroll
     for (int i = 0; i < NV; ++i) load_part(y[i], r, (at + i * 64 * W) * VE, d);
+    if constexpr (kHeld) {
+      if (a.w_after) after.load(a.w_after, at, 64 * W, d);
+      if (a.w_before) before.load(a.w_before, at, 64 * W, d);
+    }
     const float g = a.gate ? a.gate[row] : 1.f;
     float by = 1.f;
     if (a.w_after) {
@@ -96,9 +120,9 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_forward(NormsArgs a) {
       const int c = (at + i * 64 * W) * VE;
       if (a.w_after) {
         float w[VE];
-        load_part(w, a.w_after, c, d);
+        if constexpr (!kHeld) load_part(w, a.w_after, c, d);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) v[i][j] = v[i][j] * by * w[j];
+        for (int j = 0; j < VE; ++j) v[i][j] = v[i][j] * by * (kHeld ? after.v[i % (kHeld ? NV : 1)][j] : w[j]);
       }
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
@@ -114,17 +138,37 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_forward(NormsArgs a) {
     for (int i = 0; i < NV; ++i) {
       const int c = (at + i * 64 * W) * VE;
       float w[VE];
-      load_part(w, a.w_before, c, d);
+      if constexpr (!kHeld) load_part(w, a.w_before, c, d);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) w[j] *= y[i][j] * by;
+      for (int j = 0; j < VE; ++j) w[j] = (kHeld ? before.v[i % (kHeld ? NV : 1)][j] : w[j]) * (y[i][j] * by);
       store_part((N*)a.out_n + row * a.out_n_stride, w, c, d);
     }
   }
 }
 
-// A stream of rows: stream, stream + streams, ...
+// What a row's gradient is made of.
+template <typename F, typename R, typename N, int NV>
+struct RowIn {
+  Raw<F, NV> f;
+  Raw<R, NV> dy, y;
+  Raw<N, NV> dn;
+  float g;
+  __device__ __forceinline__ void load(const NormsArgs& a, int64_t row, int at, int step) {
+    f.load((const F*)a.f + row * a.f_stride, at, step, a.d);
+    dy.load((const R*)a.dy + row * a.dy_stride, at, step, a.d);
+    if (a.w_before) {
+      y.load((const R*)a.y + row * a.y_stride, at, step, a.d);
+      dn.load((const N*)a.dn + row * a.dn_stride, at, step, a.d);
+    }
+    g = a.gate ? a.gate[row] : 1.f;
+  }
+};
+
+// A stream of rows: stream, stream + streams, ... The next row is on its way while one is worked on, and the weights stay in registers,
+// up to two vectors a thread.
 template <typename F, typename R, typename N, int W, int NV>
-__global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, int streams) {
+__global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, int streams, int pitch) {
+  constexpr bool kHeld = NV <= 2;
   __shared__ float sh[2][W][4];
   RowSum<W> sum{sh};
   const int at = W == 1 ? threadIdx.x % 64 : threadIdx.x, d = a.d;
@@ -132,79 +176,73 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, i
   if (stream >= streams) return;
   const float by_d = 1.f / (float)d;
   float sum_after[NV][VE] = {}, sum_before[NV][VE] = {};
+  Raw<float, NV> after, before;
+  RowIn<F, R, N, NV> in;
+  if constexpr (kHeld) {
+    if (a.w_after) after.load(a.w_after, at, 64 * W, d);
+    if (a.w_before) before.load(a.w_before, at, 64 * W, d);
+    in.load(a, stream, at, 64 * W);
+  }
   for (int64_t row = stream; row < a.T; row += streams) {
-    float f[NV][VE], y[NV][VE], dn[NV][VE], dy[NV][VE];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (at + i * 64 * W) * VE;
-      load_part(f[i], (const F*)a.f + row * a.f_stride, c, d);
-      load_part(dy[i], (const R*)a.dy + row * a.dy_stride, c, d);
-      if (a.w_before) {
-        load_part(y[i], (const R*)a.y + row * a.y_stride, c, d);
-        load_part(dn[i], (const N*)a.dn + row * a.dn_stride, c, d);
-      }
+    if constexpr (!kHeld) {
+      in.load(a, row, at, 64 * W);
+      if (a.w_after) after.load(a.w_after, at, 64 * W, d);
+      if (a.w_before) before.load(a.w_before, at, 64 * W, d);
     }
-    const float g = a.gate ? a.gate[row] : 1.f;
+    const RowIn<F, R, N, NV> now = in;
+    if (kHeld && row + streams < a.T) in.load(a, row + streams, at, 64 * W);
+    const float g = now.g;
     float s[3] = {0.f, 0.f, 0.f};      // y . y, (dn w) . y, f . f
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if (a.w_before) {
-        float w[VE];
-        load_part(w, a.w_before, (at + i * 64 * W) * VE, d);
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < VE; ++j) s[0] += y[i][j] * y[i][j], s[1] += dn[i][j] * w[j] * y[i][j];
+      for (int j = 0; j < VE; ++j) {
+        if (a.w_before) {
+          const float y = (float)now.y.v[i][j];
+          s[0] += y * y, s[1] += (float)now.dn.v[i][j] * before.v[i][j] * y;
+        }
+        s[2] += (float)now.f.v[i][j] * (float)now.f.v[i][j];
       }
-#pragma unroll
-      for (int j = 0; j < VE; ++j) s[2] += f[i][j] * f[i][j];
-    }
     sum(s);
     const float by = 1.f / sqrtf(s[0] * by_d + a.eps), mean = s[1] * by * by_d;      // of y; of dn w u(y)
     const float bf = a.w_after ? 1.f / sqrtf(s[2] * by_d + a.eps) : 1.f;
-    float t[1] = {0.f};
+    float t[1] = {0.f}, dy[NV][VE];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (at + i * 64 * W) * VE;
-      if (a.w_before) {
-        float w[VE];
-        load_part(w, a.w_before, c, d);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-          const float u = y[i][j] * by;
-          sum_before[i][j] += dn[i][j] * u;
-          dy[i][j] += by * (dn[i][j] * w[j] - u * mean);
-        }
-      }
-      float w[VE];
-      if (a.w_after) load_part(w, a.w_after, c, d);
+      float out[VE];
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        t[0] += dy[i][j] * (a.w_after ? f[i][j] * bf * w[j] : f[i][j]);
-        y[i][j] = a.alpha * dy[i][j];
+        dy[i][j] = (float)now.dy.v[i][j];
+        if (a.w_before) {
+          const float u = (float)now.y.v[i][j] * by, dn = (float)now.dn.v[i][j];
+          sum_before[i][j] += dn * u;
+          dy[i][j] += by * (dn * before.v[i][j] - u * mean);
+        }
+        const float f = (float)now.f.v[i][j];
+        t[0] += dy[i][j] * (a.w_after ? f * bf * after.v[i][j] : f);
+        out[j] = a.alpha * dy[i][j];
       }
-      store_part((R*)a.out_y + row * a.out_y_stride, y[i], c, d);
+      store_part((R*)a.out_y + row * a.out_y_stride, out, (at + i * 64 * W) * VE, d);
     }
     if (a.gate || a.w_after) sum(t);
     if (a.gate && at == 0) a.dgate[row] = t[0];
     const float back = g * t[0] * by_d;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (at + i * 64 * W) * VE;
-      float w[VE];
-      if (a.w_after) load_part(w, a.w_after, c, d);
+      float out[VE];
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        float v = a.gate ? dy[i][j] * g : dy[i][j];
+        out[j] = a.gate ? dy[i][j] * g : dy[i][j];
         if (a.w_after) {
-          const float u = f[i][j] * bf;
-          sum_after[i][j] += v * u;
-          v = bf * (v * w[j] - u * back);
+          const float u = (float)now.f.v[i][j] * bf;
+          sum_after[i][j] += out[j] * u;
+          out[j] = bf * (out[j] * after.v[i][j] - u * back);
         }
-        w[j] = v;
       }
-      store_part((F*)a.out_n + row * a.out_n_stride, w, c, d);
+      store_part((F*)a.out_n + row * a.out_n_stride, out, (at + i * 64 * W) * VE, d);
     }
   }
-  float* part = a.ws + (int64_t)stream * 2 * d;
+  float* part = a.ws + (int64_t)stream * 2 * pitch;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (at + i * 64 * W) * VE;
@@ -212,39 +250,53 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, i
     for (int j = 0; j < VE; ++j)
       if (c + j < d) {
         if (a.w_after) part[c + j] = sum_after[i][j];
-        if (a.w_before) part[d + c + j] = sum_before[i][j];
+        if (a.w_before) part[pitch + c + j] = sum_before[i][j];
       }
   }
 }
 
-// The weights' gradients from the streams': 64 columns a workgroup, 16 shares of the streams.
-__global__ __launch_bounds__(1024) void k_norms_join(NormsArgs a, int streams) {
-  __shared__ float sh[16][64];
+// The weights' gradients from the streams': 64 columns a workgroup, 64 shares of the streams, four columns a thread.
+__global__ __launch_bounds__(1024) void k_norms_join(NormsArgs a, int streams, int pitch) {
+  __shared__ float sh[64][65];
   float* out = blockIdx.y ? a.dw_before : a.dw_after;
   if (!out) return;
-  const int c = blockIdx.x * 64 + threadIdx.x % 64, share = threadIdx.x / 64;
-  float s = 0.f;
-  if (c < a.d)
-    for (int i = share; i < streams; i += 16) s += a.ws[((int64_t)i * 2 + blockIdx.y) * a.d + c];
-  sh[share][threadIdx.x % 64] = s;
+  const int q = threadIdx.x % 16 * 4, c = blockIdx.x * 64 + q, share = threadIdx.x / 16;
+  float s[4] = {};
+  if (c < a.d) {      // (the pitch is a multiple of 4; what lies behind the last column is added and not written)
+    const float* from = a.ws + blockIdx.y * pitch + c;
+#pragma unroll 8
+    for (int i = share; i < streams; i += 64) {
+      float v[4];
+      __builtin_memcpy(v, __builtin_assume_aligned(from + (int64_t)i * 2 * pitch, 16), 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += v[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sh[share][q + j] = s[j];
   __syncthreads();
-  if (share || c >= a.d) return;
-  for (int i = 1; i < 16; ++i) s += sh[i][threadIdx.x];
-  out[c] = s;
+  const int col = threadIdx.x / 16, part = threadIdx.x % 16;
+  float v = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v += sh[part * 4 + i][col];
+#pragma unroll
+  for (int i = 1; i < 16; i *= 2) v += __shfl_xor(v, i);
+  if (part == 0 && blockIdx.x * 64 + col < a.d) out[blockIdx.x * 64 + col] = v;
 }
 
+inline int up4(int d) { return (d + 3) / 4 * 4; }
 // Streams of a backward call: enough to fill the card, few enough that their sums are little beside the rows.
 int streams_of(int32_t T, int32_t d) { return std::min(T, d <= 1024 ? 2048 : 512); }
 
-// Wavefronts and vectors of a row.
-template <typename F>
+// Wavefronts and vectors of a row; WIDE: wavefronts of rows of up to 4096.
+template <int WIDE, typename F>
 hipError_t by_width(int32_t d, F&& f) {
   using std::integral_constant;
   auto go = [&](auto w, auto nv) { return f(w, nv); };
   if (d <= 512) return go(integral_constant<int, 1>{}, integral_constant<int, 1>{});
   if (d <= 1024) return go(integral_constant<int, 1>{}, integral_constant<int, 2>{});
   if (d <= 2048) return go(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-  if (d <= 4096) return go(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  if (d <= 4096) return go(integral_constant<int, WIDE>{}, integral_constant<int, 8 / WIDE>{});
   if (d <= 8192) return go(integral_constant<int, 8>{}, integral_constant<int, 2>{});
   return go(integral_constant<int, 8>{}, integral_constant<int, 4>{});
 }
@@ -273,11 +325,11 @@ hipError_t by_types(const NormsArgs& a, F&& f) {
 
 }  // namespace
 
-size_t norms_ws_bytes(int32_t T, int32_t d) { return (size_t)streams_of(T, d) * 2 * d * 4; }
+size_t norms_ws_bytes(int32_t T, int32_t d) { return (size_t)streams_of(T, d) * 2 * up4(d) * 4; }
 
 hipError_t launch_norms_forward(const NormsArgs& a, hipStream_t st) {
   return by_types(a, [&](auto f, auto r, auto n) {
-    return by_width(a.d, [&](auto w, auto nv) {
+    return by_width<4>(a.d, [&](auto w, auto nv) {
       constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
       const int64_t groups = ((int64_t)a.T + kRowsOf<W> - 1) / kRowsOf<W>;
       k_norms_forward<decltype(f), decltype(r), decltype(n), W, NV><<<(uint32_t)std::min<int64_t>(groups, 1 << 20), kThreadsOf<W>, 0, st>>>(a);
@@ -290,16 +342,16 @@ hipError_t launch_norms_backward(const NormsArgs& a, hipStream_t st) {
   const int streams = streams_of(a.T, a.d);
   if (a.T > 0) {
     const hipError_t e = by_types(a, [&](auto f, auto r, auto n) {
-      return by_width(a.d, [&](auto w, auto nv) {
+      return by_width<8>(a.d, [&](auto w, auto nv) {
         constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-        k_norms_backward<decltype(f), decltype(r), decltype(n), W, NV><<<(streams + kRowsOf<W> - 1) / kRowsOf<W>, kThreadsOf<W>, 0, st>>>(a, streams);
+        k_norms_backward<decltype(f), decltype(r), decltype(n), W, NV><<<(streams + kRowsOf<W> - 1) / kRowsOf<W>, kThreadsOf<W>, 0, st>>>(a, streams, up4(a.d));
         return hipGetLastError();
       });
     });
     if (e != hipSuccess) return e;
   }
   if (!a.dw_after && !a.dw_before) return hipSuccess;
-  k_norms_join<<<dim3((a.d + 63) / 64, 2), 1024, 0, st>>>(a, streams);
+  k_norms_join<<<dim3((a.d + 63) / 64, 2), 1024, 0, st>>>(a, streams, up4(a.d));
   return hipGetLastError();
 }
 

@@ -359,7 +359,7 @@ moeq_status moe_block_norms_backward(int32_t n_tokens, int32_t d, float residual
     return MOEQ_EINVAL;
   if (n_tokens && (w_after_opt || w_before_opt)) {
     if (!ws || ws_bytes < norms_ws_bytes(n_tokens, d)) return MOEQ_EWORKSPACE;
-    if (!aligned(ws, 4)) return MOEQ_EINVAL;
+    if (!aligned(ws, 16)) return MOEQ_EINVAL;
   }
   return done(launch_norms_backward(a, (hipStream_t)stream));
 }

@@ -44,6 +44,7 @@ struct Product {
   Side a, b;
   int32_t steps, first_steps;      // of the sum; of the first matrix (kBehind)
   int32_t tiles_m, tiles_n;
+  int32_t n_from;      // the launch's first column
 };
 
 __device__ __forceinline__ void mma(Sums<float>& c, i32x4 b, i32x4 a, __bf16) {
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_tile(Product p, Epi epi) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int tm, tn;
   tile_of(p, tm, tn);
-  const int m0 = tm * BM, n0 = tn * BN, z = blockIdx.y;
+  const int m0 = tm * BM, n0 = p.n_from + tn * BN, z = blockIdx.y;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int share = (p.steps + gridDim.z - 1) / gridDim.z, from = blockIdx.z * share, to = min(from + share, p.steps);
   Sums<T> acc[MB][NB];
@@ -379,7 +380,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   int tm, tn;
   tile_of(p, tm, tn);
-  const int m0 = tm * BM, n0 = tn * BN, z = blockIdx.y;
+  const int m0 = tm * BM, n0 = p.n_from + tn * BN, z = blockIdx.y;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int share = (p.steps + gridDim.z - 1) / gridDim.z, from = blockIdx.z * share, to = min(from + share, p.steps);
   Sums<T> acc[MB][NB];
@@ -647,7 +648,7 @@ bool straight(const Side& s, bool rows, Made made) {
 // The tile of a product, by the time it would take. A step's time is what was measured (bf16, us at the clock that the card keeps under
 // it), with as many workgroups a compute unit as their LDS leaves room for; a share has its beginning and end besides.
 enum Tile { kTile256, kTile128x256, kTile128, kTile128Two, kTile64 };
-struct Choice { Tile tile; int shares; };
+struct Choice { Tile tile; int shares, whole_columns; };      // whole_columns: of the rounds that fill the card with the largest tile, the rest in smaller ones
 constexpr int kMaxShares = 8;
 constexpr size_t kRoomMost = (size_t)48 << 20;      // of the sums of shares
 inline int64_t part_pitch(int64_t N) { return (N + 63) / 64 * 64; }
@@ -657,7 +658,7 @@ inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bo
   static constexpr Form kStraight[] = {{kTile256, 256, 256, 1, 1.75f, 8.f}, {kTile128x256, 128, 256, 1, 1.1f, 5.f}, {kTile128, 128, 128, 1, 0.7f, 4.f},
                                        {kTile128Two, 128, 128, 2, 1.2f, 5.f}, {kTile64, 64, 128, 2, 0.8f, 4.f}};
   static constexpr Form kThrough[] = {{kTile128, 128, 128, 2, 2.0f, 6.f}, {kTile64, 64, 128, 3, 2.0f, 5.f}};
-  Choice best = {kTile128, 1};
+  Choice best = {kTile128, 1, 0};
   float least = 1e30f;
   const auto look = [&](const Form& f) {
     for (int shares = 1; shares <= (room && batch == 1 ? kMaxShares : 1); ++shares) {
@@ -665,11 +666,22 @@ inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bo
       const int64_t tiles = (M + f.bm - 1) / f.bm * ((N + f.bn - 1) / f.bn) * batch * shares, rounds = (tiles + 256 * f.at_once - 1) / (256 * f.at_once);
       const float join = shares == 1 ? 0.f : 4.f + (float)(shares * M * N) * 8.f / 4e6f;      // (written and read at 4 TB/s)
       const float time = (float)rounds * ((float)((steps + shares - 1) / shares) * f.step + f.ends) + join;
-      if (time < least) least = time, best = {f.tile, shares};
+      if (time < least) least = time, best = {f.tile, shares, 0};
     }
   };
-  if (direct) for (const Form& f : kStraight) look(f);
-  else for (const Form& f : kThrough) look(f);
+  if (!direct) {
+    for (const Form& f : kThrough) look(f);
+    return best;
+  }
+  for (const Form& f : kStraight) look(f);
+  // Rounds of 256 of the largest tile, and what is left in tiles of half its rows.
+  const Form &large = kStraight[0], &half = kStraight[1];
+  const int64_t rows = (M + 255) / 256 * batch, columns = (N + 255) / 256, full = rows * columns / 256, whole = rows ? full * 256 / rows : 0;
+  if (full >= 1 && whole >= 1 && whole < columns) {
+    const int64_t rest = (M + 127) / 128 * batch * (columns - whole);
+    const float time = (float)full * ((float)steps * large.step + large.ends) + (float)((rest + 255) / 256) * ((float)steps * half.step + half.ends) + 3.f;
+    if (time < least) best = {kTile256, 1, (int)(whole * 256)};
+  }
   return best;
 }
 
@@ -710,7 +722,7 @@ __global__ __launch_bounds__(256) void k_join(Part<Word> p, int shares, int piec
 
 // S: the steps in LDS of a side that goes there straight; 0: through registers.
 template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, int S, Made B_MADE, class Epi>
-hipError_t launch_one(Product p, int M, int N, int batch, int shares, const Epi& epi, hipStream_t st) {
+hipError_t launch_one(Product p, int M, int N, int batch, int shares, int to_columns, const Epi& epi, hipStream_t st) {
   constexpr int kLds = (S ? S : 2) * (BM + BN) * kStepBytes;
   static_assert(WM * WN * finish_bytes(BN / WN / 32) <= kLds && kLds <= 160 * 1024, "the epilogue's rows; a compute unit's LDS");
   void (*kernel)(Product, Epi);
@@ -720,16 +732,17 @@ hipError_t launch_one(Product p, int M, int N, int batch, int shares, const Epi&
     static const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
     if (e != hipSuccess) return e;
   }
-  p.tiles_m = (M + BM - 1) / BM, p.tiles_n = (N + BN - 1) / BN;
+  p.tiles_m = (M + BM - 1) / BM, p.tiles_n = (N - p.n_from + BN - 1) / BN;
+  if (to_columns) p.tiles_n = std::min(p.tiles_n, to_columns / BN);
   kernel<<<dim3(p.tiles_m * p.tiles_n, batch, shares), 64 * WM * WN, kLds, st>>>(p, epi);
   return hipGetLastError();
 }
 template <typename T, bool A_ROWS, bool B_ROWS, int BM, int BN, int WM, int WN, int S, Made B_MADE, class Epi>
 hipError_t launch_as(const Product& p, int M, int N, int batch, int shares, void* room, const Epi& epi, hipStream_t st) {
-  if (shares == 1) return launch_one<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, B_MADE>(p, M, N, batch, 1, epi, st);
+  if (shares == 1) return launch_one<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, B_MADE>(p, M, N, batch, 1, 0, epi, st);
   using Word = WordOf<T>;
   const Part<Word> part = {(Word*)room, part_pitch(N), M};
-  if (hipError_t e = launch_one<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, B_MADE>(p, M, N, 1, shares, part, st); e != hipSuccess) return e;
+  if (hipError_t e = launch_one<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, B_MADE>(p, M, N, 1, shares, 0, part, st); e != hipSuccess) return e;
   const int pieces = (int)part.pitch / (B_MADE == kTurns ? 16 : 8);
   k_join<Word, B_MADE, Epi><<<(uint32_t)(((int64_t)M * pieces + 255) / 256), 256, 0, st>>>(part, shares, pieces, epi);
   return hipGetLastError();
@@ -748,7 +761,11 @@ hipError_t launch_tile(Product p, int M, int N, int batch, void* room, const Epi
     return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 0, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
   }
   switch (c.tile) {
-    case kTile256: return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 4, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    case kTile256:
+      if (c.whole_columns == 0) return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 4, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+      if (hipError_t e = launch_one<T, A_ROWS, B_ROWS, 256, 256, 2, 4, 2, B_MADE>(p, M, N, batch, 1, c.whole_columns, epi, st); e != hipSuccess) return e;
+      p.n_from = c.whole_columns;
+      return launch_one<T, A_ROWS, B_ROWS, 128, 256, 2, 2, 3, B_MADE>(p, M, N, batch, 1, 0, epi, st);
     case kTile128x256: return launch_as<T, A_ROWS, B_ROWS, 128, 256, 2, 2, 3, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
     case kTile128: return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 4, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
     case kTile128Two: return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
