@@ -167,7 +167,7 @@ struct RowIn {
 // A stream of rows: stream, stream + streams, ... The next row is on its way while one is worked on, and the weights stay in registers,
 // up to two vectors a thread.
 template <typename F, typename R, typename N, int W, int NV>
-__global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, int streams, int pitch) {
+__global__ __launch_bounds__(kThreadsOf<W>, NV == 1 ? 4 : 2) void k_norms_backward(NormsArgs a, int streams, int pitch) {
   constexpr bool kHeld = NV <= 2;
   __shared__ float sh[2][W][4];
   RowSum<W> sum{sh};
@@ -176,7 +176,13 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, i
   if (stream >= streams) return;
   const float by_d = 1.f / (float)d;
   float sum_after[NV][VE] = {}, sum_before[NV][VE] = {};
-  Raw<float, NV> after, before;
+  Raw<float, kHeld ? NV : 1> after, before;
+  const auto weight = [&](const Raw<float, kHeld ? NV : 1>& held, const float* w, int i, float (&v)[VE]) {
+    if constexpr (!kHeld) load_part(v, w, (at + i * 64 * W) * VE, d);
+    else
+#pragma unroll
+      for (int j = 0; j < VE; ++j) v[j] = held.v[i][j];
+  };
   RowIn<F, R, N, NV> in;
   if constexpr (kHeld) {
     if (a.w_after) after.load(a.w_after, at, 64 * W, d);
@@ -186,40 +192,43 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, i
   for (int64_t row = stream; row < a.T; row += streams) {
     if constexpr (!kHeld) {
       in.load(a, row, at, 64 * W);
-      if (a.w_after) after.load(a.w_after, at, 64 * W, d);
-      if (a.w_before) before.load(a.w_before, at, 64 * W, d);
     }
     const RowIn<F, R, N, NV> now = in;
     if (kHeld && row + streams < a.T) in.load(a, row + streams, at, 64 * W);
     const float g = now.g;
     float s[3] = {0.f, 0.f, 0.f};      // y . y, (dn w) . y, f . f
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+      float wb[VE];
+      if (a.w_before) weight(before, a.w_before, i, wb);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
         if (a.w_before) {
           const float y = (float)now.y.v[i][j];
-          s[0] += y * y, s[1] += (float)now.dn.v[i][j] * before.v[i][j] * y;
+          s[0] += y * y, s[1] += (float)now.dn.v[i][j] * wb[j] * y;
         }
         s[2] += (float)now.f.v[i][j] * (float)now.f.v[i][j];
       }
+    }
     sum(s);
     const float by = 1.f / sqrtf(s[0] * by_d + a.eps), mean = s[1] * by * by_d;      // of y; of dn w u(y)
     const float bf = a.w_after ? 1.f / sqrtf(s[2] * by_d + a.eps) : 1.f;
     float t[1] = {0.f}, dy[NV][VE];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float out[VE];
+      float out[VE], wb[VE], wa[VE];
+      if (a.w_before) weight(before, a.w_before, i, wb);
+      if (a.w_after) weight(after, a.w_after, i, wa);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
         dy[i][j] = (float)now.dy.v[i][j];
         if (a.w_before) {
           const float u = (float)now.y.v[i][j] * by, dn = (float)now.dn.v[i][j];
           sum_before[i][j] += dn * u;
-          dy[i][j] += by * (dn * before.v[i][j] - u * mean);
+          dy[i][j] += by * (dn * wb[j] - u * mean);
         }
         const float f = (float)now.f.v[i][j];
-        t[0] += dy[i][j] * (a.w_after ? f * bf * after.v[i][j] : f);
+        t[0] += dy[i][j] * (a.w_after ? f * bf * wa[j] : f);
         out[j] = a.alpha * dy[i][j];
       }
       store_part((R*)a.out_y + row * a.out_y_stride, out, (at + i * 64 * W) * VE, d);
@@ -229,14 +238,15 @@ __global__ __launch_bounds__(kThreadsOf<W>) void k_norms_backward(NormsArgs a, i
     const float back = g * t[0] * by_d;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      float out[VE];
+      float out[VE], wa[VE];
+      if (a.w_after) weight(after, a.w_after, i, wa);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
         out[j] = a.gate ? dy[i][j] * g : dy[i][j];
         if (a.w_after) {
           const float u = (float)now.f.v[i][j] * bf;
           sum_after[i][j] += out[j] * u;
-          out[j] = bf * (out[j] * after.v[i][j] - u * back);
+          out[j] = bf * (out[j] * wa[j] - u * back);
         }
       }
       store_part((F*)a.out_n + row * a.out_n_stride, out, (at + i * 64 * W) * VE, d);

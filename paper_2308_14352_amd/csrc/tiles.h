@@ -504,12 +504,11 @@ __device__ __forceinline__ void mma16(f32x4& c, i32x4 b, i32x4 a, float) {
 }
 __device__ __forceinline__ void mma16(i32x4& c, i32x4 b, i32x4 a, int8_t) { c = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0); }
 
-constexpr int kDeep = 4;
 template <typename T, int RB, int NG, int W, Made MADE, class Epi>
 __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   using Word = std::conditional_t<std::is_same<T, int8_t>::value, int32_t, float>;
   using Acc = std::conditional_t<std::is_same<T, int8_t>::value, i32x4, f32x4>;
-  constexpr int kRows = RB * 16;
+  constexpr int kRows = RB * 16, kDeep = 4;      // lines ahead (2 or 1 for the four blocks, so that two workgroups share a compute unit: up of one token 54.6, 52.1 us instead of 50.4)
   __shared__ __attribute__((aligned(16))) Word sums[W][NG * 16][kRows + 4];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, at = lane / 16 * kPiece<T>;
   const int n0 = blockIdx.x * (MADE == kTurns ? kRows / 2 : kRows);
@@ -624,17 +623,21 @@ hipError_t few_as(const Product& p, const Epi& epi, hipStream_t st) {
   k_few<T, RB, NG, W, MADE, Epi><<<(p.b.n + kRows - 1) / kRows, 64 * W, 0, st>>>(p, epi);
   return hipGetLastError();
 }
-// a.n <= kFewRows; b and a by rows, at any alignment.
+// a.n <= kFewRows; b and a by rows, at any alignment. Two blocks of b's rows a workgroup where that leaves one for every compute unit
+// (three rows, 14336 x 4096 codes: 14.0 us, with one 15.0; 4096 x 14336 bf16: 34.9 with two, 22.6 with one).
 template <typename T, Made MADE, class Epi>
 hipError_t launch_few(const Product& p, const Epi& epi, hipStream_t st) {
-  constexpr int kRB = MADE == kTurns ? 4 : 1;
-  auto go = [&](auto ng, auto w) { return few_as<T, kRB, decltype(ng)::value, decltype(w)::value, MADE>(p, epi, st); };
   using std::integral_constant;
   const bool short_sum = p.b.k <= 16 * kStep<T>;
-  if (p.a.n <= 16) return short_sum ? go(integral_constant<int, 1>{}, integral_constant<int, 4>{}) : go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
-  // (64 rows of b and 32 of a: eight wavefronts' sums would be 70 KB)
-  if (short_sum || MADE == kTurns) return go(integral_constant<int, 2>{}, integral_constant<int, 4>{});
-  return go(integral_constant<int, 2>{}, integral_constant<int, MADE == kTurns ? 4 : 8>{});
+  const auto by_blocks = [&](auto rb) {
+    const auto go = [&](auto ng, auto w) { return few_as<T, decltype(rb)::value, decltype(ng)::value, decltype(w)::value, MADE>(p, epi, st); };
+    if (p.a.n <= 16) return short_sum ? go(integral_constant<int, 1>{}, integral_constant<int, 4>{}) : go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    // (64 rows of b and 32 of a: eight wavefronts' sums would be 70 KB)
+    if (short_sum || MADE == kTurns) return go(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+    return go(integral_constant<int, 2>{}, integral_constant<int, MADE == kTurns ? 4 : 8>{});
+  };
+  if constexpr (MADE == kTurns) return by_blocks(integral_constant<int, 4>{});
+  else return p.b.n >= 256 * 32 ? by_blocks(integral_constant<int, 2>{}) : by_blocks(integral_constant<int, 1>{});
 }
 
 // Whether a side can go straight to LDS: every row that is read (rows of the product or of the sum) at a multiple of 16 bytes and whole
