@@ -140,26 +140,84 @@ struct Act {
 };
 
 inline int64_t up_to(int64_t n, int64_t by) { return (n + by - 1) / by * by; }
+
+// Rows copied to rows of whole steps, zeros behind their ends: operands whose rows end inside 16 bytes (odd widths) cannot go straight to
+// LDS, and through registers a product takes twice as long. Up to five matrices a launch.
+struct Copies {
+  struct One { const char* from; int64_t stride; char* to; int32_t rows, width, pitch; } of[5];
+  int32_t n;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_copy_rows(Copies c) {
+  const Copies::One& m = c.of[blockIdx.y];
+  const int pieces = m.pitch / kPiece<T>;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)m.rows * pieces; i += (int64_t)gridDim.x * 256) {
+    const int row = (int)(i / pieces), at = (int)(i - (int64_t)row * pieces) * kPiece<T>;
+    const uint4 v = piece<T>(m.from + row * m.stride, at, m.width);
+    __builtin_memcpy(__builtin_assume_aligned(m.to + ((int64_t)row * m.pitch + at) * (int64_t)sizeof(T), 16), &v, 16);
+  }
+}
+// Calls of fewer rows do not win the copies back, as weights are read and written for them (us without and with: forward and gradient of
+// 2048 rows of 2051 x 5637 bf16 379 / 219, 1112 / 461; of 600 rows of 1001 x 2731 55 / 43, 136 / 92).
+constexpr int kCopyRows = 512;
+
 // The workspace's parts, each at a multiple of 256 bytes.
 struct FfnPlan {
   int64_t Tp, Fp, Dp;
-  size_t h, dab, x, ab, room, bytes;
+  bool copy_in, copy_out, copy_rows;      // w_in and w_gate, w_out, x and dy go through copies
+  size_t h, dab, x, dy, ab, w_in, w_gate, w_out, room, bytes;
   FfnPlan(const FfnArgs& a, bool backward) : Tp(up_to(a.T, 64)) {
     const size_t e = dtype_bytes(a.dtype);
+    const auto odd = [&](const void* w, int64_t width) { return a.T >= kCopyRows && ((uintptr_t)w % 16 || width * e % 16); };
     Fp = up_to(a.F, kStepBytes / e), Dp = up_to(a.D, kStepBytes / e);      // (whole steps, each with a column that there is)
+    copy_in = odd(a.w_in, a.D) || odd(a.w_gate, a.D), copy_out = odd(a.w_out, a.F), copy_rows = odd(nullptr, a.D);
     size_t at = 0;
     auto take = [&](size_t n) { const size_t here = at; at += (n + 255) / 256 * 256; return here; };
     h = take(Tp * Fp * e);
-    dab = x = ab = at;
+    dab = x = dy = ab = w_in = w_gate = w_out = at;
+    if (copy_rows || (backward && a.x_codes)) x = take((size_t)a.T * Dp * e);
     if (backward) {
       dab = take(Tp * 2 * Fp * e);
-      if (a.x_codes) x = take((size_t)a.T * Dp * e);
+      if (copy_rows) dy = take((size_t)a.T * Dp * e);
       if (a.keep == MOEQ_KEEP_NONE) ab = take((size_t)2 * a.T * a.F * e);
     }
+    if (copy_in) w_in = take((size_t)a.F * Dp * e), w_gate = take((size_t)a.F * Dp * e);
+    if (copy_out) w_out = take((size_t)a.D * Fp * e);
     room = take(std::max(room_bytes(Tp, 2 * Fp), room_bytes(a.T, a.D)));
     bytes = at;
   }
 };
+
+// A matrix as the products read it.
+struct Rows { const void* p; int64_t stride; int32_t width; };      // elements
+struct FfnOperands { Rows x, dy, w_in, w_gate, w_out; };
+template <typename T>
+hipError_t operands(const FfnArgs& a, const FfnPlan& plan, bool backward, FfnOperands& o, hipStream_t st) {
+  char* ws = (char*)a.ws;
+  o = {{a.x, a.x_stride, a.D}, {a.dy, a.dy_stride, a.D}, {a.w_in, a.D, a.D}, {a.w_gate, a.D, a.D}, {a.w_out, a.F, a.F}};
+  if (a.T == 0) return hipSuccess;
+  Copies c = {};
+  int64_t most = 0;
+  const auto copy = [&](Rows& r, size_t to, int32_t rows, int64_t pitch) {
+    c.of[c.n++] = {(const char*)r.p, r.stride * (int64_t)sizeof(T), ws + to, rows, r.width, (int32_t)pitch};
+    most = std::max(most, rows * pitch / kPiece<T>);
+    r = {ws + to, pitch, (int32_t)pitch};
+  };
+  if (a.x_codes) {      // (rows of Dp columns, of which D are written)
+    Rows8Args r = {};
+    r.T = a.T, r.d = a.D, r.dtype = a.dtype, r.codes = (int8_t*)a.x_codes, r.exps = (int8_t*)a.x_exps, r.out = ws + plan.x, r.out_stride = plan.Dp;
+    if (hipError_t s = launch_unpack8(r, st); s != hipSuccess) return s;
+    o.x = {r.out, plan.Dp, a.D};
+  } else if (plan.copy_rows) {
+    copy(o.x, plan.x, a.T, plan.Dp);
+  }
+  if (backward && plan.copy_rows) copy(o.dy, plan.dy, a.T, plan.Dp);
+  if (plan.copy_in) copy(o.w_in, plan.w_in, a.F, plan.Dp), copy(o.w_gate, plan.w_gate, a.F, plan.Dp);
+  if (plan.copy_out) copy(o.w_out, plan.w_out, a.D, plan.Fp);
+  if (!c.n) return hipSuccess;
+  k_copy_rows<T><<<dim3((uint32_t)std::min<int64_t>((most + 255) / 256, 1 << 14), c.n), 256, 0, st>>>(c);
+  return hipGetLastError();
+}
 
 template <typename T>
 Side side(const void* p, int64_t stride, int32_t n, int32_t k, const void* q = nullptr) {
@@ -168,8 +226,10 @@ Side side(const void* p, int64_t stride, int32_t n, int32_t k, const void* q = n
 template <typename T> int32_t steps_of(int64_t k) { return (int32_t)((k + kStep<T> - 1) / kStep<T>); }
 
 template <typename T>
-hipError_t up(const FfnArgs& a, const void* x, int64_t x_stride, const Up<T>& epi, void* room, hipStream_t st) {
-  Product p = {side<T>(x, x_stride, a.T, a.D), side<T>(a.w_in, a.D, a.F, a.D, a.w_gate), steps_of<T>(a.D), 0};
+hipError_t up(const FfnArgs& a, const FfnOperands& o, const Up<T>& epi, void* room, hipStream_t st) {
+  // (where one side's rows go on in zeros and the other's end, the sum ends with the shorter)
+  const int32_t k = std::min(o.x.width, o.w_in.width);
+  Product p = {side<T>(o.x.p, o.x.stride, a.T, k), side<T>(o.w_in.p, o.w_in.stride, a.F, k, o.w_gate.p), steps_of<T>(k), 0};
   if (a.T <= kFewRows) return launch_few<T, kTurns>(p, epi, st);
   return launch_tile<T, true, true, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, room, epi, st);
 }
@@ -177,15 +237,19 @@ hipError_t up(const FfnArgs& a, const void* x, int64_t x_stride, const Up<T>& ep
 template <typename T>
 hipError_t ffn_forward(const FfnArgs& a, hipStream_t st) {
   const FfnPlan plan(a, false);
+  FfnOperands o;
+  if (hipError_t s = operands<T>(a, plan, false, o, st); s != hipSuccess) return s;
   T* h = (T*)((char*)a.ws + plan.h);
+  void* room = (char*)a.ws + plan.room;
   Up<T> e = {h, plan.Fp, a.T, a.F, (int32_t)plan.Tp, (int32_t)plan.Fp, a.keep, (T*)a.ab, (int8_t*)a.ab, a.ab_exps};
-  if (hipError_t s = up<T>(a, a.x, a.x_stride, e, (char*)a.ws + plan.room, st); s != hipSuccess) return s;
-  Product p = {side<T>(h, plan.Fp, a.T <= kFewRows ? a.T : (int32_t)plan.Tp, (int32_t)plan.Fp), side<T>(a.w_out, a.F, a.D, a.F), steps_of<T>(a.F), 0};
-  auto down = [&](auto o) {
-    using O = decltype(o);
+  if (hipError_t s = up<T>(a, o, e, room, st); s != hipSuccess) return s;
+  const int32_t k = o.w_out.width;
+  Product p = {side<T>(h, plan.Fp, a.T <= kFewRows ? a.T : (int32_t)plan.Tp, (int32_t)plan.Fp), side<T>(o.w_out.p, o.w_out.stride, a.D, k), steps_of<T>(k), 0};
+  auto down = [&](auto t) {
+    using O = decltype(t);
     Store<O> out = {{(O*)a.y, nullptr}, a.y_stride, (const O*)a.base, a.base_stride, a.T, a.D};
     if (a.T <= kFewRows) return launch_few<T, kOne>(p, out, st);
-    return launch_tile<T, true, true, kOne>(p, a.T, a.D, 1, (char*)a.ws + plan.room, out, st);
+    return launch_tile<T, true, true, kOne>(p, a.T, a.D, 1, room, out, st);
   };
   if (a.y_dtype == a.dtype) return down(T{});
   return down(0.f);
@@ -196,38 +260,35 @@ hipError_t ffn_backward(const FfnArgs& a, hipStream_t st) {
   const FfnPlan plan(a, true);
   char* ws = (char*)a.ws;
   T *h = (T*)(ws + plan.h), *dab = (T*)(ws + plan.dab);
+  void* room = ws + plan.room;
   const int32_t Tp = (int32_t)plan.Tp, Fp = (int32_t)plan.Fp;
-  const void* x = a.x;
-  int64_t x_stride = a.x_stride;
+  FfnOperands o;
+  if (hipError_t s = operands<T>(a, plan, true, o, st); s != hipSuccess) return s;
   if (a.T > 0) {
-    if (a.x_codes) {
-      Rows8Args r = {};
-      r.T = a.T, r.d = a.D, r.dtype = a.dtype, r.codes = (int8_t*)a.x_codes, r.exps = (int8_t*)a.x_exps, r.out = ws + plan.x, r.out_stride = plan.Dp;
-      if (hipError_t s = launch_unpack8(r, st); s != hipSuccess) return s;
-      x = r.out, x_stride = plan.Dp;
-    }
     const T* ab = (const T*)a.ab;
     if (a.keep == MOEQ_KEEP_NONE) {
       T* made = (T*)(ws + plan.ab);
       Up<T> e = {nullptr, 0, a.T, a.F, Tp, Fp, MOEQ_KEEP_OWN, made, nullptr, nullptr};
-      if (hipError_t s = up<T>(a, x, x_stride, e, ws + plan.room, st); s != hipSuccess) return s;
+      if (hipError_t s = up<T>(a, o, e, room, st); s != hipSuccess) return s;
       ab = made;
     }
     const bool eight = a.keep == MOEQ_KEEP_8;
     Act<T> e = {eight ? nullptr : ab, eight ? (const int8_t*)a.ab : nullptr, a.ab_exps, dab, h, a.T, a.F, Tp, Fp};
-    Product p = {side<T>(a.dy, a.dy_stride, a.T, a.D), side<T>(a.w_out, a.F, a.F, a.D), steps_of<T>(a.D), 0};
-    if (hipError_t s = launch_tile<T, true, false, kOne>(p, Tp, Fp, 1, ws + plan.room, e, st); s != hipSuccess) return s;
+    // (the sum goes over w_out's rows: D of them)
+    Product p = {side<T>(o.dy.p, o.dy.stride, a.T, o.dy.width), side<T>(o.w_out.p, o.w_out.stride, o.w_out.width, a.D), steps_of<T>(a.D), 0};
+    if (hipError_t s = launch_tile<T, true, false, kOne>(p, Tp, Fp, 1, room, e, st); s != hipSuccess) return s;
     if (a.dx) {
-      Product q = {side<T>(dab, 2 * plan.Fp, Tp, 2 * Fp), side<T>(a.w_in, a.D, a.D, a.F, a.w_gate), 2 * steps_of<T>(Fp), steps_of<T>(Fp)};
+      Product q = {side<T>(dab, 2 * plan.Fp, Tp, 2 * Fp), side<T>(o.w_in.p, o.w_in.stride, o.w_in.width, a.F, o.w_gate.p), 2 * steps_of<T>(Fp), steps_of<T>(Fp)};
       Store<T> out = {{(T*)a.dx, nullptr}, a.dx_stride, nullptr, 0, a.T, a.D};
-      if (hipError_t s = launch_tile<T, true, false, kBehind>(q, a.T, a.D, 1, ws + plan.room, out, st); s != hipSuccess) return s;
+      if (hipError_t s = launch_tile<T, true, false, kBehind>(q, a.T, a.D, 1, room, out, st); s != hipSuccess) return s;
     }
   }
-  // (the workspace's rows are zero from row T on, those of x and dy end there)
-  Product p = {side<T>(dab, 2 * plan.Fp, a.F, Tp, dab + Fp), side<T>(x, x_stride, a.D, a.T), steps_of<T>(a.T), 0};
+  // (the workspace's rows are zero from row T on, those of x and dy end there; what stands behind the columns of unpacked rows comes out
+  // in columns that are not stored)
+  Product p = {side<T>(dab, 2 * plan.Fp, Fp, Tp, dab + Fp), side<T>(o.x.p, o.x.stride, a.x_codes ? (int32_t)plan.Dp : o.x.width, a.T), steps_of<T>(a.T), 0};
   Store<T> out = {{(T*)a.dw_in, (T*)a.dw_gate}, a.D, nullptr, 0, a.F, a.D};
   if (hipError_t s = launch_tile<T, false, false, kOne>(p, a.F, a.D, 2, nullptr, out, st); s != hipSuccess) return s;
-  p.a = side<T>(a.dy, a.dy_stride, a.D, a.T), p.b = side<T>(h, plan.Fp, a.F, Tp);
+  p.a = side<T>(o.dy.p, o.dy.stride, o.dy.width, a.T), p.b = side<T>(h, plan.Fp, Fp, Tp);
   out = {{(T*)a.dw_out, nullptr}, a.F, nullptr, 0, a.D, a.F};
   return launch_tile<T, false, false, kOne>(p, a.D, a.F, 1, nullptr, out, st);
 }

@@ -60,6 +60,33 @@ __device__ __forceinline__ void mma(Sums<float>& c, i32x4 b, i32x4 a, float) {
 }
 __device__ __forceinline__ void mma(Sums<int8_t>& c, i32x4 b, i32x4 a, int8_t) { c = __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, c, 0, 0, 0); }
 
+// fp32 operands of sides that go straight to LDS: three bf16 pieces each, x = h + m + l to the last bit (each piece is what is left, rounded
+// to nearest), and of the nine products of pieces the six that reach fp32's precision: what is left out is below 2^-25 of |a b|. The chip's
+// fp32 matrix instructions take 512 cycles for 16 of the sum's length where these six take 192. (Past bf16's largest number, 3.39e38, h is
+// infinite and the sum NaN.)
+struct Pieces { bf16x8 h, m, l; };
+__device__ __forceinline__ Pieces in_pieces(const i32x4 (&x)[2]) {
+  Pieces p;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const f32x4 half = __builtin_bit_cast(f32x4, x[i / 4]);
+    const float v = half[i % 4];
+    p.h[i] = (__bf16)v;
+    const float r = v - (float)p.h[i];
+    p.m[i] = (__bf16)r;
+    p.l[i] = (__bf16)(r - (float)p.m[i]);
+  }
+  return p;
+}
+__device__ __forceinline__ void mma(Sums<float>& c, const Pieces& b, const Pieces& a) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.l, a.h, c, 0, 0, 0);      // (small ones first)
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.h, a.l, c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.m, a.m, c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.m, a.h, c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.h, a.m, c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.h, a.h, c, 0, 0, 0);
+}
+
 // Where 16 bytes of a tile of R rows lie in LDS: piece `at` of tile row `row` (rows), or of k `row` (columns).
 template <typename T, bool ROWS, int R>
 __device__ __forceinline__ int place(int row, int at) {
@@ -373,7 +400,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   constexpr int NT = 64 * WM * WN, MB = BM / WM / 32, NB = BN / WN / 32, kBuffer = (BM + BN) * kStepBytes;
   using FA = Fetch<T, A_ROWS, BM, NT, A_MADE>;
   using FB = Fetch<T, B_ROWS, BN, NT, B_MADE>;
-  constexpr int LA = FA::kPieces, L = LA + FB::kPieces, kSlots = MB * NB;      // requests of a step; matrix instructions of a slice
+  constexpr int LA = FA::kPieces, L = LA + FB::kPieces, kSlots = MB * NB, kParts = std::is_same<T, float>::value ? 2 : 1, kSlices = 4 / kParts;      // requests of a step; matrix instructions of a slice
   constexpr int kGap = kSlots >= 2 * (MB + NB) ? 2 : 1;      // where there is room, a read and a request go with instructions of their own
   constexpr int kTurnsOf = kSlots / kGap, kReads = (MB + NB + kTurnsOf - 1) / kTurnsOf, kAsks = (L + 2 * kTurnsOf - 1) / (2 * kTurnsOf);      // (a step's requests go with two slices, a slice's reads with one)
   constexpr int kAtOnce = kTurnsOf * kAsks < L ? kTurnsOf * kAsks : L;      // requests with the first of them
@@ -394,7 +421,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
   a.init(p.a, z, m0, __builtin_amdgcn_readfirstlane(lds_base));
   b.init(p.b, 0, n0, __builtin_amdgcn_readfirstlane(lds_base + BM * kStepBytes));
   a.lds = __builtin_amdgcn_readfirstlane(a.lds), b.lds = __builtin_amdgcn_readfirstlane(b.lds);
-  i32x4 u[2][MB], v[2][NB];
+  // (an operand: 16 bytes a lane of each of `kParts` slices of 32 bytes, two for the pieces of fp32)
+  i32x4 u[2][MB][kParts], v[2][NB][kParts];
   // Where step `step`'s requests go: its scalar addresses, computed once.
   const char *ask_a = nullptr, *ask_b[2] = {nullptr, nullptr};
   auto aim = [&](int step) {
@@ -414,8 +442,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
     else if (j < L) b.piece(j - LA, ask_b[B_MADE == kTurns && NT == 256 ? (j - LA) % 2 : 0], buffer);
   };
   auto read = [&](int set, int j, const char* at, int slice) {      // one operand: those of b first
-    if (j < NB) v[set][j] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice);
-    else if (j < NB + MB) u[set][j - NB] = operand<T, A_ROWS, BM>(at, wm + (j - NB) * 32, slice);
+#pragma unroll
+    for (int h = 0; h < kParts; ++h) {
+      if (j < NB) v[set][j][h] = operand<T, B_ROWS, BN>(at + BM * kStepBytes, wn + j * 32, slice * kParts + h);
+      else if (j < NB + MB) u[set][j - NB][h] = operand<T, A_ROWS, BM>(at, wm + (j - NB) * 32, slice * kParts + h);
+    }
   };
   auto ask_some = [&](int turn, int buffer) {
 #pragma unroll
@@ -448,14 +479,21 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
       const char *here = lds + buffer * kBuffer, *next = lds + following * kBuffer;
       const int left = step - from;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
+      for (int s = 0; s < kSlices; ++s) {
         const int cur = s % 2;
+        Pieces pu[kParts == 2 ? MB : 1], pv[kParts == 2 ? NB : 1];
+        if constexpr (kParts == 2) {
+#pragma unroll
+          for (int i = 0; i < MB; ++i) pu[i] = in_pieces(u[cur][i]);
+#pragma unroll
+          for (int j = 0; j < NB; ++j) pv[j] = in_pieces(v[cur][j]);
+        }
 #pragma unroll
         for (int t = 0; t < kSlots; ++t) {
           __builtin_amdgcn_sched_barrier(0);
           const int turn = t / kGap;
           const bool reads = t % kGap == 0, asks = t % kGap == kGap - 1;
-          if (s < 3) {
+          if (s < kSlices - 1) {
             if (reads) read_some(cur ^ 1, turn, here, s + 1);
             if (s == 0 && more && asks && left >= S - 1) ask_some(kTurnsOf + turn, freed);
           } else if (more) {
@@ -471,7 +509,8 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
             if (reads) read_some(0, turn, next, 0);
             if (asks && left >= S) ask_some(turn, buffer);
           }
-          mma(acc[t / NB][t % NB], v[cur][t % NB], u[cur][t / NB], T{});
+          if constexpr (kParts == 2) mma(acc[t / NB][t % NB], pv[t % NB], pu[t / NB]);
+          else mma(acc[t / NB][t % NB], v[cur][t % NB][0], u[cur][t / NB][0], T{});
         }
       }
     };
@@ -515,8 +554,8 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   const char *bp[RB], *ap[NG];
 #pragma unroll
   for (int r = 0; r < RB; ++r) {
-    const int n = MADE == kTurns ? n0 + r % (RB / 2) * 16 + row : n0 + r * 16 + row;
-    bp[r] = p.b.p[MADE == kTurns ? r / (RB / 2) : 0] + min(n, p.b.n - 1) * p.b.stride;
+    const int n = MADE == kTurns ? n0 + r % ((RB + 1) / 2) * 16 + row : n0 + r * 16 + row;
+    bp[r] = p.b.p[MADE == kTurns ? r / ((RB + 1) / 2) : 0] + min(n, p.b.n - 1) * p.b.stride;
   }
 #pragma unroll
   for (int g = 0; g < NG; ++g) ap[g] = p.a.p[0] + min(g * 16 + row, p.a.n - 1) * p.a.stride;
@@ -656,7 +695,8 @@ constexpr int kMaxShares = 8;
 constexpr size_t kRoomMost = (size_t)48 << 20;      // of the sums of shares
 inline int64_t part_pitch(int64_t N) { return (N + 63) / 64 * 64; }
 inline size_t room_bytes(int64_t M, int64_t N) { return std::min((size_t)(kMaxShares * M * part_pitch(N) * 4), kRoomMost); }
-inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bool room) {
+// The pieces of fp32 leave no registers for the largest tiles.
+inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bool room, bool fp32) {
   struct Form { Tile tile; int bm, bn, at_once; float step, ends; };
   static constexpr Form kStraight[] = {{kTile256, 256, 256, 1, 1.75f, 8.f}, {kTile128x256, 128, 256, 1, 1.1f, 5.f}, {kTile128, 128, 128, 1, 0.7f, 4.f},
                                        {kTile128Two, 128, 128, 2, 1.2f, 5.f}, {kTile64, 64, 128, 2, 0.8f, 4.f}};
@@ -676,13 +716,18 @@ inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bo
     for (const Form& f : kThrough) look(f);
     return best;
   }
+  static constexpr Form kPieces[] = {{kTile128, 128, 128, 1, 1.6f, 5.f}, {kTile128Two, 128, 128, 2, 2.2f, 6.f}, {kTile64, 64, 128, 2, 1.5f, 5.f}};
+  if (fp32) {
+    for (const Form& f : kPieces) look(f);
+    return best;
+  }
   for (const Form& f : kStraight) look(f);
   // Rounds of 256 of the largest tile, and what is left in tiles of half its rows.
   const Form &large = kStraight[0], &half = kStraight[1];
-  const int64_t rows = (M + 255) / 256 * batch, columns = (N + 255) / 256, full = rows * columns / 256, whole = rows ? full * 256 / rows : 0;
-  if (full >= 1 && whole >= 1 && whole < columns) {
+  const int64_t rows = (M + 255) / 256 * batch, columns = (N + 255) / 256, rounds = rows * columns / 256, whole = rows ? rounds * 256 / rows : 0;
+  if (rounds >= 1 && whole >= 1 && whole < columns) {
     const int64_t rest = (M + 127) / 128 * batch * (columns - whole);
-    const float time = (float)full * ((float)steps * large.step + large.ends) + (float)((rest + 255) / 256) * ((float)steps * half.step + half.ends) + 3.f;
+    const float time = (float)rounds * ((float)steps * large.step + large.ends) + (float)((rest + 255) / 256) * ((float)steps * half.step + half.ends) + 3.f;
     if (time < least) best = {kTile256, 1, (int)(whole * 256)};
   }
   return best;
@@ -758,12 +803,16 @@ hipError_t launch_tile(Product p, int M, int N, int batch, void* room, const Epi
   if (p.a.k == 1 && !A_ROWS) p.a.stride = 0;
   if (p.b.k == 1 && !B_ROWS) p.b.stride = 0;
   const bool direct = straight<T>(p.a, A_ROWS, batch == 2 ? kTurns : kOne) && straight<T>(p.b, B_ROWS, B_MADE);
-  const Choice c = choose(M, N, batch, p.steps, direct, room != nullptr);
+  const Choice c = choose(M, N, batch, p.steps, direct, room != nullptr, std::is_same<T, float>::value);
   if (!direct) {
     if (c.tile == kTile64) return launch_as<T, A_ROWS, B_ROWS, 64, 128, 2, 2, 0, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
     return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 0, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
   }
-  switch (c.tile) {
+  if constexpr (std::is_same<T, float>::value) {
+    if (c.tile == kTile128) return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 4, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    if (c.tile == kTile128Two) return launch_as<T, A_ROWS, B_ROWS, 128, 128, 2, 2, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+    return launch_as<T, A_ROWS, B_ROWS, 64, 128, 2, 2, 3, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
+  } else switch (c.tile) {
     case kTile256:
       if (c.whole_columns == 0) return launch_as<T, A_ROWS, B_ROWS, 256, 256, 2, 4, 2, B_MADE>(p, M, N, batch, c.shares, room, epi, st);
       if (hipError_t e = launch_one<T, A_ROWS, B_ROWS, 256, 256, 2, 4, 2, B_MADE>(p, M, N, batch, 1, c.whole_columns, epi, st); e != hipSuccess) return e;

@@ -113,7 +113,9 @@ def test_forward_and_gradient(T, d, f, kind):
 
 # enough rows or columns for the largest tiles
 @pytest.mark.parametrize("T,d,f,kind", [(1030, 256, 4224, "bf16"), (2056, 512, 1032, "bf16"), (520, 1160, 2080, "f16"), (1100, 520, 2056, "f32"), (40, 2048, 3000, "bf16"),
-                                        (12, 4096, 2752, "f16"), (900, 2304, 1100, "bf16"), (130, 2051, 1037, "bf16")])
+                                        (12, 4096, 2752, "f16"), (900, 2304, 1100, "bf16"), (130, 2051, 1037, "bf16"),
+                                        # rows that are copied: odd widths on either side, one of the types each
+                                        (600, 129, 257, "bf16"), (515, 131, 64, "f16"), (520, 72, 131, "bf16"), (512, 33, 70, "f32"), (511, 131, 130, "bf16")])
 def test_larger(T, d, f, kind):
     whole(T, d, f, kind)
 
