@@ -549,7 +549,9 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   using Acc = std::conditional_t<std::is_same<T, int8_t>::value, i32x4, f32x4>;
   constexpr int kRows = RB * 16, kDeep = 4;      // lines ahead (2 or 1 for the four blocks, so that two workgroups share a compute unit: up of one token 54.6, 52.1 us instead of 50.4)
   __shared__ __attribute__((aligned(16))) Word sums[W][NG * 16][kRows + 4];
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16, at = lane / 16 * kPiece<T>;
+  const int lane = threadIdx.x % 64, row = lane % 16, at = lane / 16 * kPiece<T>;
+  // (known to be the same in all lanes: conditions around matrix instructions, which write whatever lanes are masked, have to be branches)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int n0 = blockIdx.x * (MADE == kTurns ? kRows / 2 : kRows);
   const char *bp[RB], *ap[NG];
 #pragma unroll
