@@ -700,8 +700,8 @@ inline size_t room_bytes(int64_t M, int64_t N) { return std::min((size_t)(kMaxSh
 // The pieces of fp32 leave no registers for the largest tiles.
 inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bool room, bool fp32) {
   struct Form { Tile tile; int bm, bn, at_once; float step, ends; };
-  static constexpr Form kStraight[] = {{kTile256, 256, 256, 1, 1.75f, 8.f}, {kTile128x256, 128, 256, 1, 1.1f, 5.f}, {kTile128, 128, 128, 1, 0.7f, 4.f},
-                                       {kTile128Two, 128, 128, 2, 1.2f, 5.f}, {kTile64, 64, 128, 2, 0.8f, 4.f}};
+  static constexpr Form kStraight[] = {{kTile256, 256, 256, 1, 1.7f, 9.f}, {kTile128x256, 128, 256, 1, 1.1f, 7.f}, {kTile128, 128, 128, 1, 0.7f, 7.f},
+                                       {kTile128Two, 128, 128, 2, 1.2f, 8.f}, {kTile64, 64, 128, 2, 0.8f, 5.f}};
   static constexpr Form kThrough[] = {{kTile128, 128, 128, 2, 2.0f, 6.f}, {kTile64, 64, 128, 3, 2.0f, 5.f}};
   Choice best = {kTile128, 1, 0};
   float least = 1e30f;
@@ -709,7 +709,7 @@ inline Choice choose(int64_t M, int64_t N, int batch, int steps, bool direct, bo
     for (int shares = 1; shares <= (room && batch == 1 ? kMaxShares : 1); ++shares) {
       if (shares > 1 && (steps < 4 * shares || shares * M * part_pitch(N) * 4 > (int64_t)kRoomMost)) break;
       const int64_t tiles = (M + f.bm - 1) / f.bm * ((N + f.bn - 1) / f.bn) * batch * shares, rounds = (tiles + 256 * f.at_once - 1) / (256 * f.at_once);
-      const float join = shares == 1 ? 0.f : 4.f + (float)(shares * M * N) * 8.f / 4e6f;      // (written and read at 4 TB/s)
+      const float join = shares == 1 ? 0.f : 4.f + (float)(shares * M * N) * 8.f / 5e6f;      // (written and read at 5 TB/s)
       const float time = (float)rounds * ((float)((steps + shares - 1) / shares) * f.step + f.ends) + join;
       if (time < least) least = time, best = {f.tile, shares, 0};
     }

@@ -115,7 +115,12 @@ def test_forward_and_gradient(T, d, f, kind):
 @pytest.mark.parametrize("T,d,f,kind", [(1030, 256, 4224, "bf16"), (2056, 512, 1032, "bf16"), (520, 1160, 2080, "f16"), (1100, 520, 2056, "f32"), (40, 2048, 3000, "bf16"),
                                         (12, 4096, 2752, "f16"), (900, 2304, 1100, "bf16"), (130, 2051, 1037, "bf16"),
                                         # rows that are copied: odd widths on either side, one of the types each
-                                        (600, 129, 257, "bf16"), (515, 131, 64, "f16"), (520, 72, 131, "bf16"), (512, 33, 70, "f32"), (511, 131, 130, "bf16")])
+                                        (600, 129, 257, "bf16"), (515, 131, 64, "f16"), (520, 72, 131, "bf16"), (512, 33, 70, "f32"), (511, 131, 130, "bf16"),
+                                        # grids that each of the tiles takes, whole rounds of the largest with the rest in smaller ones, sums in shares
+                                        (2346, 72, 6800, "bf16"), (1837, 72, 4616, "f16"), (4234, 3968, 216, "bf16"), (69, 1784, 4720, "bf16"), (66, 2984, 5456, "f16"),
+                                        (3845, 272, 2488, "bf16"), (4126, 144, 2144, "bf16"), (3597, 1032, 1496, "bf16"), (194, 3544, 4208, "bf16"),
+                                        (2800, 3808, 392, "f16"), (116, 64, 184, "bf16"), (128, 800, 64, "f16"), (41, 112, 432, "bf16"), (2691, 2832, 72, "bf16"),
+                                        (2550, 88, 1544, "bf16"), (43, 3048, 2608, "bf16"), (700, 800, 2056, "f32"), (300, 2056, 1032, "f32")])
 def test_larger(T, d, f, kind):
     whole(T, d, f, kind)
 
