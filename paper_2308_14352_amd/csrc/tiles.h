@@ -12,6 +12,7 @@
 // consecutive n in every four sums.
 #pragma once
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "operators.h"
@@ -526,7 +527,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
 }
 
 // ---- few rows of a: b is read once, from memory to registers ----
-// A workgroup has RB blocks of 16 rows of b (kTurns: 32 rows of each matrix) and all rows of a (NG groups of 16); its W wavefronts share
+// A workgroup has RB blocks of 16 rows of b (kTurns: 32 rows of each matrix) and all rows of a (up to 16); its W wavefronts share
 // the sum, line by line (128 bytes of a row) in turn, and join in LDS. The matrix instructions are of 16 x 16: their operand is 16 bytes a
 // lane as above, lane / 16 choosing one quarter of 64 bytes. Memory bounds it; a line of each of a block's rows is asked for by two loads
 // next to each other, kDeep lines ahead.
@@ -543,47 +544,41 @@ __device__ __forceinline__ void mma16(f32x4& c, i32x4 b, i32x4 a, float) {
 }
 __device__ __forceinline__ void mma16(i32x4& c, i32x4 b, i32x4 a, int8_t) { c = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0); }
 
-template <typename T, int RB, int NG, int W, Made MADE, class Epi>
+template <typename T, int RB, int W, Made MADE, class Epi>
 __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   using Word = std::conditional_t<std::is_same<T, int8_t>::value, int32_t, float>;
   using Acc = std::conditional_t<std::is_same<T, int8_t>::value, i32x4, f32x4>;
   constexpr int kRows = RB * 16, kDeep = 4;      // lines ahead (2 or 1 for the four blocks, so that two workgroups share a compute unit: up of one token 54.6, 52.1 us instead of 50.4)
-  __shared__ __attribute__((aligned(16))) Word sums[W][NG * 16][kRows + 4];
+  __shared__ __attribute__((aligned(16))) Word sums[W][16][kRows + 4];
   const int lane = threadIdx.x % 64, row = lane % 16, at = lane / 16 * kPiece<T>;
   // (known to be the same in all lanes: conditions around matrix instructions, which write whatever lanes are masked, have to be branches)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int n0 = blockIdx.x * (MADE == kTurns ? kRows / 2 : kRows);
-  const char *bp[RB], *ap[NG];
+  const char* bp[RB];
 #pragma unroll
   for (int r = 0; r < RB; ++r) {
     const int n = MADE == kTurns ? n0 + r % ((RB + 1) / 2) * 16 + row : n0 + r * 16 + row;
     bp[r] = p.b.p[MADE == kTurns ? r / ((RB + 1) / 2) : 0] + min(n, p.b.n - 1) * p.b.stride;
   }
+  const char* ap = p.a.p[0] + min(row, p.a.n - 1) * p.a.stride;
+  Acc acc[RB];
 #pragma unroll
-  for (int g = 0; g < NG; ++g) ap[g] = p.a.p[0] + min(g * 16 + row, p.a.n - 1) * p.a.stride;
-  Acc acc[RB][NG];
-#pragma unroll
-  for (int r = 0; r < RB; ++r)
-#pragma unroll
-    for (int g = 0; g < NG; ++g) acc[r][g] = Acc{};
+  for (int r = 0; r < RB; ++r) acc[r] = Acc{};
   const int k = p.b.k, whole = k / kStep<T>;
-  struct Line { i32x4 b[RB][2], a[NG][2]; };
+  struct Line { i32x4 b[RB][2], a[2]; };
   auto load = [&](Line& l, int step) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
       for (int r = 0; r < RB; ++r) __builtin_memcpy(&l.b[r][h], (const T*)bp[r] + step * kStep<T> + h * (kStep<T> / 2) + at, 16);
-#pragma unroll
-      for (int g = 0; g < NG; ++g) __builtin_memcpy(&l.a[g][h], (const T*)ap[g] + step * kStep<T> + h * (kStep<T> / 2) + at, 16);
+      __builtin_memcpy(&l.a[h], (const T*)ap + step * kStep<T> + h * (kStep<T> / 2) + at, 16);
     }
   };
   auto multiply = [&](const Line& l) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) mma16(acc[r][g], l.b[r][h], l.a[g][h], T{});
+      for (int r = 0; r < RB; ++r) mma16(acc[r], l.b[r][h], l.a[h], T{});
   };
   Line line[kDeep];
 #pragma unroll
@@ -613,21 +608,18 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
       const int from = whole * kStep<T> + h * (kStep<T> / 2) + at;
 #pragma unroll
       for (int r = 0; r < RB; ++r) l.b[r][h] = __builtin_bit_cast(i32x4, piece<T>(bp[r], from, k));
-#pragma unroll
-      for (int g = 0; g < NG; ++g) l.a[g][h] = __builtin_bit_cast(i32x4, piece<T>(ap[g], from, k));
+      l.a[h] = __builtin_bit_cast(i32x4, piece<T>(ap, from, k));
     }
     multiply(l);
   }
 #pragma unroll
-  for (int r = 0; r < RB; ++r)
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const Word w[4] = {acc[r][g][0], acc[r][g][1], acc[r][g][2], acc[r][g][3]};
-      __builtin_memcpy(__builtin_assume_aligned(&sums[wave][g * 16 + row][r * 16 + lane / 16 * 4], 16), w, 16);
-    }
+  for (int r = 0; r < RB; ++r) {
+    const Word w[4] = {acc[r][0], acc[r][1], acc[r][2], acc[r][3]};
+    __builtin_memcpy(__builtin_assume_aligned(&sums[wave][row][r * 16 + lane / 16 * 4], 16), w, 16);
+  }
   __syncthreads();
   constexpr int kQuads = kRows / 4;
-  for (int i = threadIdx.x; i < NG * 16 * kQuads; i += 64 * W) {      // (the wavefronts' sums in their order)
+  for (int i = threadIdx.x; i < 16 * kQuads; i += 64 * W) {      // (the wavefronts' sums in their order)
     Word* to = &sums[0][i / kQuads][i % kQuads * 4];
     Word s[4];
     __builtin_memcpy(s, to, 16);
@@ -639,7 +631,7 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   }
   __syncthreads();
   constexpr int kPieces = kRows / 8 / (MADE == kTurns ? 2 : 1);
-  for (int i = threadIdx.x; i < NG * 16 * kPieces; i += 64 * W) {
+  for (int i = threadIdx.x; i < 16 * kPieces; i += 64 * W) {
     const int m = i / kPieces, n = i % kPieces * 8;
     typename Epi::Beside beside;
     epi.ask(beside, m, n0 + n);
@@ -656,12 +648,12 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
     }
   }
 }
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 16;      // (32 rows of 4096 x 14336 as two groups of 16: 115 us, in tiles 86)
 
-template <typename T, int RB, int NG, int W, Made MADE, class Epi>
+template <typename T, int RB, int W, Made MADE, class Epi>
 hipError_t few_as(const Product& p, const Epi& epi, hipStream_t st) {
   constexpr int kRows = MADE == kTurns ? RB * 8 : RB * 16;
-  k_few<T, RB, NG, W, MADE, Epi><<<(p.b.n + kRows - 1) / kRows, 64 * W, 0, st>>>(p, epi);
+  k_few<T, RB, W, MADE, Epi><<<(p.b.n + kRows - 1) / kRows, 64 * W, 0, st>>>(p, epi);
   return hipGetLastError();
 }
 // a.n <= kFewRows; b and a by rows, at any alignment. Two blocks of b's rows a workgroup where that leaves one for every compute unit
@@ -669,13 +661,9 @@ hipError_t few_as(const Product& p, const Epi& epi, hipStream_t st) {
 template <typename T, Made MADE, class Epi>
 hipError_t launch_few(const Product& p, const Epi& epi, hipStream_t st) {
   using std::integral_constant;
-  const bool short_sum = p.b.k <= 16 * kStep<T>;
   const auto by_blocks = [&](auto rb) {
-    const auto go = [&](auto ng, auto w) { return few_as<T, decltype(rb)::value, decltype(ng)::value, decltype(w)::value, MADE>(p, epi, st); };
-    if (p.a.n <= 16) return short_sum ? go(integral_constant<int, 1>{}, integral_constant<int, 4>{}) : go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
-    // (64 rows of b and 32 of a: eight wavefronts' sums would be 70 KB)
-    if (short_sum || MADE == kTurns) return go(integral_constant<int, 2>{}, integral_constant<int, 4>{});
-    return go(integral_constant<int, 2>{}, integral_constant<int, MADE == kTurns ? 4 : 8>{});
+    constexpr int kBlocks = decltype(rb)::value;
+    return p.b.k <= 16 * kStep<T> ? few_as<T, kBlocks, 4, MADE>(p, epi, st) : few_as<T, kBlocks, 8, MADE>(p, epi, st);
   };
   if constexpr (MADE == kTurns) return by_blocks(integral_constant<int, 4>{});
   else return p.b.n >= 256 * 32 ? by_blocks(integral_constant<int, 2>{}) : by_blocks(integral_constant<int, 1>{});
@@ -779,8 +767,14 @@ hipError_t launch_one(Product p, int M, int N, int batch, int shares, int to_col
   if constexpr (S > 0) kernel = k_direct<T, A_ROWS, B_ROWS, BM, BN, WM, WN, S, kOne, B_MADE, Epi>;
   else kernel = k_tile<T, A_ROWS, B_ROWS, BM, BN, WM, WN, kOne, B_MADE, Epi>;
   if constexpr (kLds > 64 * 1024) {
-    static const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-    if (e != hipSuccess) return e;
+    static std::atomic<uint64_t> set{0};      // the devices whose kernel may have that much
+    int device;
+    if (hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
+    const uint64_t bit = (uint64_t)1 << (device % 64);
+    if (!(set.load(std::memory_order_relaxed) & bit)) {
+      if (hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds); e != hipSuccess) return e;
+      set.fetch_or(bit, std::memory_order_relaxed);
+    }
   }
   p.tiles_m = (M + BM - 1) / BM, p.tiles_n = (N - p.n_from + BN - 1) / BN;
   if (to_columns) p.tiles_n = std::min(p.tiles_n, to_columns / BN);
