@@ -8,6 +8,9 @@
 // that share it. n is the norm of y before its rounding; the backward pass takes the y that the forward pass left. The weights' gradients
 // are sums over rows: a stream of rows keeps its columns' sums in registers, and a second kernel adds the streams in their order, so that
 // the same call gives the same bits. All in fp32.
+// 2048 rows of 4096 (fp32 branch, bf16 stream) 14.3 us, 5.9 TB/s; the gradient of 8192 bf16 rows with both norms and a gate 104 us (3.9 TB/s)
+// and 5 for the join: 512 threads a row with 8 columns each and the next row on its way, in 128 registers, so that two workgroups share a
+// compute unit (140 registers and one workgroup: 140 us; 256 threads with 16 columns and no row ahead: 146).
 #include <algorithm>
 
 #include "operators.h"
@@ -295,10 +298,11 @@ __global__ __launch_bounds__(1024) void k_norms_join(NormsArgs a, int streams, i
 }
 
 inline int up4(int d) { return (d + 3) / 4 * 4; }
-// Streams of a backward call: enough to fill the card, few enough that their sums are little beside the rows.
+// Streams of a backward call: two workgroups a compute unit (us at 8192 rows of 4096: 256 streams 121, 512 106, 768 123, 1024 117).
 int streams_of(int32_t T, int32_t d) { return std::min(T, d <= 1024 ? 2048 : 512); }
 
-// Wavefronts and vectors of a row; WIDE: wavefronts of rows of up to 4096.
+// Wavefronts and vectors of a row: the fewest vectors a thread with which a wavefront or workgroup still has the row (registers bound what is
+// in flight); rows of up to 1024 by a wavefront alone, without barriers. WIDE: wavefronts of rows of up to 4096.
 template <int WIDE, typename F>
 hipError_t by_width(int32_t d, F&& f) {
   using std::integral_constant;

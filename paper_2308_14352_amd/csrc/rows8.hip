@@ -8,6 +8,9 @@
 // Rows for products in 8-bit integers: a scale for each row, scale = max |x| / 127 (at least 2^-126), code = rint(x / scale) with the
 // quotient of fp32. A row with a NaN or an infinity has the scale NaN and codes of zero. Rows lie a multiple of 128 bytes apart, zeros
 // behind the last column: the product reads them by whole cache lines.
+//
+// Memory bounds all three: 8192 rows of 4096 bf16 packed in 20.9 us (4.8 TB/s), unpacked in 15 (6.6, the codes from the cache), to rows of
+// codes in 22.9 (4.4); a few rows are a launch's latency, 3.4 to 4.4.
 #include <algorithm>
 
 #include "operators.h"
@@ -30,7 +33,8 @@ __device__ __forceinline__ void load_part(float (&v)[N], const T* row, int c, in
   }
 }
 
-// ---- packed: a thread has 16 bytes of the elements, 4 or 8 lanes a block; U pieces a thread are in flight together ----
+// ---- packed: a thread has 16 bytes of the elements, 4 or 8 lanes a block; U pieces a thread are in flight together. A piece is as many
+// elements, so that a wavefront reads 1 KB in a row and the largest of a block is two or three exchanges away ----
 constexpr int kThreads = 256;
 template <typename T> constexpr int kE = 16 / sizeof(T);
 template <typename T> constexpr int kLanes = kPackBlock / kE<T>;

@@ -10,6 +10,9 @@
 // An operand is 16 bytes a lane whatever its type, lane / 32 choosing one half of 32 bytes of the sum: v_mfma_*_32x32x16 of 16 bits,
 // v_mfma_i32_32x32x32_i8, or four v_mfma_f32_32x32x2_f32. The matrix instruction takes b first, so that a lane has one row m and four
 // consecutive n in every four sums.
+//
+// What bounds them: the largest tiles the chip's power (1.26 PFLOP/s bf16, 2.1 POP/s in 8 bits at 1.7 to 1.8 GHz, where matrix instructions
+// alone reach 1.79) and 64 KB a step and compute unit out of L2; small grids the latency of their first lines and their epilogue, some 7 us.
 #pragma once
 #include <algorithm>
 #include <atomic>
