@@ -393,14 +393,14 @@ moeq_status moe_block_norms_backward(int32_t n_tokens, int32_t d, float residual
 
 /* Tensors kept in 8 bits. Blocks of 32 columns of a row share a power of two: e = floor(log2(largest |x|)) - 6, at least -126 (fp16:
  * -24), code = rint(x 2^-e) in [-127, 127], value = code 2^e, which dtype holds exactly. codes [rows][d] int8, exps
- * [rows][ceil(d / 32)] int8, contiguous. A block that holds a NaN or an infinity comes back as NaN (exponent -128). */
+ * [rows][ceil(d / 32)] int8, contiguous; d <= 2^30. A block that holds a NaN or an infinity comes back as NaN (exponent -128). */
 moeq_status moe_pack8(const void *x, int64_t x_stride, int32_t dtype, int32_t rows, int32_t d, int8_t *codes, int8_t *exps,
                       void *stream);
 moeq_status moe_unpack8(const int8_t *codes, const int8_t *exps, int32_t rows, int32_t d, int32_t dtype, void *x, int64_t x_stride,
                         void *stream);
 
 /* A gated feed-forward block: w_in and w_gate [d_ff][d_model], w_out [d_model][d_ff] in dtype, contiguous device memory that the
- * caller keeps. Widths <= 65536. */
+ * caller keeps. Widths <= 65536, at most 2^20 tokens a call, tokens times the larger width at most 2^35. */
 typedef struct {
   int32_t d_model, d_ff, dtype;
   const void *w_in, *w_gate, *w_out;
@@ -425,7 +425,8 @@ moeq_status moe_gated_ffn_forward(const moeq_gated_ffn *ffn, const void *x, int6
 
 /* Its gradient: dx (dx_opt NULL: not wanted) and dw_in, dw_gate, dw_out (the weights' shapes, contiguous), all in dtype; base's is dy.
  * x: rows in dtype, or x_codes and x_exps as moe_pack8 leaves them (x NULL). keep, ab, ab_exps: as the forward pass left them;
- * MOEQ_KEEP_NONE computes a and b again. No rows: the weights' gradients are zeros. The sums' order does not depend on timing. */
+ * MOEQ_KEEP_NONE computes a and b again. No rows: the weights' gradients are zeros. The sums' order does not depend on timing.
+ * Rounding between the products and infinities as in the forward pass. */
 moeq_status moe_gated_ffn_backward(const moeq_gated_ffn *ffn, const void *x, int64_t x_stride, const int8_t *x_codes,
                                    const int8_t *x_exps, int32_t n_tokens, const void *dy, int64_t dy_stride, int32_t keep,
                                    const void *ab, const int8_t *ab_exps, void *dx_opt, int64_t dx_stride, void *dw_in, void *dw_gate,
@@ -439,7 +440,8 @@ moeq_status moe_quantize_rows(const void *x, int64_t x_stride, int32_t dtype, in
                               void *stream);
 
 /* y[t][n] = base[t][n] + x_scale[t] w_scale[n] sum over k of x[t][k] w[n][k], x [n_tokens] and w [n_out] rows of k codes in the form
- * above (any int8, also -128; what lies behind column k has to be zero). The sums are exact. base_opt NULL: zeros; base may be y
+ * above (any int8, also -128; what lies behind column k has to be zero), each at most 2^20 rows, the product of both at most 2^36. The
+ * sums are exact. base_opt NULL: zeros; base may be y
  * itself; both are dtype. ws: moe_matmul_q8_workspace_bytes (may be 0), 16-byte aligned. */
 size_t moe_matmul_q8_workspace_bytes(int32_t max_tokens, int32_t n_out, int32_t k);
 moeq_status moe_matmul_q8(const int8_t *x, const float *x_scale, int32_t n_tokens, const int8_t *w, const float *w_scale, int32_t n_out,

@@ -1,6 +1,7 @@
 // Host side of the operators beside the layer: argument checks (all before the first HIP call) and launches.
 #include "operators.h"
 
+#include <algorithm>
 #include <initializer_list>
 
 using namespace moeq;
@@ -125,7 +126,8 @@ moeq_status norms_ok(const NormsArgs& a) {
 moeq_status ffn_ok(const moeq_gated_ffn* f, int32_t n_tokens, int32_t keep) {
   if (!f || f->d_model <= 0 || f->d_ff <= 0 || !type_ok(f->dtype) || n_tokens < 0) return MOEQ_EINVAL;
   if (keep != MOEQ_KEEP_NONE && keep != MOEQ_KEEP_OWN && keep != MOEQ_KEEP_8) return MOEQ_EINVAL;
-  if (f->d_model > kFfnMaxWidth || f->d_ff > kFfnMaxWidth || n_tokens > kProductMaxRows) return MOEQ_EUNSUPPORTED;
+  if (f->d_model > kFfnMaxWidth || f->d_ff > kFfnMaxWidth || n_tokens > kProductMaxRows || (int64_t)n_tokens * 2 * std::max(f->d_model, f->d_ff) > kProductMaxOut)
+    return MOEQ_EUNSUPPORTED;
   const size_t e = dtype_bytes(f->dtype);
   if (!f->w_in || !f->w_gate || !f->w_out || !aligned(f->w_in, e) || !aligned(f->w_gate, e) || !aligned(f->w_out, e)) return MOEQ_EINVAL;
   return MOEQ_OK;
@@ -366,6 +368,7 @@ moeq_status moe_block_norms_backward(int32_t n_tokens, int32_t d, float residual
 
 moeq_status moe_pack8(const void* x, int64_t x_stride, int32_t dtype, int32_t rows, int32_t d, int8_t* codes, int8_t* exps, void* stream) {
   if (rows < 0 || d <= 0 || !type_ok(dtype) || !matrix_ok(x, rows, x_stride, d, dtype, true) || (rows && (!codes || !exps))) return MOEQ_EINVAL;
+  if (d > kPackMaxWidth) return MOEQ_EUNSUPPORTED;
   const Block c = codes_of(codes, (int64_t)rows * d), e = codes_of(exps, (int64_t)rows * ((d + kPackBlock - 1) / kPackBlock));
   if (!apart({c, e}, {{x, rows, x_stride, d, dtype}})) return MOEQ_EINVAL;
   if (rows == 0) return MOEQ_OK;
@@ -376,6 +379,7 @@ moeq_status moe_pack8(const void* x, int64_t x_stride, int32_t dtype, int32_t ro
 
 moeq_status moe_unpack8(const int8_t* codes, const int8_t* exps, int32_t rows, int32_t d, int32_t dtype, void* x, int64_t x_stride, void* stream) {
   if (rows < 0 || d <= 0 || !type_ok(dtype) || !matrix_ok(x, rows, x_stride, d, dtype, false) || (rows && (!codes || !exps))) return MOEQ_EINVAL;
+  if (d > kPackMaxWidth) return MOEQ_EUNSUPPORTED;
   if (!apart({{x, rows, x_stride, d, dtype}},
              {codes_of(codes, (int64_t)rows * d), codes_of(exps, (int64_t)rows * ((d + kPackBlock - 1) / kPackBlock))}))
     return MOEQ_EINVAL;
@@ -452,7 +456,7 @@ moeq_status moe_quantize_rows(const void* x, int64_t x_stride, int32_t dtype, in
 }
 
 size_t moe_matmul_q8_workspace_bytes(int32_t max_tokens, int32_t n_out, int32_t k) {
-  if (max_tokens <= 0 || n_out <= 0 || k <= 0 || k > kQuantMaxWidth || max_tokens > kProductMaxRows || n_out > kProductMaxRows / 8) return 0;
+  if (max_tokens <= 0 || n_out <= 0 || k <= 0 || k > kQuantMaxWidth || max_tokens > kProductMaxRows || n_out > kProductMaxRows) return 0;
   return q8_ws_bytes(max_tokens, n_out, k);
 }
 
@@ -460,7 +464,7 @@ moeq_status moe_matmul_q8(const int8_t* x, const float* x_scale, int32_t n_token
                           int32_t k, const void* base_opt, int64_t base_stride, int32_t dtype, void* y, int64_t y_stride, void* ws,
                           size_t ws_bytes, void* stream) {
   if (n_tokens < 0 || n_out <= 0 || k <= 0 || !type_ok(dtype) || !w || !w_scale || !aligned(w, 16) || !aligned(w_scale, 4)) return MOEQ_EINVAL;
-  if (k > kQuantMaxWidth || n_tokens > kProductMaxRows || n_out > kProductMaxRows / 8) return MOEQ_EUNSUPPORTED;
+  if (k > kQuantMaxWidth || n_tokens > kProductMaxRows || n_out > kProductMaxRows || (int64_t)n_tokens * n_out > kProductMaxOut) return MOEQ_EUNSUPPORTED;
   if (n_tokens == 0) return MOEQ_OK;
   if (!x || !x_scale || !aligned(x, 16) || !aligned(x_scale, 4) || !matrix_ok(y, n_tokens, y_stride, n_out, dtype, false)) return MOEQ_EINVAL;
   if (base_opt && !matrix_ok(base_opt, n_tokens, base_stride, n_out, dtype, true)) return MOEQ_EINVAL;

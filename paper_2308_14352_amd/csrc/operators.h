@@ -95,7 +95,7 @@ hipError_t launch_norms_forward(const NormsArgs& a, hipStream_t st);
 hipError_t launch_norms_backward(const NormsArgs& a, hipStream_t st);
 
 // ---- rows8.hip ----
-constexpr int32_t kPackBlock = 32, kPackNan = -128;      // columns that share an exponent; the exponent of a block that is NaN
+constexpr int32_t kPackMaxWidth = 1 << 30, kPackBlock = 32, kPackNan = -128;      // columns that share an exponent; the exponent of a block that is NaN
 constexpr int32_t kQuantMaxWidth = 65536;
 inline int64_t q8_pitch(int64_t k) { return (k + 127) / 128 * 128; }
 struct Rows8Args {
@@ -110,7 +110,8 @@ hipError_t launch_unpack8(const Rows8Args& a, hipStream_t st);
 hipError_t launch_quantize_rows(const Rows8Args& a, hipStream_t st);
 
 // ---- gated_ffn.hip ----
-constexpr int32_t kFfnMaxWidth = 65536, kProductMaxRows = 1 << 20;      // (so that a launch has fewer than 2^32 threads)
+constexpr int32_t kFfnMaxWidth = 65536, kProductMaxRows = 1 << 20;
+constexpr int64_t kProductMaxOut = (int64_t)1 << 36;      // rows times columns of a product (so that a launch has fewer than 2^32 threads)
 struct FfnArgs {
   int32_t T, D, F, dtype;
   const void *w_in, *w_gate, *w_out;

@@ -530,7 +530,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_direct(Product p, Epi epi) {
 }
 
 // ---- few rows of a: b is read once, from memory to registers ----
-// A workgroup has RB blocks of 16 rows of b (kTurns: 32 rows of each matrix) and all rows of a (up to 16); its W wavefronts share
+// A workgroup has RB blocks of 16 rows of b (kTurns: half of them of each matrix) and all rows of a (up to 16); its W wavefronts share
 // the sum, line by line (128 bytes of a row) in turn, and join in LDS. The matrix instructions are of 16 x 16: their operand is 16 bytes a
 // lane as above, lane / 16 choosing one quarter of 64 bytes. Memory bounds it; a line of each of a block's rows is asked for by two loads
 // next to each other, kDeep lines ahead.
@@ -551,7 +551,7 @@ template <typename T, int RB, int W, Made MADE, class Epi>
 __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   using Word = std::conditional_t<std::is_same<T, int8_t>::value, int32_t, float>;
   using Acc = std::conditional_t<std::is_same<T, int8_t>::value, i32x4, f32x4>;
-  constexpr int kRows = RB * 16, kDeep = 4;      // lines ahead (2 or 1 for the four blocks, so that two workgroups share a compute unit: up of one token 54.6, 52.1 us instead of 50.4)
+  constexpr int kRows = RB * 16, kDeep = 4;      // lines ahead
   __shared__ __attribute__((aligned(16))) Word sums[W][16][kRows + 4];
   const int lane = threadIdx.x % 64, row = lane % 16, at = lane / 16 * kPiece<T>;
   // (known to be the same in all lanes: conditions around matrix instructions, which write whatever lanes are masked, have to be branches)
@@ -660,7 +660,9 @@ hipError_t few_as(const Product& p, const Epi& epi, hipStream_t st) {
   return hipGetLastError();
 }
 // a.n <= kFewRows; b and a by rows, at any alignment. Two blocks of b's rows a workgroup where that leaves one for every compute unit
-// (three rows, 14336 x 4096 codes: 14.0 us, with one 15.0; 4096 x 14336 bf16: 34.9 with two, 22.6 with one).
+// (three rows, 14336 x 4096 codes: 14.0 us, with one 15.0; 4096 x 14336 bf16: 34.9 with two, 22.6 with one). In turns one of each matrix, but two
+// where a and b are packed, which takes 32 columns (one token, 2 x 14336 x 4096 bf16: 44.2, with two of each 54.3: 448 workgroups of 200 registers
+// are not as even).
 template <typename T, Made MADE, class Epi>
 hipError_t launch_few(const Product& p, const Epi& epi, hipStream_t st) {
   using std::integral_constant;
@@ -668,7 +670,7 @@ hipError_t launch_few(const Product& p, const Epi& epi, hipStream_t st) {
     constexpr int kBlocks = decltype(rb)::value;
     return p.b.k <= 16 * kStep<T> ? few_as<T, kBlocks, 4, MADE>(p, epi, st) : few_as<T, kBlocks, 8, MADE>(p, epi, st);
   };
-  if constexpr (MADE == kTurns) return by_blocks(integral_constant<int, 4>{});
+  if constexpr (MADE == kTurns) return epi.keep == MOEQ_KEEP_8 ? by_blocks(integral_constant<int, 4>{}) : by_blocks(integral_constant<int, 2>{});
   else return p.b.n >= 256 * 32 ? by_blocks(integral_constant<int, 2>{}) : by_blocks(integral_constant<int, 1>{});
 }
 

@@ -57,7 +57,9 @@ Q8 = dict(x=P, xs=P + 65536, T=4, w=Q, ws=Q + (1 << 20), n=100, k=300, base=None
     ("moe_quantize_rows", ROWS, dict(d=65537, x_stride=65537), UNSUPPORTED), ("moe_quantize_rows", ROWS, dict(codes=R + 8), INVALID),
     ("moe_quantize_rows", ROWS, dict(scale=None), INVALID), ("moe_quantize_rows", ROWS, dict(scale=R + 508), INVALID), ("moe_quantize_rows", ROWS, dict(x=None), INVALID),
     ("moe_matmul_q8", Q8, dict(T=-1), INVALID), ("moe_matmul_q8", Q8, dict(n=0), INVALID), ("moe_matmul_q8", Q8, dict(k=0), INVALID),
-    ("moe_matmul_q8", Q8, dict(k=65537), UNSUPPORTED), ("moe_matmul_q8", Q8, dict(T=(1 << 20) + 1), UNSUPPORTED), ("moe_matmul_q8", Q8, dict(n=(1 << 17) + 1), UNSUPPORTED),
+    ("moe_matmul_q8", Q8, dict(k=65537), UNSUPPORTED), ("moe_matmul_q8", Q8, dict(T=(1 << 20) + 1), UNSUPPORTED), ("moe_matmul_q8", Q8, dict(n=(1 << 20) + 1), UNSUPPORTED),
+    ("moe_matmul_q8", Q8, dict(T=1 << 18, n=(1 << 18) + 1), UNSUPPORTED), ("moe_pack8", PACK, dict(d=(1 << 30) + 1, x_stride=1 << 31), UNSUPPORTED),
+    ("moe_unpack8", UNPACK, dict(d=(1 << 30) + 1, x_stride=1 << 31), UNSUPPORTED),
     ("moe_matmul_q8", Q8, dict(x=None), INVALID), ("moe_matmul_q8", Q8, dict(w=Q + 8), INVALID), ("moe_matmul_q8", Q8, dict(xs=P + 2), INVALID),
     ("moe_matmul_q8", Q8, dict(y=Q + 128), INVALID), ("moe_matmul_q8", Q8, dict(y_stride=99), INVALID), ("moe_matmul_q8", Q8, dict(base=R + 4, base_stride=100), INVALID),
     ("moe_matmul_q8", Q8, dict(dtype=4), INVALID),
@@ -75,7 +77,7 @@ def desc(**kw):
 @pytest.mark.parametrize("kw,bad,status", [
     (dict(d_model=0), {}, INVALID), (dict(d_ff=-1), {}, INVALID), (dict(dtype=7), {}, INVALID), (dict(w_in=None), {}, INVALID), (dict(w_gate=P + 1), {}, INVALID),
     (dict(w_out=None), {}, INVALID), (dict(d_model=65537), {}, UNSUPPORTED), (dict(d_ff=65537), {}, UNSUPPORTED),
-    ({}, dict(T=-1), INVALID), ({}, dict(T=(1 << 20) + 1), UNSUPPORTED), ({}, dict(keep=2), INVALID), ({}, dict(x=None), INVALID), ({}, dict(x_stride=63), INVALID),
+    (dict(d_ff=65536), dict(T=(1 << 19) + 1), UNSUPPORTED), ({}, dict(T=-1), INVALID), ({}, dict(T=(1 << 20) + 1), UNSUPPORTED), ({}, dict(keep=2), INVALID), ({}, dict(x=None), INVALID), ({}, dict(x_stride=63), INVALID),
     ({}, dict(out=None), INVALID), ({}, dict(out=Q), INVALID), ({}, dict(out_stride=0), INVALID), ({}, dict(ab=None), INVALID), ({}, dict(ab=S + 1), INVALID),
     ({}, dict(keep=8, exps=None), INVALID), ({}, dict(ws=None), WORKSPACE), ({}, dict(ws_bytes=100), WORKSPACE), ({}, dict(ws=S + (1 << 30) + 16), INVALID),
 ])

@@ -118,7 +118,7 @@ def test_products(T, k, n, kind, base):
     product(T, k, n, kind, base)
 
 
-@pytest.mark.parametrize("T,k,n", [(1, 14336, 4100), (5, 65536, 40), (12, 6000, 5000), (40, 9000, 1030), (1030, 3000, 1030), (2100, 256, 4000)])
+@pytest.mark.parametrize("T,k,n", [(1, 14336, 4100), (5, 65536, 40), (12, 6000, 5000), (40, 9000, 1030), (1030, 3000, 1030), (2100, 256, 4000), (2304, 640, 8200), (20, 300, 140000)])
 def test_larger_products(T, k, n):
     product(T, k, n, "bf16", True)
 
