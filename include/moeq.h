@@ -417,8 +417,8 @@ typedef struct {
 size_t moe_gated_ffn_workspace_bytes(const moeq_gated_ffn *ffn, int32_t max_tokens, int32_t backward, int32_t x_packed, int32_t keep);
 
 /* y = base + (silu(x w_in^T) * (x w_gate^T)) w_out^T, silu(a) = a / (1 + exp(-a)). base_opt NULL: zeros; base may be y itself; base and
- * y are y_dtype: dtype or MOEQ_F32. Sums are held in fp32, the rows between the products are rounded to dtype (fp16: infinite past
- * 65504). An infinity in an operand may come out as a NaN. */
+ * y are y_dtype: dtype or MOEQ_F32. Sums are held in fp32, the rows between the products are rounded to dtype (to twice its bits in calls of
+ * up to 8 tokens; fp16: infinite or NaN past 65504). An infinity in an operand may come out as a NaN. */
 moeq_status moe_gated_ffn_forward(const moeq_gated_ffn *ffn, const void *x, int64_t x_stride, int32_t n_tokens, const void *base_opt,
                                   int64_t base_stride, int32_t y_dtype, void *y, int64_t y_stride, int32_t keep, void *ab,
                                   int8_t *ab_exps, void *ws, size_t ws_bytes, void *stream);

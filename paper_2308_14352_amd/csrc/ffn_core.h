@@ -7,7 +7,7 @@
 // db and h. h, da and db are rounded to the type (as a program in that type holds them): an output has that rounding and its own. They lie
 // in the workspace, rows of whole steps (64 elements, 32 of fp32), zeros behind the last column and in rows up to a multiple of 64,
 // which later products sum over; da and db of a row side by side, so that dx is one product through both weights.
-// bf16 at 4096 x 14336, us: one token 71 (two kernels, 5 TB/s of weights), 2048 rows 640 (1.13 PFLOP/s), gradient of 4096 rows 2480 (1.16):
+// bf16 at 4096 x 14336, us: one token 68 (two kernels, 5.2 TB/s of weights), 2048 rows 640 (1.13 PFLOP/s), gradient of 4096 rows 2480 (1.16):
 // the products run at the chip's power, as a library's do (1.26 to 1.41). Through the activation 612 of it: 570 MB of a, b, da, db and h
 // pass beside that product.
 #pragma once
@@ -52,6 +52,7 @@ struct Up {
   int32_t keep;
   T* ab;                    // MOEQ_KEEP_OWN
   int8_t *codes, *exps;     // MOEQ_KEEP_8
+  bool pairs;               // (up to kPairRows rows) what h's rounding left goes to the row kPairRows behind
   static constexpr bool kRaw = false;
   struct Beside {};
   __device__ __forceinline__ void ask(Beside&, int, int) const {}
@@ -72,11 +73,16 @@ struct Up {
   __device__ __forceinline__ void pair(const Beside&, int m, int f, const float (&a)[8], const float (&b)[8]) const {
     if (keep == MOEQ_KEEP_8) keep8(0, m, f, a), keep8(1, m, f, b);
     if (m >= Tp || f >= Fp) return;
-    if (h) {
+    if (h && !(pairs && m >= kPairRows)) {
       float w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = m < T_ && f + i < F ? a[i] * sigmoid<T>(a[i]) * b[i] : 0.f;
       store_n(h + m * pitch + f, w);
+      if (pairs && m < kPairRows) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] -= (float)(T)w[i];
+        store_n(h + (m + kPairRows) * pitch + f, w);
+      }
     }
     if (keep == MOEQ_KEEP_OWN && m < T_ && f < F) {
       store8(ab + (int64_t)m * F, f, F, a);
@@ -233,7 +239,7 @@ hipError_t up(const FfnArgs& a, const FfnOperands& o, const Up<T>& epi, void* ro
   // (where one side's rows go on in zeros and the other's end, the sum ends with the shorter)
   const int32_t k = std::min(o.x.width, o.w_in.width);
   Product p = {side<T>(o.x.p, o.x.stride, a.T, k), side<T>(o.w_in.p, o.w_in.stride, a.F, k, o.w_gate.p), steps_of<T>(k), 0};
-  if (a.T <= kFewRows) return launch_few<T, kTurns>(p, epi, st);
+  if (a.T <= kFewRows) return launch_few<T, false, kTurns>(p, epi, st);
   return launch_tile<T, true, true, kTurns>(p, epi.Tp, 2 * epi.Fp, 1, room, epi, st);
 }
 
@@ -244,14 +250,17 @@ hipError_t ffn_forward(const FfnArgs& a, hipStream_t st) {
   if (hipError_t s = operands<T>(a, plan, false, o, st); s != hipSuccess) return s;
   T* h = (T*)((char*)a.ws + plan.h);
   void* room = (char*)a.ws + plan.room;
-  Up<T> e = {h, plan.Fp, a.T, a.F, (int32_t)plan.Tp, (int32_t)plan.Fp, a.keep, (T*)a.ab, (int8_t*)a.ab, a.ab_exps};
+  // Of so few rows h is kept to twice the type's bits: a few values' errors add up to less than a rounding of the output only by chance.
+  const bool pairs = a.T <= kPairRows && sizeof(T) == 2;
+  Up<T> e = {h, plan.Fp, a.T, a.F, (int32_t)plan.Tp, (int32_t)plan.Fp, a.keep, (T*)a.ab, (int8_t*)a.ab, a.ab_exps, pairs};
   if (hipError_t s = up<T>(a, o, e, room, st); s != hipSuccess) return s;
   const int32_t k = o.w_out.width;
   Product p = {side<T>(h, plan.Fp, a.T <= kFewRows ? a.T : (int32_t)plan.Tp, (int32_t)plan.Fp), side<T>(o.w_out.p, o.w_out.stride, a.D, k), steps_of<T>(k), 0};
   auto down = [&](auto t) {
     using O = decltype(t);
     Store<O> out = {{(O*)a.y, nullptr}, a.y_stride, (const O*)a.base, a.base_stride, a.T, a.D};
-    if (a.T <= kFewRows) return launch_few<T, kOne>(p, out, st);
+    if (pairs) return launch_few<T, true, kOne>(p, out, st);
+    if (a.T <= kFewRows) return launch_few<T, false, kOne>(p, out, st);
     return launch_tile<T, true, true, kOne>(p, a.T, a.D, 1, room, out, st);
   };
   if (a.y_dtype == a.dtype) return down(T{});
@@ -271,7 +280,7 @@ hipError_t ffn_backward(const FfnArgs& a, hipStream_t st) {
     const T* ab = (const T*)a.ab;
     if (a.keep == MOEQ_KEEP_NONE) {
       T* made = (T*)(ws + plan.ab);
-      Up<T> e = {nullptr, 0, a.T, a.F, Tp, Fp, MOEQ_KEEP_OWN, made, nullptr, nullptr};
+      Up<T> e = {nullptr, 0, a.T, a.F, Tp, Fp, MOEQ_KEEP_OWN, made, nullptr, nullptr, false};
       if (hipError_t s = up<T>(a, o, e, room, st); s != hipSuccess) return s;
       ab = made;
     }

@@ -48,7 +48,7 @@ hipError_t launch_matmul_q8(const Q8Args& a, hipStream_t st) {
     const int32_t pitch = (int32_t)q8_pitch(a.K);
     Product p = {Side{{(const char*)a.x, nullptr}, pitch, a.T, pitch}, Side{{(const char*)a.w, nullptr}, pitch, a.N, pitch}, pitch / kStepBytes, 0};
     Scaled<O> e = {(O*)a.y, a.y_stride, (const O*)a.base, a.base_stride, a.x_scale, a.w_scale, a.T, a.N};
-    if (a.T <= kFewRows) return launch_few<int8_t, kOne>(p, e, st);
+    if (a.T <= kFewRows) return launch_few<int8_t, false, kOne>(p, e, st);
     return launch_tile<int8_t, true, true, kOne>(p, a.T, a.N, 1, a.ws, e, st);
   });
 }

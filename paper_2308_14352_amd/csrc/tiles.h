@@ -547,7 +547,10 @@ __device__ __forceinline__ void mma16(f32x4& c, i32x4 b, i32x4 a, float) {
 }
 __device__ __forceinline__ void mma16(i32x4& c, i32x4 b, i32x4 a, int8_t) { c = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0); }
 
-template <typename T, int RB, int W, Made MADE, class Epi>
+// PAIRS: up to 8 rows of a come as two rows of T each, row m and what its rounding left in row m + 8, which the matrix instructions take in
+// the same step; their sums are added (kPairRows).
+constexpr int kPairRows = 8;
+template <typename T, bool PAIRS, int RB, int W, Made MADE, class Epi>
 __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   using Word = std::conditional_t<std::is_same<T, int8_t>::value, int32_t, float>;
   using Acc = std::conditional_t<std::is_same<T, int8_t>::value, i32x4, f32x4>;
@@ -563,7 +566,7 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
     const int n = MADE == kTurns ? n0 + r % ((RB + 1) / 2) * 16 + row : n0 + r * 16 + row;
     bp[r] = p.b.p[MADE == kTurns ? r / ((RB + 1) / 2) : 0] + min(n, p.b.n - 1) * p.b.stride;
   }
-  const char* ap = p.a.p[0] + min(row, p.a.n - 1) * p.a.stride;
+  const char* ap = p.a.p[0] + (PAIRS ? row / kPairRows * kPairRows + min(row % kPairRows, p.a.n - 1) : min(row, p.a.n - 1)) * p.a.stride;
   Acc acc[RB];
 #pragma unroll
   for (int r = 0; r < RB; ++r) acc[r] = Acc{};
@@ -634,13 +637,13 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
   }
   __syncthreads();
   constexpr int kPieces = kRows / 8 / (MADE == kTurns ? 2 : 1);
-  for (int i = threadIdx.x; i < 16 * kPieces; i += 64 * W) {
+  for (int i = threadIdx.x; i < (PAIRS ? kPairRows : 16) * kPieces; i += 64 * W) {
     const int m = i / kPieces, n = i % kPieces * 8;
     typename Epi::Beside beside;
     epi.ask(beside, m, n0 + n);
     Word v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = sums[0][m][n + j];
+    for (int j = 0; j < 8; ++j) v[j] = PAIRS ? sums[0][m][n + j] + sums[0][m + kPairRows][n + j] : sums[0][m][n + j];
     if constexpr (MADE == kTurns) {
       Word w[8];
 #pragma unroll
@@ -653,22 +656,22 @@ __global__ __launch_bounds__(64 * W) void k_few(Product p, Epi epi) {
 }
 constexpr int kFewRows = 16;      // (32 rows of 4096 x 14336 as two groups of 16: 115 us, in tiles 86)
 
-template <typename T, int RB, int W, Made MADE, class Epi>
+template <typename T, bool PAIRS, int RB, int W, Made MADE, class Epi>
 hipError_t few_as(const Product& p, const Epi& epi, hipStream_t st) {
   constexpr int kRows = MADE == kTurns ? RB * 8 : RB * 16;
-  k_few<T, RB, W, MADE, Epi><<<(p.b.n + kRows - 1) / kRows, 64 * W, 0, st>>>(p, epi);
+  k_few<T, PAIRS, RB, W, MADE, Epi><<<(p.b.n + kRows - 1) / kRows, 64 * W, 0, st>>>(p, epi);
   return hipGetLastError();
 }
 // a.n <= kFewRows; b and a by rows, at any alignment. Two blocks of b's rows a workgroup where that leaves one for every compute unit
 // (three rows, 14336 x 4096 codes: 14.0 us, with one 15.0; 4096 x 14336 bf16: 34.9 with two, 22.6 with one). In turns one of each matrix, but two
 // where a and b are packed, which takes 32 columns (one token, 2 x 14336 x 4096 bf16: 44.2, with two of each 54.3: 448 workgroups of 200 registers
 // are not as even).
-template <typename T, Made MADE, class Epi>
+template <typename T, bool PAIRS, Made MADE, class Epi>
 hipError_t launch_few(const Product& p, const Epi& epi, hipStream_t st) {
   using std::integral_constant;
   const auto by_blocks = [&](auto rb) {
     constexpr int kBlocks = decltype(rb)::value;
-    return p.b.k <= 16 * kStep<T> ? few_as<T, kBlocks, 4, MADE>(p, epi, st) : few_as<T, kBlocks, 8, MADE>(p, epi, st);
+    return p.b.k <= 16 * kStep<T> ? few_as<T, PAIRS, kBlocks, 4, MADE>(p, epi, st) : few_as<T, PAIRS, kBlocks, 8, MADE>(p, epi, st);
   };
   if constexpr (MADE == kTurns) return epi.keep == MOEQ_KEEP_8 ? by_blocks(integral_constant<int, 4>{}) : by_blocks(integral_constant<int, 2>{});
   else return p.b.n >= 256 * 32 ? by_blocks(integral_constant<int, 2>{}) : by_blocks(integral_constant<int, 1>{});
